@@ -344,6 +344,192 @@ fal_status_t fal_stack_forward(fal_ctx_t* ctx, const void* params, const float* 
  * workspace after a step; valid until the next step. */
 fal_status_t fal_residual_out(fal_ctx_t* ctx, const float** x_last);
 
+/* ------------------------------------------------------------------------
+ * Attention over a sliding window, and the losses that tune a trained model.
+ *
+ * The calls without a context (fal_window_attention_*, fal_token_logprobs,
+ * fal_policy_loss, fal_preference_loss) enqueue on the stream given, allocate
+ * nothing and keep nothing between calls; all their scratch is the workspace
+ * of the call, which no other call may use until this one's work is done
+ * (two captured graphs that may run at once need one each).  They run on the
+ * current HIP device, which must be the one that holds the buffers.
+ * fal_last_error(NULL) returns the message of the last failed call of this
+ * kind on the calling thread. */
+
+/* Shape of a windowed attention call.  Query t of a sequence of n tokens sees
+ * the keys j <= t with t - j < window or j < sinks; with a window of seq_len
+ * or more this is the causal mask. */
+typedef struct {
+  int32_t batch;     /* B, 1 .. 65535                                       */
+  int32_t seq_len;   /* T, 1 .. 2^22                                        */
+  int32_t n_head;    /* query heads H                                       */
+  int32_t n_kv_head; /* key/value heads: 0 (H) or a divisor of n_head       */
+  int32_t head_dim;  /* 16, 32, 64 or 128                                   */
+  int32_t dtype;     /* fal_dtype_t of qkv, out and their gradients         */
+  int32_t window;    /* >= 1                                                */
+  int32_t sinks;     /* first keys that stay visible, 0 .. 128              */
+  int64_t ld_qkv;    /* elements between token rows of qkv,
+                        >= (H + 2 Hkv) * head_dim                           */
+  int64_t ld_out;    /* elements between token rows of out and d_out,
+                        >= H * head_dim                                     */
+} fal_window_attention_t;
+
+/* Bytes of workspace fal_window_attention_bwd needs (host only). */
+fal_status_t fal_window_attention_workspace_bytes(const fal_window_attention_t* shape, size_t* bytes);
+
+/* Attention of the window over packed [Q | K | V] rows (the layout of W_QKV's
+ * columns; scores scaled by 1/sqrt(head_dim); query head h reads key/value
+ * head h / (H / Hkv)).
+ *   qkv   device dtype, token row (b, t) at (b * T + t) * ld_qkv
+ *   lens  device int32 [B] or NULL: tokens of each sequence, clamped to
+ *         [0, T]; NULL: all have T.  Rows at or past a sequence's length may
+ *         hold anything and get out = 0, lse = -inf.  Rows inside must be
+ *         finite.
+ *   out   device dtype, rows of H * head_dim at stride ld_out (the rest of a
+ *         wider row is left as it was)
+ *   lse   device fp32 [B, H, T], natural log of the softmax denominators:
+ *         what the backward needs
+ * Pointers and row strides must be multiples of 16 bytes (lse, lens: 4).
+ * bf16: products of bf16 operands with fp32 sums, the probabilities rounded
+ * to bf16 for the second product; fp32: fp32 throughout.
+ * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes, misalignment or
+ * outputs that overlap an input; FAL_ERR_UNSUPPORTED for another head_dim or
+ * more than 128 sinks; FAL_ERR_HIP when a launch fails. */
+fal_status_t fal_window_attention_fwd(const fal_window_attention_t* shape, const void* qkv, const int32_t* lens,
+                                      void* out, float* lse, void* stream);
+
+/* Gradient of fal_window_attention_fwd.  qkv, lens, out, lse: as given to and
+ * written by the forward; d_out: gradient of out, rows like out's.
+ *   d_qkv  device dtype, rows of (H + 2 Hkv) * head_dim at stride ld_d_qkv,
+ *          all written (zeros past a sequence's length).  A shared
+ *          key/value head receives the sum over its query heads.
+ *   workspace  device, 256-byte aligned, at least
+ *          fal_window_attention_workspace_bytes
+ * Deterministic: every sum has a fixed order.  Errors as the forward, and
+ * FAL_ERR_WORKSPACE. */
+fal_status_t fal_window_attention_bwd(const fal_window_attention_t* shape, const void* qkv, const int32_t* lens,
+                                      const void* out, const void* d_out, const float* lse, void* d_qkv,
+                                      int64_t ld_d_qkv, void* workspace, size_t ws_bytes, void* stream);
+
+/* Windowed attention in a context's model and block calls: every later
+ * forward and backward of ctx uses the window and sinks above in place of the
+ * full causal mask (set it between steps, not between a forward and its
+ * backward).  window 0 (with sinks 0) restores the full mask, the state after
+ * fal_init.  Errors: FAL_ERR_INVALID_ARG for negative values, sinks without a
+ * window or a bidirectional config; FAL_ERR_UNSUPPORTED for more than 128
+ * sinks, or sinks of so many heads that their partial sums exceed the
+ * context's scratch. */
+fal_status_t fal_set_attention_window(fal_ctx_t* ctx, int32_t window, int32_t sinks);
+
+/* Rows of logits with the token each of them is to score: row (b, t) of
+ * logits holds V scores at (b * T + t) * ld_logits, its target id is
+ * targets[b * ld_targets + t] (tokens + 1 with ld_targets = T + 1 for the
+ * [B, T+1] tokens of fal_model_step; ids outside [0, V) are clamped). */
+typedef struct {
+  int32_t batch;        /* B >= 1                                           */
+  int32_t seq_len;      /* T >= 1; B * T at most 2^24                       */
+  int32_t vocab;        /* V, 1 .. 2^20                                     */
+  int32_t dtype;        /* fal_dtype_t of logits and dlogits                */
+  int64_t ld_logits;    /* elements between logit rows, >= V                */
+  int64_t ld_targets;   /* elements between sequences' targets, >= T        */
+  int64_t ld_dlogits;   /* elements between gradient rows                   */
+  int32_t dlogits_cols; /* columns written of each gradient row: V of them
+                           the gradient, the rest zeros; V .. ld_dlogits    */
+  float temperature;    /* > 0: the scores are logits / temperature         */
+} fal_logit_rows_t;
+
+/* Log-probability of each row's target under softmax(logits / temperature),
+ * and the softmax's entropy, without gradients: the old and reference values
+ * that the losses below take.
+ *   logits   device dtype; rows need no alignment beyond their element's
+ *   targets  device int32
+ *   mask     device uint8 [B, T] or NULL: rows whose byte is zero are not
+ *            read and get 0
+ *   logp     device fp32 [B, T]
+ *   entropy  device fp32 [B, T] or NULL
+ * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes or misaligned
+ * arrays; FAL_ERR_HIP when a launch fails. */
+fal_status_t fal_token_logprobs(const fal_logit_rows_t* rows, const void* logits, const int32_t* targets,
+                                const uint8_t* mask, float* logp, float* entropy, void* stream);
+
+/* Bytes of workspace either loss below needs (host only). */
+fal_status_t fal_logit_loss_workspace_bytes(const fal_logit_rows_t* rows, size_t* bytes);
+
+typedef struct {
+  float clip_low;        /* the ratio is held in [1 - clip_low, 1 + clip_high]: */
+  float clip_high;       /* both >= 0, clip_low <= 1                           */
+  float kl_coef;         /* weight of the KL term, >= 0                        */
+  int32_t sequence_mean; /* 0: mean over all counted rows; 1: the mean over the
+                            batch of each sequence's mean (a sequence without
+                            counted rows adds zero)                            */
+} fal_policy_t;
+
+/* Clipped policy-gradient loss with a KL term, and its gradient with respect
+ * to the logits, in one pass over them.  With logp as above,
+ * r = exp(logp - old_logp), A the advantage and d = ref_logp - logp, a counted
+ * row's loss is
+ *   -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (e^d - d - 1),
+ * its gradient in logp -[not clipped] r A + kl_coef (1 - e^d).  A zero
+ * advantage adds nothing whatever the ratio.
+ *   old_logp, advantages  device fp32 [B, T]
+ *   ref_logp  device fp32 [B, T], or NULL: no KL term
+ *   stats     device fp32 [4]: loss, its policy part, the mean of
+ *             e^d - d - 1, the share of rows whose ratio the clip holds
+ *   logp      device fp32 [B, T] or NULL (0 in rows that do not count)
+ *   dlogits   device dtype: gradient of the loss; zeros in rows that do not
+ *             count, whatever their logits hold.  May be the logits
+ *             themselves with the same row stride.
+ *   workspace device, 256-byte aligned
+ * Values of rows that do not count are never read.  A batch without counted
+ * rows has a loss of 0 and a gradient of zeros.  Errors as
+ * fal_token_logprobs, and FAL_ERR_WORKSPACE. */
+fal_status_t fal_policy_loss(const fal_logit_rows_t* rows, const fal_policy_t* hp, const void* logits,
+                             const int32_t* targets, const uint8_t* mask, const float* old_logp,
+                             const float* ref_logp, const float* advantages, float* stats, float* logp,
+                             void* dlogits, void* workspace, size_t ws_bytes, void* stream);
+
+typedef struct {
+  float beta;            /* > 0                                               */
+  float label_smoothing; /* in [0, 0.5]; 0 with ipo                           */
+  int32_t ipo;           /* 0: -(1 - s) log sigmoid(beta h) - s log sigmoid(-beta h);
+                            1: (h - 1 / (2 beta))^2                           */
+  int32_t length_mean;   /* 1: a sequence's log-probability is the mean of its
+                            counted rows', not their sum                      */
+} fal_preference_t;
+
+/* Preference loss over pairs of sequences, and its gradient with respect to
+ * the logits: sequence b < B/2 is preferred to sequence b + B/2 (B even).
+ * lp = sum of logp over a sequence's counted rows, h = (lp - ref_logp) of the
+ * preferred sequence minus that of the other; the loss is the mean over pairs
+ * of the function above.
+ *   ref_logp  device fp32 [B]: the reference model's lp
+ *   loss      device fp32 scalar
+ *   seq_logp  device fp32 [B] or NULL: lp
+ *   dlogits, workspace  as for fal_policy_loss
+ * Sums over a sequence are fp64.  Errors as fal_policy_loss. */
+fal_status_t fal_preference_loss(const fal_logit_rows_t* rows, const fal_preference_t* hp, const void* logits,
+                                 const int32_t* targets, const uint8_t* mask, const float* ref_logp, float* loss,
+                                 float* seq_logp, void* dlogits, void* workspace, size_t ws_bytes, void* stream);
+
+/* fal_model_forward with the per-token scores in place of the loss: logp (and
+ * entropy, or NULL) of tokens[:, 1:] as fal_token_logprobs defines them.
+ *   mask  device uint8 [B, T] or NULL, over the T predicted tokens */
+fal_status_t fal_model_logprobs(fal_ctx_t* ctx, const void* params, const int32_t* tokens, const uint8_t* mask,
+                                float temperature, float* logp, float* entropy);
+
+/* One training step of the language model under the policy loss: the forward
+ * pass, stats and logp of fal_policy_loss over tokens[:, 1:] (all [B, T]
+ * arrays run over the T predicted tokens), and the gradient of its loss with
+ * respect to every parameter.  Takes no workspace beyond the context's. */
+fal_status_t fal_policy_step(fal_ctx_t* ctx, const void* params, const fal_policy_t* hp, const int32_t* tokens,
+                             const uint8_t* mask, float temperature, const float* old_logp, const float* ref_logp,
+                             const float* advantages, float* stats, float* logp, float* grads);
+
+/* The same under the preference loss; the config's batch must be even. */
+fal_status_t fal_preference_step(fal_ctx_t* ctx, const void* params, const fal_preference_t* hp,
+                                 const int32_t* tokens, const uint8_t* mask, float temperature,
+                                 const float* ref_logp, float* loss, float* seq_logp, float* grads);
+
 /* Kernel timing, for measurement.  While enabled, each launch of the
  * classes below is bracketed by HIP events recorded on the stream the
  * kernel runs on; fal_profile_read synchronises the context's streams and
@@ -367,8 +553,9 @@ fal_status_t fal_profile_read(fal_ctx_t* ctx, int32_t cls, int64_t* launches, do
                               double* flops, double* bytes);
 
 const char* fal_status_string(fal_status_t status);
-/* "" if none.  ctx NULL: the message of the last failed context-free call
- * (fal_adamw_step_noalloc) on the calling thread. */
+/* "" if none.  ctx NULL: the message of the last failed call on the calling
+ * thread of those that take no context (fal_adamw_step_noalloc and the
+ * window attention, log-probability and loss calls). */
 const char* fal_last_error(const fal_ctx_t* ctx);
 
 #ifdef __cplusplus

@@ -31,9 +31,15 @@
 #include <vector>
 
 #include "../../include/fal.h"
+#include "api_checks.h"
 #include "kernels.h"
 
 using namespace fal;
+
+std::string& fal::noctx_error() {
+  static thread_local std::string err;
+  return err;
+}
 
 namespace {
 
@@ -303,6 +309,7 @@ struct fal_ctx {
   // next block's backward; forked from and joined back to the main stream
   hipStream_t sb = nullptr;
   hipEvent_t ev_bfork = nullptr, ev_bdone = nullptr, ev_hdone = nullptr;
+  int window = 0, sinks = 0;  // fal_set_attention_window; window 0: the full mask
   int device;
   std::string err;
   // kernel timing (fal_profile_enable)
@@ -439,12 +446,33 @@ struct Run {
     return p;
   }
   int causal() const { return ctx->cfg.bidirectional ? 0 : 1; }
-  // twice the keys each query sees on average: T + 1 causal, 2T unmasked
-  double attn_keys2() const { return ctx->cfg.bidirectional ? 2.0 * ctx->D.T : ctx->D.T + 1.0; }
+  // twice the keys each query sees on average: T + 1 causal, 2T unmasked;
+  // under a window the rows past window + sinks see that many
+  double attn_keys2() const {
+    const double T = ctx->D.T;
+    if (ctx->cfg.bidirectional) return 2.0 * T;
+    if (!ctx->window) return T + 1.0;
+    const double most = (double)ctx->window + ctx->sinks, n = std::min(T, most);
+    return (n * (n + 1.0) + 2.0 * (T - n) * most) / T;
+  }
+  WindowAttn window_args() const {
+    const Dims& D = ctx->D;
+    WindowAttn a;
+    memset(&a, 0, sizeof(a));
+    a.B = D.B; a.T = D.T; a.H = D.H; a.Hkv = D.Hkv; a.hd = D.hd;
+    a.window = std::min(ctx->window, D.T); a.sinks = ctx->sinks;
+    a.ldq = a.lddq = D.dqkv;
+    a.ldo = a.lddo = D.dA + D.f;
+    return a;
+  }
   void attention_fwd(const LayerSlot& S, hipStream_t s) {
     const Dims& D = ctx->D;
     const double fl = 2.0 * D.B * D.H * (double)D.hd * D.T * attn_keys2();
     Span span(ctx, FAL_PROF_ATTN_FWD, s, fl, (double)D.es * D.M * ((double)D.dqkv + D.dA));
+    if (ctx->window) {
+      FAL_TRY(window_attention_fwd(dt, window_args(), S.qkv, S.og, S.lse, s));
+      return;
+    }
     FAL_TRY(attn_fwd(dt, S.qkv, D.B, D.T, D.H, D.Hkv, D.hd, causal(), S.og, D.dA + D.f, S.lse, s));
   }
   void ln(const LnFwdArgs& a, hipStream_t s) {
@@ -746,8 +774,13 @@ struct Run {
     {
       const double fl = 4.0 * D.B * D.H * (double)D.hd * D.T * attn_keys2();
       Span span(ctx, FAL_PROF_ATTN_BWD, s, fl, (double)D.es * D.M * (2.0 * D.dqkv + 2.0 * D.dA));
-      FAL_TRY(attn_bwd(dt, S.qkv, S.og, D.dA + D.f, W.dog, D.dA + D.f, S.lse, D.B, D.T, D.H, D.Hkv, D.hd,
-                       causal(), W.dqkv, W.Dvec, nullptr, s));
+      // the split-K partials of the main stream's GEMMs hold nothing here:
+      // they take the sink keys' partial sums
+      if (ctx->window)
+        FAL_TRY(window_attention_bwd(dt, window_args(), S.qkv, S.og, W.dog, S.lse, W.Dvec, W.splitk_main, W.dqkv, s));
+      else
+        FAL_TRY(attn_bwd(dt, S.qkv, S.og, D.dA + D.f, W.dog, D.dA + D.f, S.lse, D.B, D.T, D.H, D.Hkv, D.hd,
+                         causal(), W.dqkv, W.Dvec, nullptr, s));
     }
     GemmProblem ph = dgrad(W.dqkv, D.dqkv, P(bp, FAL_B_W_QKV), D.d, D.dqkv, D.M);
     ph.epi = EPI_STORE; ph.out_f32 = 1; ph.out = W.dh1; ph.ldo = D.d;
@@ -900,10 +933,7 @@ const char* fal_status_string(fal_status_t s) {
   return "unknown status";
 }
 
-// Message of the last failed call made without a context on this thread.
-static thread_local std::string g_noctx_err;
-
-const char* fal_last_error(const fal_ctx_t* ctx) { return ctx ? ctx->err.c_str() : g_noctx_err.c_str(); }
+const char* fal_last_error(const fal_ctx_t* ctx) { return ctx ? ctx->err.c_str() : noctx_error().c_str(); }
 
 fal_status_t fal_validate_config(const fal_config_t* cfg) {
   const char* why = validate(cfg);
@@ -1052,12 +1082,12 @@ fal_status_t fal_block_bwd(fal_ctx_t* ctx, int32_t layer, const void* block_para
   return FAL_OK;
 }
 
-fal_status_t fal_model_step(fal_ctx_t* ctx, const void* params, const int32_t* tokens, float* loss,
-                            float* logits, float* grads) {
-  fal_status_t st = check_ctx(ctx);
-  if (st != FAL_OK) return st;
-  if (!ctx->cfg.has_embed_head) return bad(ctx, "fal_model_step needs has_embed_head = 1 (use fal_stack_step)");
-  if (!params || !tokens || !loss || !grads) return bad(ctx, "NULL params, tokens, loss or grads");
+// One training step of the language model: forward, the loss that
+// head_loss() evaluates from the logits in W.logits (leaving their gradient
+// in W.dlogits, columns V .. Vp-1 zero), and the backward of all of it.
+extern "C++" template <typename HeadLoss>
+static fal_status_t model_step(fal_ctx_t* ctx, const void* params, const int32_t* tokens, float* grads,
+                               HeadLoss head_loss) {
   const Dims& D = ctx->D;
   const Layout& Lo = ctx->Lo;
   Work& W = ctx->W;
@@ -1095,11 +1125,7 @@ fal_status_t fal_model_step(fal_ctx_t* ctx, const void* params, const int32_t* t
     // cross-entropy works in fp32 from them
     ph.epi = EPI_STORE; ph.out_f32 = r.dt == F32; ph.out = W.logits; ph.ldo = D.Vp;
     r.gemm1(1, 1, ph, sm);
-    {
-      Span span(ctx, FAL_PROF_CE, sm, 0.0, (double)D.M * (double)D.es * (D.V + D.Vp));
-      FAL_TRY(cross_entropy(r.dt, W.logits, D.Vp, tokens, D.B, D.T, D.V, W.dlogits, D.Vp, W.row_loss, loss, sm));
-    }
-    if (logits) FAL_TRY(rows_to_f32(r.dt, W.logits, D.Vp, logits, D.V, D.M, D.V, sm));
+    head_loss(r);
     // head backward: dHf = dlogits wte ; dwte = dlogits^T Hf
     GemmProblem pd = Run::prob(W.dlogits, D.Vp, gparam(FAL_P_WTE), D.d, D.M, D.d, D.V);
     pd.epi = EPI_STORE; pd.out_f32 = 1; pd.out = W.dh1; pd.ldo = D.d;
@@ -1146,12 +1172,26 @@ fal_status_t fal_model_step(fal_ctx_t* ctx, const void* params, const int32_t* t
   return FAL_OK;
 }
 
-fal_status_t fal_model_forward(fal_ctx_t* ctx, const void* params, const int32_t* tokens, float* loss,
-                               float* logits) {
+fal_status_t fal_model_step(fal_ctx_t* ctx, const void* params, const int32_t* tokens, float* loss,
+                            float* logits, float* grads) {
   fal_status_t st = check_ctx(ctx);
   if (st != FAL_OK) return st;
-  if (!ctx->cfg.has_embed_head) return bad(ctx, "fal_model_forward needs has_embed_head = 1 (use fal_stack_forward)");
-  if (!params || !tokens) return bad(ctx, "NULL params or tokens");
+  if (!ctx->cfg.has_embed_head) return bad(ctx, "fal_model_step needs has_embed_head = 1 (use fal_stack_step)");
+  if (!params || !tokens || !loss || !grads) return bad(ctx, "NULL params, tokens, loss or grads");
+  return model_step(ctx, params, tokens, grads, [&](Run& r) {
+    const Dims& D = ctx->D;
+    Work& W = ctx->W;
+    {
+      Span span(ctx, FAL_PROF_CE, ctx->sm, 0.0, (double)D.M * (double)D.es * (D.V + D.Vp));
+      FAL_TRY(cross_entropy(r.dt, W.logits, D.Vp, tokens, D.B, D.T, D.V, W.dlogits, D.Vp, W.row_loss, loss, ctx->sm));
+    }
+    if (logits) FAL_TRY(rows_to_f32(r.dt, W.logits, D.Vp, logits, D.V, D.M, D.V, ctx->sm));
+  });
+}
+
+// Forward pass up to the logits in W.logits, then head(r).
+extern "C++" template <typename Head>
+static fal_status_t model_forward(fal_ctx_t* ctx, const void* params, const int32_t* tokens, Head head) {
   const Dims& D = ctx->D;
   const Layout& Lo = ctx->Lo;
   Work& W = ctx->W;
@@ -1177,15 +1217,119 @@ fal_status_t fal_model_forward(fal_ctx_t* ctx, const void* params, const int32_t
     GemmProblem ph = Run::prob(W.hf, D.d, gparam(FAL_P_WTE), D.d, D.M, D.V, D.d);
     ph.epi = EPI_STORE; ph.out_f32 = r.dt == F32; ph.out = W.logits; ph.ldo = D.Vp;
     r.gemm1(1, 1, ph, sm);
-    if (loss) {
-      Span span(ctx, FAL_PROF_CE, sm, 0.0, (double)D.M * (double)D.es * D.V);
-      FAL_TRY(cross_entropy(r.dt, W.logits, D.Vp, tokens, D.B, D.T, D.V, nullptr, D.Vp, W.row_loss, loss, sm));
-    }
-    if (logits) FAL_TRY(rows_to_f32(r.dt, W.logits, D.Vp, logits, D.V, D.M, D.V, sm));
+    head(r);
   } catch (Fail&) {
     return FAL_ERR_HIP;
   }
   return FAL_OK;
+}
+
+fal_status_t fal_model_forward(fal_ctx_t* ctx, const void* params, const int32_t* tokens, float* loss,
+                               float* logits) {
+  fal_status_t st = check_ctx(ctx);
+  if (st != FAL_OK) return st;
+  if (!ctx->cfg.has_embed_head) return bad(ctx, "fal_model_forward needs has_embed_head = 1 (use fal_stack_forward)");
+  if (!params || !tokens) return bad(ctx, "NULL params or tokens");
+  return model_forward(ctx, params, tokens, [&](Run& r) {
+    const Dims& D = ctx->D;
+    Work& W = ctx->W;
+    if (loss) {
+      Span span(ctx, FAL_PROF_CE, ctx->sm, 0.0, (double)D.M * (double)D.es * D.V);
+      FAL_TRY(cross_entropy(r.dt, W.logits, D.Vp, tokens, D.B, D.T, D.V, nullptr, D.Vp, W.row_loss, loss, ctx->sm));
+    }
+    if (logits) FAL_TRY(rows_to_f32(r.dt, W.logits, D.Vp, logits, D.V, D.M, D.V, ctx->sm));
+  });
+}
+
+// The logits and next-token targets of a context's step as LogitRows.
+static LogitRows step_rows(fal_ctx_t* ctx, const int32_t* tokens, const uint8_t* mask, float temperature) {
+  const Dims& D = ctx->D;
+  LogitRows r;
+  r.logits = ctx->W.logits; r.targets = tokens + 1; r.mask = mask;
+  r.B = D.B; r.T = D.T; r.V = D.V; r.width = D.Vp;
+  r.ldl = r.ldd = D.Vp; r.ldt = D.T + 1;
+  r.inv_temp = 1.f / temperature;
+  return r;
+}
+
+// The loss scratch of a context's step: W.dh1 holds nothing between the
+// forward pass and the head's backward, and d_model >= 8 gives it 8 floats a
+// token, more than logit_loss_scratch's 3 a token and 4 a sequence.
+static float* loss_scratch(fal_ctx_t* ctx) { return ctx->W.dh1; }
+
+fal_status_t fal_model_logprobs(fal_ctx_t* ctx, const void* params, const int32_t* tokens, const uint8_t* mask,
+                                float temperature, float* logp, float* entropy) {
+  fal_status_t st = check_ctx(ctx);
+  if (st != FAL_OK) return st;
+  if (!ctx->cfg.has_embed_head) return bad(ctx, "fal_model_logprobs needs has_embed_head = 1");
+  if (!params || !tokens || !logp) return bad(ctx, "NULL params, tokens or logp");
+  if (const char* why = check_temperature(temperature)) return bad(ctx, why);
+  return model_forward(ctx, params, tokens, [&](Run& r) {
+    const Dims& D = ctx->D;
+    Span span(ctx, FAL_PROF_CE, ctx->sm, 0.0, (double)D.M * (double)D.es * D.V);
+    FAL_TRY(token_logprobs(r.dt, step_rows(ctx, tokens, mask, temperature), logp, entropy, ctx->sm));
+  });
+}
+
+fal_status_t fal_policy_step(fal_ctx_t* ctx, const void* params, const fal_policy_t* hp, const int32_t* tokens,
+                             const uint8_t* mask, float temperature, const float* old_logp, const float* ref_logp,
+                             const float* advantages, float* stats, float* logp, float* grads) {
+  fal_status_t st = check_ctx(ctx);
+  if (st != FAL_OK) return st;
+  if (!ctx->cfg.has_embed_head) return bad(ctx, "fal_policy_step needs has_embed_head = 1");
+  if (!params || !tokens || !old_logp || !advantages || !stats || !grads)
+    return bad(ctx, "NULL params, tokens, old_logp, advantages, stats or grads");
+  if (const char* why = check_temperature(temperature)) return bad(ctx, why);
+  if (const char* why = check_policy(hp)) return bad(ctx, why);
+  return model_step(ctx, params, tokens, grads, [&](Run& r) {
+    const Dims& D = ctx->D;
+    Span span(ctx, FAL_PROF_CE, ctx->sm, 0.0, (double)D.M * (double)D.es * (D.V + D.Vp));
+    const PolicyArgs p{old_logp, ref_logp, advantages, hp->clip_low, hp->clip_high, hp->kl_coef, hp->sequence_mean,
+                       stats, logp};
+    FAL_TRY(policy_loss(r.dt, step_rows(ctx, tokens, mask, temperature), p, ctx->W.dlogits, loss_scratch(ctx),
+                        ctx->sm));
+  });
+}
+
+fal_status_t fal_preference_step(fal_ctx_t* ctx, const void* params, const fal_preference_t* hp,
+                                 const int32_t* tokens, const uint8_t* mask, float temperature,
+                                 const float* ref_logp, float* loss, float* seq_logp, float* grads) {
+  fal_status_t st = check_ctx(ctx);
+  if (st != FAL_OK) return st;
+  if (!ctx->cfg.has_embed_head) return bad(ctx, "fal_preference_step needs has_embed_head = 1");
+  if (!params || !tokens || !ref_logp || !loss || !grads)
+    return bad(ctx, "NULL params, tokens, ref_logp, loss or grads");
+  if (ctx->D.B % 2) return bad(ctx, "preference pairs need an even batch");
+  if (const char* why = check_temperature(temperature)) return bad(ctx, why);
+  if (const char* why = check_preference(hp)) return bad(ctx, why);
+  return model_step(ctx, params, tokens, grads, [&](Run& r) {
+    const Dims& D = ctx->D;
+    Span span(ctx, FAL_PROF_CE, ctx->sm, 0.0, (double)D.M * (double)D.es * (2.0 * D.V + D.Vp));
+    const PreferenceArgs p{ref_logp, hp->beta, hp->label_smoothing, hp->ipo, hp->length_mean, loss, seq_logp};
+    FAL_TRY(preference_loss(r.dt, step_rows(ctx, tokens, mask, temperature), p, ctx->W.dlogits, loss_scratch(ctx),
+                            ctx->sm));
+  });
+}
+
+fal_status_t fal_set_attention_window(fal_ctx_t* ctx, int32_t window, int32_t sinks) {
+  fal_status_t st = check_ctx(ctx);
+  if (st != FAL_OK) return st;
+  if (window < 0 || sinks < 0) return bad(ctx, "window and sinks must be >= 0");
+  if (window == 0 && sinks > 0) return bad(ctx, "sinks need a window (window 0 is the full mask)");
+  if (window > 0 && ctx->cfg.bidirectional) return bad(ctx, "a window needs causal attention");
+  const int old_window = ctx->window, old_sinks = ctx->sinks;
+  ctx->window = window;
+  ctx->sinks = sinks;
+  const char* why = nullptr;
+  if (window > 0 && ctx->D.T > kMaxWindowSeq) why = "seq_len above 2^22 is not supported with a window";
+  else if (sinks > kMaxSinks) why = "more than 128 sinks are not supported";
+  else if (window > 0 && window_attention_scratch(Run(ctx).window_args()) > ctx->W.splitk_floats)
+    why = "sinks of this many heads are not supported: their partial sums exceed the context's scratch";
+  if (!why) return FAL_OK;
+  ctx->window = old_window;
+  ctx->sinks = old_sinks;
+  ctx->err = why;
+  return FAL_ERR_UNSUPPORTED;
 }
 
 fal_status_t fal_stack_forward(fal_ctx_t* ctx, const void* params, const float* x_in, float* x_out) {
@@ -1249,11 +1393,6 @@ fal_status_t fal_stack_step(fal_ctx_t* ctx, const void* params, const float* x_i
     return FAL_ERR_HIP;
   }
   return FAL_OK;
-}
-
-static bool overlaps(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + (uintptr_t)bbytes && y < x + (uintptr_t)abytes;
 }
 
 // Host checks shared by both AdamW entry points; on success fills the
@@ -1331,22 +1470,22 @@ fal_status_t fal_adamw_step(fal_ctx_t* ctx, const fal_adamw_t* hp, int64_t step,
 fal_status_t fal_adamw_step_noalloc(const fal_adamw_t* hp, int64_t step, int64_t n, int32_t dtype, float* master,
                                     void* params, const float* grads, float* m, float* v, float* norm_out,
                                     void* stream) {
-  g_noctx_err.clear();
+  noctx_error().clear();
   if (dtype != FAL_F32 && dtype != FAL_BF16) {
-    g_noctx_err = "unknown dtype";
+    noctx_error() = "unknown dtype";
     return FAL_ERR_INVALID_ARG;
   }
   AdamwConsts k;
   int lp_mode = 0;
   const char* why = adamw_args(hp, step, n, dtype == FAL_BF16, master, params, grads, m, v, norm_out, &k, &lp_mode);
   if (why) {
-    g_noctx_err = why;
+    noctx_error() = why;
     return FAL_ERR_INVALID_ARG;
   }
   const hipError_t e = adamw_static_scratch(lp_mode, master, params, grads, m, v, n, hp->max_grad_norm, k, norm_out,
                                             static_cast<hipStream_t>(stream));
   if (e != hipSuccess) {
-    g_noctx_err = std::string("fal_adamw_step_noalloc: ") + hipGetErrorString(e);
+    noctx_error() = std::string("fal_adamw_step_noalloc: ") + hipGetErrorString(e);
     return FAL_ERR_HIP;
   }
   return FAL_OK;

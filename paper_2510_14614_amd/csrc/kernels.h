@@ -213,6 +213,27 @@ hipError_t attn_bwd(DType dt, const void* qkv, const void* O, int64_t ldo, const
                     int64_t lddo, const float* lse, int B, int T, int H, int Hkv, int hd, int causal, void* dqkv,
                     float* Dvec, float* dq_acc, hipStream_t s);
 
+// Causal attention over a sliding window with a few first keys that stay
+// visible, on packed QKV rows as above: query t of sequence b (n tokens)
+// sees keys j <= t with t - j < window or j < sinks.  Rows past n: O = 0,
+// lse = -inf, zero gradients.  Any head_dim of the library, fp32 or bf16.
+// Strides in elements, rows and pointers 16-byte aligned; window in [1, T],
+// sinks in [0, kMaxSinks].
+constexpr int kMaxSinks = 128;           // one block of keys of the dK/dV kernel
+constexpr int kMaxWindowSeq = 1 << 22;  // blocks of 128 tokens are a grid's z dimension
+struct WindowAttn {
+  int B, T, H, Hkv, hd;
+  int window, sinks;
+  const int32_t* lens;  // [B], clamped to [0, T]; NULL: every sequence has T tokens
+  int64_t ldq, ldo;     // row strides of QKV and O
+  int64_t lddo, lddq;   // backward: of dO and dQKV
+};
+hipError_t window_attention_fwd(DType dt, const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s);
+// Dvec: fp32 [B, H, T] scratch; part: window_attention_scratch floats.
+hipError_t window_attention_bwd(DType dt, const WindowAttn& a, const void* qkv, const void* O, const void* dO,
+                                const float* lse, float* Dvec, float* part, void* dqkv, hipStream_t s);
+int64_t window_attention_scratch(const WindowAttn& a);
+
 // ------------------------------------------------ embedding / loss / misc ----
 // X[m, :] = wte[tok[b, t]] + wpe[t]  (fp32 out), tokens [B, T+1].
 hipError_t embed_fwd(DType dt, const int32_t* tokens, int B, int T, int V, int d, const void* wte,
@@ -238,6 +259,55 @@ int64_t embed_bwd_scratch(int M);
 hipError_t cross_entropy(DType dt, const void* logits, int64_t ldl, const int32_t* tokens, int B,
                          int T, int V, void* dlogits, int64_t ldd, float* row_loss, float* loss,
                          hipStream_t s);
+// ------------------------------------- losses of sampled tokens' log-probs ----
+// Rows of logits [B, T, V] (dtype, row stride ldl) with a target id each
+// (targets[b * ldt + t], clamped to [0, V)) and a mask byte each ([B, T];
+// NULL: every row counts).  x = logits * inv_temp; a row's log-probability is
+// x[target] - logsumexp(x).  Rows whose byte is zero are not read: their
+// log-probability is 0 and their gradient row zeros.  Gradient rows have
+// `width` columns (>= V, the rest zeros) at stride ldd and may be the logits
+// themselves.
+struct LogitRows {
+  const void* logits;
+  const int32_t* targets;
+  const uint8_t* mask;
+  int B, T, V, width;
+  int64_t ldl, ldt, ldd;
+  float inv_temp;
+};
+// logp [B, T]; entropy [B, T] or NULL.
+hipError_t token_logprobs(DType dt, const LogitRows& r, float* logp, float* entropy, hipStream_t s);
+
+// Clipped policy loss with a KL term against a reference: with
+// ratio = exp(logp - old) and d = ref - logp, each counted row adds
+//   w (-min(ratio A, clip(ratio, 1 - low, 1 + high) A) + kl (e^d - d - 1)),
+// w = 1 / counted rows, or 1 / (B * counted rows of its sequence).
+// stats [4]: loss, its policy part, the KL mean and the share of rows whose
+// ratio the clip holds, all under w.
+struct PolicyArgs {
+  const float *old_logp, *ref_logp, *adv;  // [B, T]; ref_logp may be NULL
+  float low, high, kl;
+  int sequence_mean;
+  float *stats, *logp;  // logp [B, T] or NULL
+};
+hipError_t policy_loss(DType dt, const LogitRows& r, const PolicyArgs& p, void* dlogits, float* scratch,
+                       hipStream_t s);
+// Preference loss: sequences b < B/2 are preferred to b + B/2.  A sequence's
+// log-probability is the sum (length_mean: the mean) of its counted rows';
+// h = (lp - ref)_b - (lp - ref)_{b + B/2}; the mean over pairs of
+//   -(1 - smoothing) log sigmoid(beta h) - smoothing log sigmoid(-beta h),
+// or of (h - 1 / (2 beta))^2 (ipo).
+struct PreferenceArgs {
+  const float* ref_logp;  // [B]
+  float beta, smoothing;
+  int ipo, length_mean;
+  float *loss, *seq_logp;  // loss [1]; seq_logp [B] or NULL
+};
+hipError_t preference_loss(DType dt, const LogitRows& r, const PreferenceArgs& p, void* dlogits, float* scratch,
+                           hipStream_t s);
+// floats of scratch either loss needs
+int64_t logit_loss_scratch(int B, int T);
+
 // dst[r, c] = src[r, c] widened to fp32, for r < rows and c < cols.
 hipError_t rows_to_f32(DType dt, const void* src, int64_t lds, float* dst, int64_t ldd, int rows, int cols,
                        hipStream_t s);

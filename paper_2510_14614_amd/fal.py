@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 
 import numpy as np
@@ -29,6 +30,9 @@ ABI_FUNCTIONS = (
     "fal_block_fwd", "fal_block_bwd", "fal_model_step", "fal_stack_step", "fal_residual_out",
     "fal_profile_enable", "fal_profile_read", "fal_status_string", "fal_last_error", "fal_adamw_step",
     "fal_model_forward", "fal_stack_forward", "fal_adamw_step_noalloc",
+    "fal_window_attention_workspace_bytes", "fal_window_attention_fwd", "fal_window_attention_bwd",
+    "fal_set_attention_window", "fal_token_logprobs", "fal_logit_loss_workspace_bytes", "fal_policy_loss",
+    "fal_preference_loss", "fal_model_logprobs", "fal_policy_step", "fal_preference_step",
 )
 PROF_GEMM, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_NORM, PROF_CE, PROF_EMBED, PROF_BIAS, PROF_OPTIM = range(8)
 PROF_NAMES = {PROF_GEMM: "gemm", PROF_ATTN_FWD: "attn_fwd", PROF_ATTN_BWD: "attn_bwd", PROF_NORM: "norm",
@@ -59,6 +63,38 @@ def adamw_params(**hp) -> fal_adamw_t:
     v = dict(ADAMW_PAPER)
     v.update(hp)
     return fal_adamw_t(**{k: float(v[k]) for k in ADAMW_PAPER})
+
+
+class fal_window_attention_t(ctypes.Structure):
+    _fields_ = [("batch", c_int32), ("seq_len", c_int32), ("n_head", c_int32), ("n_kv_head", c_int32),
+                ("head_dim", c_int32), ("dtype", c_int32), ("window", c_int32), ("sinks", c_int32),
+                ("ld_qkv", c_int64), ("ld_out", c_int64)]
+
+
+class fal_logit_rows_t(ctypes.Structure):
+    _fields_ = [("batch", c_int32), ("seq_len", c_int32), ("vocab", c_int32), ("dtype", c_int32),
+                ("ld_logits", c_int64), ("ld_targets", c_int64), ("ld_dlogits", c_int64), ("dlogits_cols", c_int32),
+                ("temperature", c_float)]
+
+
+class fal_policy_t(ctypes.Structure):
+    _fields_ = [("clip_low", c_float), ("clip_high", c_float), ("kl_coef", c_float), ("sequence_mean", c_int32)]
+
+
+class fal_preference_t(ctypes.Structure):
+    _fields_ = [("beta", c_float), ("label_smoothing", c_float), ("ipo", c_int32), ("length_mean", c_int32)]
+
+
+class PolicyLoss(NamedTuple):
+    stats: object    # fp32 [4]: loss, its policy part, KL mean, share of rows whose ratio the clip holds
+    logp: object     # fp32 [B, T]
+    dlogits: object  # gradient of the loss, in the logits' dtype
+
+
+class PreferenceLoss(NamedTuple):
+    loss: object      # fp32 [1]
+    seq_logp: object  # fp32 [B]
+    dlogits: object
 
 
 class FalError(RuntimeError):
@@ -98,6 +134,20 @@ def lib():
                                      c_void_p, c_void_p, c_void_p, c_void_p]
         L.fal_adamw_step_noalloc.argtypes = [POINTER(fal_adamw_t), c_int64, c_int64, c_int32, c_void_p, c_void_p,
                                              c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+        attnp, rowsp = POINTER(fal_window_attention_t), POINTER(fal_logit_rows_t)
+        L.fal_window_attention_workspace_bytes.argtypes = [attnp, POINTER(c_size_t)]
+        L.fal_window_attention_fwd.argtypes = [attnp] + [c_void_p] * 5
+        L.fal_window_attention_bwd.argtypes = ([attnp] + [c_void_p] * 6 + [c_int64, c_void_p, c_size_t, c_void_p])
+        L.fal_set_attention_window.argtypes = [c_void_p, c_int32, c_int32]
+        L.fal_token_logprobs.argtypes = [rowsp] + [c_void_p] * 6
+        L.fal_logit_loss_workspace_bytes.argtypes = [rowsp, POINTER(c_size_t)]
+        L.fal_policy_loss.argtypes = [rowsp, POINTER(fal_policy_t)] + [c_void_p] * 10 + [c_size_t, c_void_p]
+        L.fal_preference_loss.argtypes = [rowsp, POINTER(fal_preference_t)] + [c_void_p] * 8 + [c_size_t, c_void_p]
+        L.fal_model_logprobs.argtypes = [c_void_p] * 4 + [c_float] + [c_void_p] * 2
+        L.fal_policy_step.argtypes = ([c_void_p] * 2 + [POINTER(fal_policy_t)] + [c_void_p] * 2 + [c_float] +
+                                      [c_void_p] * 6)
+        L.fal_preference_step.argtypes = ([c_void_p] * 2 + [POINTER(fal_preference_t)] + [c_void_p] * 2 + [c_float] +
+                                          [c_void_p] * 4)
         L.fal_status_string.argtypes = [c_int32]
         L.fal_status_string.restype = c_char_p
         L.fal_last_error.argtypes = [c_void_p]
@@ -196,6 +246,239 @@ def adamw_step_noalloc(hp: fal_adamw_t, step: int, n: int, dtype: int, master, p
     if st != FAL_OK:
         L = lib()
         raise FalError(st, f"{L.fal_status_string(st).decode()}: {L.fal_last_error(None).decode()}")
+
+
+# ------------------------------------------- operators without a context --
+# Each takes torch device tensors, runs on the current stream of their device
+# and returns without waiting.  Outputs that are not given are allocated, as is
+# the workspace, so calls on different streams or in different captured graphs
+# share nothing.  ValueError: a tensor is not what the call needs; FalError:
+# the library refused the call.
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dtype_code(t, name):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return 1
+    _need(t.dtype == torch.float32, f"{name} must be bfloat16 or float32")
+    return 0
+
+
+def _dense(t, name, shape, dtypes, like):
+    """Checks a contiguous tensor of the given shape on like's device."""
+    _need(t.dtype in dtypes, f"{name} must be {' or '.join(str(d) for d in dtypes)}")
+    _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    _need(t.is_contiguous(), f"{name} must be contiguous")
+    _need(t.device == like.device, f"{name} must be on {like.device}")
+
+
+def _row_stride(t, name):
+    """Row stride of a [B, T, width] tensor whose rows are equally spaced."""
+    B, T, width = t.shape
+    _need(width == 1 or t.stride(2) == 1, f"{name} must be contiguous in its last dimension")
+    ld = t.stride(1) if T > 1 else t.stride(0) if B > 1 else max(width, t.stride(1))
+    _need(B == 1 or t.stride(0) == T * ld, f"the sequences of {name} must follow each other at seq_len rows")
+    return ld
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class _call:
+    """The device guard and the stream of one library call."""
+
+    def __init__(self, like):
+        import torch
+        _need(like.is_cuda, "tensors must be on a GPU")
+        self.guard = None if like.device.index == torch.cuda.current_device() else torch.cuda.device(like.device)
+        self.device = like.device
+
+    def __enter__(self):
+        import torch
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _check_noctx(status):
+    if status != FAL_OK:
+        L = lib()
+        raise FalError(status, f"{L.fal_status_string(status).decode()}: {L.fal_last_error(None).decode()}")
+
+
+def _workspace(query, shape, like):
+    import torch
+    n = c_size_t()
+    _check_noctx(query(byref(shape), byref(n)))
+    # allocations of the caching allocator start at multiples of 512 bytes
+    return torch.empty(max(n.value, 1), dtype=torch.uint8, device=like.device)
+
+
+def _window_shape(qkv, n_head, n_kv_head, window, sinks, lens):
+    import torch
+    _need(qkv.dim() == 3, "qkv must be [B, T, (n_head + 2 n_kv_head) * head_dim]")
+    B, T, width = qkv.shape
+    heads = n_head + 2 * (n_kv_head or n_head)
+    _need(n_head >= 1 and n_kv_head >= 0 and width % heads == 0,
+          "qkv's last dimension must be (n_head + 2 n_kv_head) * head_dim")
+    hd = width // heads
+    # in 32 bits: any longer window sees the whole sequence, any more sinks are refused
+    window, sinks = (max(-1, min(int(n), 2 ** 31 - 1)) for n in (window, sinks))
+    code = _dtype_code(qkv, "qkv")
+    if lens is not None:
+        _dense(lens, "lens", (B,), (torch.int32,), qkv)
+    return fal_window_attention_t(B, T, n_head, n_kv_head, hd, code, window, sinks, _row_stride(qkv, "qkv"),
+                                  n_head * hd)
+
+
+def _window_rows(t, name, like, shape, ld):
+    _need(t.dtype == like.dtype and t.device == like.device, f"{name} must have qkv's dtype and device")
+    _need(tuple(t.shape) == shape, f"{name} must have shape {shape}, not {tuple(t.shape)}")
+    _need(ld is None or _row_stride(t, name) == ld, f"{name} must have a row stride of {ld} elements")
+
+
+def window_attention_fwd(qkv, n_head, window, sinks=0, n_kv_head=0, lens=None, out=None, lse=None):
+    """Causal attention over a sliding window: query t sees the keys j <= t
+    with t - j < window or j < sinks (fal_window_attention_fwd).
+
+    qkv: [B, T, (n_head + 2 n_kv_head) * head_dim], bfloat16 or float32, rows
+    [Q | K | V] at any equal spacing; lens: int32 [B] or None.  Returns out
+    [B, T, n_head * head_dim] (rows at any equal spacing if given) and the
+    log-sum-exp, float32 [B, n_head, T]."""
+    import torch
+    a = _window_shape(qkv, n_head, n_kv_head, window, sinks, lens)
+    shape = (a.batch, a.seq_len, n_head * a.head_dim)
+    with _call(qkv) as stream:
+        if out is None:
+            out = torch.empty(shape, dtype=qkv.dtype, device=qkv.device)
+        else:
+            _window_rows(out, "out", qkv, shape, None)
+            a.ld_out = _row_stride(out, "out")
+        if lse is None:
+            lse = torch.empty(a.batch, n_head, a.seq_len, dtype=torch.float32, device=qkv.device)
+        else:
+            _dense(lse, "lse", (a.batch, n_head, a.seq_len), (torch.float32,), qkv)
+        _check_noctx(lib().fal_window_attention_fwd(byref(a), qkv.data_ptr(), _ptr(lens), out.data_ptr(),
+                                                    lse.data_ptr(), stream))
+    return out, lse
+
+
+def window_attention_bwd(qkv, out, dout, lse, n_head, window, sinks=0, n_kv_head=0, lens=None, dqkv=None):
+    """Gradient of window_attention_fwd with respect to qkv, from the out and
+    lse it returned and the gradient of out (rows spaced as out's).  dqkv, if
+    given, has rows spaced as qkv's or dense ones; returned."""
+    import torch
+    a = _window_shape(qkv, n_head, n_kv_head, window, sinks, lens)
+    _window_rows(out, "out", qkv, (a.batch, a.seq_len, n_head * a.head_dim), None)
+    a.ld_out = _row_stride(out, "out")
+    _window_rows(dout, "dout", qkv, tuple(out.shape), a.ld_out)
+    _dense(lse, "lse", (a.batch, n_head, a.seq_len), (torch.float32,), qkv)
+    with _call(qkv) as stream:
+        if dqkv is None:
+            dqkv = torch.empty(qkv.shape, dtype=qkv.dtype, device=qkv.device)
+        _window_rows(dqkv, "dqkv", qkv, tuple(qkv.shape), None)
+        ws = _workspace(lib().fal_window_attention_workspace_bytes, a, qkv)
+        _check_noctx(lib().fal_window_attention_bwd(byref(a), qkv.data_ptr(), _ptr(lens), out.data_ptr(),
+                                                    dout.data_ptr(), lse.data_ptr(), dqkv.data_ptr(),
+                                                    _row_stride(dqkv, "dqkv"), ws.data_ptr(), ws.numel(), stream))
+    return dqkv
+
+
+def _logit_rows(logits, targets, mask, vocab, temperature):
+    import torch
+    _need(logits.dim() == 3, "logits must be [B, T, vocab]")
+    B, T, width = logits.shape
+    V = width if vocab is None else vocab
+    _need(1 <= V <= width, "vocab must lie in [1, logits' last dimension]")
+    code = _dtype_code(logits, "logits")
+    _need(targets.dtype == torch.int32 and tuple(targets.shape) == (B, T) and targets.device == logits.device,
+          "targets must be int32 [B, T] on the logits' device")
+    _need(T == 1 or targets.stride(1) == 1, "targets must be contiguous in their last dimension")
+    if mask is not None:
+        _dense(mask, "mask", (B, T), (torch.bool, torch.uint8), logits)
+    ld = _row_stride(logits, "logits")
+    return fal_logit_rows_t(B, T, V, code, ld, targets.stride(0) if B > 1 else T, ld, width, temperature)
+
+
+def token_logprobs(logits, targets, mask=None, vocab=None, temperature=1.0, entropy=False):
+    """Log-probability of targets (int32 [B, T]) under softmax(logits /
+    temperature), float32 [B, T], zero where mask (bool or uint8 [B, T]) is
+    zero; with entropy=True also the entropy of each row's softmax
+    (fal_token_logprobs).  logits: [B, T, >= vocab], bfloat16 or float32."""
+    import torch
+    r = _logit_rows(logits, targets, mask, vocab, temperature)
+    with _call(logits) as stream:
+        logp = torch.empty(r.batch, r.seq_len, dtype=torch.float32, device=logits.device)
+        ent = torch.empty_like(logp) if entropy else None
+        _check_noctx(lib().fal_token_logprobs(byref(r), logits.data_ptr(), targets.data_ptr(), _ptr(mask),
+                                              logp.data_ptr(), _ptr(ent), stream))
+    return (logp, ent) if entropy else logp
+
+
+def _gradient_rows(r, logits, dlogits):
+    """The gradient's buffer: as wide as the logits and spaced as they are."""
+    import torch
+    if dlogits is None:
+        ld = r.ld_logits if r.ld_logits < r.dlogits_cols + 64 else r.dlogits_cols
+        dlogits = torch.empty(r.batch, r.seq_len, ld, dtype=logits.dtype, device=logits.device)
+        dlogits = dlogits[:, :, :r.dlogits_cols]
+    _need(dlogits.dtype == logits.dtype and dlogits.device == logits.device and dlogits.shape == logits.shape,
+          "dlogits must have the logits' shape, dtype and device")
+    r.ld_dlogits = _row_stride(dlogits, "dlogits")
+    return dlogits
+
+
+def policy_loss(logits, targets, old_logp, advantages, ref_logp=None, mask=None, vocab=None, dlogits=None, *,
+                clip_low=0.2, clip_high=0.2, kl_coef=0.0, sequence_mean=False, temperature=1.0):
+    """Clipped policy loss with a KL term, and its gradient with respect to
+    the logits (fal_policy_loss): old_logp, advantages and ref_logp are float32
+    [B, T].  The gradient has the logits' shape, zero in the columns past vocab
+    and in rows that do not count; dlogits may be the logits themselves."""
+    import torch
+    r = _logit_rows(logits, targets, mask, vocab, temperature)
+    for name, t in (("old_logp", old_logp), ("advantages", advantages), ("ref_logp", ref_logp)):
+        if t is not None or name != "ref_logp":
+            _dense(t, name, (r.batch, r.seq_len), (torch.float32,), logits)
+    hp = fal_policy_t(clip_low, clip_high, kl_coef, int(sequence_mean))
+    with _call(logits) as stream:
+        dlogits = _gradient_rows(r, logits, dlogits)
+        stats = torch.empty(4, dtype=torch.float32, device=logits.device)
+        logp = torch.empty(r.batch, r.seq_len, dtype=torch.float32, device=logits.device)
+        ws = _workspace(lib().fal_logit_loss_workspace_bytes, r, logits)
+        _check_noctx(lib().fal_policy_loss(byref(r), byref(hp), logits.data_ptr(), targets.data_ptr(), _ptr(mask),
+                                           old_logp.data_ptr(), _ptr(ref_logp), advantages.data_ptr(),
+                                           stats.data_ptr(), logp.data_ptr(), dlogits.data_ptr(), ws.data_ptr(),
+                                           ws.numel(), stream))
+    return PolicyLoss(stats, logp, dlogits)
+
+
+def preference_loss(logits, targets, ref_logp, mask=None, vocab=None, dlogits=None, *, beta=0.1, label_smoothing=0.0,
+                    ipo=False, length_mean=False, temperature=1.0):
+    """Preference loss over the pairs (b, b + B/2) of which the first is
+    preferred, and its gradient with respect to the logits
+    (fal_preference_loss): ref_logp is float32 [B], the reference model's
+    log-probability of each sequence."""
+    import torch
+    r = _logit_rows(logits, targets, mask, vocab, temperature)
+    _dense(ref_logp, "ref_logp", (r.batch,), (torch.float32,), logits)
+    hp = fal_preference_t(beta, label_smoothing, int(ipo), int(length_mean))
+    with _call(logits) as stream:
+        dlogits = _gradient_rows(r, logits, dlogits)
+        loss = torch.empty(1, dtype=torch.float32, device=logits.device)
+        seq_logp = torch.empty(r.batch, dtype=torch.float32, device=logits.device)
+        ws = _workspace(lib().fal_logit_loss_workspace_bytes, r, logits)
+        _check_noctx(lib().fal_preference_loss(byref(r), byref(hp), logits.data_ptr(), targets.data_ptr(), _ptr(mask),
+                                               ref_logp.data_ptr(), loss.data_ptr(), seq_logp.data_ptr(),
+                                               dlogits.data_ptr(), ws.data_ptr(), ws.numel(), stream))
+    return PreferenceLoss(loss, seq_logp, dlogits)
 
 
 class Fal:
@@ -299,6 +582,64 @@ class Fal:
                                    c_void_p(dx_in.data_ptr()),
                                    c_void_p(dfirst.data_ptr()) if dfirst is not None else None,
                                    c_void_p(self.block_grad_ptr(layer))), self.ctx)
+
+    # ------------------------------------------- window, tuning losses --
+    def set_attention_window(self, window, sinks=0):
+        """Every later forward and backward attends causally over the last
+        `window` keys and the first `sinks`; window 0 restores the full mask."""
+        window, sinks = (max(-1, min(int(n), 2 ** 31 - 1)) for n in (window, sinks))
+        _check(lib().fal_set_attention_window(self.ctx, window, sinks), self.ctx)
+
+    def _token_arrays(self, tokens, mask, **arrays):
+        torch = self.torch
+        B, T = self.cfg.batch, self.cfg.seq_len
+        _dense(tokens, "tokens", (B, T + 1), (torch.int32,), self.params)
+        if mask is not None:
+            _dense(mask, "mask", (B, T), (torch.bool, torch.uint8), self.params)
+        for name, t in arrays.items():
+            if t is not None:
+                _dense(t, name, (B,) if name == "ref_seq_logp" else (B, T), (torch.float32,), self.params)
+
+    def model_logprobs(self, tokens, mask=None, temperature=1.0, entropy=False):
+        """Log-probabilities of tokens[:, 1:] under the model, float32 [B, T]
+        (zero where mask, over the T predicted tokens, is zero); with
+        entropy=True also the entropies."""
+        torch = self.torch
+        self._token_arrays(tokens, mask)
+        logp = torch.empty(self.cfg.batch, self.cfg.seq_len, dtype=torch.float32, device=self.device)
+        ent = torch.empty_like(logp) if entropy else None
+        _check(lib().fal_model_logprobs(self.ctx, self.params.data_ptr(), tokens.data_ptr(), _ptr(mask), temperature,
+                                        logp.data_ptr(), _ptr(ent)), self.ctx)
+        return (logp, ent) if entropy else logp
+
+    def policy_step(self, tokens, old_logp, advantages, ref_logp=None, mask=None, *, clip_low=0.2, clip_high=0.2,
+                    kl_coef=0.0, sequence_mean=False, temperature=1.0):
+        """Forward, clipped policy loss over tokens[:, 1:] and backward: fills
+        self.grads and returns the stats of policy_loss (float32 [4]) and the
+        log-probabilities (float32 [B, T])."""
+        torch = self.torch
+        self._token_arrays(tokens, mask, old_logp=old_logp, advantages=advantages, ref_logp=ref_logp)
+        hp = fal_policy_t(clip_low, clip_high, kl_coef, int(sequence_mean))
+        stats = torch.empty(4, dtype=torch.float32, device=self.device)
+        logp = torch.empty(self.cfg.batch, self.cfg.seq_len, dtype=torch.float32, device=self.device)
+        _check(lib().fal_policy_step(self.ctx, self.params.data_ptr(), byref(hp), tokens.data_ptr(), _ptr(mask),
+                                     temperature, _ptr(old_logp), _ptr(ref_logp), _ptr(advantages), stats.data_ptr(),
+                                     logp.data_ptr(), self.grads.data_ptr()), self.ctx)
+        return stats, logp
+
+    def preference_step(self, tokens, ref_logp, mask=None, *, beta=0.1, label_smoothing=0.0, ipo=False,
+                        length_mean=False, temperature=1.0):
+        """Forward, preference loss over the pairs (b, b + B/2) of tokens[:,
+        1:] and backward: fills self.grads and returns the loss (self.loss)
+        and the sequences' log-probabilities (float32 [B])."""
+        torch = self.torch
+        self._token_arrays(tokens, mask, ref_seq_logp=ref_logp)
+        hp = fal_preference_t(beta, label_smoothing, int(ipo), int(length_mean))
+        seq_logp = torch.empty(self.cfg.batch, dtype=torch.float32, device=self.device)
+        _check(lib().fal_preference_step(self.ctx, self.params.data_ptr(), byref(hp), tokens.data_ptr(), _ptr(mask),
+                                         temperature, _ptr(ref_logp), self.loss.data_ptr(), seq_logp.data_ptr(),
+                                         self.grads.data_ptr()), self.ctx)
+        return self.loss, seq_logp
 
     # ----------------------------------------------------------- optimizer --
     def init_optimizer(self):
