@@ -39,6 +39,11 @@ namespace fal {
 
 namespace {
 
+// Kernels whose registers leave one or two wavefronts to a SIMD keep the LDS
+// reads of the next four MFMAs in flight.
+template <typename S, int HD>
+constexpr bool kAhead = HD == 128 && sizeof(S) == 2;
+
 template <int HD>
 constexpr int n_tiles() { return HD < 32 ? 1 : HD / 32; }
 
@@ -63,17 +68,55 @@ struct Stage {
     for (int k = 0; k < N; ++k) {
       const int i = tid + 256 * k;
       const int row = min(row0 + i / CH, n - 1);
-      if (i < AT * CH) v[k] = *reinterpret_cast<const uint4*>(src + (int64_t)row * ld + E * (i % CH));
+      if (256 * (k + 1) <= AT * CH || i < AT * CH)
+        v[k] = *reinterpret_cast<const uint4*>(src + (int64_t)row * ld + E * (i % CH));
     }
   }
-  __device__ __forceinline__ void store(S* s, int row0, int n, int tid) const {
+  __device__ __forceinline__ void store(S* s, int row0, int n, int tid) {
+    if (row0 + AT > n) {  // the sequence's last tile
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const uint32_t keep = row0 + (tid + 256 * k) / CH < n ? ~0u : 0u;
+        v[k].x &= keep; v[k].y &= keep; v[k].z &= keep; v[k].w &= keep;
+      }
+    }
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const int i = tid + 256 * k;
-      if (i >= AT * CH) continue;
-      const int r = i / CH;
-      *reinterpret_cast<uint4*>(s + row_off<HD>(s, r) + E * (i % CH)) = row0 + r < n ? v[k] : make_uint4(0, 0, 0, 0);
+      if (256 * (k + 1) <= AT * CH || i < AT * CH)
+        *reinterpret_cast<uint4*>(s + row_off<HD>(s, i / CH) + E * (i % CH)) = v[k];
     }
+  }
+};
+
+// The window's mask over a 32x32 score tile whose tile rows are keys: row `off`
+// (from the lane half's first) is hidden from the lane's query if it lies
+// after it, or before its window and past the sinks.  No branches: the three
+// comparisons join in the scalar unit.
+struct KeyMask {
+  int last, before, sink;
+  __device__ __forceinline__ KeyMask(const WindowAttn& a, int kb, int g, int tq, int n) {
+    const int key0 = kb + 4 * g;
+    last = min(tq, n - 1) - key0;
+    before = tq - a.window - key0;
+    sink = a.sinks - key0;
+  }
+  __device__ __forceinline__ bool hides(int r) const {
+    const int off = acc_row(r, 0);
+    return (bool)((off > last) | ((off <= before) & (off >= sink)));
+  }
+};
+// The same where tile rows are queries and the lane has the key.
+struct QueryMask {
+  int first, past;
+  __device__ __forceinline__ QueryMask(const WindowAttn& a, int qs, int g, int key) {
+    const int q0 = qs + 4 * g;
+    first = key - q0;
+    past = key < a.sinks ? 1 << 30 : key + a.window - q0;
+  }
+  __device__ __forceinline__ bool hides(int r) const {
+    const int off = acc_row(r, 0);
+    return (bool)((off < first) | (off >= past));
   }
 };
 
@@ -221,7 +264,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
   const S* Qg = qkv + (int64_t)b * a.T * a.ldq + h * HD;
   const S* Kg = qkv + (int64_t)b * a.T * a.ldq + (a.H + kvh) * HD;
   const S* Vg = Kg + a.Hkv * HD;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, c = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
   const int q0 = qb + wave * 32, tq = q0 + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
@@ -259,11 +302,9 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
         f32x16v s = zero16();
         dot_rows<HD>(sK, 32 * sub, c, g, q, s);
         if (kb + 31 > q0 || kb + 31 >= n || q0 + 31 - kb >= a.window) {
+          const KeyMask mask(a, kb, g, tq, n);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = kb + acc_row(r, g);
-            if (key > tq || key >= n || (tq - key >= a.window && key >= a.sinks)) s[r] = -INFINITY;
-          }
+          for (int r = 0; r < 16; ++r) s[r] = mask.hides(r) ? -INFINITY : s[r];
         }
         float mx = s[0];
 #pragma unroll
@@ -312,7 +353,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq(WindowAttn a, const S* 
   const int64_t row0 = (int64_t)b * a.T;
   const S* Kg = qkv + row0 * a.ldq + (a.H + kvh) * HD;
   const S* Vg = Kg + a.Hkv * HD;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, c = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
   const int q0 = qb + wave * 32, tq = q0 + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
@@ -355,16 +396,20 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq(WindowAttn a, const S* 
         f32x16v s = zero16(), dp = zero16();
         dot_rows<HD>(sK, 32 * sub, c, g, q, s);
         dot_rows<HD>(sV, 32 * sub, c, g, d, dp);
-        // keys past n are rows of zeros: their dS multiplies a zero key
-        const bool edge = kb + 31 > q0 || q0 + 31 - kb >= a.window;
+        if (kAhead<S, HD>) lds_ahead<HD / 8, 1, 4>();
+        if (kb + 31 > q0 || kb + 31 >= n || q0 + 31 - kb >= a.window) {
+          const KeyMask mask(a, kb, g, tq, n);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = mask.hides(r) ? -INFINITY : s[r];
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int key = kb + acc_row(r, g);
-          float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -L2));
-          if (edge && (key > tq || (tq - key >= a.window && key >= a.sinks))) p = 0.f;
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -L2));
           dp[r] = p * (dp[r] - D);
         }
+        if (kAhead<S, HD>) __builtin_amdgcn_sched_barrier(0);
         add_rows<HD>(sK, 32 * sub, lane, dp, dq);
+        if (kAhead<S, HD>) lds_ahead<HD / 16, 2, 4>();
       }
     }
   }
@@ -394,7 +439,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_sinks(Wind
   const S* dOg = dO + row0 * a.lddo + h * HD;
   const float* Lg = lse + ((int64_t)b * a.H + h) * a.T;
   const float* Dg = Dvec + ((int64_t)b * a.H + h) * a.T;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, c = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
   const int n = length_of(a, b), key = kw + c;
   const int qbeg = far + ck * chunk, qend = min(n, qbeg + chunk);
   const float sl2 = kLog2e / sqrtf((float)HD);
@@ -433,8 +478,8 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_sinks(Wind
       for (int r = 0; r < 16; ++r) {
         const int qr = 32 * sub + acc_row(r, g);
         const float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[qr]));
-        s[r] = key < a.sinks ? p : 0.f;
-        dp[r] = key < a.sinks ? p * (dp[r] - sD[qr]) : 0.f;
+        s[r] = p;
+        dp[r] = p * (dp[r] - sD[qr]);
       }
       add_rows<HD>(sdO, 32 * sub, lane, s, dv);
       add_rows<HD>(sQ, 32 * sub, lane, dp, dk);
@@ -475,7 +520,7 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_dkdv(Windo
   const int kvh = blockIdx.x, b = blockIdx.y, kb0 = 128 * blockIdx.z, grp = a.H / a.Hkv;
   const int64_t row0 = (int64_t)b * a.T;
   const S* Kg = qkv + row0 * a.ldq + (a.H + kvh) * HD;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, c = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
   const int kw = kb0 + wave * 32, key = kw + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
@@ -522,18 +567,24 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_dkdv(Windo
         f32x16v s = zero16(), dp = zero16();
         dot_rows<HD>(sQ, 32 * sub, c, g, k, s);
         dot_rows<HD>(sdO, 32 * sub, c, g, v, dp);
+        if (kAhead<S, HD>) lds_ahead<HD / 8, 1, 4>();
         // queries past n have zero Q, dO, L and D: they add nothing
-        const bool edge = qs < kw + 32 || qs + 31 - kw >= a.window;
+        if (qs < kw + 32 || qs + 31 - kw >= a.window) {
+          const QueryMask mask(a, qs, g, key);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = mask.hides(r) ? -INFINITY : s[r];
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int qr = 32 * sub + acc_row(r, g), tq = q0 + qr;
-          float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[qr]));
-          if (edge && (key > tq || (tq - key >= a.window && key >= a.sinks))) p = 0.f;
+          const int qr = 32 * sub + acc_row(r, g);
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[qr]));
           s[r] = p;
           dp[r] = p * (dp[r] - sD[qr]);
         }
+        if (kAhead<S, HD>) __builtin_amdgcn_sched_barrier(0);
         add_rows<HD>(sdO, 32 * sub, lane, s, dv);
         add_rows<HD>(sQ, 32 * sub, lane, dp, dk);
+        if (kAhead<S, HD>) lds_ahead<HD / 8, 2, 4>();
       }
     }
     if (part && key < a.sinks) {

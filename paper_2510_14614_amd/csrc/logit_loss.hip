@@ -57,6 +57,8 @@ struct Chunk<float> {
   }
 };
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 // A row of `cols` elements seen through aligned chunks: element 0 is element
 // `shift` of chunk 0.
 template <typename S, typename P>
@@ -72,8 +74,14 @@ struct Row {
   __device__ __forceinline__ int chunks() const { return (shift + cols + E - 1) / E; }
   __device__ __forceinline__ int column(int c) const { return c * E - shift; }
   __device__ __forceinline__ bool inside(int c) const { return column(c) >= 0 && column(c) + E <= cols; }
+  // ONCE: nothing reads the chunk again, so it need not stay in a cache
+  template <bool ONCE>
   __device__ __forceinline__ uint4 load(int c) const {
-    if (inside(c)) return *reinterpret_cast<const uint4*>(base + (int64_t)c * E);
+    if (inside(c)) {
+      const u32x4* p = reinterpret_cast<const u32x4*>(base + (int64_t)c * E);
+      const u32x4 q = ONCE ? __builtin_nontemporal_load(p) : *p;
+      return make_uint4(q.x, q.y, q.z, q.w);
+    }
     float v[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -82,9 +90,12 @@ struct Row {
     }
     return Chunk<S>::of(v);
   }
+  // stores pass by the caches: a gradient is larger than they are, and what
+  // they hold of the logits is still to be read
   __device__ __forceinline__ void store(int c, const float (&v)[E]) const {
     if (inside(c)) {
-      *reinterpret_cast<uint4*>(base + (int64_t)c * E) = Chunk<S>::of(v);
+      const uint4 q = Chunk<S>::of(v);
+      __builtin_nontemporal_store(u32x4{q.x, q.y, q.z, q.w}, reinterpret_cast<u32x4*>(base + (int64_t)c * E));
       return;
     }
 #pragma unroll
@@ -140,7 +151,7 @@ __device__ __forceinline__ void chunk_add(const uint4& u, Stat& st, float k) {
 struct Shared {
   Stat st;
   float target;  // the target's logit
-  int count;     // counted rows of the whole batch (policy, mean over rows)
+  int count;     // the sum of the threads' counts
 };
 
 // Joins the statistics of the G threads of a row (and sums their counts);
@@ -179,6 +190,8 @@ __device__ __forceinline__ int target_of(const LogitRows& r, int b, int t) {
   return min(max(r.targets[(int64_t)b * r.ldt + t], 0), r.V - 1);
 }
 
+constexpr int kStream = 4;  // chunks in flight of a row that is not held
+
 // ---- a row's gradient -------------------------------------------------------
 // out chunk c from logits chunk c of the same shift: zero past V.
 template <typename S>
@@ -200,6 +213,26 @@ __device__ __forceinline__ void grad_chunk(const uint4& u, int col0, int V, int 
 #pragma unroll
     for (int e = 0; e < E; ++e)
       if (col0 + e >= 0 && col0 + e < V) out.base[out.shift + col0 + e] = from_f<S>(v[e]);
+  }
+}
+
+// the chunks t, t + G, ... of a row's gradient, read from its logits
+template <typename S, int G, bool ONCE>
+__device__ __forceinline__ void row_grad(const Row<S, const S>& in, const Row<S, S>& out, int t, int end, int tgt,
+                                         float k, float top, float log2sum, float scale) {
+  const int nc = in.chunks();
+  for (int c0 = t; c0 < end; c0 += kStream * G) {
+    uint4 u[kStream];
+#pragma unroll
+    for (int i = 0; i < kStream; ++i) {
+      u[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (c0 + G * i < nc) u[i] = in.template load<ONCE>(c0 + G * i);
+    }
+#pragma unroll
+    for (int i = 0; i < kStream; ++i) {
+      const int c = c0 + G * i;
+      if (c < end) grad_chunk<S>(u[i], in.column(c), in.cols, tgt, k, top, log2sum, scale, out, c);
+    }
   }
 }
 
@@ -273,12 +306,13 @@ __global__ __launch_bounds__(256) void mask_counts(const uint8_t* mask, int T, i
 }
 
 // ------------------------------------------------------------ row kernels --
-enum Mode { LOGP, LOGP_ENTROPY, POLICY };
+// STATS: log-probabilities, with what preference_rows needs of each row.
+enum Mode { LOGP, LOGP_ENTROPY, STATS, POLICY };
 struct RowOut {
   float *logp, *entropy;  // [B, T], each may be NULL
-  float *top, *log2sum;   // [B, T] or NULL: a row's largest logit, and log2 of its sum relative to it
+  float *top, *log2sum;   // STATS, [B, T]: a row's largest logit, and log2 of its sum relative to it
   PolicyArgs p;
-  const int32_t* count;  // counted rows of each sequence (NULL: T)
+  const int32_t* count;  // POLICY: counted rows of each sequence; NULL: each row's threads count the mask
   float* terms;          // [3][B * T]
   void* dlogits;
 };
@@ -308,9 +342,18 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
   const int nc = in.chunks(), b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T));
   const float k = r.inv_temp * kLog2e;
   const float xt = t == 0 ? to_f(l[tgt]) : 0.f;
-  int n = 0;
-  if (MODE == POLICY && o.count && !o.p.sequence_mean)
-    for (int i = t; i < r.B; i += G) n += o.count[i];
+  int n = 0;  // this thread's share of the counted rows that the mean is over
+  if (MODE == POLICY && r.mask) {
+    if (!o.count) {
+      const uint8_t* mask = o.p.sequence_mean ? r.mask + (int64_t)b * r.T : r.mask;
+      const int64_t len = o.p.sequence_mean ? r.T : N;
+      for (int64_t i = t; i < len; i += G) n += mask[i] != 0;
+    } else if (o.p.sequence_mean) {
+      n = t == 0 ? o.count[b] : 0;
+    } else {
+      for (int i = t; i < r.B; i += G) n += o.count[i];
+    }
+  }
 
   uint4 raw[NPT ? NPT : 1];
   Stat st{-INFINITY, 0.f, 0.f};
@@ -318,7 +361,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
 #pragma unroll
     for (int i = 0; i < NPT; ++i) {
       const int c = t + G * i;
-      if (c < nc) raw[i] = in.load(c);
+      if (c < nc) raw[i] = in.template load<MODE != STATS>(c);
     }
 #pragma unroll
     for (int i = 0; i < NPT; ++i)
@@ -329,14 +372,24 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
         if (t + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(raw[i], st, k);
     }
   } else {
-    for (int c = t; c < nc; c += G) {
-      const uint4 u = in.load(c);
-      const float top = chunk_max<S>(u, -INFINITY);
+    for (int c0 = t; c0 < nc; c0 += kStream * G) {
+      uint4 u[kStream];
+#pragma unroll
+      for (int i = 0; i < kStream; ++i)
+        if (c0 + G * i < nc) u[i] = in.template load<MODE == LOGP || MODE == LOGP_ENTROPY>(c0 + G * i);
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kStream; ++i)
+        if (c0 + G * i < nc) top = chunk_max<S>(u[i], top);
       if (top > st.m) {
         const Stat none{top, 0.f, 0.f};
         join(st, none, k);
       }
-      if (st.m != -INFINITY) chunk_add<S, MODE == LOGP_ENTROPY>(u, st, k);
+      if (st.m != -INFINITY) {
+#pragma unroll
+        for (int i = 0; i < kStream; ++i)
+          if (c0 + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(u[i], st, k);
+      }
     }
   }
   const Shared sh = exchange<G>(st, xt, n, k);
@@ -344,16 +397,15 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
   const float lp = ((sh.target - sh.st.m) * k - log2sum) * kLn2;
   if (t == 0) {
     if (o.logp) o.logp[m] = lp;
-    if (MODE == LOGP && o.top) {
+    if (MODE == STATS) {
       o.top[m] = sh.st.m;
       o.log2sum[m] = log2sum;
     }
     if (MODE == LOGP_ENTROPY) o.entropy[m] = (log2sum - sh.st.dot / sh.st.sum) * kLn2;
   }
   if (MODE != POLICY) return;
-  const float rows = o.p.sequence_mean ? (float)r.B * (float)(o.count ? o.count[b] : r.T)
-                                       : (float)(o.count ? (int64_t)sh.count : N);
-  const float w = 1.f / rows;
+  const float rows = r.mask ? (float)sh.count : (float)(o.p.sequence_mean ? (int64_t)r.T : N);
+  const float w = 1.f / (o.p.sequence_mean ? rows * (float)r.B : rows);
   const PolicyRow pr = policy_row(o.p, m, lp);
   if (t == 0) {
     o.terms[m] = w * pr.pg;
@@ -363,44 +415,46 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
   const float scale = pr.c * w * r.inv_temp;
   const bool same = in.shift == out.shift;
   const int end = same ? out.chunks() : nc;
-  const uint4 none = [] {
-    float v[Chunk<S>::E];
-#pragma unroll
-    for (int e = 0; e < Chunk<S>::E; ++e) v[e] = -INFINITY;
-    return Chunk<S>::of(v);
-  }();
   if (NPT) {
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);  // columns past V: any value
 #pragma unroll
     for (int i = 0; i < NPT; ++i) {
       const int c = t + G * i;
       if (c < end) grad_chunk<S>(c < nc ? raw[i] : none, in.column(c), r.V, tgt, k, sh.st.m, log2sum, scale, out, c);
     }
   } else {
-    for (int c = t; c < end; c += G)
-      grad_chunk<S>(c < nc ? in.load(c) : none, in.column(c), r.V, tgt, k, sh.st.m, log2sum, scale, out, c);
+    row_grad<S, G, false>(in, out, t, end, tgt, k, sh.st.m, log2sum, scale);
   }
   if (!same) zero_tail<S, G>(out, r.V, t);
 }
 
-__device__ __forceinline__ double block_total(double v, double* red) {
+// Sums K doubles over a workgroup of W wavefronts; every thread gets them.
+template <int K, int W>
+__device__ __forceinline__ void block_totals(double (&v)[K]) {
+  __shared__ double red[W][K];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o, FAL_WAVE);
+  if (threadIdx.x % FAL_WAVE == 0)
+#pragma unroll
+    for (int k = 0; k < K; ++k) red[threadIdx.x / FAL_WAVE][k] = v[k];
   __syncthreads();
-  red[threadIdx.x] = v;
-  __syncthreads();
-  for (int w = blockDim.x / 2; w > 0; w >>= 1) {
-    if ((int)threadIdx.x < w) red[threadIdx.x] += red[threadIdx.x + w];
-    __syncthreads();
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    v[k] = red[0][k];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v[k] += red[w][k];
   }
-  return red[0];
 }
 
 __global__ __launch_bounds__(1024) void policy_total(const float* terms, int64_t N, float kl_coef, float* stats) {
-  __shared__ double red[1024];
-  double tot[3];
-  for (int k = 0; k < 3; ++k) {
-    double s = 0.0;
-    for (int64_t i = threadIdx.x; i < N; i += 1024) s += terms[k * N + i];
-    tot[k] = block_total(s, red);
-  }
+  double tot[3] = {0.0, 0.0, 0.0};
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < N; i += 1024)
+#pragma unroll
+    for (int k = 0; k < 3; ++k) tot[k] += terms[k * N + i];
+  block_totals<3, 16>(tot);
   if (threadIdx.x == 0) {
     stats[0] = (float)(tot[0] + (double)kl_coef * tot[1]);
     for (int k = 0; k < 3; ++k) stats[1 + k] = (float)tot[k];
@@ -411,23 +465,22 @@ __global__ __launch_bounds__(1024) void policy_total(const float* terms, int64_t
 // A pair's loss and each of its sequences' coefficient of a counted row.
 __global__ __launch_bounds__(256) void preference_pairs(LogitRows r, PreferenceArgs p, const float* logp, float* coef,
                                                         double* pair_loss) {
-  __shared__ double red[256];
   const int P = r.B / 2, b0 = blockIdx.x;
+  double v[4] = {0.0, 0.0, 0.0, 0.0};  // sums and counted rows of both sequences
+  for (int t = threadIdx.x; t < r.T; t += 256)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int64_t m = (int64_t)(b0 + k * P) * r.T + t;
+      v[k] += logp[m];  // 0 where the row does not count
+      v[2 + k] += counted(r, m) ? 1.0 : 0.0;
+    }
+  block_totals<4, 4>(v);
   double gain[2], share[2];
   for (int k = 0; k < 2; ++k) {
-    const int64_t m0 = (int64_t)(b0 + k * P) * r.T;
-    double s = 0.0, n = 0.0;
-    for (int t = threadIdx.x; t < r.T; t += 256)
-      if (counted(r, m0 + t)) {
-        s += logp[m0 + t];
-        n += 1.0;
-      }
-    s = block_total(s, red);
-    n = block_total(n, red);
-    share[k] = p.length_mean ? 1.0 / fmax(n, 1.0) : 1.0;
-    s *= share[k];
-    if (threadIdx.x == 0 && p.seq_logp) p.seq_logp[b0 + k * P] = (float)s;
-    gain[k] = s - p.ref_logp[b0 + k * P];
+    share[k] = p.length_mean ? 1.0 / fmax(v[2 + k], 1.0) : 1.0;
+    gain[k] = v[k] * share[k];
+    if (threadIdx.x == 0 && p.seq_logp) p.seq_logp[b0 + k * P] = (float)gain[k];
+    gain[k] -= p.ref_logp[b0 + k * P];
   }
   if (threadIdx.x != 0) return;
   const double h = gain[0] - gain[1], beta = p.beta, sm = p.smoothing;
@@ -447,10 +500,18 @@ __global__ __launch_bounds__(256) void preference_pairs(LogitRows r, PreferenceA
 }
 
 template <typename S, int G>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void preference_rows(LogitRows r, const float* coef, const float* top,
-                                                                     const float* log2sum, S* dl) {
+__global__ __launch_bounds__(G < 256 ? 256 : G) void preference_rows(LogitRows r, const double* pair_loss,
+                                                                     const float* coef, const float* top,
+                                                                     const float* log2sum, S* dl, float* loss) {
   constexpr int RPW = (G < 256 ? 256 : G) / G;
   const int64_t N = (int64_t)r.B * r.T, m = (int64_t)blockIdx.x * RPW + threadIdx.x / G;
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x < FAL_WAVE) {  // the mean over pairs
+    double s = 0.0;
+    for (int i = threadIdx.x; i < r.B / 2; i += FAL_WAVE) s += pair_loss[i];
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, FAL_WAVE);
+    if (threadIdx.x == 0) *loss = (float)(s / (r.B / 2));
+  }
   if (RPW > 1 && m >= N) return;
   const int t = threadIdx.x % G;
   const Row<S, S> out(dl + m * r.ldd, r.width);
@@ -459,24 +520,12 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void preference_rows(LogitRows r
     return;
   }
   const Row<S, const S> in(static_cast<const S*>(r.logits) + m * r.ldl, r.V);
-  const int b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T)), nc = in.chunks();
+  const int b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T));
   const float k = r.inv_temp * kLog2e, scale = coef[b] * r.inv_temp, mx = top[m], ls = log2sum[m];
   const bool same = in.shift == out.shift;
-  const int end = same ? out.chunks() : nc;
-  for (int c = t; c < end; c += G) {
-    uint4 u = make_uint4(0u, 0u, 0u, 0u);
-    if (c < nc) u = in.load(c);
-    grad_chunk<S>(u, in.column(c), r.V, tgt, k, mx, ls, scale, out, c);
-  }
+  const int end = same ? out.chunks() : in.chunks();
+  row_grad<S, G, true>(in, out, t, end, tgt, k, mx, ls, scale);
   if (!same) zero_tail<S, G>(out, r.V, t);
-}
-
-__global__ __launch_bounds__(256) void preference_total(const double* pair_loss, int P, float* loss) {
-  __shared__ double red[256];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < P; i += 256) s += pair_loss[i];
-  s = block_total(s, red);
-  if (threadIdx.x == 0) *loss = (float)(s / P);
 }
 
 // ------------------------------------------------------------- launching --
@@ -488,36 +537,57 @@ hipError_t launch(const LogitRows& r, const RowOut& o, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The threads of a row: enough that none holds more than eight chunks, up to
-// a workgroup of 1024 that holds sixteen each; longer rows are read twice.
+// Rows that are only scored are streamed: held or not, they are read once.
+// 256 threads keep enough loads in flight and leave a compute unit several
+// rows (8192 rows of 50257 bf16, half of them counted, with entropy: 78 us
+// against 85 with 512 threads and 127 with 1024); while the rows are fewer
+// than the chip has places for such workgroups, 1024 threads shorten each
+// (128 rows: 5.4 us against 8.1).
 template <typename S, Mode MODE>
-hipError_t rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
-  constexpr int E = Chunk<S>::E;
-  const int cols = MODE == POLICY ? r.width : r.V;
-  const int n = (cols + 2 * (E - 1)) / E;  // chunks of a row at any alignment
-  if (n <= 64) return launch<S, 64, 1, MODE>(r, o, s);
-  if (n <= 128) return launch<S, 64, 2, MODE>(r, o, s);
-  if (n <= 256) return launch<S, 64, 4, MODE>(r, o, s);
-  if (n <= 512) return launch<S, 64, 8, MODE>(r, o, s);
-  if (n <= 1024) return launch<S, 256, 4, MODE>(r, o, s);
-  if (n <= 2048) return launch<S, 256, 8, MODE>(r, o, s);
-  if (n <= 4096) return launch<S, 1024, 4, MODE>(r, o, s);
-  if (n <= 7168) return launch<S, 1024, 7, MODE>(r, o, s);
-  if (n <= 13312) return launch<S, 1024, 13, MODE>(r, o, s);
-  if (n <= 16384) return launch<S, 1024, 16, MODE>(r, o, s);
-  return launch<S, 1024, 0, MODE>(r, o, s);
+hipError_t scored_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
+  if (r.V <= 512 * Chunk<S>::E) return launch<S, 64, 0, MODE>(r, o, s);
+  if ((int64_t)r.B * r.T < 1024) return launch<S, 1024, 0, MODE>(r, o, s);
+  return launch<S, 256, 0, MODE>(r, o, s);
 }
 
+// Rows with a gradient are held by as few threads as can (up to 26 chunks
+// each, 16 in a workgroup of 1024, whose registers are half as many): several
+// rows then share a compute unit and one's exchange and stores pass under
+// another's loads (rows of 50257 bf16 as above: 273 us with 256 x 26, 314 with
+// 512 x 13, 338 with 1024 x 7; 50257 fp32: 238 with 1024 x 13, 247 with
+// 512 x 26).  Longer rows are read twice.
 template <typename S>
-hipError_t preference_grad(const LogitRows& r, const float* coef, const RowOut& o, S* dl, hipStream_t s) {
+hipError_t policy_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
+  constexpr int E = Chunk<S>::E;
+  const int n = (r.width + 2 * (E - 1)) / E;  // chunks of a row at any alignment
+  if (n <= 64) return launch<S, 64, 1, POLICY>(r, o, s);
+  if (n <= 128) return launch<S, 64, 2, POLICY>(r, o, s);
+  if (n <= 256) return launch<S, 64, 4, POLICY>(r, o, s);
+  if (n <= 512) return launch<S, 64, 8, POLICY>(r, o, s);
+  if (n <= 1024) return launch<S, 256, 4, POLICY>(r, o, s);
+  if (n <= 2048) return launch<S, 256, 8, POLICY>(r, o, s);
+  if (n <= 4096) return launch<S, 256, 16, POLICY>(r, o, s);
+  if (n <= 6656) return launch<S, 256, 26, POLICY>(r, o, s);
+  if (n <= 13312) return launch<S, 1024, 13, POLICY>(r, o, s);
+  if (n <= 16384) return launch<S, 1024, 16, POLICY>(r, o, s);
+  return launch<S, 1024, 0, POLICY>(r, o, s);
+}
+
+template <typename S, int G>
+hipError_t preference_grad(const LogitRows& r, const double* pair_loss, const float* coef, const RowOut& o, void* dl,
+                           float* loss, hipStream_t s) {
+  constexpr int WG = G < 256 ? 256 : G;
   const int64_t N = (int64_t)r.B * r.T;
-  if (r.width <= 8192)
-    hipLaunchKernelGGL((preference_rows<S, 64>), dim3((unsigned)((N + 3) / 4)), dim3(256), 0, s, r, coef, o.top,
-                       o.log2sum, dl);
-  else
-    hipLaunchKernelGGL((preference_rows<S, 1024>), dim3((unsigned)N), dim3(1024), 0, s, r, coef, o.top,
-                       o.log2sum, dl);
+  hipLaunchKernelGGL((preference_rows<S, G>), dim3((unsigned)((N + WG / G - 1) / (WG / G))), dim3(WG), 0, s, r,
+                     pair_loss, coef, o.top, o.log2sum, static_cast<S*>(dl), loss);
   return hipGetLastError();
+}
+template <typename S>
+hipError_t preference_grad(const LogitRows& r, const double* pair_loss, const float* coef, const RowOut& o, void* dl,
+                           float* loss, hipStream_t s) {
+  if (r.width <= 512 * Chunk<S>::E) return preference_grad<S, 64>(r, pair_loss, coef, o, dl, loss, s);
+  if (r.width <= 2048 * Chunk<S>::E) return preference_grad<S, 256>(r, pair_loss, coef, o, dl, loss, s);
+  return preference_grad<S, 1024>(r, pair_loss, coef, o, dl, loss, s);
 }
 
 }  // namespace
@@ -528,8 +598,8 @@ hipError_t token_logprobs(DType dt, const LogitRows& r, float* logp, float* entr
   RowOut o{};
   o.logp = logp;
   o.entropy = entropy;
-  if (dt == BF16) return entropy ? rows<bf16, LOGP_ENTROPY>(r, o, s) : rows<bf16, LOGP>(r, o, s);
-  return entropy ? rows<float, LOGP_ENTROPY>(r, o, s) : rows<float, LOGP>(r, o, s);
+  if (dt == BF16) return entropy ? scored_rows<bf16, LOGP_ENTROPY>(r, o, s) : scored_rows<bf16, LOGP>(r, o, s);
+  return entropy ? scored_rows<float, LOGP_ENTROPY>(r, o, s) : scored_rows<float, LOGP>(r, o, s);
 }
 
 hipError_t policy_loss(DType dt, const LogitRows& r, const PolicyArgs& p, void* dlogits, float* scratch,
@@ -540,12 +610,15 @@ hipError_t policy_loss(DType dt, const LogitRows& r, const PolicyArgs& p, void* 
   o.p = p;
   o.terms = scratch;
   o.dlogits = dlogits;
-  if (r.mask) {
+  // the rows' threads count the mask themselves while that is a few bytes
+  // each, which saves a launch
+  const int64_t span = p.sequence_mean ? r.T : N;
+  if (r.mask && span > 16 * (r.width > 512 * (dt == BF16 ? 8 : 4) ? 256 : 64)) {
     int32_t* count = reinterpret_cast<int32_t*>(scratch + 3 * N);
     hipLaunchKernelGGL(mask_counts, dim3(r.B), dim3(256), 0, s, r.mask, r.T, count);
     o.count = count;
   }
-  const hipError_t e = dt == BF16 ? rows<bf16, POLICY>(r, o, s) : rows<float, POLICY>(r, o, s);
+  const hipError_t e = dt == BF16 ? policy_rows<bf16>(r, o, s) : policy_rows<float>(r, o, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(policy_total, dim3(1), dim3(1024), 0, s, scratch, N, p.kl, p.stats);
   return hipGetLastError();
@@ -560,14 +633,11 @@ hipError_t preference_loss(DType dt, const LogitRows& r, const PreferenceArgs& p
   o.logp = coef + r.B;  // [B, T], as the two that follow
   o.top = o.logp + N;
   o.log2sum = o.top + N;
-  hipError_t e = dt == BF16 ? rows<bf16, LOGP>(r, o, s) : rows<float, LOGP>(r, o, s);
+  hipError_t e = dt == BF16 ? scored_rows<bf16, STATS>(r, o, s) : scored_rows<float, STATS>(r, o, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(preference_pairs, dim3(r.B / 2), dim3(256), 0, s, r, p, o.logp, coef, pair_loss);
-  e = dt == BF16 ? preference_grad(r, coef, o, static_cast<bf16*>(dlogits), s)
-                 : preference_grad(r, coef, o, static_cast<float*>(dlogits), s);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(preference_total, dim3(1), dim3(256), 0, s, pair_loss, r.B / 2, p.loss);
-  return hipGetLastError();
+  return dt == BF16 ? preference_grad<bf16>(r, pair_loss, coef, o, dlogits, p.loss, s)
+                    : preference_grad<float>(r, pair_loss, coef, o, dlogits, p.loss, s);
 }
 
 }  // namespace fal

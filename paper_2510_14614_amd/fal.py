@@ -8,9 +8,10 @@ libfal.so is missing the import of :func:`lib` raises; there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
-from typing import NamedTuple
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
+from typing import NamedTuple
 
 import numpy as np
 
@@ -254,33 +255,42 @@ def adamw_step_noalloc(hp: fal_adamw_t, step: int, n: int, dtype: int, master, p
 # the workspace, so calls on different streams or in different captured graphs
 # share nothing.  ValueError: a tensor is not what the call needs; FalError:
 # the library refused the call.
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+# A small call's time is the host's, so the checks read each attribute once and
+# format messages only to raise them.
+def _refuse(what):
+    raise ValueError(what)
 
 
 def _dtype_code(t, name):
     import torch
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return 1
-    _need(t.dtype == torch.float32, f"{name} must be bfloat16 or float32")
+    if t.dtype is not torch.float32:
+        _refuse(f"{name} must be bfloat16 or float32")
     return 0
 
 
-def _dense(t, name, shape, dtypes, like):
-    """Checks a contiguous tensor of the given shape on like's device."""
-    _need(t.dtype in dtypes, f"{name} must be {' or '.join(str(d) for d in dtypes)}")
-    _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    _need(t.is_contiguous(), f"{name} must be contiguous")
-    _need(t.device == like.device, f"{name} must be on {like.device}")
+def _dense(t, name, shape, dtypes, device):
+    """Checks a contiguous tensor of the given shape on a device."""
+    if t.dtype not in dtypes:
+        _refuse(f"{name} must be {' or '.join(str(d) for d in dtypes)}")
+    if t.shape != shape:
+        _refuse(f"{name} must have shape {shape}, not {tuple(t.shape)}")
+    if not t.is_contiguous():
+        _refuse(f"{name} must be contiguous")
+    if t.device != device:
+        _refuse(f"{name} must be on {device}")
 
 
 def _row_stride(t, name):
     """Row stride of a [B, T, width] tensor whose rows are equally spaced."""
     B, T, width = t.shape
-    _need(width == 1 or t.stride(2) == 1, f"{name} must be contiguous in its last dimension")
-    ld = t.stride(1) if T > 1 else t.stride(0) if B > 1 else max(width, t.stride(1))
-    _need(B == 1 or t.stride(0) == T * ld, f"the sequences of {name} must follow each other at seq_len rows")
+    sb, st, sw = t.stride()
+    if width > 1 and sw != 1:
+        _refuse(f"{name} must be contiguous in its last dimension")
+    ld = st if T > 1 else sb if B > 1 else max(width, st)
+    if B > 1 and sb != T * ld:
+        _refuse(f"the sequences of {name} must follow each other at seq_len rows")
     return ld
 
 
@@ -290,12 +300,14 @@ def _ptr(t):
 
 class _call:
     """The device guard and the stream of one library call."""
+    __slots__ = ("device", "guard")
 
-    def __init__(self, like):
+    def __init__(self, device):
         import torch
-        _need(like.is_cuda, "tensors must be on a GPU")
-        self.guard = None if like.device.index == torch.cuda.current_device() else torch.cuda.device(like.device)
-        self.device = like.device
+        if device.type != "cuda":
+            _refuse("tensors must be on a GPU")
+        self.device = device
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
     def __enter__(self):
         import torch
@@ -314,35 +326,50 @@ def _check_noctx(status):
         raise FalError(status, f"{L.fal_status_string(status).decode()}: {L.fal_last_error(None).decode()}")
 
 
-def _workspace(query, shape, like):
-    import torch
+@functools.lru_cache(maxsize=1024)
+def _window_workspace(*shape):
     n = c_size_t()
-    _check_noctx(query(byref(shape), byref(n)))
-    # allocations of the caching allocator start at multiples of 512 bytes
-    return torch.empty(max(n.value, 1), dtype=torch.uint8, device=like.device)
+    _check_noctx(lib().fal_window_attention_workspace_bytes(byref(fal_window_attention_t(*shape)), byref(n)))
+    return n.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _loss_workspace(B, T):
+    n = c_size_t()
+    r = fal_logit_rows_t(B, T, 1, 0, 1, T, 1, 1, 1.0)
+    _check_noctx(lib().fal_logit_loss_workspace_bytes(byref(r), byref(n)))
+    return n.value
+
+
+def _clamp32(n):
+    # past 32 bits every window is the whole sequence and every number of
+    # sinks too many
+    return n if -1 <= n <= 2147483647 else max(-1, min(n, 2147483647))
 
 
 def _window_shape(qkv, n_head, n_kv_head, window, sinks, lens):
+    """The call's shape, with dense rows of out."""
     import torch
-    _need(qkv.dim() == 3, "qkv must be [B, T, (n_head + 2 n_kv_head) * head_dim]")
+    if qkv.dim() != 3:
+        _refuse("qkv must be [B, T, (n_head + 2 n_kv_head) * head_dim]")
     B, T, width = qkv.shape
     heads = n_head + 2 * (n_kv_head or n_head)
-    _need(n_head >= 1 and n_kv_head >= 0 and width % heads == 0,
-          "qkv's last dimension must be (n_head + 2 n_kv_head) * head_dim")
+    if n_head < 1 or n_kv_head < 0 or width % heads:
+        _refuse("qkv's last dimension must be (n_head + 2 n_kv_head) * head_dim")
     hd = width // heads
-    # in 32 bits: any longer window sees the whole sequence, any more sinks are refused
-    window, sinks = (max(-1, min(int(n), 2 ** 31 - 1)) for n in (window, sinks))
     code = _dtype_code(qkv, "qkv")
     if lens is not None:
-        _dense(lens, "lens", (B,), (torch.int32,), qkv)
-    return fal_window_attention_t(B, T, n_head, n_kv_head, hd, code, window, sinks, _row_stride(qkv, "qkv"),
-                                  n_head * hd)
+        _dense(lens, "lens", (B,), (torch.int32,), qkv.device)
+    return (B, T, n_head, n_kv_head, hd, code, _clamp32(window), _clamp32(sinks), _row_stride(qkv, "qkv"),
+            n_head * hd)
 
 
-def _window_rows(t, name, like, shape, ld):
-    _need(t.dtype == like.dtype and t.device == like.device, f"{name} must have qkv's dtype and device")
-    _need(tuple(t.shape) == shape, f"{name} must have shape {shape}, not {tuple(t.shape)}")
-    _need(ld is None or _row_stride(t, name) == ld, f"{name} must have a row stride of {ld} elements")
+def _window_rows(t, name, like, shape):
+    if t.dtype is not like.dtype or t.device != like.device:
+        _refuse(f"{name} must have qkv's dtype and device")
+    if t.shape != shape:
+        _refuse(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    return _row_stride(t, name)
 
 
 def window_attention_fwd(qkv, n_head, window, sinks=0, n_kv_head=0, lens=None, out=None, lse=None):
@@ -354,18 +381,19 @@ def window_attention_fwd(qkv, n_head, window, sinks=0, n_kv_head=0, lens=None, o
     [B, T, n_head * head_dim] (rows at any equal spacing if given) and the
     log-sum-exp, float32 [B, n_head, T]."""
     import torch
-    a = _window_shape(qkv, n_head, n_kv_head, window, sinks, lens)
-    shape = (a.batch, a.seq_len, n_head * a.head_dim)
-    with _call(qkv) as stream:
+    shape = _window_shape(qkv, n_head, n_kv_head, window, sinks, lens)
+    B, T = shape[:2]
+    device = qkv.device
+    a = fal_window_attention_t(*shape)
+    with _call(device) as stream:
         if out is None:
-            out = torch.empty(shape, dtype=qkv.dtype, device=qkv.device)
+            out = torch.empty((B, T, shape[9]), dtype=qkv.dtype, device=device)
         else:
-            _window_rows(out, "out", qkv, shape, None)
-            a.ld_out = _row_stride(out, "out")
+            a.ld_out = _window_rows(out, "out", qkv, (B, T, shape[9]))
         if lse is None:
-            lse = torch.empty(a.batch, n_head, a.seq_len, dtype=torch.float32, device=qkv.device)
+            lse = torch.empty((B, n_head, T), dtype=torch.float32, device=device)
         else:
-            _dense(lse, "lse", (a.batch, n_head, a.seq_len), (torch.float32,), qkv)
+            _dense(lse, "lse", (B, n_head, T), (torch.float32,), device)
         _check_noctx(lib().fal_window_attention_fwd(byref(a), qkv.data_ptr(), _ptr(lens), out.data_ptr(),
                                                     lse.data_ptr(), stream))
     return out, lse
@@ -374,38 +402,47 @@ def window_attention_fwd(qkv, n_head, window, sinks=0, n_kv_head=0, lens=None, o
 def window_attention_bwd(qkv, out, dout, lse, n_head, window, sinks=0, n_kv_head=0, lens=None, dqkv=None):
     """Gradient of window_attention_fwd with respect to qkv, from the out and
     lse it returned and the gradient of out (rows spaced as out's).  dqkv, if
-    given, has rows spaced as qkv's or dense ones; returned."""
+    given, has rows at any equal spacing; returned."""
     import torch
-    a = _window_shape(qkv, n_head, n_kv_head, window, sinks, lens)
-    _window_rows(out, "out", qkv, (a.batch, a.seq_len, n_head * a.head_dim), None)
-    a.ld_out = _row_stride(out, "out")
-    _window_rows(dout, "dout", qkv, tuple(out.shape), a.ld_out)
-    _dense(lse, "lse", (a.batch, n_head, a.seq_len), (torch.float32,), qkv)
-    with _call(qkv) as stream:
+    shape = _window_shape(qkv, n_head, n_kv_head, window, sinks, lens)
+    B, T = shape[:2]
+    device = qkv.device
+    a = fal_window_attention_t(*shape)
+    a.ld_out = ld = _window_rows(out, "out", qkv, (B, T, shape[9]))
+    if _window_rows(dout, "dout", qkv, (B, T, shape[9])) != ld:
+        _refuse(f"dout must have out's row stride of {ld} elements")
+    _dense(lse, "lse", (B, n_head, T), (torch.float32,), device)
+    with _call(device) as stream:
         if dqkv is None:
-            dqkv = torch.empty(qkv.shape, dtype=qkv.dtype, device=qkv.device)
-        _window_rows(dqkv, "dqkv", qkv, tuple(qkv.shape), None)
-        ws = _workspace(lib().fal_window_attention_workspace_bytes, a, qkv)
+            dqkv = torch.empty(qkv.shape, dtype=qkv.dtype, device=device)
+        ld = _window_rows(dqkv, "dqkv", qkv, qkv.shape)
+        n = _window_workspace(*shape)
+        # allocations of the caching allocator start at multiples of 512 bytes
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
         _check_noctx(lib().fal_window_attention_bwd(byref(a), qkv.data_ptr(), _ptr(lens), out.data_ptr(),
-                                                    dout.data_ptr(), lse.data_ptr(), dqkv.data_ptr(),
-                                                    _row_stride(dqkv, "dqkv"), ws.data_ptr(), ws.numel(), stream))
+                                                    dout.data_ptr(), lse.data_ptr(), dqkv.data_ptr(), ld,
+                                                    ws.data_ptr(), n, stream))
     return dqkv
 
 
 def _logit_rows(logits, targets, mask, vocab, temperature):
     import torch
-    _need(logits.dim() == 3, "logits must be [B, T, vocab]")
+    if logits.dim() != 3:
+        _refuse("logits must be [B, T, vocab]")
     B, T, width = logits.shape
     V = width if vocab is None else vocab
-    _need(1 <= V <= width, "vocab must lie in [1, logits' last dimension]")
+    if not 1 <= V <= width:
+        _refuse("vocab must lie in [1, logits' last dimension]")
     code = _dtype_code(logits, "logits")
-    _need(targets.dtype == torch.int32 and tuple(targets.shape) == (B, T) and targets.device == logits.device,
-          "targets must be int32 [B, T] on the logits' device")
-    _need(T == 1 or targets.stride(1) == 1, "targets must be contiguous in their last dimension")
+    if targets.dtype is not torch.int32 or targets.shape != (B, T) or targets.device != logits.device:
+        _refuse("targets must be int32 [B, T] on the logits' device")
+    sb, st = targets.stride()
+    if T > 1 and st != 1:
+        _refuse("targets must be contiguous in their last dimension")
     if mask is not None:
-        _dense(mask, "mask", (B, T), (torch.bool, torch.uint8), logits)
+        _dense(mask, "mask", (B, T), (torch.bool, torch.uint8), logits.device)
     ld = _row_stride(logits, "logits")
-    return fal_logit_rows_t(B, T, V, code, ld, targets.stride(0) if B > 1 else T, ld, width, temperature)
+    return fal_logit_rows_t(B, T, V, code, ld, sb if B > 1 else T, ld, width, temperature)
 
 
 def token_logprobs(logits, targets, mask=None, vocab=None, temperature=1.0, entropy=False):
@@ -415,8 +452,8 @@ def token_logprobs(logits, targets, mask=None, vocab=None, temperature=1.0, entr
     (fal_token_logprobs).  logits: [B, T, >= vocab], bfloat16 or float32."""
     import torch
     r = _logit_rows(logits, targets, mask, vocab, temperature)
-    with _call(logits) as stream:
-        logp = torch.empty(r.batch, r.seq_len, dtype=torch.float32, device=logits.device)
+    with _call(logits.device) as stream:
+        logp = torch.empty(targets.shape, dtype=torch.float32, device=logits.device)
         ent = torch.empty_like(logp) if entropy else None
         _check_noctx(lib().fal_token_logprobs(byref(r), logits.data_ptr(), targets.data_ptr(), _ptr(mask),
                                               logp.data_ptr(), _ptr(ent), stream))
@@ -428,10 +465,10 @@ def _gradient_rows(r, logits, dlogits):
     import torch
     if dlogits is None:
         ld = r.ld_logits if r.ld_logits < r.dlogits_cols + 64 else r.dlogits_cols
-        dlogits = torch.empty(r.batch, r.seq_len, ld, dtype=logits.dtype, device=logits.device)
+        dlogits = torch.empty((r.batch, r.seq_len, ld), dtype=logits.dtype, device=logits.device)
         dlogits = dlogits[:, :, :r.dlogits_cols]
-    _need(dlogits.dtype == logits.dtype and dlogits.device == logits.device and dlogits.shape == logits.shape,
-          "dlogits must have the logits' shape, dtype and device")
+    elif dlogits.dtype is not logits.dtype or dlogits.device != logits.device or dlogits.shape != logits.shape:
+        _refuse("dlogits must have the logits' shape, dtype and device")
     r.ld_dlogits = _row_stride(dlogits, "dlogits")
     return dlogits
 
@@ -444,19 +481,22 @@ def policy_loss(logits, targets, old_logp, advantages, ref_logp=None, mask=None,
     and in rows that do not count; dlogits may be the logits themselves."""
     import torch
     r = _logit_rows(logits, targets, mask, vocab, temperature)
-    for name, t in (("old_logp", old_logp), ("advantages", advantages), ("ref_logp", ref_logp)):
-        if t is not None or name != "ref_logp":
-            _dense(t, name, (r.batch, r.seq_len), (torch.float32,), logits)
+    shape, device, f32 = targets.shape, logits.device, (torch.float32,)
+    _dense(old_logp, "old_logp", shape, f32, device)
+    _dense(advantages, "advantages", shape, f32, device)
+    if ref_logp is not None:
+        _dense(ref_logp, "ref_logp", shape, f32, device)
     hp = fal_policy_t(clip_low, clip_high, kl_coef, int(sequence_mean))
-    with _call(logits) as stream:
+    with _call(device) as stream:
         dlogits = _gradient_rows(r, logits, dlogits)
-        stats = torch.empty(4, dtype=torch.float32, device=logits.device)
-        logp = torch.empty(r.batch, r.seq_len, dtype=torch.float32, device=logits.device)
-        ws = _workspace(lib().fal_logit_loss_workspace_bytes, r, logits)
+        stats = torch.empty(4, dtype=torch.float32, device=device)
+        logp = torch.empty(shape, dtype=torch.float32, device=device)
+        n = _loss_workspace(*shape)
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
         _check_noctx(lib().fal_policy_loss(byref(r), byref(hp), logits.data_ptr(), targets.data_ptr(), _ptr(mask),
                                            old_logp.data_ptr(), _ptr(ref_logp), advantages.data_ptr(),
-                                           stats.data_ptr(), logp.data_ptr(), dlogits.data_ptr(), ws.data_ptr(),
-                                           ws.numel(), stream))
+                                           stats.data_ptr(), logp.data_ptr(), dlogits.data_ptr(), ws.data_ptr(), n,
+                                           stream))
     return PolicyLoss(stats, logp, dlogits)
 
 
@@ -468,16 +508,19 @@ def preference_loss(logits, targets, ref_logp, mask=None, vocab=None, dlogits=No
     log-probability of each sequence."""
     import torch
     r = _logit_rows(logits, targets, mask, vocab, temperature)
-    _dense(ref_logp, "ref_logp", (r.batch,), (torch.float32,), logits)
+    device = logits.device
+    B, T = targets.shape
+    _dense(ref_logp, "ref_logp", (B,), (torch.float32,), device)
     hp = fal_preference_t(beta, label_smoothing, int(ipo), int(length_mean))
-    with _call(logits) as stream:
+    with _call(device) as stream:
         dlogits = _gradient_rows(r, logits, dlogits)
-        loss = torch.empty(1, dtype=torch.float32, device=logits.device)
-        seq_logp = torch.empty(r.batch, dtype=torch.float32, device=logits.device)
-        ws = _workspace(lib().fal_logit_loss_workspace_bytes, r, logits)
+        loss = torch.empty(1, dtype=torch.float32, device=device)
+        seq_logp = torch.empty(B, dtype=torch.float32, device=device)
+        n = _loss_workspace(B, T)
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
         _check_noctx(lib().fal_preference_loss(byref(r), byref(hp), logits.data_ptr(), targets.data_ptr(), _ptr(mask),
                                                ref_logp.data_ptr(), loss.data_ptr(), seq_logp.data_ptr(),
-                                               dlogits.data_ptr(), ws.data_ptr(), ws.numel(), stream))
+                                               dlogits.data_ptr(), ws.data_ptr(), n, stream))
     return PreferenceLoss(loss, seq_logp, dlogits)
 
 
@@ -587,18 +630,17 @@ class Fal:
     def set_attention_window(self, window, sinks=0):
         """Every later forward and backward attends causally over the last
         `window` keys and the first `sinks`; window 0 restores the full mask."""
-        window, sinks = (max(-1, min(int(n), 2 ** 31 - 1)) for n in (window, sinks))
-        _check(lib().fal_set_attention_window(self.ctx, window, sinks), self.ctx)
+        _check(lib().fal_set_attention_window(self.ctx, _clamp32(window), _clamp32(sinks)), self.ctx)
 
     def _token_arrays(self, tokens, mask, **arrays):
         torch = self.torch
         B, T = self.cfg.batch, self.cfg.seq_len
-        _dense(tokens, "tokens", (B, T + 1), (torch.int32,), self.params)
+        _dense(tokens, "tokens", (B, T + 1), (torch.int32,), self.device)
         if mask is not None:
-            _dense(mask, "mask", (B, T), (torch.bool, torch.uint8), self.params)
+            _dense(mask, "mask", (B, T), (torch.bool, torch.uint8), self.device)
         for name, t in arrays.items():
             if t is not None:
-                _dense(t, name, (B,) if name == "ref_seq_logp" else (B, T), (torch.float32,), self.params)
+                _dense(t, name, (B,) if name == "ref_seq_logp" else (B, T), (torch.float32,), self.device)
 
     def model_logprobs(self, tokens, mask=None, temperature=1.0, entropy=False):
         """Log-probabilities of tokens[:, 1:] under the model, float32 [B, T]
