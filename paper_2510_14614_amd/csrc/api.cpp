@@ -1323,7 +1323,7 @@ fal_status_t fal_set_attention_window(fal_ctx_t* ctx, int32_t window, int32_t si
   const char* why = nullptr;
   if (window > 0 && ctx->D.T > kMaxWindowSeq) why = "seq_len above 2^22 is not supported with a window";
   else if (sinks > kMaxSinks) why = "more than 128 sinks are not supported";
-  else if (window > 0 && window_attention_scratch(Run(ctx).window_args()) > ctx->W.splitk_floats)
+  else if (window > 0 && window_attention_scratch(Run(ctx).dt, Run(ctx).window_args()) > ctx->W.splitk_floats)
     why = "sinks of this many heads are not supported: their partial sums exceed the context's scratch";
   if (!why) return FAL_OK;
   ctx->window = old_window;

@@ -93,11 +93,11 @@ bool meets(const Extent& out, std::initializer_list<Extent> others) {
   return false;
 }
 
-int64_t window_scratch_bytes(const WindowAttn& a, int64_t* part_off) {
+int64_t window_scratch_bytes(int32_t dtype, const WindowAttn& a, int64_t* part_off) {
   int64_t n = (int64_t)a.B * a.H * a.T * 4;
   n = (n + kWorkspaceAlign - 1) / kWorkspaceAlign * kWorkspaceAlign;
   *part_off = n;
-  return n + window_attention_scratch(a) * 4;
+  return n + window_attention_scratch(dtype == FAL_BF16 ? BF16 : F32, a) * 4;
 }
 
 // ------------------------------------------------------------ logit rows --
@@ -172,7 +172,7 @@ fal_status_t fal_window_attention_workspace_bytes(const fal_window_attention_t* 
     if (no.why) return fail(no.st, no.why);
     if (!bytes) return fail(FAL_ERR_INVALID_ARG, "NULL bytes");
     int64_t off;
-    *bytes = (size_t)window_scratch_bytes(window_args(shape, nullptr), &off);
+    *bytes = (size_t)window_scratch_bytes(shape->dtype, window_args(shape, nullptr), &off);
     return FAL_OK;
   });
 }
@@ -213,7 +213,7 @@ fal_status_t fal_window_attention_bwd(const fal_window_attention_t* shape, const
     WindowAttn a = window_args(shape, lens);
     a.lddq = ld_d_qkv;
     int64_t part_off;
-    const int64_t need = window_scratch_bytes(a, &part_off);
+    const int64_t need = window_scratch_bytes(shape->dtype, a, &part_off);
     if (!workspace || ws_bytes < (size_t)need || !aligned(workspace, kWorkspaceAlign))
       return fail(FAL_ERR_WORKSPACE, "workspace NULL, too small or not 256-byte aligned");
     const int64_t es = element_bytes(shape->dtype), M = (int64_t)a.B * a.T;

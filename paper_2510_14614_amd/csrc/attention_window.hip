@@ -39,13 +39,50 @@ namespace fal {
 
 namespace {
 
-// Kernels whose registers leave one or two wavefronts to a SIMD keep the LDS
-// reads of the next four MFMAs in flight.
+// Kernels that need more registers than two wavefronts a SIMD have.
 template <typename S, int HD>
-constexpr bool kAhead = HD == 128 && sizeof(S) == 2;
+constexpr bool kWide = HD == 128 && sizeof(S) == 4;
+// dK/dV of wide bf16 heads: the keys stay in LDS rather than in registers, and
+// the tiles are fetched when they are due, not one ahead, so that two
+// workgroups fit a compute unit and cover each other's waits.
+template <typename S, int HD>
+constexpr bool kKeysInLds = HD >= 64 && sizeof(S) == 2;
 
 template <int HD>
 constexpr int n_tiles() { return HD < 32 ? 1 : HD / 32; }
+
+// N groups of R LDS reads and the M MFMAs that they feed: the reads of LA
+// groups stay in flight.  Ends the scheduling region.
+template <int N, int R, int M, int LA>
+__device__ __forceinline__ void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, R * LA, 0);
+#pragma unroll
+  for (int q = 0; q < N - LA; ++q) {
+    __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, M * LA, 0);
+  __builtin_amdgcn_sched_barrier(0);
+}
+// ... of P products over head_dim, and of P sums over a tile's rows
+template <typename S, int HD, int P>
+__device__ __forceinline__ void dots_ahead() {
+  if (sizeof(S) == 2 && HD >= 64) reads_ahead<P * HD / 16, 1, 1, 4>();
+  if (sizeof(S) == 4) reads_ahead<P * HD / 8, 1, 4, 2>();
+}
+template <typename S, int HD, int P>
+__device__ __forceinline__ void sums_ahead() {
+  if (sizeof(S) == 2 && HD >= 64) reads_ahead<P * HD / 16, 2, 1, 4>();
+  if (sizeof(S) == 4) reads_ahead<P * 16, (n_tiles<HD>() + 1) / 2, n_tiles<HD>(), 2>();
+}
+
+// x of this lane and of lane ^ 32: one swap of half wavefronts
+__device__ __forceinline__ void both_halves(float x, float& lo, float& hi) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  lo = __uint_as_float(r[0]);
+  hi = __uint_as_float(r[1]);
+}
+
 
 // ---- 64-row LDS tiles -----------------------------------------------------
 // bf16 tiles have the slot order of attn_tiles.h; fp32 rows follow each other
@@ -58,18 +95,32 @@ template <typename S, int HD>
 constexpr int tile_len() { return AT * (HD + 16 / (int)sizeof(S)); }
 
 // Rows row0 .. row0 + 63 of a head, through registers; rows at or past n are
-// zeros (a clamped row is read in their place).
+// zeros (a clamped row is read in their place).  A whole tile's addresses are
+// a uniform base and the thread's own offset, computed once.
 template <typename S, int HD>
 struct Stage {
   static constexpr int E = 16 / (int)sizeof(S), CH = HD / E, N = (AT * CH + 255) / 256;
   uint4 v[N];
-  __device__ __forceinline__ void load(const S* src, int64_t ld, int row0, int n, int tid) {
+  const S* src;
+  int64_t ld, own;
+  __device__ __forceinline__ Stage(const S* src_, int64_t ld_, int tid) : src(src_), ld(ld_) {
+    own = (tid / CH) * ld + E * (tid % CH);
+  }
+  __device__ __forceinline__ void load(int row0, int n, int tid) {
+    if (row0 + AT <= n) {
+      const S* tile = src + row0 * ld;
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (256 * (k + 1) <= AT * CH || tid + 256 * k < AT * CH)
+          v[k] = *reinterpret_cast<const uint4*>(tile + k * (256 / CH) * ld + own);
+      return;
+    }
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       const int i = tid + 256 * k;
       const int row = min(row0 + i / CH, n - 1);
       if (256 * (k + 1) <= AT * CH || i < AT * CH)
-        v[k] = *reinterpret_cast<const uint4*>(src + (int64_t)row * ld + E * (i % CH));
+        v[k] = *reinterpret_cast<const uint4*>(src + row * ld + E * (i % CH));
     }
   }
   __device__ __forceinline__ void store(S* s, int row0, int n, int tid) {
@@ -89,36 +140,44 @@ struct Stage {
   }
 };
 
-// The window's mask over a 32x32 score tile whose tile rows are keys: row `off`
-// (from the lane half's first) is hidden from the lane's query if it lies
-// after it, or before its window and past the sinks.  No branches: the three
-// comparisons join in the scalar unit.
-struct KeyMask {
-  int last, before, sink;
-  __device__ __forceinline__ KeyMask(const WindowAttn& a, int kb, int g, int tq, int n) {
-    const int key0 = kb + 4 * g;
-    last = min(tq, n - 1) - key0;
-    before = tq - a.window - key0;
-    sink = a.sinks - key0;
+// The window's mask over a 32x32 score tile whose rows are the keys from kb on
+// and whose lane has query tq, one of q0 .. q0 + 31: -inf for keys after the
+// query (or past n), and for keys before its window and past the sinks.  Each
+// edge is tested where it crosses the tile, without branches.
+__device__ __forceinline__ void mask_keys(const WindowAttn& a, int kb, int q0, int tq, int n, int g, f32x16v& s) {
+  const int key0 = kb + 4 * g;
+  if (kb + 31 > q0 || kb + 31 >= n) {
+    const int last = min(tq, n - 1) - key0;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = acc_row(r, 0) > last ? -INFINITY : s[r];
   }
-  __device__ __forceinline__ bool hides(int r) const {
-    const int off = acc_row(r, 0);
-    return (bool)((off > last) | ((off <= before) & (off >= sink)));
+  if (q0 + 31 - kb >= a.window) {
+    const int before = tq - a.window - key0, sink = a.sinks - key0;
+    if (kb >= a.sinks) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = acc_row(r, 0) <= before ? -INFINITY : s[r];
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        s[r] = ((int)(acc_row(r, 0) <= before) & (int)(acc_row(r, 0) >= sink)) ? -INFINITY : s[r];
+    }
   }
-};
-// The same where tile rows are queries and the lane has the key.
-struct QueryMask {
-  int first, past;
-  __device__ __forceinline__ QueryMask(const WindowAttn& a, int qs, int g, int key) {
-    const int q0 = qs + 4 * g;
-    first = key - q0;
-    past = key < a.sinks ? 1 << 30 : key + a.window - q0;
+}
+// The same where the rows are the queries from qs on and the lane has the key,
+// one of kw .. kw + 31.
+__device__ __forceinline__ void mask_queries(const WindowAttn& a, int qs, int kw, int key, int g, f32x16v& s) {
+  const int q0 = qs + 4 * g;
+  if (qs < kw + 32) {
+    const int first = key - q0;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = acc_row(r, 0) < first ? -INFINITY : s[r];
   }
-  __device__ __forceinline__ bool hides(int r) const {
-    const int off = acc_row(r, 0);
-    return (bool)((off < first) | (off >= past));
+  if (qs + 31 - kw >= a.window) {
+    const int past = key < a.sinks ? 1 << 30 : key + a.window - q0;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = acc_row(r, 0) >= past ? -INFINITY : s[r];
   }
-};
+}
 
 // ---- operands -------------------------------------------------------------
 // The lane's own row (row c of the wavefront's 32) as the B operand of the
@@ -181,6 +240,16 @@ __device__ __forceinline__ void dot_rows(const float* s, int rowbase, int c, int
   }
 }
 
+// The same with the own rows in LDS as well (bf16).
+template <int HD>
+__device__ __forceinline__ void dot_rows(const bf16* s, int rowbase, int c, int g, const bf16* own, f32x16v& acc) {
+#pragma unroll
+  for (int k = 0; k < HD / 16; ++k)
+    acc = mfma32(frag_rows<HD>(s, rowbase, c, k, g), frag_rows<HD>(own, 0, c, k, g), acc);
+}
+template <int HD>
+__device__ __forceinline__ void dot_rows(const float*, int, int, int, const float*, f32x16v&) {}
+
 // acc[t][dim 32 t + .][own row] += sum over the 32 tile rows from rowbase of
 // tile[row][dim] * p[row][own row].  head_dim 16: dims 16..31 repeat 0..15
 // and are not stored.
@@ -238,12 +307,12 @@ __device__ __forceinline__ int length_of(const WindowAttn& a, int b) {
   return a.lens ? min(max(a.lens[b], 0), a.T) : a.T;
 }
 
-// Key tiles of a block of 128 queries from qb on: `sink` tiles from key 0,
+// Key tiles of a block of `rows` queries from qb on: `sink` tiles from key 0,
 // then the window's tiles from `first` (a multiple of AT) up to `end`.
 struct KeyTiles {
   int sink, first, end, count;
-  __device__ __forceinline__ KeyTiles(const WindowAttn& a, int qb, int n) {
-    end = min(n, qb + 128);
+  __device__ __forceinline__ KeyTiles(const WindowAttn& a, int qb, int rows, int n) {
+    end = min(n, qb + rows);
     first = max(0, qb - a.window + 1) / AT * AT;
     sink = (min(a.sinks, first) + AT - 1) / AT;
     count = sink + (end - first + AT - 1) / AT;
@@ -251,21 +320,57 @@ struct KeyTiles {
   __device__ __forceinline__ int at(int i) const { return i < sink ? AT * i : first + AT * (i - sink); }
 };
 
+// A workgroup's four wavefronts own 32 rows each and walk both 32-row halves
+// of every tile, or (SPLIT) in pairs the same 32 rows, one half of the tiles
+// each, joining their sums at the end: half the rows and half the walk a
+// workgroup.
+template <bool SPLIT>
+constexpr int block_rows() { return SPLIT ? 64 : 128; }
+
+// LDS of a kernel: two tiles, the join's registers of two wavefronts, or a row
+// of sums for each of 32 sink keys
+template <typename S, int HD, bool SPLIT>
+constexpr int lds_bytes() {
+  const int tiles = 2 * tile_len<S, HD>() * (int)sizeof(S), join = SPLIT ? 2 * n_tiles<HD>() * 16 * 64 * 4 + 1024 : 0;
+  const int sums = 32 * (HD + 1) * 4, most = tiles > join ? tiles : join;
+  return (most > sums ? most : sums) / 16 * 16 + 16;
+}
+
+// Adds the second wavefront of a pair's sums to the first's.
+template <int HD>
+__device__ __forceinline__ void join_acc(float* lds, int wave, int lane, f32x16v (&acc)[n_tiles<HD>()]) {
+  float* p = lds + (wave & 1) * (n_tiles<HD>() * 16 * 64) + lane;
+  __syncthreads();
+  if (wave >= 2) {
+#pragma unroll
+    for (int t = 0; t < n_tiles<HD>(); ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[64 * (16 * t + r)] = acc[t][r];
+  }
+  __syncthreads();
+  if (wave < 2) {
+#pragma unroll
+    for (int t = 0; t < n_tiles<HD>(); ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[t][r] += p[64 * (16 * t + r)];
+  }
+}
+
 }  // namespace
 
 // ------------------------------------------------------------- forward --
-template <typename S, int HD>
+template <typename S, int HD, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S* qkv, S* O, float* lse) {
   constexpr int NT = n_tiles<HD>();
-  __shared__ __attribute__((aligned(16))) S sK[tile_len<S, HD>()];
-  __shared__ __attribute__((aligned(16))) S sV[tile_len<S, HD>()];
-  const int h = blockIdx.x, b = blockIdx.y, qb = 128 * blockIdx.z;
+  __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, SPLIT>()];
+  S *sK = reinterpret_cast<S*>(lds), *sV = sK + tile_len<S, HD>();
+  const int h = blockIdx.x, b = blockIdx.y, qb = block_rows<SPLIT>() * blockIdx.z;
   const int kvh = h / (a.H / a.Hkv);
   const S* Qg = qkv + (int64_t)b * a.T * a.ldq + h * HD;
   const S* Kg = qkv + (int64_t)b * a.T * a.ldq + (a.H + kvh) * HD;
   const S* Vg = Kg + a.Hkv * HD;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
-  const int q0 = qb + wave * 32, tq = q0 + c;
+  const int q0 = qb + (SPLIT ? wave & 1 : wave) * 32, tq = q0 + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
 
@@ -280,10 +385,10 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
   if (qb < n) {
     Own<S, HD> q;
     q.load(Qg, a.ldq, tq, n, g);
-    const KeyTiles kt(a, qb, n);
-    Stage<S, HD> rk, rv;
-    rk.load(Kg, a.ldq, kt.at(0), n, tid);
-    rv.load(Vg, a.ldq, kt.at(0), n, tid);
+    const KeyTiles kt(a, qb, block_rows<SPLIT>(), n);
+    Stage<S, HD> rk(Kg, a.ldq, tid), rv(Vg, a.ldq, tid);
+    rk.load(kt.at(0), n, tid);
+    rv.load(kt.at(0), n, tid);
     for (int i = 0; i < kt.count; ++i) {
       const int k0 = kt.at(i);
       __syncthreads();
@@ -291,25 +396,26 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
       rv.store(sV, k0, n, tid);
       __syncthreads();
       if (i + 1 < kt.count) {
-        rk.load(Kg, a.ldq, kt.at(i + 1), n, tid);
-        rv.load(Vg, a.ldq, kt.at(i + 1), n, tid);
+        rk.load(kt.at(i + 1), n, tid);
+        rv.load(kt.at(i + 1), n, tid);
       }
 #pragma unroll
-      for (int sub = 0; sub < AT / 32; ++sub) {
+      for (int u = 0; u < (SPLIT ? 1 : AT / 32); ++u) {
+        const int sub = SPLIT ? wave >> 1 : u;
         const int kb = k0 + 32 * sub;
         if (kb > q0 + 31 || kb >= n) break;
         if (kb >= a.sinks && q0 - (kb + 31) >= a.window) continue;  // before the window of every row
         f32x16v s = zero16();
+        __builtin_amdgcn_sched_barrier(0);
         dot_rows<HD>(sK, 32 * sub, c, g, q, s);
-        if (kb + 31 > q0 || kb + 31 >= n || q0 + 31 - kb >= a.window) {
-          const KeyMask mask(a, kb, g, tq, n);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = mask.hides(r) ? -INFINITY : s[r];
-        }
+        dots_ahead<S, HD, 1>();
+        mask_keys(a, kb, q0, tq, n, g, s);
         float mx = s[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2;
+        float lo, hi;
+        both_halves(mx, lo, hi);
+        mx = fmaxf(lo, hi) * sl2;
         if (__any(mx > mref + kSlack)) {
           if (mx > mref + kSlack) {
             const float alpha = __builtin_amdgcn_exp2f(mref - mx);
@@ -328,9 +434,42 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
           s[r] = p;
           lsum += p;
         }
+        if (sizeof(S) == 4) __builtin_amdgcn_sched_barrier(0);
         add_rows<HD>(sV, 32 * sub, lane, s, acc);
+        if (sizeof(S) == 4) sums_ahead<S, HD, 1>();
       }
     }
+  }
+  if (SPLIT) {  // join the pair's softmaxes
+    float* p = reinterpret_cast<float*>(lds) + 2 * NT * 16 * 64 + 2 * (lane + 64 * (wave & 1));
+    __syncthreads();
+    if (wave >= 2) {
+      p[0] = mref;
+      p[1] = lsum;
+    }
+    __syncthreads();
+    if (wave < 2) {
+      const float m1 = p[0], top = fmaxf(mref, m1);
+      const float f0 = mref == top ? 1.f : __builtin_amdgcn_exp2f(mref - top);
+      const float f1 = m1 == top ? 1.f : __builtin_amdgcn_exp2f(m1 - top);
+      lsum = lsum * f0 + p[1] * f1;
+      mref = top;
+      p[0] = f1;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[t][r] *= f0;
+    }
+    __syncthreads();
+    if (wave >= 2) {
+      const float f1 = p[0];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[t][r] *= f1;
+    }
+    join_acc<HD>(reinterpret_cast<float*>(lds), wave, lane, acc);
+    if (wave >= 2) return;
   }
   const float l = lsum + __shfl_xor(lsum, 32, 64);
   if (tq < a.T) {
@@ -342,19 +481,19 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
 
 // ----------------------------------------------------------- backward: dQ --
 // Also writes D = rowsum(dO * O) for the kernels that follow.
-template <typename S, int HD>
-__global__ __launch_bounds__(256, 2) void window_attn_dq(WindowAttn a, const S* qkv, const S* O, const S* dO,
+template <typename S, int HD, bool SPLIT>
+__global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_dq(WindowAttn a, const S* qkv, const S* O, const S* dO,
                                                          const float* lse, float* Dvec, S* dqkv) {
   constexpr int NT = n_tiles<HD>();
-  __shared__ __attribute__((aligned(16))) S sK[tile_len<S, HD>()];
-  __shared__ __attribute__((aligned(16))) S sV[tile_len<S, HD>()];
-  const int h = blockIdx.x, b = blockIdx.y, qb = 128 * blockIdx.z;
+  __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, SPLIT>()];
+  S *sK = reinterpret_cast<S*>(lds), *sV = sK + tile_len<S, HD>();
+  const int h = blockIdx.x, b = blockIdx.y, qb = block_rows<SPLIT>() * blockIdx.z;
   const int kvh = h / (a.H / a.Hkv);
   const int64_t row0 = (int64_t)b * a.T;
   const S* Kg = qkv + row0 * a.ldq + (a.H + kvh) * HD;
   const S* Vg = Kg + a.Hkv * HD;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
-  const int q0 = qb + wave * 32, tq = q0 + c;
+  const int q0 = qb + (SPLIT ? wave & 1 : wave) * 32, tq = q0 + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
 
@@ -373,11 +512,11 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq(WindowAttn a, const S* 
     D += __shfl_xor(D, 32, 64);
     const int64_t stat = ((int64_t)b * a.H + h) * a.T + tq;
     const float L2 = tq < n ? lse[stat] * kLog2e : 0.f;
-    if (g == 0 && tq < n) Dvec[stat] = D;
-    const KeyTiles kt(a, qb, n);
-    Stage<S, HD> rk, rv;
-    rk.load(Kg, a.ldq, kt.at(0), n, tid);
-    rv.load(Vg, a.ldq, kt.at(0), n, tid);
+    if (g == 0 && tq < n && (!SPLIT || wave < 2)) Dvec[stat] = D;
+    const KeyTiles kt(a, qb, block_rows<SPLIT>(), n);
+    Stage<S, HD> rk(Kg, a.ldq, tid), rv(Vg, a.ldq, tid);
+    rk.load(kt.at(0), n, tid);
+    rv.load(kt.at(0), n, tid);
     for (int i = 0; i < kt.count; ++i) {
       const int k0 = kt.at(i);
       __syncthreads();
@@ -385,33 +524,34 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq(WindowAttn a, const S* 
       rv.store(sV, k0, n, tid);
       __syncthreads();
       if (i + 1 < kt.count) {
-        rk.load(Kg, a.ldq, kt.at(i + 1), n, tid);
-        rv.load(Vg, a.ldq, kt.at(i + 1), n, tid);
+        rk.load(kt.at(i + 1), n, tid);
+        rv.load(kt.at(i + 1), n, tid);
       }
 #pragma unroll
-      for (int sub = 0; sub < AT / 32; ++sub) {
+      for (int u = 0; u < (SPLIT ? 1 : AT / 32); ++u) {
+        const int sub = SPLIT ? wave >> 1 : u;
         const int kb = k0 + 32 * sub;
         if (kb > q0 + 31 || kb >= n) break;
         if (kb >= a.sinks && q0 - (kb + 31) >= a.window) continue;
         f32x16v s = zero16(), dp = zero16();
         dot_rows<HD>(sK, 32 * sub, c, g, q, s);
         dot_rows<HD>(sV, 32 * sub, c, g, d, dp);
-        if (kAhead<S, HD>) lds_ahead<HD / 8, 1, 4>();
-        if (kb + 31 > q0 || kb + 31 >= n || q0 + 31 - kb >= a.window) {
-          const KeyMask mask(a, kb, g, tq, n);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = mask.hides(r) ? -INFINITY : s[r];
-        }
+        dots_ahead<S, HD, 2>();
+        mask_keys(a, kb, q0, tq, n, g, s);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -L2));
           dp[r] = p * (dp[r] - D);
         }
-        if (kAhead<S, HD>) __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_sched_barrier(0);
         add_rows<HD>(sK, 32 * sub, lane, dp, dq);
-        if (kAhead<S, HD>) lds_ahead<HD / 16, 2, 4>();
+        sums_ahead<S, HD, 1>();
       }
     }
+  }
+  if (SPLIT) {
+    join_acc<HD>(reinterpret_cast<float*>(lds), wave, lane, dq);
+    if (wave >= 2) return;
   }
   if (tq < a.T)
     put_row<S, HD>(dqkv + (row0 + tq) * a.lddq + h * HD, g, dq, 1.f / sqrtf((float)HD), tq < n);
@@ -419,109 +559,99 @@ __global__ __launch_bounds__(256, 2) void window_attn_dq(WindowAttn a, const S* 
 
 // ------------------------------------------- backward: dK, dV of the sinks --
 // Queries from `far` on see of the first key block only the sink keys.  One
-// workgroup takes a chunk of them for one query head and 32 sink keys, its
-// wavefronts alternating over 32-query rows; the four sums are joined in LDS
-// and written as fp32 partials [b][h][chunk][dK, dV][sinks][HD].
+// workgroup takes a chunk of them, of every query head of a group, and 32
+// sink keys; of its wavefronts two sum dV and two dK, over one half of each
+// tile (half the sums a wavefront, so three share a SIMD).  The halves are
+// joined in LDS and written as fp32 partials [b][kv head][chunk][dK, dV]
+// [sinks][HD].
 template <typename S, int HD>
-__global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_sinks(WindowAttn a, const S* qkv, const S* dO,
-                                                                            const float* lse, const float* Dvec,
-                                                                            int far, int chunk, int nchunk,
-                                                                            float* part) {
+__global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_sinks(WindowAttn a, const S* qkv, const S* dO, const float* lse,
+                                                            const float* Dvec, int rows, int far, int chunk, int nchunk,
+                                                            float* part) {
   constexpr int NT = n_tiles<HD>();
-  __shared__ __attribute__((aligned(16))) S sQ[tile_len<S, HD>()];
-  __shared__ __attribute__((aligned(16))) S sdO[tile_len<S, HD>()];
+  __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, true>()];
+  S *sQ = reinterpret_cast<S*>(lds), *sdO = sQ + tile_len<S, HD>();
   __shared__ float sL[AT], sD[AT];
-  const int h = blockIdx.x, b = blockIdx.y, ck = blockIdx.z % nchunk, kw = 32 * (blockIdx.z / nchunk);
-  const int kvh = h / (a.H / a.Hkv);
+  const int kvh = blockIdx.x, b = blockIdx.y, ck = blockIdx.z % nchunk, kw = 32 * (blockIdx.z / nchunk);
+  const int grp = a.H / a.Hkv;
   const int64_t row0 = (int64_t)b * a.T;
-  const S* Qg = qkv + row0 * a.ldq + h * HD;
   const S* Kg = qkv + row0 * a.ldq + (a.H + kvh) * HD;
-  const S* dOg = dO + row0 * a.lddo + h * HD;
-  const float* Lg = lse + ((int64_t)b * a.H + h) * a.T;
-  const float* Dg = Dvec + ((int64_t)b * a.H + h) * a.T;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
-  const int n = length_of(a, b), key = kw + c;
-  const int qbeg = far + ck * chunk, qend = min(n, qbeg + chunk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5;
+  const int c = lane & 31, n = length_of(a, b), key = kw + c, sub = wave >> 1;
+  const bool keys = wave & 1;  // this wavefront sums dK
+  // (a key block past the first one's `rows` keys covers as many more queries)
+  const int qbeg = max(far + ck * chunk, far + kw / rows * rows), qend = min(n, far + (ck + 1) * chunk);
   const float sl2 = kLog2e / sqrtf((float)HD);
 
-  f32x16v dk[NT], dv[NT];
-  zero_acc<HD>(dk);
-  zero_acc<HD>(dv);
+  f32x16v acc[NT];
+  zero_acc<HD>(acc);
   if (qbeg < qend) {
     Own<S, HD> k, v;
     k.load(Kg, a.ldq, key, n, g);
-    v.load(Kg + a.Hkv * HD, a.ldq, key, n, g);
-    Stage<S, HD> rq, ro;
-    rq.load(Qg, a.ldq, qbeg, qend, tid);
-    ro.load(dOg, a.lddo, qbeg, qend, tid);
-    for (int q0 = qbeg; q0 < qend; q0 += AT) {
-      __syncthreads();
-      rq.store(sQ, q0, qend, tid);
-      ro.store(sdO, q0, qend, tid);
-      if (tid < AT) {
-        const int tq = q0 + tid;
-        sL[tid] = tq < qend ? Lg[tq] * kLog2e : 0.f;
-        sD[tid] = tq < qend ? Dg[tq] : 0.f;
-      }
-      __syncthreads();
-      if (q0 + AT < qend) {
-        rq.load(Qg, a.ldq, q0 + AT, qend, tid);
-        ro.load(dOg, a.lddo, q0 + AT, qend, tid);
-      }
-      // two wavefronts share a tile, the next tile's two the other pair
-      const int sub = wave & 1;
-      if ((((q0 - qbeg) / AT) & 1) != (wave >> 1)) continue;
-      f32x16v s = zero16(), dp = zero16();
-      dot_rows<HD>(sQ, 32 * sub, c, g, k, s);
-      dot_rows<HD>(sdO, 32 * sub, c, g, v, dp);
+    if (keys) v.load(Kg + a.Hkv * HD, a.ldq, key, n, g);
+    Stage<S, HD> rq(qkv + row0 * a.ldq + kvh * grp * HD, a.ldq, tid);
+    Stage<S, HD> ro(dO + row0 * a.lddo + kvh * grp * HD, a.lddo, tid);
+    for (int h = kvh * grp; h < (kvh + 1) * grp; ++h) {
+      for (int q0 = qbeg; q0 < qend; q0 += AT) {
+        rq.load(q0, qend, tid);
+        ro.load(q0, qend, tid);
+        __syncthreads();
+        rq.store(sQ, q0, qend, tid);
+        ro.store(sdO, q0, qend, tid);
+        if (tid < AT) {
+          const int tq = q0 + tid;
+          const int64_t stat = ((int64_t)b * a.H + h) * a.T + tq;
+          sL[tid] = tq < qend ? lse[stat] * kLog2e : 0.f;
+          sD[tid] = tq < qend ? Dvec[stat] : 0.f;
+        }
+        __syncthreads();
+        f32x16v s = zero16();
+        dot_rows<HD>(sQ, 32 * sub, c, g, k, s);
+        if (keys) {
+          f32x16v dp = zero16();
+          dot_rows<HD>(sdO, 32 * sub, c, g, v, dp);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int qr = 32 * sub + acc_row(r, g);
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[qr]));
-        s[r] = p;
-        dp[r] = p * (dp[r] - sD[qr]);
+          for (int r = 0; r < 16; ++r) {
+            const int qr = 32 * sub + acc_row(r, g);
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[qr])) * (dp[r] - sD[qr]);
+          }
+          add_rows<HD>(sQ, 32 * sub, lane, s, acc);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[32 * sub + acc_row(r, g)]));
+          add_rows<HD>(sdO, 32 * sub, lane, s, acc);
+        }
       }
-      add_rows<HD>(sdO, 32 * sub, lane, s, dv);
-      add_rows<HD>(sQ, 32 * sub, lane, dp, dk);
+      rq.src += HD;
+      ro.src += HD;
     }
   }
-  // join the wavefronts' sums in order, one at a time through LDS
-  __shared__ __attribute__((aligned(16))) float sum[2][32][HD];
-  for (int w = 0; w < 4; ++w) {
-    __syncthreads();
-    if (wave != w) continue;
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int r = 0; r < (HD < 32 ? 8 : 16); ++r) {
-        const int dim = 32 * t + acc_row(r, g);
-        sum[0][c][dim] = (w ? sum[0][c][dim] : 0.f) + dk[t][r];
-        sum[1][c][dim] = (w ? sum[1][c][dim] : 0.f) + dv[t][r];
-      }
-  }
-  __syncthreads();
-  float* out = part + ((((int64_t)b * a.H + h) * nchunk + ck) * 2) * a.sinks * HD;
-  const int rows = min(32, a.sinks - kw);
-  for (int i = tid; i < rows * HD; i += 256) {
-    out[kw * HD + i] = sum[0][i / HD][i % HD];
-    out[(a.sinks + kw) * HD + i] = sum[1][i / HD][i % HD];
-  }
+  join_acc<HD>(reinterpret_cast<float*>(lds), wave, lane, acc);
+  if (wave < 2 && key < a.sinks)
+    put_row<float, HD>(part + ((((int64_t)b * a.Hkv + kvh) * nchunk + ck) * 2 + (1 - wave)) * a.sinks * HD + key * HD, g, acc,
+                       1.f, true);
 }
 
 // ------------------------------------------------------- backward: dK, dV --
-template <typename S, int HD>
-__global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_dkdv(WindowAttn a, const S* qkv, const S* dO,
+// A group's query heads may be divided over `parts` workgroups, which then
+// write fp32 sums [part][b][t][dK, dV][kv head][HD] for window_attn_kv_sum.
+template <typename S, int HD, bool SPLIT>
+__global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD == 64 ? 3 : 2)) void window_attn_dkdv(WindowAttn a, const S* qkv, const S* dO,
                                                                            const float* lse, const float* Dvec,
-                                                                           const float* part, int nchunk, S* dqkv) {
+                                                                           const float* part, int nchunk, int parts,
+                                                                           float* heads, S* dqkv) {
   constexpr int NT = n_tiles<HD>();
-  __shared__ __attribute__((aligned(16))) S sQ[tile_len<S, HD>()];
-  __shared__ __attribute__((aligned(16))) S sdO[tile_len<S, HD>()];
+  constexpr bool KL = kKeysInLds<S, HD>;
+  __shared__ __attribute__((aligned(16))) S sK[KL ? block_rows<SPLIT>() / AT * tile_len<S, HD>() : 8];
+  __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, SPLIT>()];
+  S *sQ = reinterpret_cast<S*>(lds), *sdO = sQ + tile_len<S, HD>();
   __shared__ float sL[AT], sD[AT];
-  const int kvh = blockIdx.x, b = blockIdx.y, kb0 = 128 * blockIdx.z, grp = a.H / a.Hkv;
+  const int kvh = blockIdx.x / parts, b = blockIdx.y, kb0 = block_rows<SPLIT>() * blockIdx.z;
+  const int grp = a.H / a.Hkv / parts, h0 = blockIdx.x * grp;  // this workgroup's query heads
   const int64_t row0 = (int64_t)b * a.T;
   const S* Kg = qkv + row0 * a.ldq + (a.H + kvh) * HD;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
-  const int kw = kb0 + wave * 32, key = kw + c;
+  const int kw = kb0 + (SPLIT ? wave & 1 : wave) * 32, key = kw + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
 
@@ -530,17 +660,33 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_dkdv(Windo
   zero_acc<HD>(dv);
   if (kb0 < n) {
     Own<S, HD> k, v;
-    k.load(Kg, a.ldq, key, n, g);
+    if (KL) {
+      for (int r0 = 0; r0 < block_rows<SPLIT>(); r0 += AT) {
+        Stage<S, HD> rk(Kg, a.ldq, tid);
+        rk.load(kb0 + r0, n, tid);
+        rk.store(sK + r0 / AT * tile_len<S, HD>(), kb0 + r0, n, tid);
+      }
+    } else {
+      k.load(Kg, a.ldq, key, n, g);
+    }
+    const S* ownK = sK + row_off<HD>(sK, kw - kb0);
     v.load(Kg + a.Hkv * HD, a.ldq, key, n, g);
     // query tiles kb0 + 64 i that some key of the block has in its window
-    const int nq = (min(n - kb0, 127 + a.window) + AT - 1) / AT;
+    const int nq = (min(n - kb0, block_rows<SPLIT>() - 1 + a.window) + AT - 1) / AT;
     const int nit = grp * nq;
-    Stage<S, HD> rq, ro;
-    rq.load(qkv + row0 * a.ldq + kvh * grp * HD, a.ldq, kb0, n, tid);
-    ro.load(dO + row0 * a.lddo + kvh * grp * HD, a.lddo, kb0, n, tid);
-    int h = kvh * grp, qi = 0;
+    Stage<S, HD> rq(qkv + row0 * a.ldq + h0 * HD, a.ldq, tid);
+    Stage<S, HD> ro(dO + row0 * a.lddo + h0 * HD, a.lddo, tid);
+    if (!KL) {
+      rq.load(kb0, n, tid);
+      ro.load(kb0, n, tid);
+    }
+    int h = h0, qi = 0;
     for (int it = 0; it < nit; ++it) {
       const int q0 = kb0 + AT * qi;
+      if (KL) {
+        rq.load(q0, n, tid);
+        ro.load(q0, n, tid);
+      }
       __syncthreads();
       rq.store(sQ, q0, n, tid);
       ro.store(sdO, q0, n, tid);
@@ -554,26 +700,26 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_dkdv(Windo
       if (++qi == nq) {
         qi = 0;
         ++h;
+        rq.src += HD;
+        ro.src += HD;
       }
-      if (it + 1 < nit) {
-        rq.load(qkv + row0 * a.ldq + h * HD, a.ldq, kb0 + AT * qi, n, tid);
-        ro.load(dO + row0 * a.lddo + h * HD, a.lddo, kb0 + AT * qi, n, tid);
+      if (!KL && it + 1 < nit) {
+        rq.load(kb0 + AT * qi, n, tid);
+        ro.load(kb0 + AT * qi, n, tid);
       }
 #pragma unroll
-      for (int sub = 0; sub < AT / 32; ++sub) {
+      for (int u = 0; u < (SPLIT ? 1 : AT / 32); ++u) {
+        const int sub = SPLIT ? wave >> 1 : u;
         const int qs = q0 + 32 * sub;
         if (qs + 31 < kw || qs >= n) continue;                      // before this wavefront's keys, or past the end
         if (kw >= a.sinks && qs - (kw + 31) >= a.window) continue;  // past the window of all its keys
         f32x16v s = zero16(), dp = zero16();
-        dot_rows<HD>(sQ, 32 * sub, c, g, k, s);
+        if (KL) dot_rows<HD>(sQ, 32 * sub, c, g, ownK, s);
+        else dot_rows<HD>(sQ, 32 * sub, c, g, k, s);
         dot_rows<HD>(sdO, 32 * sub, c, g, v, dp);
-        if (kAhead<S, HD>) lds_ahead<HD / 8, 1, 4>();
+        dots_ahead<S, HD, 2>();
         // queries past n have zero Q, dO, L and D: they add nothing
-        if (qs < kw + 32 || qs + 31 - kw >= a.window) {
-          const QueryMask mask(a, qs, g, key);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = mask.hides(r) ? -INFINITY : s[r];
-        }
+        mask_queries(a, qs, kw, key, g, s);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int qr = 32 * sub + acc_row(r, g);
@@ -581,26 +727,58 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_dkdv(Windo
           s[r] = p;
           dp[r] = p * (dp[r] - sD[qr]);
         }
-        if (kAhead<S, HD>) __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_sched_barrier(0);
         add_rows<HD>(sdO, 32 * sub, lane, s, dv);
         add_rows<HD>(sQ, 32 * sub, lane, dp, dk);
-        if (kAhead<S, HD>) lds_ahead<HD / 8, 2, 4>();
+        sums_ahead<S, HD, 2>();
       }
     }
-    if (part && key < a.sinks) {
-      for (int hh = kvh * grp; hh < (kvh + 1) * grp; ++hh)
-        for (int ck = 0; ck < nchunk; ++ck) {
-          const float* pk = part + ((((int64_t)b * a.H + hh) * nchunk + ck) * 2 * a.sinks + key) * HD;
-          const float* pv = pk + a.sinks * HD;
+  }
+  if (SPLIT) {
+    join_acc<HD>(reinterpret_cast<float*>(lds), wave, lane, dk);
+    join_acc<HD>(reinterpret_cast<float*>(lds), wave, lane, dv);
+  }
+  if (part && parts == 1 && kb0 < a.sinks && kb0 < n) {
+    // the far queries' partials: for each 32 keys the workgroup sums the
+    // chunks into LDS, in order, and the keys' wavefront adds them
+    float* sum = reinterpret_cast<float*>(lds);
+    const float* base = part + ((int64_t)b * a.Hkv + kvh) * nchunk * 2 * a.sinks * HD;
+    for (int k0 = kb0; k0 < min(kb0 + block_rows<SPLIT>(), a.sinks); k0 += 32) {
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+        const float* p = base + (which * a.sinks + k0) * HD;
+        for (int i = tid; i < min(32, a.sinks - k0) * (HD / 4); i += 256) {
+          f32x4v t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+          for (int ck = 0; ck < nchunk; ++ck)
+            t += *reinterpret_cast<const f32x4v*>(p + (int64_t)ck * 2 * a.sinks * HD + 4 * i);
+          float* to = sum + (HD + 1) * (i / (HD / 4)) + 4 * (i % (HD / 4));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) to[j] = t[j];
+        }
+        __syncthreads();
+        if (kw == k0 && key < a.sinks) {
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < (HD < 32 ? 8 : 16); ++r) {
-              dk[t][r] += pk[32 * t + acc_row(r, g)];
-              dv[t][r] += pv[32 * t + acc_row(r, g)];
+              const float x = sum[(HD + 1) * c + 32 * t + acc_row(r, g)];
+              if (which) dv[t][r] += x;
+              else dk[t][r] += x;
             }
         }
+      }
     }
+  }
+  if (SPLIT && wave >= 2) return;
+  if (parts > 1) {
+    if (key < n) {
+      float* row = heads + ((((blockIdx.x % parts) * (int64_t)a.B + b) * a.T + key) * 2 * a.Hkv + kvh) * HD;
+      put_row<float, HD>(row, g, dk, 1.f, true);
+      put_row<float, HD>(row + a.Hkv * HD, g, dv, 1.f, true);
+    }
+    return;
   }
   if (key < a.T) {
     S* row = dqkv + (row0 + key) * a.lddq + (a.H + kvh) * HD;
@@ -609,79 +787,176 @@ __global__ __launch_bounds__(256, HD == 128 ? 1 : 2) void window_attn_dkdv(Windo
   }
 }
 
+// Joins the parts of a group's heads and, for sink keys, the far queries'
+// chunks, each in order: four dims a thread.
+template <typename S, int HD>
+__global__ __launch_bounds__(256) void window_attn_kv_sum(WindowAttn a, const float* part, int nchunk, int parts,
+                                                          const float* heads, S* dqkv) {
+  const int width = 2 * a.Hkv * HD;
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, rows = (int64_t)a.B * a.T;
+  if (i >= rows * width) return;
+  const int64_t row = i / width;
+  const int col = (int)(i % width), b = (int)(row / a.T), key = (int)(row % a.T);
+  f32x4v t = {0.f, 0.f, 0.f, 0.f};
+  if (key < length_of(a, b)) {
+    for (int p = 0; p < parts; ++p) t += *reinterpret_cast<const f32x4v*>(heads + p * rows * width + i);
+    if (part && key < a.sinks) {
+      const int which = col / (a.Hkv * HD), kvh = col % (a.Hkv * HD) / HD, dim = col % HD;
+      const float* p = part + (((int64_t)b * a.Hkv + kvh) * nchunk * 2 + which) * a.sinks * HD + key * HD + dim;
+#pragma unroll 8
+      for (int ck = 0; ck < nchunk; ++ck) t += *reinterpret_cast<const f32x4v*>(p + (int64_t)ck * 2 * a.sinks * HD);
+    }
+  }
+  const float mul = col < a.Hkv * HD ? 1.f / sqrtf((float)HD) : 1.f;
+  put4(dqkv + row * a.lddq + a.H * HD + col, t[0] * mul, t[1] * mul, t[2] * mul, t[3] * mul);
+}
+
 // ------------------------------------------------------------- launching --
 namespace {
 
-// Queries from here on reach the first key block through its sink keys only
-// (the end of the last tile its own range walks).
-int far_start(const WindowAttn& a) { return (int)(((int64_t)a.window + 127 + AT - 1) / AT * AT); }
+// Whether to halve the blocks: while whole ones would not fill the chip's 256
+// compute units `per_cu` times over, what counts is the time of one (one
+// sequence of 2048 tokens, 8 heads of 64, window 512, 128 workgroups: forward
+// 16.8 -> 11.7 us, dQ 19.1 -> 14.2, dK/dV 23.6 -> 17.4); past that the halves
+// read the other dimension's tiles twice as often (8 sequences of 1024, 12
+// heads, window 256, 768 workgroups: 21.2 -> 23.6, 26.7 -> 31.0, 35.1 ->
+// 37.6).
+bool split_rows(const WindowAttn& a, int heads, int per_cu) {
+  return (int64_t)heads * a.B * cdiv(a.T, 128) < 256 * per_cu;
+}
+// Workgroups that share a compute unit: as the registers have it.
+template <typename S, int HD>
+constexpr int kPerCu = HD < 64 ? 3 : 2;
+template <typename S, int HD>
+constexpr int kPerCuDq = kWide<S, HD> ? 1 : kPerCu<S, HD>;
+template <typename S, int HD>
+constexpr int kPerCuDkdv = kWide<S, HD> ? 1 : kPerCu<S, HD>;
 
-// Chunks of the far queries: enough workgroups to fill the chip twice over,
-// and no chunk under 128 queries.
-int sink_chunks(const WindowAttn& a) {
-  const int64_t far = a.sinks > 0 ? (int64_t)a.T - far_start(a) : 0;
-  if (far <= 0) return 0;
-  const int64_t want = (512 + (int64_t)a.B * a.H - 1) / ((int64_t)a.B * a.H);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(want, (far + 127) / 128));
+template <typename S, int HD, bool SPLIT>
+hipError_t fwd(const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s) {
+  hipLaunchKernelGGL((window_attn_fwd<S, HD, SPLIT>), dim3(a.H, a.B, cdiv(a.T, block_rows<SPLIT>())), dim3(256), 0, s, a,
+                     static_cast<const S*>(qkv), static_cast<S*>(O), lse);
+  return hipGetLastError();
 }
 
+template <typename S, int HD, bool SPLIT>
+hipError_t dq(const WindowAttn& a, const void* qkv, const void* O, const void* dO, const float* lse, float* Dvec,
+              void* dqkv, hipStream_t s) {
+  hipLaunchKernelGGL((window_attn_dq<S, HD, SPLIT>), dim3(a.H, a.B, cdiv(a.T, block_rows<SPLIT>())), dim3(256), 0, s, a,
+                     static_cast<const S*>(qkv), static_cast<const S*>(O), static_cast<const S*>(dO), lse, Dvec,
+                     static_cast<S*>(dqkv));
+  return hipGetLastError();
+}
+
+// How dK and dV of a shape are computed.
+struct Plan {
+  int parts;       // workgroups that share a key/value head's query heads
+  bool split;      // blocks of 64 keys
+  int far, chunk, nchunk;
+  int64_t sinks, heads;  // floats of partial sums
+};
 template <typename S, int HD>
-hipError_t fwd(const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s) {
-  hipLaunchKernelGGL((window_attn_fwd<S, HD>), dim3(a.H, a.B, cdiv(a.T, 128)), dim3(256), 0, s, a,
-                     static_cast<const S*>(qkv), static_cast<S*>(O), lse);
+Plan plan_dkdv(const WindowAttn& a) {
+  Plan p;
+  // Shared key/value heads make few workgroups of much work: where halved
+  // blocks would not fill the chip either, their query heads are divided until
+  // they do (one sequence of 4096 tokens, 16 heads of 128 sharing 2, window
+  // 1024, the backward pass: 307 -> 159 us), while the fp32 sums of the parts
+  // fit the scratch.
+  constexpr int kFull = kPerCuDkdv<S, HD>;
+  const int grp = a.H / a.Hkv;
+  const int64_t per_part = (int64_t)a.B * a.T * 2 * a.Hkv * HD;
+  p.parts = 1;
+  if (split_rows(a, 2 * a.Hkv, kFull))
+    for (int d = 2; d <= grp; ++d)
+      if (grp % d == 0 && split_rows(a, a.Hkv * p.parts, kFull) && d * per_part <= kWindowPartFloats) p.parts = d;
+  p.split = split_rows(a, a.Hkv * p.parts, kFull);
+  // Queries from `far` on reach the first key block through its sink keys
+  // only (the end of the last tile that its own range walks).  Their chunks:
+  // enough workgroups to fill the chip twice over, and none under a tile.
+  const int rows = p.split ? 64 : 128;
+  p.far = (int)(((int64_t)a.window + rows - 1 + AT - 1) / AT * AT);
+  p.nchunk = p.chunk = 0;
+  if (a.sinks > 0 && p.far < a.T) {
+    const int64_t have = (int64_t)a.B * a.Hkv * cdiv(a.sinks, 32);
+    p.nchunk = (int)std::min<int64_t>((512 + have - 1) / have, cdiv(a.T - p.far, AT));
+    p.chunk = cdiv(cdiv(a.T - p.far, p.nchunk), AT) * AT;
+  }
+  p.sinks = (int64_t)a.B * a.Hkv * p.nchunk * 2 * a.sinks * HD;
+  p.heads = p.parts > 1 ? p.parts * per_part : 0;
+  return p;
+}
+
+template <typename S, int HD, bool SPLIT>
+hipError_t dkdv(const WindowAttn& a, const Plan& p, const void* qkv, const void* dO, const float* lse,
+                const float* Dvec, float* part, void* dqkv, hipStream_t s) {
+  const S *x = static_cast<const S*>(qkv), *g = static_cast<const S*>(dO);
+  float* heads = part + p.sinks;
+  if (p.nchunk > 0) {
+    hipLaunchKernelGGL((window_attn_sinks<S, HD>), dim3(a.Hkv, a.B, p.nchunk * cdiv(a.sinks, 32)), dim3(256), 0, s, a, x,
+                       g, lse, Dvec, block_rows<SPLIT>(), p.far, p.chunk, p.nchunk, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (p.nchunk == 0) part = nullptr;
+  hipLaunchKernelGGL((window_attn_dkdv<S, HD, SPLIT>), dim3(a.Hkv * p.parts, a.B, cdiv(a.T, block_rows<SPLIT>())),
+                     dim3(256), 0, s, a, x, g, lse, Dvec, part, p.nchunk, p.parts, heads, static_cast<S*>(dqkv));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.parts == 1) return e;
+  const int64_t quads = (int64_t)a.B * a.T * 2 * a.Hkv * HD / 4;
+  hipLaunchKernelGGL((window_attn_kv_sum<S, HD>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, a, part,
+                     p.nchunk, p.parts, heads, static_cast<S*>(dqkv));
   return hipGetLastError();
 }
 
 template <typename S, int HD>
 hipError_t bwd(const WindowAttn& a, const void* qkv, const void* O, const void* dO, const float* lse, float* Dvec,
                float* part, void* dqkv, hipStream_t s) {
-  const S *x = static_cast<const S*>(qkv), *g = static_cast<const S*>(dO);
-  S* dx = static_cast<S*>(dqkv);
-  hipLaunchKernelGGL((window_attn_dq<S, HD>), dim3(a.H, a.B, cdiv(a.T, 128)), dim3(256), 0, s, a, x,
-                     static_cast<const S*>(O), g, lse, Dvec, dx);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = split_rows(a, a.H, kPerCuDq<S, HD>) ? dq<S, HD, true>(a, qkv, O, dO, lse, Dvec, dqkv, s)
+                                                           : dq<S, HD, false>(a, qkv, O, dO, lse, Dvec, dqkv, s);
   if (e != hipSuccess) return e;
-  const int nc = sink_chunks(a);
-  if (nc > 0) {
-    const int far = far_start(a), chunk = cdiv(cdiv(a.T - far, nc), AT) * AT;
-    hipLaunchKernelGGL((window_attn_sinks<S, HD>), dim3(a.H, a.B, nc * cdiv(a.sinks, 32)), dim3(256), 0, s, a, x, g,
-                       lse, Dvec, far, chunk, nc, part);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL((window_attn_dkdv<S, HD>), dim3(a.Hkv, a.B, cdiv(a.T, 128)), dim3(256), 0, s, a, x, g, lse, Dvec,
-                     nc > 0 ? part : nullptr, nc, dx);
-  return hipGetLastError();
+  const Plan p = plan_dkdv<S, HD>(a);
+  return p.split ? dkdv<S, HD, true>(a, p, qkv, dO, lse, Dvec, part, dqkv, s)
+                 : dkdv<S, HD, false>(a, p, qkv, dO, lse, Dvec, part, dqkv, s);
+}
+
+template <typename S, int HD>
+int64_t scratch(const WindowAttn& a) {
+  const Plan p = plan_dkdv<S, HD>(a);
+  return p.sinks + p.heads;
 }
 
 }  // namespace
 
-int64_t window_attention_scratch(const WindowAttn& a) {
-  return (int64_t)a.B * a.H * sink_chunks(a) * 2 * a.sinks * a.hd;
-}
-
-#define FAL_BY_HEAD(S, CALL)                                  \
+#define FAL_BY_HEAD(S, CALL, bad)                                \
   switch (a.hd) {                                             \
     case 16: return CALL(S, 16);                              \
     case 32: return CALL(S, 32);                              \
     case 64: return CALL(S, 64);                              \
     case 128: return CALL(S, 128);                            \
-    default: return hipErrorInvalidValue;                     \
+    default: return bad;                                      \
   }
 
 hipError_t window_attention_fwd(DType dt, const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s) {
-#define FAL_FWD(S, HD) (fwd<S, HD>(a, qkv, O, lse, s))
-  if (dt == BF16) FAL_BY_HEAD(bf16, FAL_FWD)
-  FAL_BY_HEAD(float, FAL_FWD)
+#define FAL_FWD(S, HD) (split_rows(a, a.H, kPerCu<S, HD>) ? fwd<S, HD, true>(a, qkv, O, lse, s) : fwd<S, HD, false>(a, qkv, O, lse, s))
+  if (dt == BF16) FAL_BY_HEAD(bf16, FAL_FWD, hipErrorInvalidValue)
+  FAL_BY_HEAD(float, FAL_FWD, hipErrorInvalidValue)
 #undef FAL_FWD
 }
 
 hipError_t window_attention_bwd(DType dt, const WindowAttn& a, const void* qkv, const void* O, const void* dO,
                                 const float* lse, float* Dvec, float* part, void* dqkv, hipStream_t s) {
 #define FAL_BWD(S, HD) (bwd<S, HD>(a, qkv, O, dO, lse, Dvec, part, dqkv, s))
-  if (dt == BF16) FAL_BY_HEAD(bf16, FAL_BWD)
-  FAL_BY_HEAD(float, FAL_BWD)
+  if (dt == BF16) FAL_BY_HEAD(bf16, FAL_BWD, hipErrorInvalidValue)
+  FAL_BY_HEAD(float, FAL_BWD, hipErrorInvalidValue)
 #undef FAL_BWD
+}
+
+int64_t window_attention_scratch(DType dt, const WindowAttn& a) {
+#define FAL_SCRATCH(S, HD) (scratch<S, HD>(a))
+  if (dt == BF16) FAL_BY_HEAD(bf16, FAL_SCRATCH, 0)
+  FAL_BY_HEAD(float, FAL_SCRATCH, 0)
+#undef FAL_SCRATCH
 }
 #undef FAL_BY_HEAD
 

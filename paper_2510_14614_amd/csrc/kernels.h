@@ -229,10 +229,12 @@ struct WindowAttn {
   int64_t lddo, lddq;   // backward: of dO and dQKV
 };
 hipError_t window_attention_fwd(DType dt, const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s);
-// Dvec: fp32 [B, H, T] scratch; part: window_attention_scratch floats.
+// Dvec: fp32 [B, H, T] scratch; part: window_attention_scratch floats, of which
+// all but the sink keys' partial sums stay within kWindowPartFloats.
+constexpr int64_t kWindowPartFloats = (int64_t)1 << 23;
 hipError_t window_attention_bwd(DType dt, const WindowAttn& a, const void* qkv, const void* O, const void* dO,
                                 const float* lse, float* Dvec, float* part, void* dqkv, hipStream_t s);
-int64_t window_attention_scratch(const WindowAttn& a);
+int64_t window_attention_scratch(DType dt, const WindowAttn& a);
 
 // ------------------------------------------------ embedding / loss / misc ----
 // X[m, :] = wte[tok[b, t]] + wpe[t]  (fp32 out), tokens [B, T+1].

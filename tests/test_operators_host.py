@@ -87,17 +87,21 @@ def test_window_attention_refuses_pointers():
 
 
 def test_window_attention_workspace():
-    # D = rowsum(dO * O), fp32 [B, H, T], and for sinks that later queries
-    # see alone partial sums of their dK and dV
+    # D = rowsum(dO * O), fp32 [B, H, T]; for sinks that later queries see
+    # alone, partial sums of their dK and dV; for shared key/value heads, sums
+    # of parts of their query heads
     def size(**kw):
         n = ctypes.c_size_t()
-        assert fal.lib().fal_window_attention_workspace_bytes(byref(window(**kw)), byref(n)) == fal.FAL_OK
+        shape = window(**{"n_kv_head": 0, "ld_qkv": 768, **kw})
+        assert fal.lib().fal_window_attention_workspace_bytes(byref(shape), byref(n)) == fal.FAL_OK
         return n.value
     stat = (2 * 4 * 300 * 4 + 255) // 256 * 256
     assert size(sinks=0) == stat
     assert size(window=300) == stat  # every key in every window
     assert size() > stat
     assert (size() - stat) % (2 * 4 * 2 * 4 * 64 * 4) == 0  # whole [B, H, chunk, dK | dV, sinks, hd]
+    shared = size(sinks=0, n_kv_head=1) - stat
+    assert shared > 0 and shared % (2 * 300 * 2 * 64 * 4) == 0  # whole [part, B, T, dK | dV, hd]
 
 
 @pytest.mark.parametrize("kw,word", [
