@@ -140,6 +140,8 @@ struct Stage {
   }
 };
 
+constexpr int kFewKeys = 64;
+
 // The window's mask over a 32x32 score tile whose rows are the keys from kb on
 // and whose lane has query tq, one of q0 .. q0 + 31: -inf for keys after the
 // query (or past n), and for keys before its window and past the sinks.  Each
@@ -480,7 +482,12 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
 }
 
 // ----------------------------------------------------------- backward: dQ --
-// Also writes D = rowsum(dO * O) for the kernels that follow.
+// Also writes D = rowsum(dO * O) for the kernels that follow.  O as it was
+// stored carries its rounding into D, which a row of many keys averages out
+// and one of few does not (bf16 gradients of a window of 2 keys: 2.7e-3 off
+// against 2.2e-3 with D exact, of 20: 2.42e-3 against 2.36e-3; 1.65e-3 is the
+// rounding of the gradients alone).  So bf16 rows of at most kFewKeys keys sum
+// D = rowsum(P * dP) in a walk of their own over their few tiles.
 template <typename S, int HD, bool SPLIT>
 __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_dq(WindowAttn a, const S* qkv, const S* O, const S* dO,
                                                          const float* lse, float* Dvec, S* dqkv) {
@@ -512,9 +519,50 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_dq(Wi
     D += __shfl_xor(D, 32, 64);
     const int64_t stat = ((int64_t)b * a.H + h) * a.T + tq;
     const float L2 = tq < n ? lse[stat] * kLog2e : 0.f;
-    if (g == 0 && tq < n && (!SPLIT || wave < 2)) Dvec[stat] = D;
     const KeyTiles kt(a, qb, block_rows<SPLIT>(), n);
     Stage<S, HD> rk(Kg, a.ldq, tid), rv(Vg, a.ldq, tid);
+    // scores of 32 keys, and dP plus what dp0 holds; false if no row of the
+    // wavefront sees them
+    f32x16v dp0 = zero16();
+    auto score = [&](int k0, int sub, f32x16v& s, f32x16v& dp) {
+      const int kb = k0 + 32 * sub;
+      if (kb > q0 + 31 || kb >= n || (kb >= a.sinks && q0 - (kb + 31) >= a.window)) return false;
+      s = zero16();
+      dp = dp0;
+      dot_rows<HD>(sK, 32 * sub, c, g, q, s);
+      dot_rows<HD>(sV, 32 * sub, c, g, d, dp);
+      dots_ahead<S, HD, 2>();
+      mask_keys(a, kb, q0, tq, n, g, s);
+      return true;
+    };
+    if (sizeof(S) == 2 && a.window + a.sinks <= kFewKeys) {
+      D = 0.f;
+      for (int i = 0; i < kt.count; ++i) {
+        rk.load(kt.at(i), n, tid);
+        rv.load(kt.at(i), n, tid);
+        __syncthreads();
+        rk.store(sK, kt.at(i), n, tid);
+        rv.store(sV, kt.at(i), n, tid);
+        __syncthreads();
+        for (int u = 0; u < (SPLIT ? 1 : AT / 32); ++u) {
+          f32x16v s, dp;
+          if (!score(kt.at(i), SPLIT ? wave >> 1 : u, s, dp)) continue;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) D = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], sl2, -L2)), dp[r], D);
+        }
+      }
+      D += __shfl_xor(D, 32, 64);
+      if (SPLIT) {  // both wavefronts of a pair take the sum of their halves
+        float* sum = reinterpret_cast<float*>(lds);
+        __syncthreads();
+        sum[64 * wave + lane] = D;
+        __syncthreads();
+        D = sum[64 * (wave & 1) + lane] + sum[64 * (2 + (wave & 1)) + lane];
+      }
+    }
+    if (g == 0 && tq < n && (!SPLIT || wave < 2)) Dvec[stat] = D;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp0[r] = -D;  // the products then give dP - D
     rk.load(kt.at(0), n, tid);
     rv.load(kt.at(0), n, tid);
     for (int i = 0; i < kt.count; ++i) {
@@ -530,18 +578,12 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_dq(Wi
 #pragma unroll
       for (int u = 0; u < (SPLIT ? 1 : AT / 32); ++u) {
         const int sub = SPLIT ? wave >> 1 : u;
-        const int kb = k0 + 32 * sub;
-        if (kb > q0 + 31 || kb >= n) break;
-        if (kb >= a.sinks && q0 - (kb + 31) >= a.window) continue;
-        f32x16v s = zero16(), dp = zero16();
-        dot_rows<HD>(sK, 32 * sub, c, g, q, s);
-        dot_rows<HD>(sV, 32 * sub, c, g, d, dp);
-        dots_ahead<S, HD, 2>();
-        mask_keys(a, kb, q0, tq, n, g, s);
+        f32x16v s, dp;
+        if (!score(k0, sub, s, dp)) continue;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -L2));
-          dp[r] = p * (dp[r] - D);
+          dp[r] *= p;
         }
         __builtin_amdgcn_sched_barrier(0);
         add_rows<HD>(sK, 32 * sub, lane, dp, dq);
@@ -571,7 +613,7 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_sinks
   constexpr int NT = n_tiles<HD>();
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, true>()];
   S *sQ = reinterpret_cast<S*>(lds), *sdO = sQ + tile_len<S, HD>();
-  __shared__ float sL[AT], sD[AT];
+  __shared__ float sL[AT], sD[AT];  // of a tile's queries: -lse in log2 units, -D
   const int kvh = blockIdx.x, b = blockIdx.y, ck = blockIdx.z % nchunk, kw = 32 * (blockIdx.z / nchunk);
   const int grp = a.H / a.Hkv;
   const int64_t row0 = (int64_t)b * a.T;
@@ -601,24 +643,24 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_sinks
         if (tid < AT) {
           const int tq = q0 + tid;
           const int64_t stat = ((int64_t)b * a.H + h) * a.T + tq;
-          sL[tid] = tq < qend ? lse[stat] * kLog2e : 0.f;
-          sD[tid] = tq < qend ? Dvec[stat] : 0.f;
+          sL[tid] = tq < qend ? -lse[stat] * kLog2e : 0.f;
+          sD[tid] = tq < qend ? -Dvec[stat] : 0.f;
         }
         __syncthreads();
         f32x16v s = zero16();
         dot_rows<HD>(sQ, 32 * sub, c, g, k, s);
         if (keys) {
-          f32x16v dp = zero16();
+          f32x16v dp;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) dp[r] = sD[32 * sub + acc_row(r, g)];
           dot_rows<HD>(sdO, 32 * sub, c, g, v, dp);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int qr = 32 * sub + acc_row(r, g);
-            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[qr])) * (dp[r] - sD[qr]);
-          }
+          for (int r = 0; r < 16; ++r)
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, sL[32 * sub + acc_row(r, g)])) * dp[r];
           add_rows<HD>(sQ, 32 * sub, lane, s, acc);
         } else {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[32 * sub + acc_row(r, g)]));
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, sL[32 * sub + acc_row(r, g)]));
           add_rows<HD>(sdO, 32 * sub, lane, s, acc);
         }
       }
@@ -641,11 +683,11 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD ==
                                                                            const float* part, int nchunk, int parts,
                                                                            float* heads, S* dqkv) {
   constexpr int NT = n_tiles<HD>();
-  constexpr bool KL = kKeysInLds<S, HD>;
+  constexpr bool KL = kKeysInLds<S, HD>, LATE = KL && HD == 128;
   __shared__ __attribute__((aligned(16))) S sK[KL ? block_rows<SPLIT>() / AT * tile_len<S, HD>() : 8];
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, SPLIT>()];
   S *sQ = reinterpret_cast<S*>(lds), *sdO = sQ + tile_len<S, HD>();
-  __shared__ float sL[AT], sD[AT];
+  __shared__ float sL[AT], sD[AT];  // of a tile's queries: -lse in log2 units, -D
   const int kvh = blockIdx.x / parts, b = blockIdx.y, kb0 = block_rows<SPLIT>() * blockIdx.z;
   const int grp = a.H / a.Hkv / parts, h0 = blockIdx.x * grp;  // this workgroup's query heads
   const int64_t row0 = (int64_t)b * a.T;
@@ -676,14 +718,14 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD ==
     const int nit = grp * nq;
     Stage<S, HD> rq(qkv + row0 * a.ldq + h0 * HD, a.ldq, tid);
     Stage<S, HD> ro(dO + row0 * a.lddo + h0 * HD, a.lddo, tid);
-    if (!KL) {
+    if (!LATE) {
       rq.load(kb0, n, tid);
       ro.load(kb0, n, tid);
     }
     int h = h0, qi = 0;
     for (int it = 0; it < nit; ++it) {
       const int q0 = kb0 + AT * qi;
-      if (KL) {
+      if (LATE) {
         rq.load(q0, n, tid);
         ro.load(q0, n, tid);
       }
@@ -693,8 +735,8 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD ==
       if (tid < AT) {
         const int tq = q0 + tid;
         const int64_t stat = ((int64_t)b * a.H + h) * a.T + tq;
-        sL[tid] = tq < n ? lse[stat] * kLog2e : 0.f;
-        sD[tid] = tq < n ? Dvec[stat] : 0.f;
+        sL[tid] = tq < n ? -lse[stat] * kLog2e : 0.f;
+        sD[tid] = tq < n ? -Dvec[stat] : 0.f;
       }
       __syncthreads();
       if (++qi == nq) {
@@ -703,7 +745,7 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD ==
         rq.src += HD;
         ro.src += HD;
       }
-      if (!KL && it + 1 < nit) {
+      if (!LATE && it + 1 < nit) {
         rq.load(kb0 + AT * qi, n, tid);
         ro.load(kb0 + AT * qi, n, tid);
       }
@@ -713,7 +755,9 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD ==
         const int qs = q0 + 32 * sub;
         if (qs + 31 < kw || qs >= n) continue;                      // before this wavefront's keys, or past the end
         if (kw >= a.sinks && qs - (kw + 31) >= a.window) continue;  // past the window of all its keys
-        f32x16v s = zero16(), dp = zero16();
+        f32x16v s = zero16(), dp;  // dp from -D on: the products give dP - D
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] = sD[32 * sub + acc_row(r, g)];
         if (KL) dot_rows<HD>(sQ, 32 * sub, c, g, ownK, s);
         else dot_rows<HD>(sQ, 32 * sub, c, g, k, s);
         dot_rows<HD>(sdO, 32 * sub, c, g, v, dp);
@@ -722,10 +766,8 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD ==
         mask_queries(a, qs, kw, key, g, s);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int qr = 32 * sub + acc_row(r, g);
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, -sL[qr]));
-          s[r] = p;
-          dp[r] = p * (dp[r] - sD[qr]);
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sl2, sL[32 * sub + acc_row(r, g)]));
+          dp[r] *= s[r];
         }
         __builtin_amdgcn_sched_barrier(0);
         add_rows<HD>(sdO, 32 * sub, lane, s, dv);
