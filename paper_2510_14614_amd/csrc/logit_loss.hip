@@ -8,7 +8,8 @@
 // All of it is bound by HBM: a row is read in 16-byte chunks and, while the
 // registers of its threads hold it, read once: each thread reduces its chunks
 // to (maximum, sum of exponentials), one exchange joins the threads, and the
-// gradient is written from the registers.  A longer row is read twice.  Rows
+// gradient is written from the registers; what they cannot hold of a longer row
+// is read twice.  Rows
 // need no alignment: a chunk that a row's edge crosses is read and written
 // element by element (two of a row's chunks), columns outside the row read as
 // -inf.  Exponentials are exp2 of (x - maximum) log2(e) / temperature, sums
@@ -317,8 +318,8 @@ struct RowOut {
   void* dlogits;
 };
 
-// G threads a row, NPT chunks each held in registers; NPT = 0: the row is
-// read again for its gradient.
+// G threads a row, NPT chunks each held in registers; what a longer row has past
+// them is read again for its gradient.
 template <typename S, int G, int NPT, Mode MODE>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, RowOut o) {
   constexpr int RPW = (G < 256 ? 256 : G) / G;
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
 #pragma unroll
     for (int i = 0; i < NPT; ++i) {
       const int c = t + G * i;
-      if (c < nc) raw[i] = in.template load<MODE != STATS>(c);
+      if (c < nc) raw[i] = in.template load<true>(c);
     }
 #pragma unroll
     for (int i = 0; i < NPT; ++i)
@@ -371,25 +372,24 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
       for (int i = 0; i < NPT; ++i)
         if (t + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(raw[i], st, k);
     }
-  } else {
-    for (int c0 = t; c0 < nc; c0 += kStream * G) {
-      uint4 u[kStream];
+  }
+  for (int c0 = t + NPT * G; c0 < nc; c0 += kStream * G) {
+    uint4 u[kStream];
+#pragma unroll
+    for (int i = 0; i < kStream; ++i)
+      if (c0 + G * i < nc) u[i] = in.template load<MODE == LOGP || MODE == LOGP_ENTROPY>(c0 + G * i);
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kStream; ++i)
+      if (c0 + G * i < nc) top = chunk_max<S>(u[i], top);
+    if (top > st.m) {
+      const Stat none{top, 0.f, 0.f};
+      join(st, none, k);
+    }
+    if (st.m != -INFINITY) {
 #pragma unroll
       for (int i = 0; i < kStream; ++i)
-        if (c0 + G * i < nc) u[i] = in.template load<MODE == LOGP || MODE == LOGP_ENTROPY>(c0 + G * i);
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kStream; ++i)
-        if (c0 + G * i < nc) top = chunk_max<S>(u[i], top);
-      if (top > st.m) {
-        const Stat none{top, 0.f, 0.f};
-        join(st, none, k);
-      }
-      if (st.m != -INFINITY) {
-#pragma unroll
-        for (int i = 0; i < kStream; ++i)
-          if (c0 + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(u[i], st, k);
-      }
+        if (c0 + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(u[i], st, k);
     }
   }
   const Shared sh = exchange<G>(st, xt, n, k);
@@ -415,16 +415,13 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
   const float scale = pr.c * w * r.inv_temp;
   const bool same = in.shift == out.shift;
   const int end = same ? out.chunks() : nc;
-  if (NPT) {
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);  // columns past V: any value
+  const uint4 none = make_uint4(0u, 0u, 0u, 0u);  // columns past V: any value
 #pragma unroll
-    for (int i = 0; i < NPT; ++i) {
-      const int c = t + G * i;
-      if (c < end) grad_chunk<S>(c < nc ? raw[i] : none, in.column(c), r.V, tgt, k, sh.st.m, log2sum, scale, out, c);
-    }
-  } else {
-    row_grad<S, G, false>(in, out, t, end, tgt, k, sh.st.m, log2sum, scale);
+  for (int i = 0; i < NPT; ++i) {
+    const int c = t + G * i;
+    if (c < end) grad_chunk<S>(c < nc ? raw[i] : none, in.column(c), r.V, tgt, k, sh.st.m, log2sum, scale, out, c);
   }
+  row_grad<S, G, false>(in, out, t + NPT * G, end, tgt, k, sh.st.m, log2sum, scale);
   if (!same) zero_tail<S, G>(out, r.V, t);
 }
 
@@ -551,11 +548,13 @@ hipError_t scored_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
 }
 
 // Rows with a gradient are held by as few threads as can (up to 26 chunks
-// each, 16 in a workgroup of 1024, whose registers are half as many): several
+// each, 13 in a workgroup of 1024, whose registers are half as many): several
 // rows then share a compute unit and one's exchange and stores pass under
 // another's loads (rows of 50257 bf16 as above: 273 us with 256 x 26, 314 with
 // 512 x 13, 338 with 1024 x 7; 50257 fp32: 238 with 1024 x 13, 247 with
-// 512 x 26).  Longer rows are read twice.
+// 512 x 26).  The 1024 threads hold 13312 chunks and read the rest of a longer
+// row twice (1028 rows of 128001 fp32, half of them counted: 171 us against
+// 204 with none held and 186 with 24 chunks a thread).
 template <typename S>
 hipError_t policy_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
   constexpr int E = Chunk<S>::E;
@@ -568,9 +567,7 @@ hipError_t policy_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
   if (n <= 2048) return launch<S, 256, 8, POLICY>(r, o, s);
   if (n <= 4096) return launch<S, 256, 16, POLICY>(r, o, s);
   if (n <= 6656) return launch<S, 256, 26, POLICY>(r, o, s);
-  if (n <= 13312) return launch<S, 1024, 13, POLICY>(r, o, s);
-  if (n <= 16384) return launch<S, 1024, 16, POLICY>(r, o, s);
-  return launch<S, 1024, 0, POLICY>(r, o, s);
+  return launch<S, 1024, 13, POLICY>(r, o, s);
 }
 
 template <typename S, int G>
