@@ -435,7 +435,8 @@ typedef struct {
   int64_t ld_dlogits;   /* elements between gradient rows                   */
   int32_t dlogits_cols; /* columns written of each gradient row: V of them
                            the gradient, the rest zeros; V .. ld_dlogits    */
-  float temperature;    /* > 0: the scores are logits / temperature         */
+  float temperature;    /* > 0: the scores are logits / temperature (which
+                           must leave log2(e) / temperature finite, not 0)  */
 } fal_logit_rows_t;
 
 /* Log-probability of each row's target under softmax(logits / temperature),
@@ -536,9 +537,9 @@ fal_status_t fal_preference_step(fal_ctx_t* ctx, const void* params, const fal_p
  * returns, per class since the last enable: the number of launches, the
  * summed event time in ms, and the summed algorithmic FLOPs and bytes of
  * those launches (GEMM: 2*M*N*K; attention forward: 2*B*H*hd*T*(T+1), the
- * causal half of QK^T and PV; attention backward: twice that; norm: bytes
- * of the rows read and written; cross-entropy: logits read and dlogits
- * written; embedding: rows gathered and written forward, the position-
+ * causal half of QK^T and PV, or the pairs that a window leaves of it; attention backward: twice that; norm: bytes
+ * of the rows read and written; cross-entropy, and the log-probabilities and
+ * losses that take its place: logits read and dlogits written; embedding: rows gathered and written forward, the position-
  * gradient and scatter traffic backward; bias gradients: the column sums'
  * input; optimizer: the gradient read by the norm pass plus every array
  * the update reads and writes).  fal_profile_enable(ctx, 0) turns timing off; either call clears

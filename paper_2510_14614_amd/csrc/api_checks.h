@@ -20,15 +20,18 @@ inline bool overlaps(const void* a, int64_t abytes, const void* b, int64_t bbyte
 
 inline bool aligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
+// (the kernels multiply by log2(e) / t, which has to be finite and not zero)
 inline const char* check_temperature(float t) {
-  return std::isfinite(t) && t > 0.f && std::isfinite(1.f / t) ? nullptr : "temperature must be finite and > 0";
+  const float k = 1.4426950408889634f / t;
+  return std::isfinite(t) && t > 0.f && std::isfinite(k) && k > 0.f ? nullptr : "temperature must be finite and > 0";
 }
 
 inline const char* check_policy(const fal_policy_t* hp) {
   if (!hp) return "NULL hyper-parameters";
   if (!std::isfinite(hp->clip_low) || !std::isfinite(hp->clip_high) || !std::isfinite(hp->kl_coef))
     return "non-finite hyper-parameter";
-  if (hp->clip_low < 0.f || hp->clip_low > 1.f || hp->clip_high < 0.f) return "clip_low must lie in [0, 1], clip_high be >= 0";
+  if (hp->clip_low < 0.f || hp->clip_low > 1.f || hp->clip_high < 0.f)
+    return "clip_low must lie in [0, 1], clip_high be >= 0";
   if (hp->kl_coef < 0.f) return "kl_coef must be >= 0";
   if (hp->sequence_mean != 0 && hp->sequence_mean != 1) return "sequence_mean must be 0 or 1";
   return nullptr;

@@ -8,11 +8,10 @@
 // All of it is bound by HBM: a row is read in 16-byte chunks and, while the
 // registers of its threads hold it, read once: each thread reduces its chunks
 // to (maximum, sum of exponentials), one exchange joins the threads, and the
-// gradient is written from the registers; what they cannot hold of a longer row
-// is read twice.  Rows
-// need no alignment: a chunk that a row's edge crosses is read and written
-// element by element (two of a row's chunks), columns outside the row read as
-// -inf.  Exponentials are exp2 of (x - maximum) log2(e) / temperature, sums
+// gradient is written from the registers; what they cannot hold of a longer
+// row is read twice.  Rows need no alignment: a chunk that a row's edge crosses
+// is read and written element by element (two of a row's chunks), columns
+// outside the row read as -inf.  Exponentials are exp2 of (x - maximum) log2(e) / temperature, sums
 // fp32 within a row; sums over rows and sequences are fp64, since a sequence's
 // log-probability is large (hundreds of terms) and the losses see a small
 // difference of two.
@@ -488,7 +487,8 @@ __global__ __launch_bounds__(256) void preference_pairs(LogitRows r, PreferenceA
     dh = 2.0 * u;
   } else {
     const double z = beta * h, tail = log1p(exp(-fabs(z)));
-    loss = (1.0 - sm) * (tail + fmax(-z, 0.0)) + sm * (tail + fmax(z, 0.0));
+    loss = (1.0 - sm) * (tail + fmax(-z, 0.0));
+    if (sm > 0.0) loss += sm * (tail + fmax(z, 0.0));  // (0 times an infinite margin is no term)
     dh = beta * (1.0 / (1.0 + exp(-z)) - (1.0 - sm));
   }
   pair_loss[b0] = loss;

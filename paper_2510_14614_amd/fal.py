@@ -288,7 +288,7 @@ def _row_stride(t, name):
     sb, st, sw = t.stride()
     if width > 1 and sw != 1:
         _refuse(f"{name} must be contiguous in its last dimension")
-    ld = st if T > 1 else sb if B > 1 else max(width, st)
+    ld = st if T > 1 else sb if B > 1 else width
     if B > 1 and sb != T * ld:
         _refuse(f"the sequences of {name} must follow each other at seq_len rows")
     return ld
@@ -632,6 +632,11 @@ class Fal:
         `window` keys and the first `sinks`; window 0 restores the full mask."""
         _check(lib().fal_set_attention_window(self.ctx, _clamp32(window), _clamp32(sinks)), self.ctx)
 
+    def _empty(self, *shape):
+        """An fp32 result, allocated on the stream that will write it."""
+        with self.torch.cuda.stream(self.stream_main):
+            return self.torch.empty(shape, dtype=self.torch.float32, device=self.device)
+
     def _token_arrays(self, tokens, mask, **arrays):
         torch = self.torch
         B, T = self.cfg.batch, self.cfg.seq_len
@@ -646,10 +651,9 @@ class Fal:
         """Log-probabilities of tokens[:, 1:] under the model, float32 [B, T]
         (zero where mask, over the T predicted tokens, is zero); with
         entropy=True also the entropies."""
-        torch = self.torch
         self._token_arrays(tokens, mask)
-        logp = torch.empty(self.cfg.batch, self.cfg.seq_len, dtype=torch.float32, device=self.device)
-        ent = torch.empty_like(logp) if entropy else None
+        logp = self._empty(self.cfg.batch, self.cfg.seq_len)
+        ent = self._empty(self.cfg.batch, self.cfg.seq_len) if entropy else None
         _check(lib().fal_model_logprobs(self.ctx, self.params.data_ptr(), tokens.data_ptr(), _ptr(mask), temperature,
                                         logp.data_ptr(), _ptr(ent)), self.ctx)
         return (logp, ent) if entropy else logp
@@ -659,11 +663,9 @@ class Fal:
         """Forward, clipped policy loss over tokens[:, 1:] and backward: fills
         self.grads and returns the stats of policy_loss (float32 [4]) and the
         log-probabilities (float32 [B, T])."""
-        torch = self.torch
         self._token_arrays(tokens, mask, old_logp=old_logp, advantages=advantages, ref_logp=ref_logp)
         hp = fal_policy_t(clip_low, clip_high, kl_coef, int(sequence_mean))
-        stats = torch.empty(4, dtype=torch.float32, device=self.device)
-        logp = torch.empty(self.cfg.batch, self.cfg.seq_len, dtype=torch.float32, device=self.device)
+        stats, logp = self._empty(4), self._empty(self.cfg.batch, self.cfg.seq_len)
         _check(lib().fal_policy_step(self.ctx, self.params.data_ptr(), byref(hp), tokens.data_ptr(), _ptr(mask),
                                      temperature, _ptr(old_logp), _ptr(ref_logp), _ptr(advantages), stats.data_ptr(),
                                      logp.data_ptr(), self.grads.data_ptr()), self.ctx)
@@ -674,10 +676,9 @@ class Fal:
         """Forward, preference loss over the pairs (b, b + B/2) of tokens[:,
         1:] and backward: fills self.grads and returns the loss (self.loss)
         and the sequences' log-probabilities (float32 [B])."""
-        torch = self.torch
         self._token_arrays(tokens, mask, ref_seq_logp=ref_logp)
         hp = fal_preference_t(beta, label_smoothing, int(ipo), int(length_mean))
-        seq_logp = torch.empty(self.cfg.batch, dtype=torch.float32, device=self.device)
+        seq_logp = self._empty(self.cfg.batch)
         _check(lib().fal_preference_step(self.ctx, self.params.data_ptr(), byref(hp), tokens.data_ptr(), _ptr(mask),
                                          temperature, _ptr(ref_logp), self.loss.data_ptr(), seq_logp.data_ptr(),
                                          self.grads.data_ptr()), self.ctx)

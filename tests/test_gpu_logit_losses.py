@@ -234,6 +234,40 @@ def test_preference_loss(B, T, V, ipo, mean, smooth, dtype):
     within("dlogits", got.dlogits, torch.where(mask[:, :, None], grad, 0.0), bound)
 
 
+def test_preference_of_impossible_answers():
+    # a token of probability zero in one sequence of a pair: an infinite
+    # margin, of loss 0 where the model is right and infinite where not
+    x, y, _ = rows(4, 2, 30, F32, seed=8)
+    y.fill_(3)
+    x[2, 1, 3] = -math.inf  # rejected sequence of pair 0
+    ref = torch.zeros(4, device="cuda")
+    got = fal.preference_loss(x, y, ref)
+    lp, logp = exact(x, y, 30, 1.0)
+    h = float(logp[1].sum() - logp[3].sum())
+    assert abs(float(got.loss) - math.log1p(math.exp(-0.1 * h)) / 2) <= 1e-6
+    assert float(got.seq_logp[2]) == -math.inf and torch.isfinite(got.dlogits).all()
+    assert not got.dlogits[0].any() and not got.dlogits[2].any()
+    x[0, 0, 3], x[2, 1, 3] = -math.inf, 0.0
+    got = fal.preference_loss(x, y, ref)
+    assert float(got.loss) == math.inf and torch.isfinite(got.dlogits).all() and got.dlogits[0, 1].any()
+
+
+@pytest.mark.parametrize("temperature", [1e-38, 1e-3, 1e3, 1e38])
+def test_extreme_temperatures(temperature):
+    x, y, _ = rows(1, 3, 200, F32, seed=15)
+    y[0, 0] = int(x[0, 0].argmax())
+    logp, ent = fal.token_logprobs(x, y, temperature=temperature, entropy=True)
+    lp = (x.double() / float(torch.tensor(temperature))).log_softmax(-1)
+    want = lp.gather(-1, y.long()[:, :, None])[:, :, 0].float()
+    h = -torch.where(lp.exp() > 0, lp.exp() * lp, 0.0).sum(-1)
+    # x / temperature is off by 4 u of itself; sums as in the header
+    e = 8 * U * x.double().abs().max() / temperature + (200 / 256 + 24) * U
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(logp), fine)
+    assert bool(((logp - want)[fine].abs().double() <= e).all())
+    assert bool((ent.double() - h).abs().max() <= e * 6) and not torch.isnan(ent).any()
+
+
 @pytest.mark.parametrize("kind", ["policy", "preference"])
 def test_gradients_against_differences(kind):
     B, T, V = 2, 5, 40

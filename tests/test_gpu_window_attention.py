@@ -104,6 +104,7 @@ def check(name, got, want, bound):
 SHAPES = [
     # B, T, H, kv, hd, window, sinks, lens
     (1, 1, 1, 1, 64, 1, 0, None),          # one token
+    (5, 1, 2, 1, 64, 3, 2, (1, 0, 1, 1, 1)),
     (2, 2, 3, 3, 16, 1, 1, None),
     (2, 33, 4, 2, 32, 7, 2, (33, 0)),      # an empty sequence
     (3, 65, 2, 1, 16, 64, 3, (65, 1, 64)),
@@ -117,6 +118,15 @@ SHAPES = [
     (1, 1500, 2, 1, 128, 127, 1, None),
     (3, 385, 6, 3, 64, 64, 0, (385, 128, 129)),
     (1, 129, 8, 2, 128, 128, 2, None),
+    # grids that fill the chip, whole blocks of 128 rows (the others halve
+    # them): every head_dim, sinks seen from afar, ragged, shared heads
+    (16, 280, 32, 16, 64, 40, 3, None),
+    (16, 260, 32, 32, 128, 100, 0, (260, 259, 258, 257, 256, 255, 200, 129, 128, 127, 65, 64, 33, 1, 0, 260)),
+    (24, 270, 32, 32, 32, 30, 33, None),
+    (24, 257, 32, 32, 16, 8, 1, None),
+    # few key/value heads: the query heads of a group divided
+    (1, 600, 24, 2, 64, 200, 5, (577,)),
+    (1, 600, 6, 1, 128, 70, 40, None),
 ]
 
 

@@ -111,7 +111,7 @@ def test_window_attention_workspace():
     (dict(ld_logits=99), "ld_logits"), (dict(ld_targets=9), "ld_targets"),
     (dict(temperature=0.0), "temperature"), (dict(temperature=-1.0), "temperature"),
     (dict(temperature=float("nan")), "temperature"), (dict(temperature=float("inf")), "temperature"),
-    (dict(temperature=1e-45), "temperature"),
+    (dict(temperature=1e-45), "temperature"), (dict(temperature=4e-39), "temperature"),
 ])
 def test_logit_rows_refuse_a_shape(kw, word):
     L, r, n = fal.lib(), rows(**kw), ctypes.c_size_t()
