@@ -537,13 +537,15 @@ fal_status_t fal_preference_step(fal_ctx_t* ctx, const void* params, const fal_p
  * returns, per class since the last enable: the number of launches, the
  * summed event time in ms, and the summed algorithmic FLOPs and bytes of
  * those launches (GEMM: 2*M*N*K; attention forward: 2*B*H*hd*T*(T+1), the
- * causal half of QK^T and PV, or the pairs that a window leaves of it; attention backward: twice that; norm: bytes
- * of the rows read and written; cross-entropy, and the log-probabilities and
- * losses that take its place: logits read and dlogits written; embedding: rows gathered and written forward, the position-
- * gradient and scatter traffic backward; bias gradients: the column sums'
- * input; optimizer: the gradient read by the norm pass plus every array
- * the update reads and writes).  fal_profile_enable(ctx, 0) turns timing off; either call clears
- * the counters.  Host memory only; no device allocation. */
+ * causal half of QK^T and PV, or the pairs that a window leaves of it;
+ * attention backward: twice that; norm: bytes of the rows read and written;
+ * cross-entropy, and the log-probabilities and losses that take its place:
+ * logits read and dlogits written; embedding: rows gathered and written
+ * forward, the position-gradient and scatter traffic backward; bias
+ * gradients: the column sums' input; optimizer: the gradient read by the norm
+ * pass plus every array the update reads and writes).
+ * fal_profile_enable(ctx, 0) turns timing off; either call clears the
+ * counters.  Host memory only; no device allocation. */
 typedef enum {
   FAL_PROF_GEMM = 0, FAL_PROF_ATTN_FWD = 1, FAL_PROF_ATTN_BWD = 2, FAL_PROF_NORM = 3,
   FAL_PROF_CE = 4, FAL_PROF_EMBED = 5, FAL_PROF_BIAS = 6, FAL_PROF_OPTIM = 7,

@@ -63,7 +63,8 @@ Refusal check_shape(const fal_window_attention_t* p) {
   const int64_t chunk = p->dtype == FAL_BF16 ? 8 : 4;  // elements of 16 bytes
   if (p->ld_qkv < (p->n_head + 2 * kv) * p->head_dim) return {FAL_ERR_INVALID_ARG, "ld_qkv is smaller than a row"};
   if (p->ld_out < (int64_t)p->n_head * p->head_dim) return {FAL_ERR_INVALID_ARG, "ld_out is smaller than a row"};
-  if (p->ld_qkv % chunk || p->ld_out % chunk) return {FAL_ERR_INVALID_ARG, "row strides must be multiples of 16 bytes"};
+  if (p->ld_qkv % chunk || p->ld_out % chunk)
+    return {FAL_ERR_INVALID_ARG, "row strides must be multiples of 16 bytes"};
   if (p->ld_qkv > kMaxStride || p->ld_out > kMaxStride) return {FAL_ERR_INVALID_ARG, "row stride above 2^40 elements"};
   return kFine;
 }
@@ -108,7 +109,8 @@ Refusal check_rows(const fal_logit_rows_t* r, bool gradient) {
   if ((int64_t)r->batch * r->seq_len > (1 << 24)) return {FAL_ERR_INVALID_ARG, "batch*seq_len too large"};
   if (r->vocab < 1 || r->vocab > (1 << 20)) return {FAL_ERR_INVALID_ARG, "vocab must lie in [1, 2^20]"};
   const int64_t most = (int64_t)1 << 32;
-  if (r->ld_logits < r->vocab || r->ld_logits > most) return {FAL_ERR_INVALID_ARG, "ld_logits must lie in [vocab, 2^32]"};
+  if (r->ld_logits < r->vocab || r->ld_logits > most)
+    return {FAL_ERR_INVALID_ARG, "ld_logits must lie in [vocab, 2^32]"};
   if (r->ld_targets < r->seq_len || r->ld_targets > most)
     return {FAL_ERR_INVALID_ARG, "ld_targets must lie in [seq_len, 2^32]"};
   if (gradient && (r->dlogits_cols < r->vocab || r->ld_dlogits < r->dlogits_cols || r->ld_dlogits > most))
@@ -190,7 +192,8 @@ fal_status_t fal_window_attention_fwd(const fal_window_attention_t* shape, const
     const Extent x = rows_of(qkv, M, a.ldq, (int64_t)(a.H + 2 * a.Hkv) * a.hd, es),
                  o = rows_of(out, M, a.ldo, (int64_t)a.H * a.hd, es), l = {lse, M * a.H * 4},
                  n = {lens, (int64_t)a.B * 4};
-    if (meets(o, {x, l, n}) || meets(l, {x, n})) return fail(FAL_ERR_INVALID_ARG, "out or lse overlaps another argument");
+    if (meets(o, {x, l, n}) || meets(l, {x, n}))
+      return fail(FAL_ERR_INVALID_ARG, "out or lse overlaps another argument");
     return launched(window_attention_fwd(shape->dtype == FAL_BF16 ? BF16 : F32, a, qkv, out, lse,
                                          static_cast<hipStream_t>(stream)),
                     "fal_window_attention_fwd");
@@ -203,13 +206,16 @@ fal_status_t fal_window_attention_bwd(const fal_window_attention_t* shape, const
   return guarded([&] {
     const Refusal no = check_shape(shape);
     if (no.why) return fail(no.st, no.why);
-    if (!qkv || !out || !d_out || !lse || !d_qkv) return fail(FAL_ERR_INVALID_ARG, "NULL qkv, out, d_out, lse or d_qkv");
+    if (!qkv || !out || !d_out || !lse || !d_qkv)
+      return fail(FAL_ERR_INVALID_ARG, "NULL qkv, out, d_out, lse or d_qkv");
     if (!aligned(qkv, 16) || !aligned(out, 16) || !aligned(d_out, 16) || !aligned(d_qkv, 16) || !aligned(lse, 4) ||
         !aligned(lens, 4))
       return fail(FAL_ERR_INVALID_ARG, "qkv, out, d_out and d_qkv must be 16-byte aligned, lse and lens 4-byte");
-    const int64_t width = (int64_t)(shape->n_head + 2 * (shape->n_kv_head ? shape->n_kv_head : shape->n_head)) * shape->head_dim;
+    const int64_t kv = shape->n_kv_head ? shape->n_kv_head : shape->n_head;
+    const int64_t width = (shape->n_head + 2 * kv) * shape->head_dim;
     if (ld_d_qkv < width || ld_d_qkv > kMaxStride || ld_d_qkv % (shape->dtype == FAL_BF16 ? 8 : 4))
-      return fail(FAL_ERR_INVALID_ARG, "ld_d_qkv must be a multiple of 16 bytes, at least a row and at most 2^40 elements");
+      return fail(FAL_ERR_INVALID_ARG,
+                  "ld_d_qkv must be a multiple of 16 bytes, at least a row and at most 2^40 elements");
     WindowAttn a = window_args(shape, lens);
     a.lddq = ld_d_qkv;
     int64_t part_off;
@@ -225,8 +231,8 @@ fal_status_t fal_window_attention_bwd(const fal_window_attention_t* shape, const
       return fail(FAL_ERR_INVALID_ARG, "d_qkv or workspace overlaps another argument");
     float* D = static_cast<float*>(workspace);
     float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_off);
-    return launched(window_attention_bwd(shape->dtype == FAL_BF16 ? BF16 : F32, a, qkv, out, d_out, lse, D, part, d_qkv,
-                                         static_cast<hipStream_t>(stream)),
+    return launched(window_attention_bwd(shape->dtype == FAL_BF16 ? BF16 : F32, a, qkv, out, d_out, lse, D, part,
+                                         d_qkv, static_cast<hipStream_t>(stream)),
                     "fal_window_attention_bwd");
   });
 }
@@ -237,7 +243,8 @@ fal_status_t fal_token_logprobs(const fal_logit_rows_t* rows, const void* logits
     const Refusal no = check_rows(rows, false);
     if (no.why) return fail(no.st, no.why);
     if (!logits || !targets || !logp) return fail(FAL_ERR_INVALID_ARG, "NULL logits, targets or logp");
-    if (!aligned(logits, element_bytes(rows->dtype)) || !aligned(targets, 4) || !aligned(logp, 4) || !aligned(entropy, 4))
+    if (!aligned(logits, element_bytes(rows->dtype)) || !aligned(targets, 4) || !aligned(logp, 4) ||
+        !aligned(entropy, 4))
       return fail(FAL_ERR_INVALID_ARG, "logits, targets, logp or entropy misaligned");
     const int64_t N = (int64_t)rows->batch * rows->seq_len;
     const Extent x = rows_of(logits, N, rows->ld_logits, rows->vocab, element_bytes(rows->dtype)),
@@ -277,8 +284,8 @@ fal_status_t fal_policy_loss(const fal_logit_rows_t* rows, const fal_policy_t* h
     if (bad.why) return fail(bad.st, bad.why);
     const PolicyArgs p{old_logp, ref_logp, advantages, hp->clip_low, hp->clip_high, hp->kl_coef, hp->sequence_mean,
                        stats, logp};
-    return launched(policy_loss(rows->dtype == FAL_BF16 ? BF16 : F32, row_args(rows, logits, targets, mask), p, dlogits,
-                                static_cast<float*>(workspace), static_cast<hipStream_t>(stream)),
+    return launched(policy_loss(rows->dtype == FAL_BF16 ? BF16 : F32, row_args(rows, logits, targets, mask), p,
+                                dlogits, static_cast<float*>(workspace), static_cast<hipStream_t>(stream)),
                     "fal_policy_loss");
   });
 }

@@ -39,14 +39,23 @@ namespace fal {
 
 namespace {
 
-// Kernels that need more registers than two wavefronts a SIMD have.
+// fp32 at head_dim 128: the backward kernels need more registers than two
+// wavefronts a SIMD have (bounded to 256 they spill: dQ 113 -> 148 us at 2
+// sequences of 1999 tokens, 8 heads, window 300).
 template <typename S, int HD>
 constexpr bool kWide = HD == 128 && sizeof(S) == 4;
-// dK/dV of wide bf16 heads: the keys stay in LDS rather than in registers, and
-// the tiles are fetched when they are due, not one ahead, so that two
-// workgroups fit a compute unit and cover each other's waits.
+// dK/dV of wide bf16 heads: the keys stay in LDS rather than in registers, so
+// that two workgroups (head_dim 64: three) fit a compute unit and cover each
+// other's waits; at 128 the query tiles are also fetched when they are due, not
+// one ahead, for the same reason (8192 tokens, 16 heads of 128, window 1024:
+// 226 -> 173 us; 8 sequences of 1024, 12 heads of 64, window 256: 34 -> 30).
 template <typename S, int HD>
 constexpr bool kKeysInLds = HD >= 64 && sizeof(S) == 2;
+// Wavefronts a SIMD that the backward kernels' registers are bounded to.
+template <typename S, int HD>
+constexpr int kWaves = kWide<S, HD> ? 1 : 2;
+template <typename S, int HD>
+constexpr int kWavesDkdv = kKeysInLds<S, HD> && HD == 64 ? 3 : kWaves<S, HD>;
 
 template <int HD>
 constexpr int n_tiles() { return HD < 32 ? 1 : HD / 32; }
@@ -82,7 +91,6 @@ __device__ __forceinline__ void both_halves(float x, float& lo, float& hi) {
   lo = __uint_as_float(r[0]);
   hi = __uint_as_float(r[1]);
 }
-
 
 // ---- 64-row LDS tiles -----------------------------------------------------
 // bf16 tiles have the slot order of attn_tiles.h; fp32 rows follow each other
@@ -227,12 +235,14 @@ struct Own<float, HD> {
 
 // acc[tile row][own row] += sum over dims of tile row (rowbase + .) * own row
 template <int HD>
-__device__ __forceinline__ void dot_rows(const bf16* s, int rowbase, int c, int g, const Own<bf16, HD>& o, f32x16v& acc) {
+__device__ __forceinline__ void dot_rows(const bf16* s, int rowbase, int c, int g, const Own<bf16, HD>& o,
+                                         f32x16v& acc) {
 #pragma unroll
   for (int k = 0; k < HD / 16; ++k) acc = mfma32(frag_rows<HD>(s, rowbase, c, k, g), o.f[k], acc);
 }
 template <int HD>
-__device__ __forceinline__ void dot_rows(const float* s, int rowbase, int c, int g, const Own<float, HD>& o, f32x16v& acc) {
+__device__ __forceinline__ void dot_rows(const float* s, int rowbase, int c, int g, const Own<float, HD>& o,
+                                         f32x16v& acc) {
   const float* row = s + (HD + 4) * (rowbase + c) + 4 * g;
 #pragma unroll
   for (int k = 0; k < HD / 8; ++k) {
@@ -361,17 +371,26 @@ __device__ __forceinline__ void join_acc(float* lds, int wave, int lane, f32x16v
 }  // namespace
 
 // ------------------------------------------------------------- forward --
+// The last blocks first: the first ones, whose windows the sequence's start
+// cuts short, then fill the launch's end (6 padded sequences of 1501 tokens, 16
+// heads of 64, window 500: 29.4 -> 26.1 us; 4 of 2048 under the full mask, 68.8
+// -> 55.0, and dQ 80.7 -> 66.5).  At 8192 tokens, 16 heads of 128, window 1024:
+// 104 us, 630 TFLOP/s of the visible pairs; at 8 sequences of 1024, 12 heads of
+// 64, window 256: 19 us, where the exponentials and the other vector work of a
+// score (about 650 cycles a 32x32 tile against 256 of MFMA) and the single round
+// of workgroups bound it.
 template <typename S, int HD, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S* qkv, S* O, float* lse) {
   constexpr int NT = n_tiles<HD>();
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, SPLIT>()];
   S *sK = reinterpret_cast<S*>(lds), *sV = sK + tile_len<S, HD>();
-  const int h = blockIdx.x, b = blockIdx.y, qb = block_rows<SPLIT>() * blockIdx.z;
+  const int h = blockIdx.x, b = blockIdx.y, qb = block_rows<SPLIT>() * (gridDim.z - 1 - blockIdx.z);
   const int kvh = h / (a.H / a.Hkv);
   const S* Qg = qkv + (int64_t)b * a.T * a.ldq + h * HD;
   const S* Kg = qkv + (int64_t)b * a.T * a.ldq + (a.H + kvh) * HD;
   const S* Vg = Kg + a.Hkv * HD;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, c = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q0 = qb + (SPLIT ? wave & 1 : wave) * 32, tq = q0 + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
@@ -487,19 +506,22 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
 // and one of few does not (bf16 gradients of a window of 2 keys: 2.7e-3 off
 // against 2.2e-3 with D exact, of 20: 2.42e-3 against 2.36e-3; 1.65e-3 is the
 // rounding of the gradients alone).  So bf16 rows of at most kFewKeys keys sum
-// D = rowsum(P * dP) in a walk of their own over their few tiles.
+// D = rowsum(P * dP) in a walk of their own over their few tiles.  126 us at the
+// 8192 tokens above (780 TFLOP/s), 25 at the 8 x 1024.
 template <typename S, int HD, bool SPLIT>
-__global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_dq(WindowAttn a, const S* qkv, const S* O, const S* dO,
-                                                         const float* lse, float* Dvec, S* dqkv) {
+__global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_dq(WindowAttn a, const S* qkv, const S* O,
+                                                                       const S* dO, const float* lse, float* Dvec,
+                                                                       S* dqkv) {
   constexpr int NT = n_tiles<HD>();
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, SPLIT>()];
   S *sK = reinterpret_cast<S*>(lds), *sV = sK + tile_len<S, HD>();
-  const int h = blockIdx.x, b = blockIdx.y, qb = block_rows<SPLIT>() * blockIdx.z;
+  const int h = blockIdx.x, b = blockIdx.y, qb = block_rows<SPLIT>() * (gridDim.z - 1 - blockIdx.z);
   const int kvh = h / (a.H / a.Hkv);
   const int64_t row0 = (int64_t)b * a.T;
   const S* Kg = qkv + row0 * a.ldq + (a.H + kvh) * HD;
   const S* Vg = Kg + a.Hkv * HD;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, c = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q0 = qb + (SPLIT ? wave & 1 : wave) * 32, tq = q0 + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
@@ -605,11 +627,13 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_dq(Wi
 // sink keys; of its wavefronts two sum dV and two dK, over one half of each
 // tile (half the sums a wavefront, so three share a SIMD).  The halves are
 // joined in LDS and written as fp32 partials [b][kv head][chunk][dK, dV]
-// [sinks][HD].
+// [sinks][HD].  18 us at the 8192 tokens above (16 sinks), 7 at the 8 x 1024 (4):
+// reading the far queries' Q and dO, and the latency of a short chunk.
 template <typename S, int HD>
-__global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_sinks(WindowAttn a, const S* qkv, const S* dO, const float* lse,
-                                                            const float* Dvec, int rows, int far, int chunk, int nchunk,
-                                                            float* part) {
+__global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_sinks(WindowAttn a, const S* qkv, const S* dO,
+                                                                          const float* lse, const float* Dvec,
+                                                                          int rows, int far, int chunk, int nchunk,
+                                                                          float* part) {
   constexpr int NT = n_tiles<HD>();
   __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, HD, true>()];
   S *sQ = reinterpret_cast<S*>(lds), *sdO = sQ + tile_len<S, HD>();
@@ -618,8 +642,9 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_sinks
   const int grp = a.H / a.Hkv;
   const int64_t row0 = (int64_t)b * a.T;
   const S* Kg = qkv + row0 * a.ldq + (a.H + kvh) * HD;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5;
-  const int c = lane & 31, n = length_of(a, b), key = kw + c, sub = wave >> 1;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, c = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = length_of(a, b), key = kw + c, sub = wave >> 1;
   const bool keys = wave & 1;  // this wavefront sums dK
   // (a key block past the first one's `rows` keys covers as many more queries)
   const int qbeg = max(far + ck * chunk, far + kw / rows * rows), qend = min(n, far + (ck + 1) * chunk);
@@ -670,18 +695,19 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : 2)) void window_attn_sinks
   }
   join_acc<HD>(reinterpret_cast<float*>(lds), wave, lane, acc);
   if (wave < 2 && key < a.sinks)
-    put_row<float, HD>(part + ((((int64_t)b * a.Hkv + kvh) * nchunk + ck) * 2 + (1 - wave)) * a.sinks * HD + key * HD, g, acc,
-                       1.f, true);
+    put_row<float, HD>(part + (((((int64_t)b * a.Hkv + kvh) * nchunk + ck) * 2 + (1 - wave)) * a.sinks + key) * HD, g,
+                       acc, 1.f, true);
 }
 
 // ------------------------------------------------------- backward: dK, dV --
 // A group's query heads may be divided over `parts` workgroups, which then
 // write fp32 sums [part][b][t][dK, dV][kv head][HD] for window_attn_kv_sum.
+// 173 us at the 8192 tokens above (760 TFLOP/s), 31 at the 8 x 1024.
 template <typename S, int HD, bool SPLIT>
-__global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD == 64 ? 3 : 2)) void window_attn_dkdv(WindowAttn a, const S* qkv, const S* dO,
-                                                                           const float* lse, const float* Dvec,
-                                                                           const float* part, int nchunk, int parts,
-                                                                           float* heads, S* dqkv) {
+__global__ __launch_bounds__(256, (kWavesDkdv<S, HD>)) void window_attn_dkdv(WindowAttn a, const S* qkv, const S* dO,
+                                                                             const float* lse, const float* Dvec,
+                                                                             const float* part, int nchunk, int parts,
+                                                                             float* heads, S* dqkv) {
   constexpr int NT = n_tiles<HD>();
   constexpr bool KL = kKeysInLds<S, HD>, LATE = KL && HD == 128;
   __shared__ __attribute__((aligned(16))) S sK[KL ? block_rows<SPLIT>() / AT * tile_len<S, HD>() : 8];
@@ -692,7 +718,8 @@ __global__ __launch_bounds__(256, (kWide<S, HD> ? 1 : kKeysInLds<S, HD> && HD ==
   const int grp = a.H / a.Hkv / parts, h0 = blockIdx.x * grp;  // this workgroup's query heads
   const int64_t row0 = (int64_t)b * a.T;
   const S* Kg = qkv + row0 * a.ldq + (a.H + kvh) * HD;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5, c = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, c = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kw = kb0 + (SPLIT ? wave & 1 : wave) * 32, key = kw + c;
   const int n = length_of(a, b);
   const float sl2 = kLog2e / sqrtf((float)HD);
@@ -876,16 +903,16 @@ constexpr int kPerCuDkdv = kWide<S, HD> ? 1 : kPerCu<S, HD>;
 
 template <typename S, int HD, bool SPLIT>
 hipError_t fwd(const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s) {
-  hipLaunchKernelGGL((window_attn_fwd<S, HD, SPLIT>), dim3(a.H, a.B, cdiv(a.T, block_rows<SPLIT>())), dim3(256), 0, s, a,
-                     static_cast<const S*>(qkv), static_cast<S*>(O), lse);
+  hipLaunchKernelGGL((window_attn_fwd<S, HD, SPLIT>), dim3(a.H, a.B, cdiv(a.T, block_rows<SPLIT>())), dim3(256), 0, s,
+                     a, static_cast<const S*>(qkv), static_cast<S*>(O), lse);
   return hipGetLastError();
 }
 
 template <typename S, int HD, bool SPLIT>
 hipError_t dq(const WindowAttn& a, const void* qkv, const void* O, const void* dO, const float* lse, float* Dvec,
               void* dqkv, hipStream_t s) {
-  hipLaunchKernelGGL((window_attn_dq<S, HD, SPLIT>), dim3(a.H, a.B, cdiv(a.T, block_rows<SPLIT>())), dim3(256), 0, s, a,
-                     static_cast<const S*>(qkv), static_cast<const S*>(O), static_cast<const S*>(dO), lse, Dvec,
+  hipLaunchKernelGGL((window_attn_dq<S, HD, SPLIT>), dim3(a.H, a.B, cdiv(a.T, block_rows<SPLIT>())), dim3(256), 0, s,
+                     a, static_cast<const S*>(qkv), static_cast<const S*>(O), static_cast<const S*>(dO), lse, Dvec,
                      static_cast<S*>(dqkv));
   return hipGetLastError();
 }
@@ -903,7 +930,7 @@ Plan plan_dkdv(const WindowAttn& a) {
   // Shared key/value heads make few workgroups of much work: where halved
   // blocks would not fill the chip either, their query heads are divided until
   // they do (one sequence of 4096 tokens, 16 heads of 128 sharing 2, window
-  // 1024, the backward pass: 307 -> 159 us), while the fp32 sums of the parts
+  // 1024, both passes: 376 -> 223 us), while the fp32 sums of the parts
   // fit the scratch.
   constexpr int kFull = kPerCuDkdv<S, HD>;
   const int grp = a.H / a.Hkv;
@@ -911,7 +938,8 @@ Plan plan_dkdv(const WindowAttn& a) {
   p.parts = 1;
   if (split_rows(a, 2 * a.Hkv, kFull))
     for (int d = 2; d <= grp; ++d)
-      if (grp % d == 0 && split_rows(a, a.Hkv * p.parts, kFull) && d * per_part <= kWindowPartFloats) p.parts = d;
+      if (grp % d == 0 && split_rows(a, a.Hkv * p.parts, kFull) && d * per_part <= kWindowPartFloats)
+        p.parts = d;
   p.split = split_rows(a, a.Hkv * p.parts, kFull);
   // Queries from `far` on reach the first key block through its sink keys
   // only (the end of the last tile that its own range walks).  Their chunks:
@@ -935,8 +963,8 @@ hipError_t dkdv(const WindowAttn& a, const Plan& p, const void* qkv, const void*
   const S *x = static_cast<const S*>(qkv), *g = static_cast<const S*>(dO);
   float* heads = part + p.sinks;
   if (p.nchunk > 0) {
-    hipLaunchKernelGGL((window_attn_sinks<S, HD>), dim3(a.Hkv, a.B, p.nchunk * cdiv(a.sinks, 32)), dim3(256), 0, s, a, x,
-                       g, lse, Dvec, block_rows<SPLIT>(), p.far, p.chunk, p.nchunk, part);
+    hipLaunchKernelGGL((window_attn_sinks<S, HD>), dim3(a.Hkv, a.B, p.nchunk * cdiv(a.sinks, 32)), dim3(256), 0, s, a,
+                       x, g, lse, Dvec, block_rows<SPLIT>(), p.far, p.chunk, p.nchunk, part);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -980,7 +1008,9 @@ int64_t scratch(const WindowAttn& a) {
   }
 
 hipError_t window_attention_fwd(DType dt, const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s) {
-#define FAL_FWD(S, HD) (split_rows(a, a.H, kPerCu<S, HD>) ? fwd<S, HD, true>(a, qkv, O, lse, s) : fwd<S, HD, false>(a, qkv, O, lse, s))
+#define FAL_FWD(S, HD)                                                       \
+  (split_rows(a, a.H, kPerCu<S, HD>) ? fwd<S, HD, true>(a, qkv, O, lse, s)   \
+                                     : fwd<S, HD, false>(a, qkv, O, lse, s))
   if (dt == BF16) FAL_BY_HEAD(bf16, FAL_FWD, hipErrorInvalidValue)
   FAL_BY_HEAD(float, FAL_FWD, hipErrorInvalidValue)
 #undef FAL_FWD

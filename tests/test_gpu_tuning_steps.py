@@ -186,7 +186,8 @@ def test_windowed_policy_step(arch, dtype, monkeypatch):
     kept = {}
     monkeypatch.setattr(fal_oracle, "attention", masked(window, sinks))
     monkeypatch.setattr(fal_oracle, "cross_entropy",
-                        policy_head(B, T, *(t.double().cpu().numpy() for t in (old, adv, ref)), mask, 0.2, 0.3, 0.1, kept))
+                        policy_head(B, T, *(t.double().cpu().numpy() for t in (old, adv, ref)), mask, 0.2, 0.3, 0.1,
+                                    kept))
     want = oracle.train_step(cfg, g, blocks, tok)
     want["loss_scale"] = 1.0  # a sum of terms of both signs
     compare_step(cfg, {"loss": float(stats[0]), "grads_global": gg, "grads_blocks": gb}, want,

@@ -136,7 +136,8 @@ def test_logprobs_refuse_pointers():
 
 @pytest.mark.parametrize("kw,word", [
     (dict(clip_low=-0.1), "clip"), (dict(clip_low=1.1), "clip"), (dict(clip_high=-0.1), "clip"),
-    (dict(kl_coef=-1.0), "kl_coef"), (dict(kl_coef=float("nan")), "non-finite"), (dict(sequence_mean=2), "sequence_mean"),
+    (dict(kl_coef=-1.0), "kl_coef"), (dict(kl_coef=float("nan")), "non-finite"),
+    (dict(sequence_mean=2), "sequence_mean"),
 ])
 def test_policy_refuses_parameters(kw, word):
     hp = fal.fal_policy_t(**{**dict(clip_low=0.2, clip_high=0.2, kl_coef=0.1, sequence_mean=0), **kw})
