@@ -11,10 +11,15 @@
 // gradient is written from the registers; what they cannot hold of a longer
 // row is read twice.  Rows need no alignment: a chunk that a row's edge crosses
 // is read and written element by element (two of a row's chunks), columns
-// outside the row read as -inf.  Exponentials are exp2 of (x - maximum) log2(e) / temperature, sums
-// fp32 within a row; sums over rows and sequences are fp64, since a sequence's
-// log-probability is large (hundreds of terms) and the losses see a small
-// difference of two.
+// outside the row read as -inf.  Exponentials are exp2 of
+// (x - maximum) log2(e) / temperature, sums fp32 within a row; sums over rows
+// and sequences are fp64, since a sequence's log-probability is large (hundreds
+// of terms) and the losses see a small difference of two.
+//
+// Half of 8192 rows of 50257 bf16 counted: log-probabilities 75 us (5.4 TB/s
+// of the counted rows), policy gradient 262 us and preference gradient 204 us
+// behind its 92 us of statistics (4.7 and 6.0 TB/s of the counted rows read and
+// all of the gradient written; a copy of that size reaches 4.9).
 #include <math.h>
 
 #include <algorithm>
@@ -247,6 +252,25 @@ __device__ __forceinline__ void zero_tail(const Row<S, S>& out, int V, int t) {
   for (int col = V + t; col < out.cols; col += G) out.base[out.shift + col] = from_f<S>(0.f);
 }
 
+// ---- rows of a launch -------------------------------------------------------
+// A grid of more than 2^32 threads along x is not launched, which 2^22 rows of
+// 1024 are: past kRowGrid workgroups the rest lie along y.
+constexpr int64_t kRowGrid = 1 << 21;
+template <int G>
+constexpr int kRowThreads = G < 256 ? 256 : G;
+template <int G>
+dim3 row_grid(const LogitRows& r) {
+  constexpr int per = kRowThreads<G> / G;
+  const int64_t n = ((int64_t)r.B * r.T + per - 1) / per;
+  return dim3((unsigned)std::min(n, kRowGrid), (unsigned)((n + kRowGrid - 1) / kRowGrid));
+}
+// this thread's row; rows from B T on are none
+template <int G>
+__device__ __forceinline__ int64_t row_of() {
+  constexpr int per = kRowThreads<G> / G;
+  return ((int64_t)blockIdx.y * kRowGrid + blockIdx.x) * per + threadIdx.x / G;
+}
+
 // ---------------------------------------------------------------- policy --
 // e^d - d - 1, and e^d - 1, without their cancellation at small d
 __device__ __forceinline__ float kl_term(float d, float* em1) {
@@ -320,11 +344,10 @@ struct RowOut {
 // G threads a row, NPT chunks each held in registers; what a longer row has past
 // them is read again for its gradient.
 template <typename S, int G, int NPT, Mode MODE>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, RowOut o) {
-  constexpr int RPW = (G < 256 ? 256 : G) / G;
-  const int64_t N = (int64_t)r.B * r.T, m = (int64_t)blockIdx.x * RPW + threadIdx.x / G;
-  if (RPW > 1 && m >= N) return;  // a whole wavefront: no barrier follows
-  const int t = threadIdx.x % G;
+__global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut o) {
+  const int64_t N = (int64_t)r.B * r.T, m = row_of<G>();
+  if (m >= N) return;  // all of a row's threads, and barriers are among those only
+  const int t = threadIdx.x % G, b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T));
   const bool on = counted(r, m);
   const Row<S, S> out(MODE == POLICY ? static_cast<S*>(o.dlogits) + m * r.ldd : nullptr, r.width);
   if (!on) {
@@ -339,9 +362,9 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
   }
   const S* l = static_cast<const S*>(r.logits) + m * r.ldl;
   const Row<S, const S> in(l, r.V);
-  const int nc = in.chunks(), b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T));
+  const int nc = in.chunks();
   const float k = r.inv_temp * kLog2e;
-  const float xt = t == 0 ? to_f(l[tgt]) : 0.f;
+  S xt = from_f<S>(0.f);  // t == 0: the target's logit, asked for behind the first chunks
   int n = 0;  // this thread's share of the counted rows that the mean is over
   if (MODE == POLICY && r.mask) {
     if (!o.count) {
@@ -363,6 +386,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
       const int c = t + G * i;
       if (c < nc) raw[i] = in.template load<true>(c);
     }
+    if (t == 0) xt = l[tgt];
 #pragma unroll
     for (int i = 0; i < NPT; ++i)
       if (t + G * i < nc) st.m = chunk_max<S>(raw[i], st.m);
@@ -377,6 +401,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
 #pragma unroll
     for (int i = 0; i < kStream; ++i)
       if (c0 + G * i < nc) u[i] = in.template load<MODE == LOGP || MODE == LOGP_ENTROPY>(c0 + G * i);
+    if (!NPT && c0 == 0) xt = l[tgt];
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kStream; ++i)
@@ -391,7 +416,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void logit_rows(LogitRows r, Row
         if (c0 + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(u[i], st, k);
     }
   }
-  const Shared sh = exchange<G>(st, xt, n, k);
+  const Shared sh = exchange<G>(st, to_f(xt), n, k);
   const float log2sum = log2f(sh.st.sum);
   const float lp = ((sh.target - sh.st.m) * k - log2sum) * kLn2;
   if (t == 0) {
@@ -497,19 +522,18 @@ __global__ __launch_bounds__(256) void preference_pairs(LogitRows r, PreferenceA
 }
 
 template <typename S, int G>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void preference_rows(LogitRows r, const double* pair_loss,
-                                                                     const float* coef, const float* top,
-                                                                     const float* log2sum, S* dl, float* loss) {
-  constexpr int RPW = (G < 256 ? 256 : G) / G;
-  const int64_t N = (int64_t)r.B * r.T, m = (int64_t)blockIdx.x * RPW + threadIdx.x / G;
-  if (blockIdx.x == gridDim.x - 1 && threadIdx.x < FAL_WAVE) {  // the mean over pairs
+__global__ __launch_bounds__(kRowThreads<G>) void preference_rows(LogitRows r, const double* pair_loss,
+                                                                  const float* coef, const float* top,
+                                                                  const float* log2sum, S* dl, float* loss) {
+  const int64_t m = row_of<G>();
+  if (blockIdx.x == gridDim.x - 1 && blockIdx.y == 0 && threadIdx.x < FAL_WAVE) {  // the mean over pairs
     double s = 0.0;
     for (int i = threadIdx.x; i < r.B / 2; i += FAL_WAVE) s += pair_loss[i];
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, FAL_WAVE);
     if (threadIdx.x == 0) *loss = (float)(s / (r.B / 2));
   }
-  if (RPW > 1 && m >= N) return;
+  if (m >= (int64_t)r.B * r.T) return;
   const int t = threadIdx.x % G;
   const Row<S, S> out(dl + m * r.ldd, r.width);
   if (!counted(r, m)) {
@@ -528,23 +552,25 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void preference_rows(LogitRows r
 // ------------------------------------------------------------- launching --
 template <typename S, int G, int NPT, Mode MODE>
 hipError_t launch(const LogitRows& r, const RowOut& o, hipStream_t s) {
-  constexpr int WG = G < 256 ? 256 : G;
-  const int64_t N = (int64_t)r.B * r.T;
-  hipLaunchKernelGGL((logit_rows<S, G, NPT, MODE>), dim3((unsigned)((N + WG / G - 1) / (WG / G))), dim3(WG), 0, s, r, o);
+  hipLaunchKernelGGL((logit_rows<S, G, NPT, MODE>), row_grid<G>(r), dim3(kRowThreads<G>), 0, s, r, o);
   return hipGetLastError();
 }
 
 // Rows that are only scored are streamed: held or not, they are read once.
 // 256 threads keep enough loads in flight and leave a compute unit several
 // rows (8192 rows of 50257 bf16, half of them counted, with entropy: 78 us
-// against 85 with 512 threads and 127 with 1024); while the rows are fewer
-// than the chip has places for such workgroups, 1024 threads shorten each
-// (128 rows: 5.4 us against 8.1).
+// against 85 with 512 threads and 127 with 1024).  Of rows that leave the chip
+// places, long ones are shortened by more threads, whose exchange then costs
+// less than it gives (us with 256, 512 and 1024 threads: 270 rows of 2003
+// chunks 5.1, 5.7, 8.9; 512 of 3750 8.3, 8.6, 11.4; 128 of 6283 9.2, 7.3, 8.6;
+// 32 of 32064 21.4, 14.2, 12.7).
 template <typename S, Mode MODE>
 hipError_t scored_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
-  if (r.V <= 512 * Chunk<S>::E) return launch<S, 64, 0, MODE>(r, o, s);
-  if ((int64_t)r.B * r.T < 1024) return launch<S, 1024, 0, MODE>(r, o, s);
-  return launch<S, 256, 0, MODE>(r, o, s);
+  const int n = r.V / Chunk<S>::E;
+  if (n <= 512) return launch<S, 64, 0, MODE>(r, o, s);
+  if (n <= 4096 || (int64_t)r.B * r.T >= 1024) return launch<S, 256, 0, MODE>(r, o, s);
+  if (n <= 16384) return launch<S, 512, 0, MODE>(r, o, s);
+  return launch<S, 1024, 0, MODE>(r, o, s);
 }
 
 // Rows with a gradient are held by as few threads as can (up to 26 chunks
@@ -573,10 +599,8 @@ hipError_t policy_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
 template <typename S, int G>
 hipError_t preference_grad(const LogitRows& r, const double* pair_loss, const float* coef, const RowOut& o, void* dl,
                            float* loss, hipStream_t s) {
-  constexpr int WG = G < 256 ? 256 : G;
-  const int64_t N = (int64_t)r.B * r.T;
-  hipLaunchKernelGGL((preference_rows<S, G>), dim3((unsigned)((N + WG / G - 1) / (WG / G))), dim3(WG), 0, s, r,
-                     pair_loss, coef, o.top, o.log2sum, static_cast<S*>(dl), loss);
+  hipLaunchKernelGGL((preference_rows<S, G>), row_grid<G>(r), dim3(kRowThreads<G>), 0, s, r, pair_loss, coef, o.top,
+                     o.log2sum, static_cast<S*>(dl), loss);
   return hipGetLastError();
 }
 template <typename S>

@@ -402,3 +402,45 @@ def test_repeats_streams_and_graphs(dtype):
         for i in (0, 1):
             assert all(torch.equal(p, q) for p, q in zip(static[i][1], eager[(i + turn) % 2]))
         assert all(torch.equal(p, q) for p, q in zip(again, eager[turn % 2]))
+
+
+def test_rows_past_one_axis_of_the_grid():
+    """2^21 + 6 rows, whose last ones lie in the grid's second row: sampled
+    rows on both sides against the formula, gradients in place."""
+    B, T, V = 2, (1 << 20) + 3, 4104
+    g = torch.Generator(device="cuda").manual_seed(11)
+    x = torch.empty(B, T, V, dtype=BF16, device="cuda").normal_(generator=g).mul_(3)
+    y = torch.randint(0, V, (B, T), device="cuda", generator=g, dtype=torch.int32)
+    at = ([0] * 4 + [1] * 12, [0, 1, T // 2, T - 1, 0, 1, *range(T - 10, T)])
+    taken, ty = x[at][None].clone(), y[at][None]
+    log(f"logprobs, policy and preference, {B * T} rows")
+    lp, want = exact(taken, ty, V, 1.0)
+    e = err_lse(taken, V, 1.0)
+    logp = fal.token_logprobs(x, y)
+    within("logp", logp[at][None], want, e + 2 * U * want.abs())
+    onehot, p = torch.zeros_like(lp).scatter_(-1, ty.long()[:, :, None], 1.0), lp.exp()
+
+    def check(name, got, c, ec):
+        grad = c[:, :, None] * (onehot - p)
+        within(name, got[at][None], grad, ec[:, :, None] * (onehot + p) + c.abs()[:, :, None] * p * (e + 4 * U)
+               + 1.02 * R * grad.abs())
+
+    adv = torch.randn(B, T, device="cuda", generator=g)
+    a = adv[at][None].double() / (B * T)
+    # the ratio is that of a row with itself: one to the last bit or two
+    got = fal.policy_loss(x, y, logp.clone(), adv, clip_low=0.2, clip_high=0.2, dlogits=x)
+    assert torch.equal(got.logp, logp)
+    check("policy dlogits", got.dlogits, -a, a.abs() * 8 * U)
+
+    x.normal_(generator=g).mul_(3)
+    taken = x[at][None].clone()
+    lp, _ = exact(taken, ty, V, 1.0)
+    e, p = err_lse(taken, V, 1.0), lp.exp()
+    beta, ref = 0.5, torch.tensor([-9.0, -9.5], device="cuda")
+    got = fal.preference_loss(x, y, ref, beta=beta, length_mean=True, dlogits=x)
+    gain = got.seq_logp.double() - ref.double()
+    dh = beta * float(torch.sigmoid(beta * (gain[0] - gain[1])) - 1) / T
+    # the means come back rounded: u |mean| each, times a slope of at most beta^2 / 4
+    moved = beta * beta / 4 * U * float(got.seq_logp.double().abs().sum()) / T
+    c = torch.tensor([dh, -dh], dtype=torch.float64, device="cuda")[at[0]][None]
+    check("preference dlogits", got.dlogits, c, c.abs() * 4 * U + moved)
