@@ -897,9 +897,7 @@ bool split_rows(const WindowAttn& a, int heads, int per_cu) {
 template <typename S, int HD>
 constexpr int kPerCu = HD < 64 ? 3 : 2;
 template <typename S, int HD>
-constexpr int kPerCuDq = kWide<S, HD> ? 1 : kPerCu<S, HD>;
-template <typename S, int HD>
-constexpr int kPerCuDkdv = kWide<S, HD> ? 1 : kPerCu<S, HD>;
+constexpr int kPerCuBwd = kWide<S, HD> ? 1 : kPerCu<S, HD>;
 
 template <typename S, int HD, bool SPLIT>
 hipError_t fwd(const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s) {
@@ -932,7 +930,7 @@ Plan plan_dkdv(const WindowAttn& a) {
   // they do (one sequence of 4096 tokens, 16 heads of 128 sharing 2, window
   // 1024, both passes: 376 -> 223 us), while the fp32 sums of the parts
   // fit the scratch.
-  constexpr int kFull = kPerCuDkdv<S, HD>;
+  constexpr int kFull = kPerCuBwd<S, HD>;
   const int grp = a.H / a.Hkv;
   const int64_t per_part = (int64_t)a.B * a.T * 2 * a.Hkv * HD;
   p.parts = 1;
@@ -982,7 +980,7 @@ hipError_t dkdv(const WindowAttn& a, const Plan& p, const void* qkv, const void*
 template <typename S, int HD>
 hipError_t bwd(const WindowAttn& a, const void* qkv, const void* O, const void* dO, const float* lse, float* Dvec,
                float* part, void* dqkv, hipStream_t s) {
-  const hipError_t e = split_rows(a, a.H, kPerCuDq<S, HD>) ? dq<S, HD, true>(a, qkv, O, dO, lse, Dvec, dqkv, s)
+  const hipError_t e = split_rows(a, a.H, kPerCuBwd<S, HD>) ? dq<S, HD, true>(a, qkv, O, dO, lse, Dvec, dqkv, s)
                                                            : dq<S, HD, false>(a, qkv, O, dO, lse, Dvec, dqkv, s);
   if (e != hipSuccess) return e;
   const Plan p = plan_dkdv<S, HD>(a);

@@ -16,10 +16,10 @@
 // and sequences are fp64, since a sequence's log-probability is large (hundreds
 // of terms) and the losses see a small difference of two.
 //
-// Half of 8192 rows of 50257 bf16 counted: log-probabilities 75 us (5.4 TB/s
-// of the counted rows), policy gradient 262 us and preference gradient 204 us
-// behind its 92 us of statistics (4.7 and 6.0 TB/s of the counted rows read and
-// all of the gradient written; a copy of that size reaches 4.9).
+// 4551 of 8192 rows of 50257 bf16 counted: log-probabilities 76 us (6.0 TB/s of
+// those rows), the policy gradient 262 (4.9 TB/s of those rows read and all of
+// the gradient written, the rate of a copy); of 5002 counted, the preference
+// loss's statistics 92 (5.5 TB/s) and its gradient 204 (6.5).
 #include <math.h>
 
 #include <algorithm>
@@ -347,7 +347,7 @@ template <typename S, int G, int NPT, Mode MODE>
 __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut o) {
   const int64_t N = (int64_t)r.B * r.T, m = row_of<G>();
   if (m >= N) return;  // all of a row's threads, and barriers are among those only
-  const int t = threadIdx.x % G, b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T));
+  const int t = threadIdx.x % G;
   const bool on = counted(r, m);
   const Row<S, S> out(MODE == POLICY ? static_cast<S*>(o.dlogits) + m * r.ldd : nullptr, r.width);
   if (!on) {
@@ -362,9 +362,9 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
   }
   const S* l = static_cast<const S*>(r.logits) + m * r.ldl;
   const Row<S, const S> in(l, r.V);
-  const int nc = in.chunks();
+  const int nc = in.chunks(), b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T));
   const float k = r.inv_temp * kLog2e;
-  S xt = from_f<S>(0.f);  // t == 0: the target's logit, asked for behind the first chunks
+  const float xt = t == 0 ? to_f(l[tgt]) : 0.f;
   int n = 0;  // this thread's share of the counted rows that the mean is over
   if (MODE == POLICY && r.mask) {
     if (!o.count) {
@@ -386,7 +386,6 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
       const int c = t + G * i;
       if (c < nc) raw[i] = in.template load<true>(c);
     }
-    if (t == 0) xt = l[tgt];
 #pragma unroll
     for (int i = 0; i < NPT; ++i)
       if (t + G * i < nc) st.m = chunk_max<S>(raw[i], st.m);
@@ -401,7 +400,6 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
 #pragma unroll
     for (int i = 0; i < kStream; ++i)
       if (c0 + G * i < nc) u[i] = in.template load<MODE == LOGP || MODE == LOGP_ENTROPY>(c0 + G * i);
-    if (!NPT && c0 == 0) xt = l[tgt];
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kStream; ++i)
@@ -416,7 +414,7 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
         if (c0 + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(u[i], st, k);
     }
   }
-  const Shared sh = exchange<G>(st, to_f(xt), n, k);
+  const Shared sh = exchange<G>(st, xt, n, k);
   const float log2sum = log2f(sh.st.sum);
   const float lp = ((sh.target - sh.st.m) * k - log2sum) * kLn2;
   if (t == 0) {
