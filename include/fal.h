@@ -417,8 +417,8 @@ fal_status_t fal_window_attention_bwd(const fal_window_attention_t* shape, const
  * backward).  window 0 (with sinks 0) restores the full mask, the state after
  * fal_init.  Errors: FAL_ERR_INVALID_ARG for negative values, sinks without a
  * window or a bidirectional config; FAL_ERR_UNSUPPORTED for more than 128
- * sinks, or sinks of so many heads that their partial sums exceed the
- * context's scratch. */
+ * sinks, sinks of so many heads that their partial sums exceed the context's
+ * scratch, or a batch, n_head or seq_len that the shape above excludes. */
 fal_status_t fal_set_attention_window(fal_ctx_t* ctx, int32_t window, int32_t sinks);
 
 /* Rows of logits with the token each of them is to score: row (b, t) of

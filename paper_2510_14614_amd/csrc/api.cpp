@@ -1322,6 +1322,8 @@ fal_status_t fal_set_attention_window(fal_ctx_t* ctx, int32_t window, int32_t si
   ctx->sinks = sinks;
   const char* why = nullptr;
   if (window > 0 && ctx->D.T > kMaxWindowSeq) why = "seq_len above 2^22 is not supported with a window";
+  else if (window > 0 && std::max(ctx->D.B, ctx->D.H) > 65535)  // one axis of the kernels' grids each
+    why = "batch or n_head above 65535 is not supported with a window";
   else if (sinks > kMaxSinks) why = "more than 128 sinks are not supported";
   else if (window > 0 && window_attention_scratch(Run(ctx).dt, Run(ctx).window_args()) > ctx->W.splitk_floats)
     why = "sinks of this many heads are not supported: their partial sums exceed the context's scratch";

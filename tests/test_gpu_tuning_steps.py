@@ -151,6 +151,15 @@ def test_set_attention_window_refusals():
     F.close()
 
 
+def test_window_refuses_a_batch_past_its_grid():
+    F = fal.Fal(get_config("tiny", batch=65536, seq_len=1, has_embed_head=0, vocab=0))
+    with pytest.raises(fal.FalError, match="65535") as e:
+        F.set_attention_window(4)
+    assert e.value.status == fal.FAL_ERR_UNSUPPORTED
+    F.set_attention_window(0)
+    F.close()
+
+
 def _setup(arch, dtype, **kw):
     cfg = get_config("tiny", arch=arch, dtype=dtype, batch=4, seq_len=70, sched=SCHED_STREAMS, **kw)
     g, blocks = synth.make_params(cfg, seed=7)
