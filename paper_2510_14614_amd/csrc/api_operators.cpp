@@ -15,7 +15,8 @@ using namespace fal;
 namespace {
 
 constexpr uintptr_t kWorkspaceAlign = 256;
-constexpr int64_t kMaxStride = (int64_t)1 << 40;  // elements; rows times it stay within 64 bits
+constexpr int64_t kMaxStride = (int64_t)1 << 40;  // elements between rows
+constexpr int64_t kMaxExtent = (int64_t)1 << 47;  // elements from a matrix's first row to its last: the address space
 
 fal_status_t fail(fal_status_t st, const char* why) {
   noctx_error() = why;
@@ -46,6 +47,11 @@ struct Refusal {
 const Refusal kFine = {FAL_OK, nullptr};
 
 // ------------------------------------------------------- window attention --
+// Whether a shape's rows at a stride of ld elements stay within kMaxExtent.
+bool fits(const fal_window_attention_t* p, int64_t ld) {
+  return ld <= kMaxExtent / ((int64_t)p->batch * p->seq_len);
+}
+
 Refusal check_shape(const fal_window_attention_t* p) {
   if (!p) return {FAL_ERR_INVALID_ARG, "NULL shape"};
   if (p->dtype != FAL_F32 && p->dtype != FAL_BF16) return {FAL_ERR_INVALID_ARG, "unknown dtype"};
@@ -66,6 +72,8 @@ Refusal check_shape(const fal_window_attention_t* p) {
   if (p->ld_qkv % chunk || p->ld_out % chunk)
     return {FAL_ERR_INVALID_ARG, "row strides must be multiples of 16 bytes"};
   if (p->ld_qkv > kMaxStride || p->ld_out > kMaxStride) return {FAL_ERR_INVALID_ARG, "row stride above 2^40 elements"};
+  if (!fits(p, p->ld_qkv) || !fits(p, p->ld_out))
+    return {FAL_ERR_INVALID_ARG, "batch * seq_len rows at this stride exceed the address space"};
   return kFine;
 }
 
@@ -216,6 +224,8 @@ fal_status_t fal_window_attention_bwd(const fal_window_attention_t* shape, const
     if (ld_d_qkv < width || ld_d_qkv > kMaxStride || ld_d_qkv % (shape->dtype == FAL_BF16 ? 8 : 4))
       return fail(FAL_ERR_INVALID_ARG,
                   "ld_d_qkv must be a multiple of 16 bytes, at least a row and at most 2^40 elements");
+    if (!fits(shape, ld_d_qkv))
+      return fail(FAL_ERR_INVALID_ARG, "batch * seq_len rows of d_qkv at this stride exceed the address space");
     WindowAttn a = window_args(shape, lens);
     a.lddq = ld_d_qkv;
     int64_t part_off;

@@ -63,6 +63,20 @@ def test_window_attention_refuses_a_shape(kw, status, word):
     assert word in message()
 
 
+def test_window_attention_refuses_rows_past_the_address_space():
+    # 2^38 rows: products of sizes and strides that pass 64 bits
+    L, n = fal.lib(), ctypes.c_size_t()
+    for kw in (dict(ld_qkv=1 << 39), dict(ld_out=1 << 39), dict(ld_qkv=1 << 12), dict(ld_out=1 << 12)):
+        s = window(batch=65535, seq_len=1 << 22, **kw)
+        assert L.fal_window_attention_workspace_bytes(byref(s), byref(n)) == BAD
+        assert "address space" in message()
+        assert L.fal_window_attention_fwd(byref(s), A, None, B, C, None) == BAD
+    s = window(batch=65535, seq_len=1 << 22, n_head=1, n_kv_head=1, head_dim=16, ld_qkv=48, ld_out=16)
+    assert L.fal_window_attention_workspace_bytes(byref(s), byref(n)) == fal.FAL_OK
+    assert L.fal_window_attention_bwd(byref(s), A, None, B, C, D, E, 1 << 39, F, 1 << 62, None) == BAD
+    assert "address space" in message()
+
+
 def test_window_attention_refuses_pointers():
     L, s = fal.lib(), window()
     assert L.fal_window_attention_fwd(None, A, None, B, C, None) == BAD
