@@ -918,6 +918,21 @@ template <typename S, int HD>
 constexpr int kPerCu = HD < 64 ? 3 : 2;
 template <typename S, int HD>
 constexpr int kPerCuBwd = kWide<S, HD> ? 1 : kPerCu<S, HD>;
+// The backward kernels.  A workgroup that has a compute unit to itself (kWide)
+// runs in rounds of 256: halves are taken where they need fewer half rounds by
+// more than the ninth that they cost (heads of 128, both passes: 384 workgroups
+// of 2048 tokens, window 512, 789 -> 662 us; 896, window 300, 1138 -> 1087; but
+// 1152, 1320 -> 1337, and 256 of 1999 tokens, window 300, dQ 113 -> 121), and
+// where the longest block, which under a wide window sees most keys, would end
+// last (256 of 4096 tokens, full mask: 2223 -> 1470).
+template <typename S, int HD>
+bool split_rows_bwd(const WindowAttn& a, int heads) {
+  if (!kWide<S, HD>) return split_rows(a, heads, kPerCuBwd<S, HD>);
+  const int64_t cols = (int64_t)heads * a.B;
+  if (2 * ((int64_t)a.window + a.sinks) > a.T && cols * cdiv(a.T, 128) < 512) return true;
+  const int64_t whole = (cols * cdiv(a.T, 128) + 255) / 256, halves = (cols * cdiv(a.T, 64) + 255) / 256;
+  return 10 * halves < 18 * whole;
+}
 
 template <typename S, int HD, bool SPLIT>
 hipError_t fwd(const WindowAttn& a, const void* qkv, void* O, float* lse, hipStream_t s) {
@@ -958,7 +973,7 @@ Plan plan_dkdv(const WindowAttn& a) {
     for (int d = 2; d <= grp; ++d)
       if (grp % d == 0 && split_rows(a, a.Hkv * p.parts, kFull) && d * per_part <= kWindowPartFloats)
         p.parts = d;
-  p.split = split_rows(a, a.Hkv * p.parts, kFull);
+  p.split = split_rows_bwd<S, HD>(a, a.Hkv * p.parts);
   // Queries from `far` on reach the first key block through its sink keys
   // only (the end of the last tile that its own range walks).  Their chunks:
   // enough workgroups to fill the chip twice over, and none under a tile.
@@ -1000,8 +1015,8 @@ hipError_t dkdv(const WindowAttn& a, const Plan& p, const void* qkv, const void*
 template <typename S, int HD>
 hipError_t bwd(const WindowAttn& a, const void* qkv, const void* O, const void* dO, const float* lse, float* Dvec,
                float* part, void* dqkv, hipStream_t s) {
-  const hipError_t e = split_rows(a, a.H, kPerCuBwd<S, HD>) ? dq<S, HD, true>(a, qkv, O, dO, lse, Dvec, dqkv, s)
-                                                           : dq<S, HD, false>(a, qkv, O, dO, lse, Dvec, dqkv, s);
+  const hipError_t e = split_rows_bwd<S, HD>(a, a.H) ? dq<S, HD, true>(a, qkv, O, dO, lse, Dvec, dqkv, s)
+                                                     : dq<S, HD, false>(a, qkv, O, dO, lse, Dvec, dqkv, s);
   if (e != hipSuccess) return e;
   const Plan p = plan_dkdv<S, HD>(a);
   return p.split ? dkdv<S, HD, true>(a, p, qkv, dO, lse, Dvec, part, dqkv, s)

@@ -124,6 +124,9 @@ SHAPES = [
     (16, 260, 32, 32, 128, 100, 0, (260, 259, 258, 257, 256, 255, 200, 129, 128, 127, 65, 64, 33, 1, 0, 260)),
     (24, 270, 32, 32, 32, 30, 33, None),
     (24, 257, 32, 32, 16, 8, 1, None),
+    (8, 256, 16, 16, 128, 40, 3, None),    # ... in fp32 at head_dim 128 too: one round of the chip
+    (4, 640, 24, 24, 128, 30, 9, None),    # two and a half rounds of it
+    (2, 300, 40, 40, 128, 200, 4, None),   # the full length in most windows
     # few key/value heads: the query heads of a group divided
     (1, 600, 24, 2, 64, 200, 5, (577,)),
     (1, 600, 6, 1, 128, 70, 40, None),
