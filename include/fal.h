@@ -471,7 +471,7 @@ typedef struct {
  * row's loss is
  *   -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (e^d - d - 1),
  * its gradient in logp -[not clipped] r A + kl_coef (1 - e^d).  A zero
- * advantage adds nothing whatever the ratio.
+ * advantage adds nothing whatever the ratio, a zero kl_coef nothing whatever d.
  *   old_logp, advantages  device fp32 [B, T]
  *   ref_logp  device fp32 [B, T], or NULL: no KL term
  *   stats     device fp32 [4]: loss, its policy part, the mean of

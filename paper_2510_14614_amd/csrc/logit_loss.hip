@@ -278,7 +278,7 @@ __device__ __forceinline__ float kl_term(float d, float* em1) {
   if (fabsf(d) > 0.5f) {
     const float e = expf(d);
     *em1 = e - 1.f;
-    kl = *em1 - d;
+    kl = e < INFINITY ? *em1 - d : e;  // (d = inf: the policy cannot give the token)
   } else {
     // d^2 (1/2 + d/6 + d^2/24 + ...): the first term left out is under
     // 2^-24 of the sum
@@ -311,7 +311,7 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& p, int64_t m, 
   if (p.ref_logp) {
     float em1;
     o.kl = kl_term(p.ref_logp[m] - lp, &em1);
-    o.c -= p.kl * em1;
+    if (p.kl > 0.f) o.c -= p.kl * em1;  // (0 times an infinite term is no term)
   }
   o.clipped = held ? 1.f : 0.f;
   return o;
@@ -475,7 +475,7 @@ __global__ __launch_bounds__(1024) void policy_total(const float* terms, int64_t
     for (int k = 0; k < 3; ++k) tot[k] += terms[k * N + i];
   block_totals<3, 16>(tot);
   if (threadIdx.x == 0) {
-    stats[0] = (float)(tot[0] + (double)kl_coef * tot[1]);
+    stats[0] = (float)(kl_coef > 0.f ? tot[0] + (double)kl_coef * tot[1] : tot[0]);
     for (int k = 0; k < 3; ++k) stats[1 + k] = (float)tot[k];
   }
 }
