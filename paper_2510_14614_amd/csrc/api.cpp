@@ -1248,7 +1248,7 @@ static LogitRows step_rows(fal_ctx_t* ctx, const int32_t* tokens, const uint8_t*
   r.logits = ctx->W.logits; r.targets = tokens + 1; r.mask = mask;
   r.B = D.B; r.T = D.T; r.V = D.V; r.width = D.Vp;
   r.ldl = r.ldd = D.Vp; r.ldt = D.T + 1;
-  r.inv_temp = 1.f / temperature;
+  r.set_temperature(temperature);
   return r;
 }
 

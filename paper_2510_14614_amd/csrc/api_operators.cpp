@@ -133,7 +133,7 @@ LogitRows row_args(const fal_logit_rows_t* r, const void* logits, const int32_t*
   a.logits = logits; a.targets = targets; a.mask = mask;
   a.B = r->batch; a.T = r->seq_len; a.V = r->vocab; a.width = r->dlogits_cols;
   a.ldl = r->ld_logits; a.ldt = r->ld_targets; a.ldd = r->ld_dlogits;
-  a.inv_temp = 1.f / r->temperature;
+  a.set_temperature(r->temperature);
   return a;
 }
 

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 namespace fal {
@@ -264,7 +265,7 @@ hipError_t cross_entropy(DType dt, const void* logits, int64_t ldl, const int32_
 // ------------------------------------- losses of sampled tokens' log-probs ----
 // Rows of logits [B, T, V] (dtype, row stride ldl) with a target id each
 // (targets[b * ldt + t], clamped to [0, V)) and a mask byte each ([B, T];
-// NULL: every row counts).  x = logits * inv_temp; a row's log-probability is
+// NULL: every row counts).  x = logits / temp; a row's log-probability is
 // x[target] - logsumexp(x).  Rows whose byte is zero are not read: their
 // log-probability is 0 and their gradient row zeros.  Gradient rows have
 // `width` columns (>= V, the rest zeros) at stride ldd and may be the logits
@@ -275,7 +276,18 @@ struct LogitRows {
   const uint8_t* mask;
   int B, T, V, width;
   int64_t ldl, ldt, ldd;
-  float inv_temp;
+  float temp, inv_temp;
+  // log2(e) / temp in two parts, to 48 bits: the larger one cut off, so that the
+  // smaller is above 0 (-inf times either is -inf)
+  float log2_hi, log2_lo;
+  void set_temperature(float t) {
+    const double k = 1.4426950408889634 / (double)t;
+    temp = t;
+    inv_temp = 1.f / t;
+    log2_hi = (float)k;
+    if ((double)log2_hi >= k) log2_hi = nextafterf(log2_hi, 0.f);
+    log2_lo = fmaxf((float)(k - (double)log2_hi), 1.4e-45f);
+  }
 };
 // logp [B, T]; entropy [B, T] or NULL.
 hipError_t token_logprobs(DType dt, const LogitRows& r, float* logp, float* entropy, hipStream_t s);

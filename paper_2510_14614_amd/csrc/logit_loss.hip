@@ -14,7 +14,10 @@
 // outside the row read as -inf.  Exponentials are exp2 of
 // (x - maximum) log2(e) / temperature, sums fp32 within a row; sums over rows
 // and sequences are fp64, since a sequence's log-probability is large (hundreds
-// of terms) and the losses see a small difference of two.
+// of terms) and the losses see a small difference of two.  So that a row's error
+// is one of rounding, which such a sum averages out, the exponent's factor has
+// two parts and the log-probability is taken in natural units: log2(e) and ln 2
+// as fp32 constants would shift every row by 1e-8 of it.
 //
 // 4551 of 8192 rows of 50257 bf16 counted: log-probabilities 76 us (6.0 TB/s of
 // those rows), the policy gradient 262 (4.9 TB/s of those rows read and all of
@@ -31,7 +34,7 @@ namespace fal {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 // ---- chunks of a row --------------------------------------------------------
 template <typename S>
@@ -112,15 +115,21 @@ struct Row {
 };
 
 // ---- a row's statistics -----------------------------------------------------
-// With m the maximum, in units of log2: top = m k (k = log2(e) / temperature),
-// sum of 2^(x k - top), and dot = sum of (x k - top) 2^(x k - top).
+// With m the maximum and k = log2(e) / temperature: sum of 2^((x - m) k), and
+// dot = sum of (x - m) k 2^((x - m) k).
 struct Stat {
   float m, sum, dot;
 };
-__device__ __forceinline__ void join(Stat& a, const Stat& b, float k) {
+// k in two parts, both above 0: one fma more than a product by an fp32 k
+struct Log2Scale {
+  float hi, lo;
+};
+__device__ __forceinline__ float scaled(float d, const Log2Scale& k) { return fmaf(d, k.hi, d * k.lo); }
+
+__device__ __forceinline__ void join(Stat& a, const Stat& b, const Log2Scale& k) {
   const float m = fmaxf(a.m, b.m);
   if (m == -INFINITY) return;
-  const float da = (a.m - m) * k, db = (b.m - m) * k;  // <= 0, -inf for a side without a column
+  const float da = scaled(a.m - m, k), db = scaled(b.m - m, k);  // <= 0, -inf for a side without a column
   const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
   const float la = fa > 0.f ? fmaf(da, a.sum, a.dot) * fa : 0.f, lb = fb > 0.f ? fmaf(db, b.sum, b.dot) * fb : 0.f;
   a.sum = a.sum * fa + b.sum * fb;
@@ -136,20 +145,36 @@ __device__ __forceinline__ float chunk_max(const uint4& u, float m) {
 }
 // adds a chunk to sums relative to st.m (not -inf)
 template <typename S, bool DOT>
-__device__ __forceinline__ void chunk_add(const uint4& u, Stat& st, float k) {
+__device__ __forceinline__ void chunk_add(const uint4& u, Stat& st, const Log2Scale& k) {
   constexpr int E = Chunk<S>::E;
   float e2[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const float a = (Chunk<S>::at(u, e) - st.m) * k;
+    const float a = scaled(Chunk<S>::at(u, e) - st.m, k);
     e2[e] = __builtin_amdgcn_exp2f(a);
-    if (DOT && e2[e] > 0.f) st.dot = fmaf(a, e2[e], st.dot);
+    if (DOT) st.dot = fmaf(fmaxf(a, -200.f), e2[e], st.dot);  // (2^-200 is 0, and -inf times it no term)
   }
 #pragma unroll
   for (int w = E / 2; w > 0; w >>= 1)
 #pragma unroll
     for (int e = 0; e < w; ++e) e2[e] += e2[e + w];
   st.sum += e2[0];
+}
+
+// log x of a sum of exponentials, to one rounding and 2^-25: with x = 2^e m, m
+// in [sqrt 1/2, sqrt 2) and s = (m - 1) / (m + 1), the series
+// log m = 2 s (1 + s^2/3 + s^4/5 + ...), whose first term left out is 2e-9 of
+// it, and e ln 2 in two parts.  (logf came out 1e-7 too small on average.)
+__device__ __forceinline__ float log_of_sum(float x) {
+  float m = __builtin_amdgcn_frexp_mantf(x), e = (float)__builtin_amdgcn_frexp_expf(x);
+  if (m < 0.70710678f) {
+    m *= 2.f;
+    e -= 1.f;
+  }
+  const float s = (m - 1.f) / (m + 1.f), z = s * s;
+  const float tail = fmaf(z, fmaf(z, fmaf(z, 1.f / 9.f, 1.f / 7.f), 1.f / 5.f), 1.f / 3.f);
+  const float log_m = fmaf(2.f * s * z, tail, 2.f * s);
+  return fmaf(e, 0.693147182f, fmaf(e, -1.90465432e-9f, log_m));  // the fp32 ln 2, and what it lacks
 }
 
 // What a row's threads share after the exchange.
@@ -162,7 +187,7 @@ struct Shared {
 // Joins the statistics of the G threads of a row (and sums their counts);
 // the thread that holds the target's logit is t == 0.
 template <int G>
-__device__ __forceinline__ Shared exchange(Stat st, float target, int count, float k) {
+__device__ __forceinline__ Shared exchange(Stat st, float target, int count, const Log2Scale& k) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     const Stat b{__shfl_xor(st.m, o, FAL_WAVE), __shfl_xor(st.sum, o, FAL_WAVE), __shfl_xor(st.dot, o, FAL_WAVE)};
@@ -207,7 +232,8 @@ __device__ __forceinline__ void grad_chunk(const uint4& u, int col0, int V, int 
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     // p from x - maximum, not x - lse: the log-sum-exp alone, rounded, is off
-    // by more than all else here
+    // by more than all else here (an element's own error does not add up: the
+    // factor's first part is enough)
     v[e] = -scale * __builtin_amdgcn_exp2f(fmaf(Chunk<S>::at(u, e) - top, k, -log2sum));
     if (col0 + e == tgt) v[e] += scale;
     if (col0 + e >= V) v[e] = 0.f;
@@ -363,7 +389,7 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
   const S* l = static_cast<const S*>(r.logits) + m * r.ldl;
   const Row<S, const S> in(l, r.V);
   const int nc = in.chunks(), b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T));
-  const float k = r.inv_temp * kLog2e;
+  const Log2Scale k{r.log2_hi, r.log2_lo};
   const float xt = t == 0 ? to_f(l[tgt]) : 0.f;
   int n = 0;  // this thread's share of the counted rows that the mean is over
   if (MODE == POLICY && r.mask) {
@@ -416,14 +442,15 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
   }
   const Shared sh = exchange<G>(st, xt, n, k);
   const float log2sum = log2f(sh.st.sum);
-  const float lp = ((sh.target - sh.st.m) * k - log2sum) * kLn2;
+  const float lse = log_of_sum(sh.st.sum);  // less the maximum
+  const float lp = (sh.target - sh.st.m) / r.temp - lse;
   if (t == 0) {
     if (o.logp) o.logp[m] = lp;
     if (MODE == STATS) {
       o.top[m] = sh.st.m;
       o.log2sum[m] = log2sum;
     }
-    if (MODE == LOGP_ENTROPY) o.entropy[m] = (log2sum - sh.st.dot / sh.st.sum) * kLn2;
+    if (MODE == LOGP_ENTROPY) o.entropy[m] = lse - sh.st.dot / sh.st.sum * kLn2;
   }
   if (MODE != POLICY) return;
   const float rows = r.mask ? (float)sh.count : (float)(o.p.sequence_mean ? (int64_t)r.T : N);
@@ -441,9 +468,9 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
 #pragma unroll
   for (int i = 0; i < NPT; ++i) {
     const int c = t + G * i;
-    if (c < end) grad_chunk<S>(c < nc ? raw[i] : none, in.column(c), r.V, tgt, k, sh.st.m, log2sum, scale, out, c);
+    if (c < end) grad_chunk<S>(c < nc ? raw[i] : none, in.column(c), r.V, tgt, k.hi, sh.st.m, log2sum, scale, out, c);
   }
-  row_grad<S, G, false>(in, out, t + NPT * G, end, tgt, k, sh.st.m, log2sum, scale);
+  row_grad<S, G, false>(in, out, t + NPT * G, end, tgt, k.hi, sh.st.m, log2sum, scale);
   if (!same) zero_tail<S, G>(out, r.V, t);
 }
 
@@ -540,7 +567,7 @@ __global__ __launch_bounds__(kRowThreads<G>) void preference_rows(LogitRows r, c
   }
   const Row<S, const S> in(static_cast<const S*>(r.logits) + m * r.ldl, r.V);
   const int b = (int)(m / r.T), tgt = target_of(r, b, (int)(m % r.T));
-  const float k = r.inv_temp * kLog2e, scale = coef[b] * r.inv_temp, mx = top[m], ls = log2sum[m];
+  const float k = r.log2_hi, scale = coef[b] * r.inv_temp, mx = top[m], ls = log2sum[m];
   const bool same = in.shift == out.shift;
   const int end = same ? out.chunks() : in.chunks();
   row_grad<S, G, true>(in, out, t, end, tgt, k, mx, ls, scale);

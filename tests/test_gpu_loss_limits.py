@@ -46,3 +46,48 @@ def test_a_kl_term_without_weight_adds_nothing(dtype):
     assert torch.isfinite(want.dlogits).all() and torch.equal(got.dlogits, want.dlogits)
     assert torch.equal(got.stats[[0, 1, 3]], want.stats[[0, 1, 3]]) and torch.isfinite(got.stats[0])
     assert float(got.stats[2]) == math.inf
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("temperature", [1.0, 0.7])
+def test_errors_of_many_rows_do_not_add_up(temperature, dtype):
+    # A sequence's log-probability adds those of its rows, so what matters is
+    # their mean error.  log p lies in (-64, -32), where half a step is 2^-19:
+    # rounding once or twice leaves a mean error of 2^-19 / sqrt(3) *
+    # sqrt(2 / N) at one standard deviation, here taken six times, and the sum of
+    # exponentials one step of 2^-24.  log2(e) and ln 2 as fp32 constants would
+    # move every row by 1e-8 of log p, 5e-7.
+    N, V = 1 << 14, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    # scores within 3 of each other but for the target's, on a grid that both
+    # types hold
+    x = torch.randint(-96, 1, (1, N, V), device="cuda", generator=g).float() / 32
+    x[0, :, 5] = torch.randint(-56 * 4, -40 * 4, (N,), device="cuda", generator=g).float() / 4
+    x = (x * (1 if temperature == 1 else 0.75)).to(dtype)
+    y = torch.full((1, N), 5, device="cuda", dtype=torch.int32)
+    temp = float(torch.tensor(temperature))
+    _, want = exact(x, y, temp)
+    assert -64 < float(want.min()) and float(want.max()) < -32
+    bound = 6 * 2.0 ** -19 / math.sqrt(3) * math.sqrt(2 / N) + U
+    one = torch.ones(1, N, device="cuda")
+    for name, got in (("logprobs", fal.token_logprobs(x, y, temperature=temperature)),
+                      ("policy", fal.policy_loss(x, y, want.float(), one, temperature=temperature).logp)):
+        mean = float((got.double() - want).mean())
+        log(f"{name} {dtype} at {temperature}: mean error {mean:.2e}, bound {bound:.2e}")
+        assert abs(mean) <= bound
+
+
+@pytest.mark.parametrize("temperature", [1e-38, 1.0, 1e38])
+def test_masked_scores_at_extreme_temperatures(temperature):
+    # columns of -inf, whole chunks of them among others, have probability 0
+    # whatever the scale of the exponents
+    x, y, _ = rows(1, 3, 600, F32, seed=6)
+    kept = x[:, :, :20].clone()
+    x[:, :, 20:] = -math.inf
+    y.fill_(4)
+    want = fal.token_logprobs(kept, y, temperature=temperature, entropy=True)
+    got = fal.token_logprobs(x, y, temperature=temperature, entropy=True)
+    for a, b in zip(got, want):
+        assert not torch.isnan(a).any()
+        near = torch.isclose(a, b, rtol=4 * U * 24, atol=24 * U)  # another order of the sums
+        assert bool((near | (a == b)).all())
