@@ -343,11 +343,13 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& p, int64_t m, 
   return o;
 }
 
-// Counted rows of each sequence.
-__global__ __launch_bounds__(256) void mask_counts(const uint8_t* mask, int T, int32_t* count) {
+// Counted rows of each `span` of the N rows' mask: of each sequence, or of
+// slices of the batch.
+__global__ __launch_bounds__(256) void mask_counts(const uint8_t* mask, int64_t N, int64_t span, int32_t* count) {
   __shared__ int red[4];
   int n = 0;
-  for (int t = threadIdx.x; t < T; t += 256) n += mask[(int64_t)blockIdx.x * T + t] != 0;
+  const int64_t end = min((blockIdx.x + 1) * span, N);
+  for (int64_t i = blockIdx.x * span + threadIdx.x; i < end; i += 256) n += mask[i] != 0;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o, FAL_WAVE);
   if (threadIdx.x % FAL_WAVE == 0) red[threadIdx.x / FAL_WAVE] = n;
@@ -362,7 +364,8 @@ struct RowOut {
   float *logp, *entropy;  // [B, T], each may be NULL
   float *top, *log2sum;   // STATS, [B, T]: a row's largest logit, and log2 of its sum relative to it
   PolicyArgs p;
-  const int32_t* count;  // POLICY: counted rows of each sequence; NULL: each row's threads count the mask
+  const int32_t* count;  // POLICY: counted rows of each sequence, or of `slices` slices of the batch; NULL: each
+  int slices;            // row's threads count the mask
   float* terms;          // [3][B * T]
   void* dlogits;
 };
@@ -400,7 +403,7 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
     } else if (o.p.sequence_mean) {
       n = t == 0 ? o.count[b] : 0;
     } else {
-      for (int i = t; i < r.B; i += G) n += o.count[i];
+      for (int i = t; i < o.slices; i += G) n += o.count[i];
     }
   }
 
@@ -657,12 +660,17 @@ hipError_t policy_loss(DType dt, const LogitRows& r, const PolicyArgs& p, void* 
   o.terms = scratch;
   o.dlogits = dlogits;
   // the rows' threads count the mask themselves while that is a few bytes
-  // each, which saves a launch
+  // each, which saves a launch; past that a mean over the batch is counted in
+  // slices, as many as a row's threads add up in a few reads and as the scratch
+  // has place for, whatever the number of sequences (65536 sequences of 16 rows
+  // of 256 fp32, half of them counted: 10.0 ms with a count each, 0.80 in slices)
   const int64_t span = p.sequence_mean ? r.T : N;
   if (r.mask && span > 16 * (r.width > 512 * (dt == BF16 ? 8 : 4) ? 256 : 64)) {
-    int32_t* count = reinterpret_cast<int32_t*>(scratch + 3 * N);
-    hipLaunchKernelGGL(mask_counts, dim3(r.B), dim3(256), 0, s, r.mask, r.T, count);
+    int32_t* count = reinterpret_cast<int32_t*>(scratch + 3 * N);  // 4 B of them
     o.count = count;
+    o.slices = (int)std::min({(int64_t)256, 4 * (int64_t)r.B, (N + 1023) / 1024});
+    const int64_t of = p.sequence_mean ? r.T : (N + o.slices - 1) / o.slices;
+    hipLaunchKernelGGL(mask_counts, dim3(p.sequence_mean ? r.B : o.slices), dim3(256), 0, s, r.mask, N, of, count);
   }
   const hipError_t e = dt == BF16 ? policy_rows<bf16>(r, o, s) : policy_rows<float>(r, o, s);
   if (e != hipSuccess) return e;

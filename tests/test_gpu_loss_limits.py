@@ -91,3 +91,41 @@ def test_masked_scores_at_extreme_temperatures(temperature):
         assert not torch.isnan(a).any()
         near = torch.isclose(a, b, rtol=4 * U * 24, atol=24 * U)  # another order of the sums
         assert bool((near | (a == b)).all())
+
+
+@pytest.mark.parametrize("B,T,seq", [(1 << 24, 1, False), (65536, 16, False), (3, 2051, False), (1, 30000, False),
+                                     (1 << 14, 1024, True), (5, 1025, True)])
+def test_masks_of_many_sequences(B, T, seq):
+    # the rows that a mean runs over are counted once, however they are divided
+    # into sequences
+    V, low, high = 4, 0.2, 0.2
+    x, y, g = rows(B, T, V, BF16, seed=5)
+    mask = torch.rand(B, T, device="cuda", generator=g) < 0.3
+    if B > 1:
+        mask[B // 2] = False  # a sequence without a counted row
+    mask[0, 0] = True
+    _, logp = exact(x, y)
+    old = (logp - 0.1 * torch.randn(B, T, device="cuda", generator=g)).float()
+    adv = torch.randn(B, T, device="cuda", generator=g)
+    got = fal.policy_loss(x, y, old, adv, mask=mask, clip_low=low, clip_high=high, sequence_mean=seq)
+    ratio, a = torch.exp(logp - old.double()), adv.double()
+    n = mask.sum(-1, keepdim=True).double()
+    w = mask / n.clamp(min=1) / B if seq else mask / n.sum().clamp(min=1)
+    each = -torch.minimum(ratio * a, ratio.clamp(1 - low, 1 + high) * a) * w
+    # a ratio is off by e, a term by three more roundings, all times its size; one
+    # on a clip's border moves by no more than that; sums are fp64, rounded once
+    e = (6 * float(x.abs().max()) + 24) * U
+    bound = float(((ratio * a).abs() * w).sum()) * (e + 4 * U) + U * float(each.sum().abs())
+    log(f"{B} x {T}: {int(mask.sum())} rows, loss {float(got.stats[0]):.6e}, wanted {float(each.sum()):.6e}, "
+        f"error / bound {abs(float(got.stats[0]) - float(each.sum())) / bound:.3f}")
+    assert abs(float(got.stats[0]) - float(each.sum())) <= bound
+    assert not got.dlogits[~mask].any() and not got.logp[~mask].any()
+    # a row off the clip's borders has its whole weight
+    held = ((a > 0) & (ratio > 1 + high)) | ((a < 0) & (ratio < 1 - low))
+    near = ((ratio - 1 - high).abs() < 1e-4) | ((ratio - 1 + low).abs() < 1e-4)
+    c = torch.where(held, 0.0, -ratio * a) * w
+    p = x.double().softmax(-1)
+    want = c[:, :, None] * (torch.zeros_like(p).scatter_(-1, y.long()[:, :, None], 1.0) - p)
+    size = c.abs()[:, :, None] * (torch.zeros_like(p).scatter_(-1, y.long()[:, :, None], 1.0) + p)
+    err = (got.dlogits.double() - want).abs() - size * (2 * e + 8 * U) - 1.02 * R * want.abs()
+    assert float(err[~near].max()) <= 1e-38
