@@ -542,7 +542,7 @@ __global__ __launch_bounds__(256) void preference_pairs(LogitRows r, PreferenceA
     const double z = beta * h, tail = log1p(exp(-fabs(z)));
     loss = (1.0 - sm) * (tail + fmax(-z, 0.0));
     if (sm > 0.0) loss += sm * (tail + fmax(z, 0.0));  // (0 times an infinite margin is no term)
-    dh = beta * (1.0 / (1.0 + exp(-z)) - (1.0 - sm));
+    dh = beta * (sm - 1.0 / (1.0 + exp(z)));  // sigmoid(z) - 1 + sm without its cancellation at large z
   }
   pair_loss[b0] = loss;
   coef[b0] = (float)(dh / P * share[0]);

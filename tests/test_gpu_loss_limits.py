@@ -129,3 +129,27 @@ def test_masks_of_many_sequences(B, T, seq):
     size = c.abs()[:, :, None] * (torch.zeros_like(p).scatter_(-1, y.long()[:, :, None], 1.0) + p)
     err = (got.dlogits.double() - want).abs() - size * (2 * e + 8 * U) - 1.02 * R * want.abs()
     assert float(err[~near].max()) <= 1e-38
+
+
+@pytest.mark.parametrize("beta_h", [-60.0, -5.0, 20.0, 30.0, 45.0, 80.0])
+def test_gradients_of_settled_pairs(beta_h):
+    # the slope beta (sigmoid(z) - 1) of a pair that the model ranks right is
+    # small and no difference of numbers near one: relative accuracy at any z
+    B, T, V, beta = 2, 3, 40, 0.5
+    x, y, _ = rows(B, T, V, F32, seed=3)
+    lp, logp = exact(x, y)
+    seq = logp.sum(-1)
+    ref = torch.stack((seq[0] - beta_h / beta, seq[1])).float()
+    h = (seq[0] - ref[0].double()) - (seq[1] - ref[1].double())
+    got = fal.preference_loss(x, y, ref, beta=beta)
+    slope = -beta * torch.sigmoid(-beta * h)
+    onehot = torch.zeros_like(lp).scatter_(-1, y.long()[:, :, None], 1.0)
+    sign = torch.tensor([1.0, -1.0], dtype=torch.float64, device="cuda")[:, None, None]
+    want = sign * slope * (onehot - lp.exp())
+    # a row's log-probability and probabilities to e, h to 2 T e, the slope to
+    # beta of that relative, then three roundings; the smallest step of fp32
+    e = (6 * float(x.abs().max()) + 24) * U
+    rel = (2 * T * beta * e + 2 * e + 4 * U) * (onehot + lp.exp()) * slope.abs()
+    err = (got.dlogits.double() - want).abs()
+    log(f"z = {beta_h}: worst error / bound {float((err / (rel + 2.0 ** -148)).max()):.3f}")
+    assert bool((err <= rel + 2.0 ** -148).all())
