@@ -448,6 +448,7 @@ typedef struct {
  *            read and get 0
  *   logp     device fp32 [B, T]
  *   entropy  device fp32 [B, T] or NULL
+ * A row with a NaN score gets NaN.
  * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes or misaligned
  * arrays; FAL_ERR_HIP when a launch fails. */
 fal_status_t fal_token_logprobs(const fal_logit_rows_t* rows, const void* logits, const int32_t* targets,

@@ -128,7 +128,10 @@ __device__ __forceinline__ float scaled(float d, const Log2Scale& k) { return fm
 
 __device__ __forceinline__ void join(Stat& a, const Stat& b, const Log2Scale& k) {
   const float m = fmaxf(a.m, b.m);
-  if (m == -INFINITY) return;
+  if (m == -INFINITY) {  // sums of 0, or of NaN
+    a.sum += b.sum;
+    return;
+  }
   const float da = scaled(a.m - m, k), db = scaled(b.m - m, k);  // <= 0, -inf for a side without a column
   const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
   const float la = fa > 0.f ? fmaf(da, a.sum, a.dot) * fa : 0.f, lb = fb > 0.f ? fmaf(db, b.sum, b.dot) * fb : 0.f;
@@ -175,6 +178,15 @@ __device__ __forceinline__ float log_of_sum(float x) {
   const float tail = fmaf(z, fmaf(z, fmaf(z, 1.f / 9.f, 1.f / 7.f), 1.f / 5.f), 1.f / 3.f);
   const float log_m = fmaf(2.f * s * z, tail, 2.f * s);
   return fmaf(e, 0.693147182f, fmaf(e, -1.90465432e-9f, log_m));  // the fp32 ln 2, and what it lacks
+}
+
+// A chunk of a thread that has no maximum yet holds -inf, which adds nothing, or
+// NaN, which no maximum shows.
+template <typename S>
+__device__ __forceinline__ void chunk_nan(const uint4& u, Stat& st) {
+#pragma unroll
+  for (int e = 0; e < Chunk<S>::E; ++e)
+    if (Chunk<S>::at(u, e) != -INFINITY) st.sum = NAN;
 }
 
 // What a row's threads share after the exchange.
@@ -329,9 +341,10 @@ __device__ __forceinline__ PolicyRow policy_row(const PolicyArgs& p, int64_t m, 
   PolicyRow o;
   const float A = p.adv[m], ratio = expf(lp - p.old_logp[m]);
   const bool held = (A > 0.f && ratio > 1.f + p.high) || (A < 0.f && ratio < 1.f - p.low);
-  const float clip = fminf(fmaxf(ratio, 1.f - p.low), 1.f + p.high);
-  // a zero advantage adds nothing, whatever the ratio
-  o.pg = A == 0.f ? 0.f : -fminf(ratio * A, clip * A);
+  // where the clip does not hold the ratio, the smaller product is the ratio's own
+  // (compared, not fminf: that drops NaN); a zero advantage adds nothing,
+  // whatever the ratio
+  o.pg = A == 0.f ? 0.f : -(held ? (A > 0.f ? 1.f + p.high : 1.f - p.low) : ratio) * A;
   o.c = held || A == 0.f ? 0.f : -ratio * A;
   o.kl = 0.f;
   if (p.ref_logp) {
@@ -422,6 +435,10 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
 #pragma unroll
       for (int i = 0; i < NPT; ++i)
         if (t + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(raw[i], st, k);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NPT; ++i)
+        if (t + G * i < nc) chunk_nan<S>(raw[i], st);
     }
   }
   for (int c0 = t + NPT * G; c0 < nc; c0 += kStream * G) {
@@ -441,6 +458,10 @@ __global__ __launch_bounds__(kRowThreads<G>) void logit_rows(LogitRows r, RowOut
 #pragma unroll
       for (int i = 0; i < kStream; ++i)
         if (c0 + G * i < nc) chunk_add<S, MODE == LOGP_ENTROPY>(u[i], st, k);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kStream; ++i)
+        if (c0 + G * i < nc) chunk_nan<S>(u[i], st);
     }
   }
   const Shared sh = exchange<G>(st, xt, n, k);

@@ -153,3 +153,28 @@ def test_gradients_of_settled_pairs(beta_h):
     err = (got.dlogits.double() - want).abs()
     log(f"z = {beta_h}: worst error / bound {float((err / (rel + 2.0 ** -148)).max()):.3f}")
     assert bool((err <= rel + 2.0 ** -148).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("masked", [False, True], ids=["all", "masked"])
+@pytest.mark.parametrize("V", [300, 5003, 40001])
+def test_nan_scores_are_not_lost(V, masked, dtype):
+    # a run of NaN as long as whole chunks of a row, among scores or among columns
+    # of -inf: the row's softmax is NaN, the other rows are what they were
+    x, y, g = rows(2, 3, V, dtype, seed=4)
+    y.fill_(1)
+    clean = fal.token_logprobs(x, y, entropy=True)
+    old, adv = clean[0].clone(), torch.ones(2, 3, device="cuda")
+    good = fal.policy_loss(x, y, old, adv)
+    if masked:
+        x[0, 1, 2:] = -math.inf
+    x[0, 1, 264:296] = math.nan
+    other = torch.ones(2, 3, dtype=torch.bool, device="cuda")
+    other[0, 1] = False
+    for a, b in zip(fal.token_logprobs(x, y, entropy=True), clean):
+        assert torch.isnan(a[0, 1]) and torch.equal(a[other], b[other])
+    got = fal.policy_loss(x, y, old, adv)
+    assert torch.isnan(got.logp[0, 1]) and torch.isnan(got.dlogits[0, 1]).all() and torch.isnan(got.stats[0])
+    assert torch.equal(got.dlogits[other], good.dlogits[other])
+    got = fal.preference_loss(x, y, torch.zeros(2, device="cuda"))
+    assert torch.isnan(got.loss).all() and torch.isnan(got.seq_logp[0]) and torch.isfinite(got.seq_logp[1])
