@@ -434,7 +434,8 @@ typedef struct {
   int64_t ld_targets;   /* elements between sequences' targets, >= T        */
   int64_t ld_dlogits;   /* elements between gradient rows                   */
   int32_t dlogits_cols; /* columns written of each gradient row: V of them
-                           the gradient, the rest zeros; V .. ld_dlogits    */
+                           the gradient, the rest zeros; V .. ld_dlogits and
+                           at most 2^30                                     */
   float temperature;    /* > 0: the scores are logits / temperature (which
                            must leave log2(e) / temperature finite, not 0)  */
 } fal_logit_rows_t;

@@ -123,6 +123,8 @@ Refusal check_rows(const fal_logit_rows_t* r, bool gradient) {
     return {FAL_ERR_INVALID_ARG, "ld_targets must lie in [seq_len, 2^32]"};
   if (gradient && (r->dlogits_cols < r->vocab || r->ld_dlogits < r->dlogits_cols || r->ld_dlogits > most))
     return {FAL_ERR_INVALID_ARG, "dlogits_cols must lie in [vocab, ld_dlogits], ld_dlogits be at most 2^32"};
+  // (the kernels count columns in 32 bits, a workgroup's stride past the last one included)
+  if (gradient && r->dlogits_cols > (1 << 30)) return {FAL_ERR_INVALID_ARG, "dlogits_cols must be at most 2^30"};
   if (const char* why = check_temperature(r->temperature)) return {FAL_ERR_INVALID_ARG, why};
   return kFine;
 }

@@ -342,8 +342,8 @@ def _loss_workspace(B, T):
 
 
 def _clamp32(n):
-    # past 32 bits every window is the whole sequence and every number of
-    # sinks too many
+    # past 32 bits every window is the whole sequence, and every number of
+    # sinks and size of an array too many
     return n if -1 <= n <= 2147483647 else max(-1, min(n, 2147483647))
 
 
@@ -442,7 +442,8 @@ def _logit_rows(logits, targets, mask, vocab, temperature):
     if mask is not None:
         _dense(mask, "mask", (B, T), (torch.bool, torch.uint8), logits.device)
     ld = _row_stride(logits, "logits")
-    return fal_logit_rows_t(B, T, V, code, ld, sb if B > 1 else T, ld, width, temperature)
+    return fal_logit_rows_t(_clamp32(B), _clamp32(T), _clamp32(V), code, ld, sb if B > 1 else T, ld, _clamp32(width),
+                            temperature)
 
 
 def token_logprobs(logits, targets, mask=None, vocab=None, temperature=1.0, entropy=False):
@@ -463,6 +464,8 @@ def token_logprobs(logits, targets, mask=None, vocab=None, temperature=1.0, entr
 def _gradient_rows(r, logits, dlogits):
     """The gradient's buffer: as wide as the logits and spaced as they are."""
     import torch
+    if r.dlogits_cols > 1 << 30:
+        _refuse("logits of a gradient must have at most 2^30 columns")
     if dlogits is None:
         ld = r.ld_logits if r.ld_logits < r.dlogits_cols + 64 else r.dlogits_cols
         dlogits = torch.empty((r.batch, r.seq_len, ld), dtype=logits.dtype, device=logits.device)
