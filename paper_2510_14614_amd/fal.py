@@ -528,7 +528,12 @@ def preference_loss(logits, targets, ref_logp, mask=None, vocab=None, dlogits=No
 
 
 class Fal:
-    """A libfal context with PyTorch-owned device buffers on the current GPU."""
+    """A libfal context with PyTorch-owned device buffers on the current GPU.
+
+    Calls run on stream_main (the current stream of the constructor unless
+    given).  A caller on another stream orders the two itself, inputs before the
+    call and results after it, as between any two streams; the memory of token
+    arrays and of results is kept until both are done with it."""
 
     def __init__(self, cfg: Config, stream_main=None, stream_aux=None):
         import torch
@@ -585,6 +590,15 @@ class Fal:
         return unflatten(self.cfg, flat, global_shapes(self.cfg), block_shapes(self.cfg), self.layout)
 
     # ---------------------------------------------------------------- calls --
+    def _share(self, *tensors, result=False):
+        """Tells the allocator of the second stream that uses a tensor: the
+        context's reads the caller's, the caller's the results."""
+        current = self.torch.cuda.current_stream(self.device)
+        if current != self.stream_main:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(current if result else self.stream_main)
+
     def model_step(self, tokens, logits=None):
         """tokens: int32 device tensor [B, T+1]; logits: optional fp32 device
         tensor [B*T, V].  Returns the loss tensor (device, shape [1])."""
@@ -593,6 +607,7 @@ class Fal:
         _check(lib().fal_model_step(self.ctx, c_void_p(self.params.data_ptr()), c_void_p(tokens.data_ptr()),
                                     c_void_p(self.loss.data_ptr()), lp, c_void_p(self.grads.data_ptr())),
                self.ctx)
+        self._share(tokens, logits)
         return self.loss
 
     def model_forward(self, tokens, logits=None, loss=True):
@@ -602,6 +617,7 @@ class Fal:
         lp = c_void_p(logits.data_ptr()) if logits is not None else None
         _check(lib().fal_model_forward(self.ctx, c_void_p(self.params.data_ptr()), c_void_p(tokens.data_ptr()),
                                        c_void_p(self.loss.data_ptr()) if loss else None, lp), self.ctx)
+        self._share(tokens, logits)
         return self.loss if loss else None
 
     def stack_forward(self, x_in, x_out=None):
@@ -638,7 +654,9 @@ class Fal:
     def _empty(self, *shape):
         """An fp32 result, allocated on the stream that will write it."""
         with self.torch.cuda.stream(self.stream_main):
-            return self.torch.empty(shape, dtype=self.torch.float32, device=self.device)
+            t = self.torch.empty(shape, dtype=self.torch.float32, device=self.device)
+        self._share(t, result=True)
+        return t
 
     def _token_arrays(self, tokens, mask, **arrays):
         torch = self.torch
@@ -649,6 +667,7 @@ class Fal:
         for name, t in arrays.items():
             if t is not None:
                 _dense(t, name, (B,) if name == "ref_seq_logp" else (B, T), (torch.float32,), self.device)
+        self._share(tokens, mask, *arrays.values())
 
     def model_logprobs(self, tokens, mask=None, temperature=1.0, entropy=False):
         """Log-probabilities of tokens[:, 1:] under the model, float32 [B, T]
