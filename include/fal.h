@@ -516,7 +516,8 @@ fal_status_t fal_preference_loss(const fal_logit_rows_t* rows, const fal_prefere
 
 /* fal_model_forward with the per-token scores in place of the loss: logp (and
  * entropy, or NULL) of tokens[:, 1:] as fal_token_logprobs defines them.
- *   mask  device uint8 [B, T] or NULL, over the T predicted tokens */
+ *   mask  device uint8 [B, T] or NULL, over the T predicted tokens
+ * Outputs of this call and the two below may overlap no other argument. */
 fal_status_t fal_model_logprobs(fal_ctx_t* ctx, const void* params, const int32_t* tokens, const uint8_t* mask,
                                 float temperature, float* logp, float* entropy);
 

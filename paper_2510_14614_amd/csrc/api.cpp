@@ -1252,6 +1252,23 @@ static LogitRows step_rows(fal_ctx_t* ctx, const int32_t* tokens, const uint8_t*
   return r;
 }
 
+// The arrays of a step's tuning loss beside each other and beside what else the
+// step reads and writes (grads NULL: a forward pass).
+static const char* check_step_arrays(const fal_ctx_t* ctx, const void* params, const int32_t* tokens,
+                                     const uint8_t* mask, const float* grads, std::initializer_list<Extent> in,
+                                     std::initializer_list<Extent> out) {
+  const Dims& D = ctx->D;
+  const int64_t n = ctx->Lo.total;
+  if (!aligned(tokens, 4) || !all_aligned(in, 4) || !all_aligned(out, 4))
+    return "tokens and fp32 arrays must be 4-byte aligned";
+  if (outputs_meet(out, in) || outputs_meet(out, {{params, n * (int64_t)D.es},
+                                                  {tokens, (int64_t)D.B * (D.T + 1) * 4},
+                                                  {mask, (int64_t)D.M},
+                                                  {grads, n * 4}}))
+    return "an output overlaps another argument";
+  return nullptr;
+}
+
 // The loss scratch of a context's step: W.dh1 holds nothing between the
 // forward pass and the head's backward, and d_model >= 8 gives it 8 floats a
 // token, more than logit_loss_scratch's 3 a token and 4 a sequence.
@@ -1264,6 +1281,9 @@ fal_status_t fal_model_logprobs(fal_ctx_t* ctx, const void* params, const int32_
   if (!ctx->cfg.has_embed_head) return bad(ctx, "fal_model_logprobs needs has_embed_head = 1");
   if (!params || !tokens || !logp) return bad(ctx, "NULL params, tokens or logp");
   if (const char* why = check_temperature(temperature)) return bad(ctx, why);
+  const int64_t M4 = (int64_t)ctx->D.M * 4;
+  if (const char* why = check_step_arrays(ctx, params, tokens, mask, nullptr, {}, {{logp, M4}, {entropy, M4}}))
+    return bad(ctx, why);
   return model_forward(ctx, params, tokens, [&](Run& r) {
     const Dims& D = ctx->D;
     Span span(ctx, FAL_PROF_CE, ctx->sm, 0.0, (double)D.M * (double)D.es * D.V);
@@ -1281,6 +1301,11 @@ fal_status_t fal_policy_step(fal_ctx_t* ctx, const void* params, const fal_polic
     return bad(ctx, "NULL params, tokens, old_logp, advantages, stats or grads");
   if (const char* why = check_temperature(temperature)) return bad(ctx, why);
   if (const char* why = check_policy(hp)) return bad(ctx, why);
+  const int64_t M4 = (int64_t)ctx->D.M * 4;
+  if (const char* why = check_step_arrays(ctx, params, tokens, mask, grads,
+                                          {{old_logp, M4}, {ref_logp, M4}, {advantages, M4}},
+                                          {{stats, 16}, {logp, M4}}))
+    return bad(ctx, why);
   return model_step(ctx, params, tokens, grads, [&](Run& r) {
     const Dims& D = ctx->D;
     Span span(ctx, FAL_PROF_CE, ctx->sm, 0.0, (double)D.M * (double)D.es * (D.V + D.Vp));
@@ -1302,6 +1327,10 @@ fal_status_t fal_preference_step(fal_ctx_t* ctx, const void* params, const fal_p
   if (ctx->D.B % 2) return bad(ctx, "preference pairs need an even batch");
   if (const char* why = check_temperature(temperature)) return bad(ctx, why);
   if (const char* why = check_preference(hp)) return bad(ctx, why);
+  const int64_t B4 = (int64_t)ctx->D.B * 4;
+  if (const char* why = check_step_arrays(ctx, params, tokens, mask, grads, {{ref_logp, B4}},
+                                          {{loss, 4}, {seq_logp, B4}}))
+    return bad(ctx, why);
   return model_step(ctx, params, tokens, grads, [&](Run& r) {
     const Dims& D = ctx->D;
     Span span(ctx, FAL_PROF_CE, ctx->sm, 0.0, (double)D.M * (double)D.es * (2.0 * D.V + D.Vp));

@@ -4,6 +4,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <string>
 
 #include "../../include/fal.h"
@@ -19,6 +20,32 @@ inline bool overlaps(const void* a, int64_t abytes, const void* b, int64_t bbyte
 }
 
 inline bool aligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// An array; p NULL: one that the call was not given.
+struct Extent {
+  const void* p;
+  int64_t bytes;
+};
+inline bool meets(const Extent& out, std::initializer_list<Extent> others) {
+  for (const Extent& o : others)
+    if (o.p && overlaps(out.p, out.bytes, o.p, o.bytes)) return true;
+  return false;
+}
+inline bool all_aligned(std::initializer_list<Extent> arrays, uintptr_t bytes) {
+  for (const Extent& e : arrays)
+    if (!aligned(e.p, bytes)) return false;
+  return true;
+}
+// Whether an output overlaps another one or one of `others`.
+inline bool outputs_meet(std::initializer_list<Extent> out, std::initializer_list<Extent> others) {
+  for (const Extent& o : out) {
+    if (!o.p) continue;
+    if (meets(o, others)) return true;
+    for (const Extent& e : out)
+      if (&e != &o && meets(o, {e})) return true;
+  }
+  return false;
+}
 
 // (the kernels multiply by log2(e) / t, which has to be finite and not zero)
 inline const char* check_temperature(float t) {

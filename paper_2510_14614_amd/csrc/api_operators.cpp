@@ -88,18 +88,9 @@ WindowAttn window_args(const fal_window_attention_t* p, const int32_t* lens) {
   return a;
 }
 
-struct Extent {
-  const void* p;
-  int64_t bytes;
-};
 // A row matrix's bytes from its first element to its last.
 Extent rows_of(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t es) {
   return {p, ((rows - 1) * ld + width) * es};
-}
-bool meets(const Extent& out, std::initializer_list<Extent> others) {
-  for (const Extent& o : others)
-    if (o.p && overlaps(out.p, out.bytes, o.p, o.bytes)) return true;
-  return false;
 }
 
 int64_t window_scratch_bytes(int32_t dtype, const WindowAttn& a, int64_t* part_off) {
@@ -149,10 +140,7 @@ Refusal check_loss(const fal_logit_rows_t* r, const void* logits, const int32_t*
   const int64_t es = element_bytes(r->dtype), N = (int64_t)r->batch * r->seq_len;
   if (!aligned(logits, es) || !aligned(dlogits, es)) return {FAL_ERR_INVALID_ARG, "logits or dlogits misaligned"};
   if (!aligned(targets, 4)) return {FAL_ERR_INVALID_ARG, "targets must be 4-byte aligned"};
-  for (const Extent& e : in)
-    if (!aligned(e.p, 4)) return {FAL_ERR_INVALID_ARG, "fp32 arrays must be 4-byte aligned"};
-  for (const Extent& e : out)
-    if (!aligned(e.p, 4)) return {FAL_ERR_INVALID_ARG, "fp32 arrays must be 4-byte aligned"};
+  if (!all_aligned(in, 4) || !all_aligned(out, 4)) return {FAL_ERR_INVALID_ARG, "fp32 arrays must be 4-byte aligned"};
   const int64_t need = logit_loss_scratch(r->batch, r->seq_len) * 4;
   if (!workspace || ws_bytes < (size_t)need || !aligned(workspace, kWorkspaceAlign))
     return {FAL_ERR_WORKSPACE, "workspace NULL, too small or not 256-byte aligned"};
@@ -164,13 +152,8 @@ Refusal check_loss(const fal_logit_rows_t* r, const void* logits, const int32_t*
     return {FAL_ERR_INVALID_ARG, "dlogits or workspace overlaps an input (dlogits may only be the logits themselves)"};
   for (const Extent& e : in)
     if (meets(dx, {e}) || meets(ws, {e})) return {FAL_ERR_INVALID_ARG, "dlogits or workspace overlaps an input"};
-  for (const Extent& o : out) {
-    if (!o.p) continue;
-    bool bad = meets(o, {x, dx, tg, mk, ws});
-    for (const Extent& e : in) bad = bad || meets(o, {e});
-    for (const Extent& e : out) bad = bad || (e.p != o.p && meets(o, {e})) || (e.p == o.p && &e != &o);
-    if (bad) return {FAL_ERR_INVALID_ARG, "an output overlaps another argument"};
-  }
+  if (outputs_meet(out, {x, dx, tg, mk, ws}) || outputs_meet(out, in))
+    return {FAL_ERR_INVALID_ARG, "an output overlaps another argument"};
   return kFine;
 }
 

@@ -78,3 +78,40 @@ def test_results_stay_until_the_caller_has_read_them(call):
     assert not held & {x.data_ptr() for x in again}
     torch.cuda.synchronize()
     F.close()
+
+
+def test_steps_refuse_overlapping_and_misaligned_arrays():
+    # refused before anything is launched: a loss's rows read what the same
+    # rows' outputs would have overwritten
+    F, tok = context(torch.cuda.current_stream())
+    t = inputs(tok)
+    L, B, T = fal.lib(), *t["mask"].shape
+    p = {k: v.data_ptr() for k, v in t.items()}
+    out, seq = torch.empty(B, T, device="cuda"), torch.empty(B, device="cuda")
+    o, s, st = out.data_ptr(), seq.data_ptr(), torch.empty(4, device="cuda")
+    P, G = F.params.data_ptr(), F.grads.data_ptr()
+    pol, pref = fal.fal_policy_t(0.2, 0.2, 0.1, 0), fal.fal_preference_t(0.1, 0.0, 0, 0)
+    torch.cuda.synchronize()
+
+    def policy(old=p["old"], ref=p["ref"], adv=p["adv"], stats=st.data_ptr(), logp=o, mask=p["mask"], tokens=p["tokens"]):
+        return L.fal_policy_step(F.ctx, P, fal.byref(pol), tokens, mask, 1.0, old, ref, adv, stats, logp, G)
+
+    def preference(ref=p["seq"], loss=st.data_ptr(), seq=s, mask=p["mask"]):
+        return L.fal_preference_step(F.ctx, P, fal.byref(pref), p["tokens"], mask, 1.0, ref, loss, seq, G)
+
+    def scores(logp=o, entropy=None, mask=p["mask"]):
+        return L.fal_model_logprobs(F.ctx, P, p["tokens"], mask, 1.0, logp, entropy)
+
+    for call, kws in ((policy, (dict(logp=p["old"]), dict(logp=p["adv"]), dict(logp=p["ref"]), dict(stats=p["adv"]),
+                                dict(logp=st.data_ptr()), dict(logp=G), dict(stats=P), dict(logp=p["tokens"]),
+                                dict(mask=o), dict(old=p["old"] + 2), dict(logp=o + 1), dict(tokens=p["tokens"] + 1))),
+                      (preference, (dict(seq=p["seq"]), dict(loss=s), dict(loss=p["seq"] + 4), dict(mask=s),
+                                    dict(seq=s + 2), dict(loss=G))),
+                      (scores, (dict(entropy=o), dict(entropy=o + 4), dict(logp=p["tokens"]), dict(mask=o),
+                                dict(logp=o + 2)))):
+        for kw in kws:
+            assert call(**kw) == fal.FAL_ERR_INVALID_ARG, (call.__name__, kw)
+            assert L.fal_last_error(F.ctx)
+        assert call() == fal.FAL_OK
+    torch.cuda.synchronize()
+    F.close()
