@@ -405,6 +405,11 @@ fal_status_t fal_window_attention_fwd(const fal_window_attention_t* shape, const
  *          key/value head receives the sum over its query heads.
  *   workspace  device, 256-byte aligned, at least
  *          fal_window_attention_workspace_bytes
+ * bf16: the probabilities and the gradients of the scores are rounded to bf16
+ * for the products that follow them, and the scores' gradients take
+ * rowsum(d_out * out) from out as stored, but in rows of at most 64 keys (all
+ * rows where window + sinks <= 64, otherwise a sequence's first 64) from
+ * products in fp32.
  * Deterministic: every sum has a fixed order.  Errors as the forward, and
  * FAL_ERR_WORKSPACE. */
 fal_status_t fal_window_attention_bwd(const fal_window_attention_t* shape, const void* qkv, const int32_t* lens,

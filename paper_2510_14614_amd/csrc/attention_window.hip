@@ -169,7 +169,7 @@ struct Stats {
   }
 };
 
-constexpr int kFewKeys = 64;
+constexpr int kFewKeys = AT;
 
 // The window's mask over a 32x32 score tile whose rows are the keys from kb on
 // and whose lane has query tq, one of q0 .. q0 + 31: -inf for keys after the
@@ -527,8 +527,11 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
 // and one of few does not (bf16 gradients of a window of 2 keys: 2.7e-3 off
 // against 2.2e-3 with D exact, of 20: 2.42e-3 against 2.36e-3; 1.65e-3 is the
 // rounding of the gradients alone).  So bf16 rows of at most kFewKeys keys sum
-// D = rowsum(P * dP) in a walk of their own over their few tiles.  126 us at the
-// 8192 tokens above (780 TFLOP/s), 25 at the 8 x 1024.
+// D = rowsum(P * dP) in a walk of their own: every row of a call whose window and
+// sinks hold no more, over its few tiles, and under a longer window the first
+// kFewKeys rows of a sequence, over the first tile (dQ of the first 8 rows
+// 2.64e-3 off before, 2.18e-3 with it; no time beyond the noise of 1%).  126 us
+// at the 8192 tokens above (780 TFLOP/s), 25 at the 8 x 1024.
 template <typename S, int HD, bool SPLIT>
 __global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_dq(WindowAttn a, const S* qkv, const S* O,
                                                                        const S* dO, const float* lse, float* Dvec,
@@ -578,9 +581,10 @@ __global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_dq(WindowAtt
       mask_keys(a, kb, q0, tq, n, g, s);
       return true;
     };
-    if (sizeof(S) == 2 && a.window + a.sinks <= kFewKeys) {
-      D = 0.f;
-      for (int i = 0; i < kt.count; ++i) {
+    const bool few = a.window + a.sinks <= kFewKeys;
+    if (sizeof(S) == 2 && (few || qb == 0)) {
+      float sum_pdp = 0.f;
+      for (int i = 0; i < (few ? kt.count : 1); ++i) {
         rk.load(kt.at(i), n, tid);
         rv.load(kt.at(i), n, tid);
         __syncthreads();
@@ -589,19 +593,20 @@ __global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_dq(WindowAtt
         __syncthreads();
         for (int u = 0; u < (SPLIT ? 1 : AT / 32); ++u) {
           f32x16v s, dp;
-          if (!score(kt.at(i), SPLIT ? wave >> 1 : u, s, dp)) continue;
+          if ((!few && q0 >= kFewKeys) || !score(kt.at(i), SPLIT ? wave >> 1 : u, s, dp)) continue;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) D = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], sl2, -L2)), dp[r], D);
+          for (int r = 0; r < 16; ++r) sum_pdp = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], sl2, -L2)), dp[r], sum_pdp);
         }
       }
-      D += __shfl_xor(D, 32, 64);
+      sum_pdp += __shfl_xor(sum_pdp, 32, 64);
       if (SPLIT) {  // both wavefronts of a pair take the sum of their halves
         float* sum = reinterpret_cast<float*>(lds);
         __syncthreads();
-        sum[64 * wave + lane] = D;
+        sum[64 * wave + lane] = sum_pdp;
         __syncthreads();
-        D = sum[64 * (wave & 1) + lane] + sum[64 * (2 + (wave & 1)) + lane];
+        sum_pdp = sum[64 * (wave & 1) + lane] + sum[64 * (2 + (wave & 1)) + lane];
       }
+      if (few || q0 < kFewKeys) D = sum_pdp;
     }
     if (g == 0 && tq < n && (!SPLIT || wave < 2)) Dvec[stat] = D;
 #pragma unroll
