@@ -8,6 +8,7 @@ import torch
 
 from paper_2510_14614_amd import fal
 
+import test_gpu_logit_losses as losses
 from gpu_helpers import log
 
 pytestmark = pytest.mark.gpu
@@ -178,3 +179,12 @@ def test_nan_scores_are_not_lost(V, masked, dtype):
     assert torch.equal(got.dlogits[other], good.dlogits[other])
     got = fal.preference_loss(x, y, torch.zeros(2, device="cuda"))
     assert torch.isnan(got.loss).all() and torch.isnan(got.seq_logp[0]) and torch.isfinite(got.seq_logp[1])
+
+
+@pytest.mark.parametrize("seq", [False, True], ids=["token-mean", "sequence-mean"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V", [500, 1500, 2500, 3999, 7001, 12001, 20011, 32000, 52001])
+def test_policy_rows_of_every_held_width(V, dtype, seq):
+    # with the widths of the losses' own test, each number of threads a row and
+    # of chunks that they hold
+    losses.test_policy_loss(V, dtype, seq)

@@ -3,13 +3,16 @@ window, divided head groups with whole key blocks, scores that keep raising a
 row's maximum, and block calls of a context."""
 import math
 
-import numpy as np
 import pytest
 import torch
 
-from paper_2510_14614_amd import fal
+from oracle import fal_oracle
+from paper_2510_14614_amd import fal, synth
 
-from gpu_helpers import log
+import test_gpu_block_abi as blocks_abi
+import test_gpu_tuning_steps as steps
+import test_gpu_window_attention as attention
+from gpu_helpers import TOL, log, rel_err
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +55,90 @@ def test_first_rows_of_a_long_window(B, T, H, hd):
     worst = float(((got - want).abs() / (bound + 1e-30)).max())
     log(f"{B} x {T} x {H} x {hd}: worst error / bound {worst:.3f}")
     assert worst <= 1.0
+
+
+def plan(B, T, H, kv, hd, window, dtype):
+    """Parts that a group's query heads are divided into, from the workspace
+    (without sinks: rowsum(dO * O), then the parts' fp32 sums of dK and dV)."""
+    code = 1 if dtype == BF16 else 0
+    n = fal._window_workspace(B, T, H, kv, hd, code, window, 0, (H + 2 * kv) * hd, H * hd)
+    stat = (B * H * T * 4 + 255) // 256 * 256
+    return (n - stat) // (B * T * 2 * kv * hd * 4)
+
+
+@pytest.mark.parametrize("dtype,shape,parts", [
+    # enough parts of long sequences that whole blocks of 128 keys fill the chip,
+    # with and without sinks; in fp32 at head_dim 128 one round of them
+    (BF16, (1, 4096, 16, 1, 64, 300, 5, (4001,)), 16),
+    (F32, (1, 4096, 16, 1, 64, 300, 0, None), 16),
+    (BF16, (1, 4096, 24, 1, 32, 1000, 37, (4096,)), 24),
+    (F32, (1, 4096, 24, 1, 16, 90, 2, (3900,)), 24),
+    (BF16, (16, 60, 32, 2, 128, 40, 3, tuple(range(60, 28, -2))), 16),
+    (F32, (1, 2100, 8, 1, 128, 300, 5, (2051,)), 8),
+    # halved blocks
+    (BF16, (1, 4096, 16, 2, 128, 1024, 16, (4096,)), 4),
+    (F32, (2, 600, 16, 2, 64, 100, 3, (600, 430)), 8),
+], ids=lambda v: "x".join(map(str, v[:7])) if isinstance(v, tuple) else str(v).replace("torch.", ""))
+def test_divided_head_groups(dtype, shape, parts):
+    B, T, H, kv, hd, window = shape[:6]
+    assert plan(B, T, H, kv, hd, window, dtype) == parts
+    attention.test_against_the_formula(shape, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("B,H,hd", [(1, 2, 64), (2, 2, 128), (40, 8, 64), (20, 16, 128)])
+@pytest.mark.parametrize("kind", ["rising", "falling", "sinks"])
+def test_scores_that_move_the_maximum(kind, B, H, hd, dtype):
+    # Every 32 keys the scores of all rows move by 7: a row's maximum passes its
+    # reference by 10 log2 units at every half tile, with sums that still count
+    # for 1e-3 of what follows ("falling": never again after the first; "sinks":
+    # by 40 from the window to the sinks and back).
+    T, window, sinks = 300, 140, 3 if kind == "sinks" else 0
+    g = torch.Generator(device="cuda").manual_seed(hd + len(kind))
+    x = torch.randn(B, T, 3, H, hd, device="cuda", generator=g)
+    t = torch.arange(T, device="cuda")
+    level = {"rising": 7.0 * (t // 32), "falling": -7.0 * (t // 32), "sinks": torch.where(t < 3, 40.0, 0.0) +
+             torch.where(t % 64 < 32, 0.0, 7.0)}[kind]
+    x[:, :, 0, :, 0] = math.sqrt(hd)  # the score's part of dim 0 is the key's level
+    x[:, :, 1, :, 0] = level[None, :, None]
+    qkv = x.to(dtype).view(B, T, 3 * H * hd)
+    dout = torch.randn(B, T, H * hd, device="cuda", generator=g).to(dtype)
+    want, bound = attention.reference(qkv, H, H, hd, window, sinks, [T] * B, dout)
+    out, lse = fal.window_attention_fwd(qkv, H, window, sinks)
+    dqkv = fal.window_attention_bwd(qkv, out, dout, lse, H, window, sinks)
+    for name, got, i in (("out", out, 0), ("lse", lse, 1), ("dqkv", dqkv, 2)):
+        attention.check(name, got, want[i], bound[i])
+
+
+@pytest.mark.parametrize("dtype", [0, 1], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("arch,block1_mode", blocks_abi.CASES)
+def test_windowed_block_calls(arch, block1_mode, dtype, monkeypatch):
+    # fal_block_fwd / fal_block_bwd under a window against the oracle, and
+    # bitwise against the stack step under the same window
+    window, sinks = 37, 2
+    init = fal.Fal.__init__
+
+    def windowed(self, *args, **kw):
+        init(self, *args, **kw)
+        self.set_attention_window(window, sinks)
+
+    monkeypatch.setattr(fal.Fal, "__init__", windowed)
+    monkeypatch.setattr(fal_oracle, "attention", steps.masked(window, sinks))
+    blocks_abi.test_block_calls_match_oracle_and_stack_step(arch, block1_mode, dtype)
+
+
+def test_windowed_blocks_differ_from_the_full_mask():
+    # (the window above reaches the block calls)
+    cfg = blocks_abi._cfg(blocks_abi.ARCH_GPT, 0, 0)
+    _, params = synth.make_params(cfg, seed=70)
+    x1, gout = synth.make_stack_inputs(cfg, seed=71)
+    F = fal.Fal(cfg)
+    F.load_params({}, params)
+    full = blocks_abi._run_blocks(F, cfg, x1, gout)
+    F.set_attention_window(37, 2)
+    got = blocks_abi._run_blocks(F, cfg, x1, gout)
+    F.set_attention_window(cfg.seq_len)
+    all_of_it = blocks_abi._run_blocks(F, cfg, x1, gout)
+    F.close()
+    for a, b, c in zip(full, got, all_of_it):
+        assert rel_err(b, a) > 1e-3 and rel_err(c, a) <= TOL[0]
