@@ -247,8 +247,16 @@ __device__ __forceinline__ void grad_chunk(const uint4& u, int col0, int V, int 
     // by more than all else here (an element's own error does not add up: the
     // factor's first part is enough)
     v[e] = -scale * __builtin_amdgcn_exp2f(fmaf(Chunk<S>::at(u, e) - top, k, -log2sum));
-    if (col0 + e == tgt) v[e] += scale;
-    if (col0 + e >= V) v[e] = 0.f;
+  }
+  if ((unsigned)(tgt - col0) < (unsigned)E) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (col0 + e == tgt) v[e] += scale;
+  }
+  if (col0 + E > V) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (col0 + e >= V) v[e] = 0.f;
   }
   if (out.shift == c * E - col0) {
     out.store(c, v);
