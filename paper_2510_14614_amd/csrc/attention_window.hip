@@ -395,9 +395,9 @@ __device__ __forceinline__ void join_acc(float* lds, int wave, int lane, f32x16v
 // The last blocks first: the first ones, whose windows the sequence's start
 // cuts short, then fill the launch's end (6 padded sequences of 1501 tokens, 16
 // heads of 64, window 500: 29.4 -> 26.1 us; 4 of 2048 under the full mask, 68.8
-// -> 55.0, and dQ 80.7 -> 66.5).  At 8192 tokens, 16 heads of 128, window 1024:
-// 104 us, 630 TFLOP/s of the visible pairs; at 8 sequences of 1024, 12 heads of
-// 64, window 256: 19 us, where the exponentials and the other vector work of a
+// -> 55.0, and dQ 80.7 -> 66.5).  At 8192 tokens, 16 heads of 128, window 1024,
+// after 300 ms of such calls: 98 us, 665 TFLOP/s of the visible pairs; at 8
+// sequences of 1024, 12 heads of 64, window 256: 18 us, where the exponentials and the other vector work of a
 // score (about 650 cycles a 32x32 tile against 256 of MFMA) and the single round
 // of workgroups bound it.
 template <typename S, int HD, bool SPLIT>
@@ -530,8 +530,8 @@ __global__ __launch_bounds__(256, 2) void window_attn_fwd(WindowAttn a, const S*
 // D = rowsum(P * dP) in a walk of their own: every row of a call whose window and
 // sinks hold no more, over its few tiles, and under a longer window the first
 // kFewKeys rows of a sequence, over the first tile (dQ of the first 8 rows
-// 2.64e-3 off before, 2.18e-3 with it; no time beyond the noise of 1%).  126 us
-// at the 8192 tokens above (780 TFLOP/s), 25 at the 8 x 1024.
+// 2.64e-3 off before, 2.18e-3 with it; no time beyond the noise of 1%).  118 us
+// at the 8192 tokens above (826 TFLOP/s), 23 at the 8 x 1024.
 template <typename S, int HD, bool SPLIT>
 __global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_dq(WindowAttn a, const S* qkv, const S* O,
                                                                        const S* dO, const float* lse, float* Dvec,
@@ -653,7 +653,7 @@ __global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_dq(WindowAtt
 // sink keys; of its wavefronts two sum dV and two dK, over one half of each
 // tile (half the sums a wavefront, so three share a SIMD).  The halves are
 // joined in LDS and written as fp32 partials [b][kv head][chunk][dK, dV]
-// [sinks][HD].  18 us at the 8192 tokens above (16 sinks), 7 at the 8 x 1024 (4):
+// [sinks][HD].  19 us at the 8192 tokens above (16 sinks), 7 at the 8 x 1024 (4):
 // reading the far queries' Q and dO, and the latency of a short chunk.
 template <typename S, int HD>
 __global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_sinks(WindowAttn a, const S* qkv, const S* dO,
@@ -726,7 +726,7 @@ __global__ __launch_bounds__(256, (kWaves<S, HD>)) void window_attn_sinks(Window
 // ------------------------------------------------------- backward: dK, dV --
 // A group's query heads may be divided over `parts` workgroups, which then
 // write fp32 sums [part][b][t][dK, dV][kv head][HD] for window_attn_kv_sum.
-// 171 us at the 8192 tokens above (765 TFLOP/s), 30 at the 8 x 1024.
+// 156 us at the 8192 tokens above (838 TFLOP/s), 28 at the 8 x 1024.
 template <typename S, int HD, bool SPLIT>
 __global__ __launch_bounds__(256, (kWavesDkdv<S, HD>)) void window_attn_dkdv(WindowAttn a, const S* qkv, const S* dO,
                                                                              const float* lse, const float* Dvec,

@@ -19,10 +19,11 @@
 // two parts and the log-probability is taken in natural units: log2(e) and ln 2
 // as fp32 constants would shift every row by 1e-8 of it.
 //
-// 4551 of 8192 rows of 50257 bf16 counted: log-probabilities 76 us (6.0 TB/s of
-// those rows), the policy gradient 262 (4.9 TB/s of those rows read and all of
-// the gradient written, the rate of a copy); of 5002 counted, the preference
-// loss's statistics 92 (5.5 TB/s) and its gradient 204 (6.5).
+// 4551 of 8192 rows of 50257 bf16 counted, after 300 ms of such calls:
+// log-probabilities with entropy 80 us (5.7 TB/s of those rows), the policy
+// gradient 255 (5.0 TB/s of those rows read and all of the gradient written, the
+// rate of a copy); of 5002 counted, the preference loss's statistics 94 (5.3
+// TB/s) and its gradient 201 (6.6).
 #include <math.h>
 
 #include <algorithm>
@@ -615,8 +616,8 @@ hipError_t launch(const LogitRows& r, const RowOut& o, hipStream_t s) {
 
 // Rows that are only scored are streamed: held or not, they are read once.
 // 256 threads keep enough loads in flight and leave a compute unit several
-// rows (8192 rows of 50257 bf16, half of them counted, with entropy: 78 us
-// against 85 with 512 threads and 127 with 1024).  Of rows that leave the chip
+// rows (8192 rows of 50257 bf16, half of them counted, with entropy: 80 us
+// against 88 with 512 threads and 128 with 1024).  Of rows that leave the chip
 // places, long ones are shortened by more threads, whose exchange then costs
 // less than it gives (us with 256, 512 and 1024 threads: 270 rows of 2003
 // chunks 5.1, 5.7, 8.9; 512 of 3750 8.3, 8.6, 11.4; 128 of 6283 9.2, 7.3, 8.6;
@@ -633,11 +634,11 @@ hipError_t scored_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
 // Rows with a gradient are held by as few threads as can (up to 26 chunks
 // each, 13 in a workgroup of 1024, whose registers are half as many): several
 // rows then share a compute unit and one's exchange and stores pass under
-// another's loads (rows of 50257 bf16 as above: 273 us with 256 x 26, 314 with
-// 512 x 13, 338 with 1024 x 7; 50257 fp32: 238 with 1024 x 13, 247 with
+// another's loads (rows of 50257 bf16 as above: 264 us with 256 x 26, 307 with
+// 512 x 13, 295 with 1024 x 7; 50257 fp32: 231 with 1024 x 13, 242 with
 // 512 x 26).  The 1024 threads hold 13312 chunks and read the rest of a longer
-// row twice (1028 rows of 128001 fp32, half of them counted: 171 us against
-// 204 with none held and 186 with 24 chunks a thread).
+// row twice (1028 rows of 128001 fp32, half of them counted: 170 us against
+// 201 with none held and 185 with 24 chunks a thread).
 template <typename S>
 hipError_t policy_rows(const LogitRows& r, const RowOut& o, hipStream_t s) {
   constexpr int E = Chunk<S>::E;
