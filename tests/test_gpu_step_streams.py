@@ -9,7 +9,7 @@ from paper_2510_14614_amd import fal, get_config, synth
 
 pytestmark = pytest.mark.gpu
 
-BUSY = 20_000_000  # cycles of a kernel that only waits: at least several ms
+BUSY = 100_000_000  # cycles of a kernel that only waits: tens of ms
 
 
 def context(side):
