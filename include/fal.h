@@ -519,6 +519,62 @@ fal_status_t fal_preference_loss(const fal_logit_rows_t* rows, const fal_prefere
                                  const int32_t* targets, const uint8_t* mask, const float* ref_logp, float* loss,
                                  float* seq_logp, void* dlogits, void* workspace, size_t ws_bytes, void* stream);
 
+/* Norms of queries and keys head by head, and the rotation of their positions,
+ * over packed rows [Q | K | V] of batch * seq_len tokens.  A head x with weight
+ * w becomes n = x / sqrt(mean(x^2) + eps) * w; then the pairs of its first
+ * rotary_dim elements turn by the angle position * theta^(-2j / rotary_dim),
+ * j the pair's number: (a, b) -> (a cos - b sin, b cos + a sin).  V heads are
+ * copied. */
+typedef struct {
+  int32_t batch;       /* B >= 1                                            */
+  int32_t seq_len;     /* T >= 1; B * T below 2^31                          */
+  int32_t n_head;      /* H, 1 .. 65535                                     */
+  int32_t n_kv_head;   /* Hkv: 0 (as many as n_head) or a divisor of n_head */
+  int32_t head_dim;    /* 16, 32, 64 or 128                                 */
+  int32_t dtype;       /* fal_dtype_t of every tensor but the weights'
+                          gradients                                         */
+  int32_t rotary_dim;  /* 0 (norms only) .. head_dim, a multiple of 8       */
+  int32_t interleaved; /* 0: pairs (j, j + rotary_dim / 2); 1: (2j, 2j + 1) */
+  float theta;         /* > 1, finite                                       */
+  float eps;           /* > 0, finite                                       */
+  int64_t ld_qkv;      /* elements between rows of qkv ...                  */
+  int64_t ld_out;      /* ... and of out and d_out; both multiples of 16
+                          bytes and at least (H + 2 Hkv) * head_dim         */
+} fal_qk_norm_rope_t;
+
+/* Bytes of workspace the backward needs (host only; the forward needs none). */
+fal_status_t fal_qk_norm_rope_workspace_bytes(const fal_qk_norm_rope_t* shape, size_t* bytes);
+
+/*   qkv        device dtype, rows 16-byte aligned
+ *   q_weight, k_weight  device dtype [head_dim], each may be NULL: ones
+ *   positions  device int32 [B, T], or NULL: token t of a sequence is at t
+ *   lens       device int32 [B], or NULL: tokens a sequence holds, clamped to
+ *              [0, T].  Tokens past them are not read; their rows of out are
+ *              zeros.
+ *   out        device dtype; may be qkv itself with the same row stride (the
+ *              backward then has no input to go by)
+ * Angles are products in fp64, everything else fp32, rounded once.
+ * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes, misalignment or
+ * an output that overlaps an input; FAL_ERR_UNSUPPORTED for another head_dim
+ * or a rotary_dim that is no multiple of 8; FAL_ERR_HIP when a launch fails. */
+fal_status_t fal_qk_norm_rope_fwd(const fal_qk_norm_rope_t* shape, const void* qkv, const void* q_weight,
+                                  const void* k_weight, const int32_t* positions, const int32_t* lens, void* out,
+                                  void* stream);
+
+/* Gradient of fal_qk_norm_rope_fwd; qkv .. lens as given to it (qkv as it was
+ * before the call).
+ *   d_out       device dtype, gradient of out, rows at ld_out
+ *   d_qkv       device dtype, rows at ld_d_qkv, all written (zeros past a
+ *               sequence's tokens); may be d_out itself with the same stride
+ *   d_q_weight, d_k_weight  device fp32 [head_dim], each may be NULL: sums
+ *               over all tokens and heads, in a fixed order
+ *   workspace   device, 256-byte aligned, fal_qk_norm_rope_workspace_bytes
+ * Errors as the forward, and FAL_ERR_WORKSPACE. */
+fal_status_t fal_qk_norm_rope_bwd(const fal_qk_norm_rope_t* shape, const void* qkv, const void* q_weight,
+                                  const void* k_weight, const int32_t* positions, const int32_t* lens,
+                                  const void* d_out, void* d_qkv, int64_t ld_d_qkv, float* d_q_weight,
+                                  float* d_k_weight, void* workspace, size_t ws_bytes, void* stream);
+
 /* fal_model_forward with the per-token scores in place of the loss: logp (and
  * entropy, or NULL) of tokens[:, 1:] as fal_token_logprobs defines them.
  *   mask  device uint8 [B, T] or NULL, over the T predicted tokens
@@ -565,8 +621,8 @@ fal_status_t fal_profile_read(fal_ctx_t* ctx, int32_t cls, int64_t* launches, do
 
 const char* fal_status_string(fal_status_t status);
 /* "" if none.  ctx NULL: the message of the last failed call on the calling
- * thread of those that take no context (fal_adamw_step_noalloc and the
- * window attention, log-probability and loss calls). */
+ * thread of those that take no context (fal_adamw_step_noalloc and every call
+ * that takes a struct of sizes in a context's place). */
 const char* fal_last_error(const fal_ctx_t* ctx);
 
 #ifdef __cplusplus

@@ -2,6 +2,8 @@
 // returns NULL or the message of the first argument that does not hold.
 #pragma once
 
+#include <hip/hip_runtime.h>
+
 #include <cmath>
 #include <cstdint>
 #include <initializer_list>
@@ -13,6 +15,40 @@ namespace fal {
 
 // Message of the calling thread's last failed call without a context.
 std::string& noctx_error();
+
+constexpr uintptr_t kWorkspaceAlign = 256;
+constexpr int64_t kMaxStride = (int64_t)1 << 40;  // elements between rows
+constexpr int64_t kMaxExtent = (int64_t)1 << 47;  // elements from a matrix's first row to its last: the address space
+
+inline fal_status_t fail(fal_status_t st, const char* why) {
+  noctx_error() = why;
+  return st;
+}
+
+inline fal_status_t launched(hipError_t e, const char* call) {
+  if (e == hipSuccess) return FAL_OK;
+  noctx_error() = std::string(call) + ": " + hipGetErrorString(e);
+  return FAL_ERR_HIP;
+}
+
+// No C++ exception (the message string may fail to allocate) leaves a C entry.
+template <typename F>
+fal_status_t guarded(F f) {
+  try {
+    noctx_error().clear();
+    return f();
+  } catch (...) {
+    return FAL_ERR_HIP;
+  }
+}
+
+struct Refusal {
+  fal_status_t st;
+  const char* why;
+};
+const Refusal kFine = {FAL_OK, nullptr};
+
+inline int64_t element_bytes(int32_t dtype) { return dtype == FAL_BF16 ? 2 : 4; }
 
 inline bool overlaps(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
@@ -26,6 +62,10 @@ struct Extent {
   const void* p;
   int64_t bytes;
 };
+// A row matrix's bytes from its first element to its last.
+inline Extent rows_of(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t es) {
+  return {p, ((rows - 1) * ld + width) * es};
+}
 inline bool meets(const Extent& out, std::initializer_list<Extent> others) {
   for (const Extent& o : others)
     if (o.p && overlaps(out.p, out.bytes, o.p, o.bytes)) return true;

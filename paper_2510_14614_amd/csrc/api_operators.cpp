@@ -14,38 +14,6 @@ using namespace fal;
 
 namespace {
 
-constexpr uintptr_t kWorkspaceAlign = 256;
-constexpr int64_t kMaxStride = (int64_t)1 << 40;  // elements between rows
-constexpr int64_t kMaxExtent = (int64_t)1 << 47;  // elements from a matrix's first row to its last: the address space
-
-fal_status_t fail(fal_status_t st, const char* why) {
-  noctx_error() = why;
-  return st;
-}
-
-fal_status_t launched(hipError_t e, const char* call) {
-  if (e == hipSuccess) return FAL_OK;
-  noctx_error() = std::string(call) + ": " + hipGetErrorString(e);
-  return FAL_ERR_HIP;
-}
-
-// No C++ exception (the message string may fail to allocate) leaves a C entry.
-template <typename F>
-fal_status_t guarded(F f) {
-  try {
-    noctx_error().clear();
-    return f();
-  } catch (...) {
-    return FAL_ERR_HIP;
-  }
-}
-
-struct Refusal {
-  fal_status_t st;
-  const char* why;
-};
-const Refusal kFine = {FAL_OK, nullptr};
-
 // ------------------------------------------------------- window attention --
 // Whether a shape's rows at a stride of ld elements stay within kMaxExtent.
 bool fits(const fal_window_attention_t* p, int64_t ld) {
@@ -88,11 +56,6 @@ WindowAttn window_args(const fal_window_attention_t* p, const int32_t* lens) {
   return a;
 }
 
-// A row matrix's bytes from its first element to its last.
-Extent rows_of(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t es) {
-  return {p, ((rows - 1) * ld + width) * es};
-}
-
 int64_t window_scratch_bytes(int32_t dtype, const WindowAttn& a, int64_t* part_off) {
   int64_t n = (int64_t)a.B * a.H * a.T * 4;
   n = (n + kWorkspaceAlign - 1) / kWorkspaceAlign * kWorkspaceAlign;
@@ -129,8 +92,6 @@ LogitRows row_args(const fal_logit_rows_t* r, const void* logits, const int32_t*
   a.set_temperature(r->temperature);
   return a;
 }
-
-int64_t element_bytes(int32_t dtype) { return dtype == FAL_BF16 ? 2 : 4; }
 
 // The checks that both losses share: dlogits may be the logits, and meets
 // nothing else; the small outputs meet nothing.

@@ -237,6 +237,30 @@ hipError_t window_attention_bwd(DType dt, const WindowAttn& a, const void* qkv, 
                                 const float* lse, float* Dvec, float* part, void* dqkv, hipStream_t s);
 int64_t window_attention_scratch(DType dt, const WindowAttn& a);
 
+// ------------------------------------ head norms with rotated positions ----
+// Packed [Q | K | V] rows of `tokens` = B * T tokens at strides ldx (rows), ldy
+// (out and its gradient) and lddx (the rows' gradient): Q and K heads are
+// divided by sqrt(mean square + eps), multiplied by wq or wk (dtype [hd] or NULL:
+// ones) and their first `rotary` elements (a multiple of 8) turned by
+// position * theta^(-2j/rotary), pairs (j, j + rotary/2) or, interleaved,
+// (2j, 2j+1); V heads are copied.  positions: int32 [B, T] or NULL (the place
+// in the sequence).  Tokens past lens[b] are not read, their rows become zeros.
+// out may be x and dx dout, with one stride each.
+struct HeadNorm {
+  int64_t tokens, ldx, ldy, lddx;
+  int T, H, Hkv, hd, rotary, interleaved;
+  float eps;
+  double log2_theta_step;  // log2(theta) * 2 / rotary
+  const void *wq, *wk;
+  const int32_t *positions, *lens;
+};
+hipError_t head_norm_rope_fwd(DType dt, const HeadNorm& a, const void* x, void* out, hipStream_t s);
+// dwq, dwk: fp32 [hd], each may be NULL; part: head_norm_rope_scratch floats,
+// used where one of them is not.
+hipError_t head_norm_rope_bwd(DType dt, const HeadNorm& a, const void* x, const void* dout, void* dx, float* dwq,
+                              float* dwk, float* part, hipStream_t s);
+int64_t head_norm_rope_scratch(const HeadNorm& a);
+
 // ------------------------------------------------ embedding / loss / misc ----
 // X[m, :] = wte[tok[b, t]] + wpe[t]  (fp32 out), tokens [B, T+1].
 hipError_t embed_fwd(DType dt, const int32_t* tokens, int B, int T, int V, int d, const void* wte,

@@ -34,6 +34,7 @@ ABI_FUNCTIONS = (
     "fal_window_attention_workspace_bytes", "fal_window_attention_fwd", "fal_window_attention_bwd",
     "fal_set_attention_window", "fal_token_logprobs", "fal_logit_loss_workspace_bytes", "fal_policy_loss",
     "fal_preference_loss", "fal_model_logprobs", "fal_policy_step", "fal_preference_step",
+    "fal_qk_norm_rope_workspace_bytes", "fal_qk_norm_rope_fwd", "fal_qk_norm_rope_bwd",
 )
 PROF_GEMM, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_NORM, PROF_CE, PROF_EMBED, PROF_BIAS, PROF_OPTIM = range(8)
 PROF_NAMES = {PROF_GEMM: "gemm", PROF_ATTN_FWD: "attn_fwd", PROF_ATTN_BWD: "attn_bwd", PROF_NORM: "norm",
@@ -86,6 +87,12 @@ class fal_preference_t(ctypes.Structure):
     _fields_ = [("beta", c_float), ("label_smoothing", c_float), ("ipo", c_int32), ("length_mean", c_int32)]
 
 
+class fal_qk_norm_rope_t(ctypes.Structure):
+    _fields_ = [("batch", c_int32), ("seq_len", c_int32), ("n_head", c_int32), ("n_kv_head", c_int32),
+                ("head_dim", c_int32), ("dtype", c_int32), ("rotary_dim", c_int32), ("interleaved", c_int32),
+                ("theta", c_float), ("eps", c_float), ("ld_qkv", c_int64), ("ld_out", c_int64)]
+
+
 class PolicyLoss(NamedTuple):
     stats: object    # fp32 [4]: loss, its policy part, KL mean, share of rows whose ratio the clip holds
     logp: object     # fp32 [B, T]
@@ -96,6 +103,12 @@ class PreferenceLoss(NamedTuple):
     loss: object      # fp32 [1]
     seq_logp: object  # fp32 [B]
     dlogits: object
+
+
+class QkNormRopeGrads(NamedTuple):
+    dqkv: object       # gradient of the rows, in their dtype
+    dq_weight: object  # fp32 [head_dim], None without a weight
+    dk_weight: object
 
 
 class FalError(RuntimeError):
@@ -149,6 +162,10 @@ def lib():
                                       [c_void_p] * 6)
         L.fal_preference_step.argtypes = ([c_void_p] * 2 + [POINTER(fal_preference_t)] + [c_void_p] * 2 + [c_float] +
                                           [c_void_p] * 4)
+        normp = POINTER(fal_qk_norm_rope_t)
+        L.fal_qk_norm_rope_workspace_bytes.argtypes = [normp, POINTER(c_size_t)]
+        L.fal_qk_norm_rope_fwd.argtypes = [normp] + [c_void_p] * 7
+        L.fal_qk_norm_rope_bwd.argtypes = ([normp] + [c_void_p] * 7 + [c_int64] + [c_void_p] * 3 + [c_size_t, c_void_p])
         L.fal_status_string.argtypes = [c_int32]
         L.fal_status_string.restype = c_char_p
         L.fal_last_error.argtypes = [c_void_p]
@@ -525,6 +542,87 @@ def preference_loss(logits, targets, ref_logp, mask=None, vocab=None, dlogits=No
                                                ref_logp.data_ptr(), loss.data_ptr(), seq_logp.data_ptr(),
                                                dlogits.data_ptr(), ws.data_ptr(), n, stream))
     return PreferenceLoss(loss, seq_logp, dlogits)
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace(*shape):
+    n = c_size_t()
+    _check_noctx(lib().fal_qk_norm_rope_workspace_bytes(byref(fal_qk_norm_rope_t(*shape)), byref(n)))
+    return n.value
+
+
+def _norm_shape(qkv, n_head, n_kv_head, q_weight, k_weight, positions, lens, rotary_dim, theta, eps, interleaved):
+    """The call's shape, with the rows' own stride for out."""
+    import torch
+    if qkv.dim() != 3:
+        _refuse("qkv must be [B, T, (n_head + 2 n_kv_head) * head_dim]")
+    B, T, width = qkv.shape
+    heads = n_head + 2 * (n_kv_head or n_head)
+    if n_head < 1 or n_kv_head < 0 or width % heads:
+        _refuse("qkv's last dimension must be (n_head + 2 n_kv_head) * head_dim")
+    hd = width // heads
+    code = _dtype_code(qkv, "qkv")
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _dense(w, name, (hd,), (qkv.dtype,), qkv.device)
+    if positions is not None:
+        _dense(positions, "positions", (B, T), (torch.int32,), qkv.device)
+    if lens is not None:
+        _dense(lens, "lens", (B,), (torch.int32,), qkv.device)
+    ld = _row_stride(qkv, "qkv")
+    return (_clamp32(B), _clamp32(T), n_head, n_kv_head, _clamp32(hd), code,
+            hd if rotary_dim is None else _clamp32(rotary_dim), int(interleaved), theta, eps, ld, ld)
+
+
+def qk_norm_rope_fwd(qkv, n_head, q_weight=None, k_weight=None, positions=None, n_kv_head=0, lens=None, out=None, *,
+                     rotary_dim=None, theta=10000.0, eps=1e-6, interleaved=False):
+    """Norms of queries and keys head by head, then the rotation of their
+    positions (fal_qk_norm_rope_fwd): each head is divided by its root mean
+    square, multiplied by q_weight or k_weight ([head_dim] in qkv's dtype, or
+    None: ones), and the pairs of its first rotary_dim elements (None: all) turn
+    by position * theta^(-2j / rotary_dim).
+
+    qkv: [B, T, (n_head + 2 n_kv_head) * head_dim], bfloat16 or float32, rows
+    [Q | K | V] at any equal spacing; positions: int32 [B, T] or None (the place
+    in the sequence); lens: int32 [B] or None, tokens past them become rows of
+    zeros.  Returns out, rows at any equal spacing if given; out may be qkv."""
+    import torch
+    shape = _norm_shape(qkv, n_head, n_kv_head, q_weight, k_weight, positions, lens, rotary_dim, theta, eps,
+                        interleaved)
+    a = fal_qk_norm_rope_t(*shape)
+    with _call(qkv.device) as stream:
+        if out is None:
+            out = torch.empty(qkv.shape, dtype=qkv.dtype, device=qkv.device)
+        a.ld_out = _window_rows(out, "out", qkv, qkv.shape)
+        _check_noctx(lib().fal_qk_norm_rope_fwd(byref(a), qkv.data_ptr(), _ptr(q_weight), _ptr(k_weight),
+                                                _ptr(positions), _ptr(lens), out.data_ptr(), stream))
+    return out
+
+
+def qk_norm_rope_bwd(qkv, dout, n_head, q_weight=None, k_weight=None, positions=None, n_kv_head=0, lens=None,
+                     dqkv=None, *, rotary_dim=None, theta=10000.0, eps=1e-6, interleaved=False):
+    """Gradients of qk_norm_rope_fwd from its input and the gradient of its
+    output: of the rows, and of each weight that is given (float32, summed over
+    tokens and heads).  dqkv, if given, has rows at any equal spacing and may be
+    dout."""
+    import torch
+    shape = _norm_shape(qkv, n_head, n_kv_head, q_weight, k_weight, positions, lens, rotary_dim, theta, eps,
+                        interleaved)
+    device = qkv.device
+    a = fal_qk_norm_rope_t(*shape)
+    a.ld_out = _window_rows(dout, "dout", qkv, qkv.shape)
+    with _call(device) as stream:
+        if dqkv is None:
+            dqkv = torch.empty(qkv.shape, dtype=qkv.dtype, device=device)
+        ld = _window_rows(dqkv, "dqkv", qkv, qkv.shape)
+        dq, dk = (None if w is None else torch.empty(w.shape, dtype=torch.float32, device=device)
+                  for w in (q_weight, k_weight))
+        n = _norm_workspace(*shape)
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
+        _check_noctx(lib().fal_qk_norm_rope_bwd(byref(a), qkv.data_ptr(), _ptr(q_weight), _ptr(k_weight),
+                                                _ptr(positions), _ptr(lens), dout.data_ptr(), dqkv.data_ptr(), ld,
+                                                _ptr(dq), _ptr(dk), ws.data_ptr(), n, stream))
+    return QkNormRopeGrads(dqkv, dq, dk)
 
 
 class Fal:
