@@ -575,6 +575,59 @@ fal_status_t fal_qk_norm_rope_bwd(const fal_qk_norm_rope_t* shape, const void* q
                                   const void* d_out, void* d_qkv, int64_t ld_d_qkv, float* d_q_weight,
                                   float* d_k_weight, void* workspace, size_t ws_bytes, void* stream);
 
+/* The gated feed-forward block over rows of tokens,
+ *   y = (act(x Wg) * (x Wu)) Wd,
+ * weights stored [in, out] as everywhere: Wg and Wu [d, f], Wd [f, d] (Wg and
+ * Wu may be the halves of one [d, 2f] matrix). */
+typedef enum { FAL_GATE_SILU = 0, FAL_GATE_GELU_TANH = 1, FAL_GATE_GELU_ERF = 2 } fal_gate_t;
+typedef struct {
+  int32_t rows;       /* M >= 1                                             */
+  int32_t d_model;    /* d, 1 .. 2^20                                       */
+  int32_t d_ff;       /* f, 1 .. 2^20                                       */
+  int32_t activation; /* fal_gate_t                                         */
+  int32_t dtype;      /* fal_dtype_t of x, y, dx, dy and the weights        */
+  int32_t grad_dtype; /* of the weights' gradients: dtype, or FAL_F32       */
+  int64_t ld_x;       /* elements between rows of x                         */
+  int64_t ld_y;       /* ... of y and dy                                    */
+  int64_t ld_gate, ld_up, ld_down; /* ... of the weights                    */
+  int64_t ld_dx;      /* ... of dx; 0: as x (the forward reads none of these) */
+  int64_t ld_dgate, ld_dup, ld_ddown; /* ... of the weights' gradients; 0: as
+                         the weights                                        */
+} fal_gated_ffn_t;
+
+/* Bytes of workspace the forward and the backward need (host only; either
+ * pointer may be NULL). */
+fal_status_t fal_gated_ffn_workspace_bytes(const fal_gated_ffn_t* shape, size_t* forward, size_t* backward);
+
+/*   x, w_gate, w_up, w_down, y  device dtype
+ *   saved      device fp32 [M, 2f]: receives x Wg | x Wu for the backward, or
+ *              NULL where none follows
+ *   workspace  device, 256-byte aligned
+ * Products of bf16 operands are summed in fp32; act(x Wg) * (x Wu) is rounded
+ * to bf16 once, as the operand of the last product, and y once.
+ * bf16 takes matrices of 16-byte aligned rows: d, f and the strides multiples
+ * of 8, each operand below 2 GiB.  fp32 takes any size.
+ * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes, misalignment or
+ * an output that overlaps another argument; FAL_ERR_UNSUPPORTED for bf16 d or
+ * f that is no multiple of 8 and operands past those limits;
+ * FAL_ERR_WORKSPACE; FAL_ERR_HIP when a launch fails. */
+fal_status_t fal_gated_ffn_fwd(const fal_gated_ffn_t* shape, const void* x, const void* w_gate, const void* w_up,
+                               const void* w_down, void* y, float* saved, void* workspace, size_t ws_bytes,
+                               void* stream);
+
+/* Gradients of fal_gated_ffn_fwd.
+ *   saved  as the forward wrote it
+ *   dy     device dtype [M, d] at ld_y
+ *   dx     device dtype [M, d], or NULL
+ *   dw_gate, dw_up, dw_down  device grad_dtype, or all three NULL (dw_gate and
+ *          dw_up may be the halves of one matrix)
+ * The gradients of x Wg and x Wu, and act(x Wg) * (x Wu), are rounded to bf16
+ * as operands of the products that follow.  Deterministic.  Errors as the
+ * forward. */
+fal_status_t fal_gated_ffn_bwd(const fal_gated_ffn_t* shape, const void* x, const void* w_gate, const void* w_up,
+                               const void* w_down, const float* saved, const void* dy, void* dx, void* dw_gate,
+                               void* dw_up, void* dw_down, void* workspace, size_t ws_bytes, void* stream);
+
 /* fal_model_forward with the per-token scores in place of the loss: logp (and
  * entropy, or NULL) of tokens[:, 1:] as fal_token_logprobs defines them.
  *   mask  device uint8 [B, T] or NULL, over the T predicted tokens

@@ -1,6 +1,7 @@
 // Entry points of the C ABI that take no context, continued: the parts of a
-// gated block (head norms with rotated positions) declared in include/fal.h.
-// Argument checks, then one call of the launchers.
+// gated block (head norms with rotated positions, the gated feed-forward
+// block) declared in include/fal.h.  Argument checks, then one call of the
+// launchers.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -65,9 +66,144 @@ HeadNorm norm_args(const fal_qk_norm_rope_t* p, const void* wq, const void* wk, 
   return a;
 }
 
+// ----------------------------------------------------- gated feed-forward --
+Refusal check_gated(const fal_gated_ffn_t* p) {
+  if (!p) return {FAL_ERR_INVALID_ARG, "NULL shape"};
+  if (p->dtype != FAL_F32 && p->dtype != FAL_BF16) return {FAL_ERR_INVALID_ARG, "unknown dtype"};
+  if (p->grad_dtype != p->dtype && p->grad_dtype != FAL_F32)
+    return {FAL_ERR_INVALID_ARG, "grad_dtype must be dtype or FAL_F32"};
+  if (p->activation < FAL_GATE_SILU || p->activation > FAL_GATE_GELU_ERF)
+    return {FAL_ERR_INVALID_ARG, "unknown activation"};
+  if (p->rows < 1) return {FAL_ERR_INVALID_ARG, "rows must be >= 1"};
+  const int32_t most = 1 << 20;
+  if (p->d_model < 1 || p->d_model > most || p->d_ff < 1 || p->d_ff > most)
+    return {FAL_ERR_INVALID_ARG, "d_model and d_ff must lie in [1, 2^20]"};
+  const int64_t d = p->d_model, f = p->d_ff;
+  if (p->ld_x < d || p->ld_y < d || p->ld_gate < f || p->ld_up < f || p->ld_down < d)
+    return {FAL_ERR_INVALID_ARG, "a row stride is smaller than a row"};
+  if ((p->ld_dx && p->ld_dx < d) || (p->ld_dgate && p->ld_dgate < f) || (p->ld_dup && p->ld_dup < f) ||
+      (p->ld_ddown && p->ld_ddown < d))
+    return {FAL_ERR_INVALID_ARG, "a gradient's row stride is smaller than a row"};
+  for (int64_t ld : {p->ld_x, p->ld_y, p->ld_gate, p->ld_up, p->ld_down, p->ld_dx, p->ld_dgate, p->ld_dup, p->ld_ddown})
+    if (ld > kMaxStride) return {FAL_ERR_INVALID_ARG, "row stride above 2^40 elements"};
+  // (f32 launches count elements of [M, f] a thread each)
+  if (p->rows * f > ((int64_t)1 << 38)) return {FAL_ERR_UNSUPPORTED, "rows * d_ff above 2^38 is not supported"};
+  if (p->dtype == FAL_F32) return kFine;
+  if (d % 8 || f % 8) return {FAL_ERR_UNSUPPORTED, "bf16 d_model and d_ff must be multiples of 8 (not supported otherwise)"};
+  if (p->ld_x % 8 || p->ld_y % 8 || p->ld_gate % 8 || p->ld_up % 8 || p->ld_down % 8 || p->ld_dx % 8 ||
+      p->ld_dgate % 8 || p->ld_dup % 8 || p->ld_ddown % 8)
+    return {FAL_ERR_INVALID_ARG, "bf16 row strides must be multiples of 8"};
+  // 32-bit byte offsets inside an operand, whose last slices of k run up to 256
+  // rows past its end
+  auto fits = [](int64_t rows, int64_t ld) { return (rows + 256) * ld * 2 < ((int64_t)1 << 31) - (1 << 20); };
+  if (!fits(p->rows, p->ld_x) || !fits(p->rows, p->ld_y) || !fits(p->rows, f) || !fits(d, p->ld_gate) ||
+      !fits(d, p->ld_up) || !fits(f, p->ld_down))
+    return {FAL_ERR_UNSUPPORTED, "bf16 operands of 2 GiB or more are not supported"};
+  return kFine;
+}
+
+GatedFfn gated_args(const fal_gated_ffn_t* p) {
+  GatedFfn a;
+  a.M = p->rows; a.d = p->d_model; a.f = p->d_ff;
+  a.act = p->activation == FAL_GATE_SILU ? GATE_SILU : p->activation == FAL_GATE_GELU_TANH ? GATE_GELU_TANH
+                                                                                          : GATE_GELU_ERF;
+  a.ldx = p->ld_x; a.ldy = p->ld_y; a.ldg = p->ld_gate; a.ldu = p->ld_up; a.ldd = p->ld_down;
+  a.lddx = p->ld_dx ? p->ld_dx : p->ld_x;
+  a.lddg = p->ld_dgate ? p->ld_dgate : p->ld_gate;
+  a.lddu = p->ld_dup ? p->ld_dup : p->ld_up;
+  a.lddd = p->ld_ddown ? p->ld_ddown : p->ld_down;
+  a.grads_f32 = p->grad_dtype == FAL_F32;
+  return a;
+}
+
+// The bytes that two [rows, width] matrices of one row stride share, the halves
+// of one matrix sharing none.
+bool interleave_free(const void* a, const void* b, int64_t rows, int64_t ld_a, int64_t ld_b, int64_t width,
+                     int64_t es) {
+  if (!meets(rows_of(a, rows, ld_a, width, es), {rows_of(b, rows, ld_b, width, es)})) return true;
+  if (ld_a != ld_b) return false;
+  const int64_t apart = static_cast<const char*>(b) - static_cast<const char*>(a), step = ld_a * es;
+  const int64_t in = ((apart % step) + step) % step;
+  return in >= width * es && in + width * es <= step;
+}
+
 }  // namespace
 
 extern "C" {
+
+fal_status_t fal_gated_ffn_workspace_bytes(const fal_gated_ffn_t* shape, size_t* forward, size_t* backward) {
+  return guarded([&] {
+    const Refusal no = check_gated(shape);
+    if (no.why) return fail(no.st, no.why);
+    if (forward) *forward = (size_t)gated_ffn_scratch(type_of(shape->dtype), gated_args(shape), 0);
+    if (backward) *backward = (size_t)gated_ffn_scratch(type_of(shape->dtype), gated_args(shape), 1);
+    return FAL_OK;
+  });
+}
+
+fal_status_t fal_gated_ffn_fwd(const fal_gated_ffn_t* shape, const void* x, const void* w_gate, const void* w_up,
+                               const void* w_down, void* y, float* saved, void* workspace, size_t ws_bytes,
+                               void* stream) {
+  return guarded([&] {
+    const Refusal no = check_gated(shape);
+    if (no.why) return fail(no.st, no.why);
+    if (!x || !w_gate || !w_up || !w_down || !y) return fail(FAL_ERR_INVALID_ARG, "NULL x, y or weight");
+    const GatedFfn a = gated_args(shape);
+    const int64_t es = element_bytes(shape->dtype), to = shape->dtype == FAL_BF16 ? 16 : 4;
+    if (!aligned(x, to) || !aligned(w_gate, to) || !aligned(w_up, to) || !aligned(w_down, to) || !aligned(y, to) ||
+        !aligned(saved, 16))
+      return fail(FAL_ERR_INVALID_ARG, "an array is misaligned (bf16 and saved: 16 bytes, fp32: 4)");
+    const int64_t need = gated_ffn_scratch(type_of(shape->dtype), a, 0);
+    if (!workspace || ws_bytes < (size_t)need || !aligned(workspace, kWorkspaceAlign))
+      return fail(FAL_ERR_WORKSPACE, "workspace NULL, too small or not 256-byte aligned");
+    if (outputs_meet({rows_of(y, a.M, a.ldy, a.d, es), {saved, (int64_t)a.M * a.f * 8}, {workspace, need}},
+                     {rows_of(x, a.M, a.ldx, a.d, es), rows_of(w_gate, a.d, a.ldg, a.f, es),
+                      rows_of(w_up, a.d, a.ldu, a.f, es), rows_of(w_down, a.f, a.ldd, a.d, es)}))
+      return fail(FAL_ERR_INVALID_ARG, "y, saved or the workspace overlaps another argument");
+    return launched(gated_ffn_fwd(type_of(shape->dtype), a, x, w_gate, w_up, w_down, y, saved, workspace,
+                                  static_cast<hipStream_t>(stream)),
+                    "fal_gated_ffn_fwd");
+  });
+}
+
+fal_status_t fal_gated_ffn_bwd(const fal_gated_ffn_t* shape, const void* x, const void* w_gate, const void* w_up,
+                               const void* w_down, const float* saved, const void* dy, void* dx, void* dw_gate,
+                               void* dw_up, void* dw_down, void* workspace, size_t ws_bytes, void* stream) {
+  return guarded([&] {
+    const Refusal no = check_gated(shape);
+    if (no.why) return fail(no.st, no.why);
+    if (!x || !w_gate || !w_up || !w_down || !saved || !dy)
+      return fail(FAL_ERR_INVALID_ARG, "NULL x, weight, saved or dy");
+    if (!dw_gate != !dw_up || !dw_gate != !dw_down)
+      return fail(FAL_ERR_INVALID_ARG, "dw_gate, dw_up and dw_down must all be given or all be NULL");
+    const GatedFfn a = gated_args(shape);
+    const int64_t es = element_bytes(shape->dtype), eg = element_bytes(shape->grad_dtype);
+    const int64_t to = shape->dtype == FAL_BF16 ? 16 : 4;
+    if (!aligned(x, to) || !aligned(w_gate, to) || !aligned(w_up, to) || !aligned(w_down, to) || !aligned(dy, to) ||
+        !aligned(saved, 16) || !aligned(dx, to) || !aligned(dw_gate, to) || !aligned(dw_up, to) ||
+        !aligned(dw_down, to))
+      return fail(FAL_ERR_INVALID_ARG, "an array is misaligned (bf16 and saved: 16 bytes, fp32: 4)");
+    const int64_t need = gated_ffn_scratch(type_of(shape->dtype), a, 1);
+    if (!workspace || ws_bytes < (size_t)need || !aligned(workspace, kWorkspaceAlign))
+      return fail(FAL_ERR_WORKSPACE, "workspace NULL, too small or not 256-byte aligned");
+    const Extent in[] = {rows_of(x, a.M, a.ldx, a.d, es), rows_of(w_gate, a.d, a.ldg, a.f, es),
+                         rows_of(w_up, a.d, a.ldu, a.f, es), rows_of(w_down, a.f, a.ldd, a.d, es),
+                         {saved, (int64_t)a.M * a.f * 8}, rows_of(dy, a.M, a.ldy, a.d, es)};
+    const Extent g = rows_of(dw_gate, a.d, a.lddg, a.f, eg), u = rows_of(dw_up, a.d, a.lddu, a.f, eg),
+                 d = rows_of(dw_down, a.f, a.lddd, a.d, eg), ox = rows_of(dx, a.M, a.lddx, a.d, es),
+                 ws = {workspace, need};
+    bool bad = meets(ws, {in[0], in[1], in[2], in[3], in[4], in[5]});
+    // dw_gate and dw_up may be the halves of one matrix
+    for (const Extent& o : {g, u, d, ox}) bad = bad || (o.p && meets(o, {in[0], in[1], in[2], in[3], in[4], in[5], ws}));
+    if (dw_gate)
+      bad = bad || meets(d, {g, u}) || !interleave_free(dw_gate, dw_up, a.d, a.lddg, a.lddu, a.f, eg) ||
+            (dx && meets(ox, {g, u, d}));
+    if (bad) return fail(FAL_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
+    return launched(gated_ffn_bwd(type_of(shape->dtype), a, x, w_gate, w_up, w_down, saved, dy, dx, dw_gate, dw_up,
+                                  dw_down, workspace, static_cast<hipStream_t>(stream)),
+                    "fal_gated_ffn_bwd");
+  });
+}
 
 fal_status_t fal_qk_norm_rope_workspace_bytes(const fal_qk_norm_rope_t* shape, size_t* bytes) {
   return guarded([&] {

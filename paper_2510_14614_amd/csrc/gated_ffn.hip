@@ -1,0 +1,399 @@
+// The gated feed-forward block y = (act(x Wg) * (x Wu)) Wd and its gradients.
+//
+//   g = x Wg, u = x Wu, h = act(g) u, y = h Wd                      (forward)
+//   dh = dy Wd^T, dg = dh u act'(g), du = dh act(g),
+//   dx = dg Wg^T + du Wu^T, dWg = x^T dg, dWu = x^T du, dWd = h^T dy (backward)
+//
+// Bound by the matrix cores: 6 M d f operations forward, 12 M d f backward.
+// In bf16 two products run here: both projections in one kernel, whose tile
+// holds the same columns of g and u, so that h leaves from the accumulators;
+// and dh, whose epilogue reads g and u and writes dg, du and h.  The other
+// products are plain and go through gemm().
+//
+// g and u are kept for the backward in fp32: dg and du multiply them once more,
+// and bf16 values would add their rounding to the ones that dg and du, as
+// operands, and dx, as the result, cannot do without.
+#include <algorithm>
+#include <cstring>
+
+#include "common.h"
+#include "gemm_pipe.h"
+#include "kernels.h"
+
+namespace fal {
+
+namespace {
+
+// The activation and its derivative.  bf16 blocks take the hardware's exp2 and
+// reciprocal (one step of fp32 each, far below bf16's), fp32 ones the library's.
+template <bool EXACT>
+__device__ __forceinline__ void act_and_grad(int act, float x, float& a, float& da) {
+  if (act == GATE_GELU_ERF) {
+    // erfc keeps the relative accuracy of the left tail
+    const float cdf = 0.5f * erfcf(x * -0.7071067811865476f);
+    a = x * cdf;
+    da = fmaf(x * 0.3989422804014327f, expf(-0.5f * x * x), cdf);
+    return;
+  }
+  float w, slope;  // sigmoid(w), dw/dx
+  if (act == GATE_SILU) {
+    w = x;
+    slope = 1.f;
+  } else {
+    constexpr float kC = 1.5957691216057308f;  // 2 sqrt(2/pi)
+    const float x2 = fminf(x * x, 1e30f);      // keeps 0 * slope from becoming 0 * inf
+    w = x * fmaf(x2, kC * 0.044715f, kC);
+    slope = fmaf(x2, 3.f * kC * 0.044715f, kC);
+  }
+  float s;
+  if (EXACT) s = 1.f / (1.f + expf(-w));
+  else s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(w * -1.4426950408889634f));
+  a = x * s;
+  da = fmaf(a * (1.f - s), slope, s);
+}
+
+struct Gated {
+  const bf16 *a, *b0, *b1;  // x, Wg, Wu; or dy, Wd
+  int64_t lda, ldb0, ldb1;
+  int M, N, K;              // rows, f, d
+  int tiles_m, tiles_n, act;
+  float* saved;             // [M][2 N]: g | u
+  bf16 *h, *dg, *du;        // [M][N]
+};
+
+// One output tile of BM rows and BN columns of f.  Forward (BWD 0): both
+// projections at once, x k-contiguous, weights MN-major.  Backward: dh, both
+// operands k-contiguous.  The main loop is that of gemm_bf16_pipe: NS stages of
+// 32 k, the fragments of slice s + 1 read under the MFMAs of slice s, slice s +
+// NS - 1 asked for behind them, one barrier a slice.
+template <int BWD, int BM, int BN, int OCC, int NS>
+__global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
+  using namespace pipe;
+  constexpr int NB = BWD ? 1 : 2;
+  constexpr int WTM = BM / 2, WTN = BN / 2, FM = WTM / 16, FN = WTN / 16;
+  typedef Src<BM, 1> SA;
+  typedef Src<BN, BWD> SB;
+  constexpr int SBYTES = SA::BYTES + NB * SB::BYTES;
+  constexpr int L = SA::IPW + NB * SB::IPW;
+  static_assert(NS == 4 && L * (NS - 2) <= 63, "stages");
+  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES], st2[SBYTES], st3[SBYTES];
+  auto stage_ptr = [&](int k) -> char* { return k == 0 ? st0 : k == 1 ? st1 : k == 2 ? st2 : st3; };
+
+  int tmi, tni;
+  grouped_tile(xcd_remap(blockIdx.x, p.tiles_m * p.tiles_n), p.tiles_m, p.tiles_n, tmi, tni);
+  const int m0 = tmi * BM, n0 = tni * BN;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+
+  SA sa;
+  SB sb, sc;
+  sa.init(0, p.a, p.lda, m0, p.M, p.K, wave, lane);
+  sb.init(0, p.b0, p.ldb0, n0, p.N, p.K, wave, lane);
+  sa.clear(1);  // one segment only
+  sb.clear(1);
+  if (NB == 2) {
+    sc.init(0, p.b1, p.ldb1, n0, p.N, p.K, wave, lane);
+    sc.clear(1);
+  }
+  const int n = (p.K + KS - 1) / KS, full = p.K / KS;
+  auto issue = [&](char* stage, int s) {
+    if (s > 0 && s < full) {
+      sa.advance();
+      sb.advance();
+      if (NB == 2) sc.advance();
+    } else {
+      // the first slice, a tail of K or one past the end (zeros)
+      const bool live = s < n;
+      const int k0 = live ? s * KS : 0;
+      const int lim = live ? min(KS, p.K - k0) : 0;
+      sa.set(0, k0, lim);
+      sb.set(0, k0, BWD ? lim : (live ? KS : 0));
+      if (NB == 2) sc.set(0, k0, live ? KS : 0);
+    }
+    sa.load(stage, wave);
+    sb.load(stage + SA::BYTES, wave);
+    if (NB == 2) sc.load(stage + SA::BYTES + SB::BYTES, wave);
+  };
+
+  Frag<BM, 1, FM> fa;
+  Frag<BN, BWD, FN> fb;
+  fa.init(wm * WTM, lane);
+  fb.init(wn * WTN, lane);
+
+  f32x4_t acc[NB][FM][FN];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[b][i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  bf16x8_t ra[2][FM], rb[2][NB][FN];
+  auto read_b = [&](const char* stage, int b, int j) {
+    return fb.read(stage + SA::BYTES + b * SB::BYTES, j);
+  };
+  auto read = [&](const char* stage, int buf) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) ra[buf][i] = fa.read(stage, i);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) rb[buf][b][j] = read_b(stage, b, j);
+  };
+  auto step = [&](const char* stage, int cur) {
+    const int nxt = cur ^ 1;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          acc[b][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rb[cur][b][j], ra[cur][i], acc[b][i][j], 0, 0, 0);
+          if (i == FM - 1) rb[nxt][b][j] = read_b(stage, b, j);
+        }
+      ra[nxt][i] = fa.read(stage, i);
+    }
+  };
+  constexpr int RB = BWD ? 1 : 2;  // LDS reads of a fragment of B
+  constexpr int ROW = NB * FN, NMF = FM * ROW;
+  constexpr int DMA_EVERY = NMF / L > 0 ? NMF / L : 1;
+  auto interleave = [&]() {
+    int dma = 0;
+#pragma unroll
+    for (int q = 0; q < NMF; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+      if (q >= NMF - ROW) {
+#pragma unroll
+        for (int r = 0; r < RB; ++r) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read (B)
+      }
+      if ((q + 1) % ROW == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read (A)
+      if (q % DMA_EVERY == 0 && dma < L) {
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // buffer load to LDS
+        ++dma;
+      }
+    }
+  };
+  // the reads that a step issues may be in flight at the next one's barrier;
+  // the counter holds at most 15
+  constexpr int LGK_N = FM + ROW * RB, LGK = LGK_N < 15 ? LGK_N : 15;
+
+#pragma unroll
+  for (int k = 0; k < NS - 1; ++k) issue(stage_ptr(k), k);
+  FAL_WAITCNT(L * (NS - 2), 0);
+  bar();
+  read(st0, 0);
+  // slices past the end load zeros in both operands and add nothing
+  const int tend = (n + NS - 1) / NS * NS;
+  for (int t = 0; t < tend; t += NS) {
+#pragma unroll
+    for (int U = 0; U < NS; ++U) {
+      FAL_WAITCNT(L * (NS - 3), LGK);
+      bar();
+      __builtin_amdgcn_sched_barrier(0);
+      issue(stage_ptr((U + NS - 1) % NS), t + U + NS - 1);
+      step(stage_ptr((U + 1) % NS), U & 1);
+      interleave();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  FAL_WAITCNT(0, 0);
+  bar();
+
+  // Epilogue: strips of 16 rows through LDS, so that consecutive lanes hold
+  // consecutive columns; g, u and dh meet in one lane.
+  constexpr int PITCH = NB * WTN + 4, LPR = WTN / 4, RPI = 64 / LPR;
+  static_assert(2 * 16 * PITCH * 4 <= SBYTES, "epilogue staging exceeds a stage");
+  float* strip = reinterpret_cast<float*>(wm ? st1 : st0) + wn * 16 * PITCH;
+  const int rr = lane / LPR, cc = lane % LPR * 4;
+  const int64_t nn = n0 + wn * WTN + cc;
+  const int mw = m0 + wm * WTM;
+#pragma clang loop unroll(full)
+  for (int i = 0; i < FM; ++i) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        *reinterpret_cast<float4*>(strip + (lane & 15) * PITCH + b * WTN + 16 * j + 4 * (lane >> 4)) =
+            make_float4(acc[b][i][j][0], acc[b][i][j][1], acc[b][i][j][2], acc[b][i][j][3]);
+    wave_lds_order();
+#pragma unroll
+    for (int k = 0; k < 16 / RPI; ++k) {
+      const int r = k * RPI + rr;
+      const int64_t m = mw + 16 * i + r;
+      const float4 v0 = *reinterpret_cast<const float4*>(strip + r * PITCH + cc);
+      float4 v1 = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (NB == 2) v1 = *reinterpret_cast<const float4*>(strip + r * PITCH + WTN + cc);
+      // (f is a multiple of 8: a lane's four columns are all inside or none is)
+      if (m >= p.M || nn >= p.N) continue;
+      const int64_t o = m * p.N + nn;
+      if (!BWD) {
+        if (p.saved) {
+          *reinterpret_cast<float4*>(p.saved + m * 2 * p.N + nn) = v0;
+          *reinterpret_cast<float4*>(p.saved + m * 2 * p.N + p.N + nn) = v1;
+        }
+        const float g[4] = {v0.x, v0.y, v0.z, v0.w}, u[4] = {v1.x, v1.y, v1.z, v1.w};
+        float h[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float a, da;
+          act_and_grad<false>(p.act, g[c], a, da);
+          h[c] = a * u[c];
+        }
+        st4(p.h + o, h);
+      } else {
+        const float4 g4 = *reinterpret_cast<const float4*>(p.saved + m * 2 * p.N + nn);
+        const float4 u4 = *reinterpret_cast<const float4*>(p.saved + m * 2 * p.N + p.N + nn);
+        const float dh[4] = {v0.x, v0.y, v0.z, v0.w}, g[4] = {g4.x, g4.y, g4.z, g4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
+        float h[4], dg[4], du[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float a, da;
+          act_and_grad<false>(p.act, g[c], a, da);
+          h[c] = a * u[c];
+          dg[c] = dh[c] * u[c] * da;
+          du[c] = dh[c] * a;
+        }
+        st4(p.h + o, h);
+        st4(p.dg + o, dg);
+        st4(p.du + o, du);
+      }
+    }
+    wave_lds_order();
+  }
+}
+
+// fp32: h from g | u, and the backward's elementwise part (dh in dg's place).
+__global__ __launch_bounds__(256) void gate_fwd_f32(const float* gu, int64_t n, int f, int act, float* h) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int64_t m = i / f, c = i % f;
+  float a, da;
+  act_and_grad<true>(act, gu[m * 2 * f + c], a, da);
+  h[i] = a * gu[m * 2 * f + f + c];
+}
+__global__ __launch_bounds__(256) void gate_bwd_f32(const float* gu, int64_t n, int f, int act, float* dg, float* du,
+                                                    float* h) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int64_t m = i / f, c = i % f;
+  const float u = gu[m * 2 * f + f + c], dh = dg[i];
+  float a, da;
+  act_and_grad<true>(act, gu[m * 2 * f + c], a, da);
+  h[i] = a * u;
+  dg[i] = dh * u * da;
+  du[i] = dh * a;
+}
+
+GemmProblem product(const void* A, int64_t lda, const void* B, int64_t ldb, int M, int N, int K, void* out,
+                    int64_t ldo, int f32) {
+  GemmProblem p;
+  memset(&p, 0, sizeof(p));
+  p.A = A; p.B = B; p.lda = lda; p.ldb = ldb;
+  p.M = M; p.N = N; p.K = K;
+  p.epi = EPI_STORE; p.out_f32 = f32; p.out = out; p.ldo = ldo;
+  return p;
+}
+
+hipError_t run(DType dt, int a_kmaj, int b_kmaj, std::initializer_list<GemmProblem> ps, hipStream_t s,
+               float* split = nullptr, int64_t split_floats = 0) {
+  GemmGroup g;
+  memset(&g, 0, sizeof(g));
+  for (const GemmProblem& p : ps) g.p[g.n++] = p;
+  const char* why;
+  return gemm(dt, a_kmaj, b_kmaj, g, 0, s, &why, split, split_floats);
+}
+
+// The larger tile while it fills the chip (launch times as gemm()'s model has
+// them for tiles of the same size: 0.85 us a slice and 10 a round of 256; 0.54
+// and 3 a round of 512).
+template <int BWD>
+hipError_t launch_gated(Gated p, hipStream_t s) {
+  constexpr int BN = BWD ? 256 : 128, BNS = BWD ? 128 : 64;
+  auto tiles = [&](int bm, int bn) { return (int64_t)cdiv(p.M, bm) * cdiv(p.N, bn); };
+  const double ns = cdiv(p.K, pipe::KS);
+  const double large = cdiv(tiles(256, BN), 256) * (10.0 + ns * 0.85);
+  const int64_t small_tiles = tiles(128, BNS), rounds = small_tiles / 512, rest = small_tiles % 512;
+  const double small = rounds * (3.0 + ns * 0.54) + (rest ? 3.0 + ns * (rest > 256 ? 0.54 : 0.39) : 0.0);
+  const int bm = large <= small ? 256 : 128, bn = large <= small ? BN : BNS;
+  p.tiles_m = cdiv(p.M, bm);
+  p.tiles_n = cdiv(p.N, bn);
+  const dim3 grid((unsigned)tiles(bm, bn)), block(256);
+  if (large <= small) hipLaunchKernelGGL((gated_mfma<BWD, 256, BN, 1, 4>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((gated_mfma<BWD, 128, BNS, 2, 4>), grid, block, 0, s, p);
+  return hipGetLastError();
+}
+
+int64_t round_up(int64_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+int64_t gated_ffn_scratch(DType dt, const GatedFfn& a, int backward) {
+  const int64_t one = round_up((int64_t)a.M * a.f * (dt == BF16 ? 2 : 4));
+  return backward ? 3 * one : dt == BF16 ? one : 3 * one;
+}
+
+hipError_t gated_ffn_fwd(DType dt, const GatedFfn& a, const void* x, const void* wg, const void* wu, const void* wd,
+                         void* y, float* saved, void* scratch, hipStream_t s) {
+  hipError_t e;
+  void* h = scratch;
+  if (dt == BF16) {
+    Gated p;
+    memset(&p, 0, sizeof(p));
+    p.a = static_cast<const bf16*>(x); p.b0 = static_cast<const bf16*>(wg); p.b1 = static_cast<const bf16*>(wu);
+    p.lda = a.ldx; p.ldb0 = a.ldg; p.ldb1 = a.ldu;
+    p.M = a.M; p.N = a.f; p.K = a.d; p.act = a.act;
+    p.saved = saved;
+    p.h = static_cast<bf16*>(h);
+    e = launch_gated<0>(p, s);
+  } else {
+    const int64_t n = (int64_t)a.M * a.f;
+    float* gu = saved ? saved : reinterpret_cast<float*>(static_cast<char*>(scratch) + round_up(n * 4));
+    e = run(F32, 1, 0, {product(x, a.ldx, wg, a.ldg, a.M, a.f, a.d, gu, 2 * (int64_t)a.f, 1),
+                        product(x, a.ldx, wu, a.ldu, a.M, a.f, a.d, gu + a.f, 2 * (int64_t)a.f, 1)}, s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(gate_fwd_f32, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, gu, n, a.f, a.act,
+                       static_cast<float*>(h));
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) return e;
+  return run(dt, 1, 0, {product(h, a.f, wd, a.ldd, a.M, a.d, a.f, y, a.ldy, dt == F32)}, s);
+}
+
+hipError_t gated_ffn_bwd(DType dt, const GatedFfn& a, const void* x, const void* wg, const void* wu, const void* wd,
+                         const float* saved, const void* dy, void* dx, void* dwg, void* dwu, void* dwd, void* scratch,
+                         hipStream_t s) {
+  const int64_t n = (int64_t)a.M * a.f, one = round_up(n * (dt == BF16 ? 2 : 4));
+  char* base = static_cast<char*>(scratch);
+  void *dg = base, *du = base + one, *h = base + 2 * one;
+  hipError_t e;
+  if (dt == BF16) {
+    Gated p;
+    memset(&p, 0, sizeof(p));
+    p.a = static_cast<const bf16*>(dy); p.b0 = static_cast<const bf16*>(wd);
+    p.lda = a.ldy; p.ldb0 = a.ldd;
+    p.M = a.M; p.N = a.f; p.K = a.d; p.act = a.act;
+    p.saved = const_cast<float*>(saved);
+    p.h = static_cast<bf16*>(h); p.dg = static_cast<bf16*>(dg); p.du = static_cast<bf16*>(du);
+    e = launch_gated<1>(p, s);
+  } else {
+    e = run(F32, 1, 1, {product(dy, a.ldy, wd, a.ldd, a.M, a.f, a.d, dg, a.f, 1)}, s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(gate_bwd_f32, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, saved, n, a.f, a.act,
+                       static_cast<float*>(dg), static_cast<float*>(du), static_cast<float*>(h));
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) return e;
+  if (dx) {
+    GemmProblem p = product(dg, a.f, wg, a.ldg, a.M, a.d, a.f, dx, a.lddx, dt == F32);
+    p.A2 = du; p.lda2 = a.f; p.B2 = wu; p.ldb2 = a.ldu; p.K2 = a.f;
+    e = run(dt, 1, 1, {p}, s);
+    if (e != hipSuccess) return e;
+  }
+  if (!dwg) return hipSuccess;
+  const int f32 = dt == F32 || a.grads_f32;
+  return run(dt, 0, 0, {product(x, a.ldx, dg, a.f, a.d, a.f, a.M, dwg, a.lddg, f32),
+                        product(x, a.ldx, du, a.f, a.d, a.f, a.M, dwu, a.lddu, f32),
+                        product(h, a.f, dy, a.ldy, a.f, a.d, a.M, dwd, a.lddd, f32)}, s);
+}
+
+}  // namespace fal

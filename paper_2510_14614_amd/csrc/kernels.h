@@ -261,6 +261,26 @@ hipError_t head_norm_rope_bwd(DType dt, const HeadNorm& a, const void* x, const 
                               float* dwk, float* part, hipStream_t s);
 int64_t head_norm_rope_scratch(const HeadNorm& a);
 
+// ------------------------------------------------- gated feed-forward ----
+// y = (act(x Wg) * (x Wu)) Wd over M rows: x [M, d] at ldx, y [M, d] at ldy, Wg
+// and Wu [d, f] at ldg and ldu, Wd [f, d] at ldd, all dtype.  bf16: 16-byte
+// aligned, d, f and the strides multiples of 8, every operand below 2 GiB.
+enum Gate : int { GATE_SILU = 0, GATE_GELU_TANH = 1, GATE_GELU_ERF = 2 };
+struct GatedFfn {
+  int M, d, f, act;
+  int64_t ldx, ldy, ldg, ldu, ldd;
+  int64_t lddx, lddg, lddu, lddd;  // of the gradients
+  int grads_f32;  // the weights' gradients are fp32, not dtype
+};
+// saved: fp32 [M, 2 f] (x Wg | x Wu) or NULL; scratch: gated_ffn_scratch bytes.
+hipError_t gated_ffn_fwd(DType dt, const GatedFfn& a, const void* x, const void* wg, const void* wu, const void* wd,
+                         void* y, float* saved, void* scratch, hipStream_t s);
+// dy at ldy; dx may be NULL; dwg, dwu and dwd may all be NULL.
+hipError_t gated_ffn_bwd(DType dt, const GatedFfn& a, const void* x, const void* wg, const void* wu, const void* wd,
+                         const float* saved, const void* dy, void* dx, void* dwg, void* dwu, void* dwd, void* scratch,
+                         hipStream_t s);
+int64_t gated_ffn_scratch(DType dt, const GatedFfn& a, int backward);
+
 // ------------------------------------------------ embedding / loss / misc ----
 // X[m, :] = wte[tok[b, t]] + wpe[t]  (fp32 out), tokens [B, T+1].
 hipError_t embed_fwd(DType dt, const int32_t* tokens, int B, int T, int V, int d, const void* wte,

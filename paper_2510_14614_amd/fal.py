@@ -35,6 +35,7 @@ ABI_FUNCTIONS = (
     "fal_set_attention_window", "fal_token_logprobs", "fal_logit_loss_workspace_bytes", "fal_policy_loss",
     "fal_preference_loss", "fal_model_logprobs", "fal_policy_step", "fal_preference_step",
     "fal_qk_norm_rope_workspace_bytes", "fal_qk_norm_rope_fwd", "fal_qk_norm_rope_bwd",
+    "fal_gated_ffn_workspace_bytes", "fal_gated_ffn_fwd", "fal_gated_ffn_bwd",
 )
 PROF_GEMM, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_NORM, PROF_CE, PROF_EMBED, PROF_BIAS, PROF_OPTIM = range(8)
 PROF_NAMES = {PROF_GEMM: "gemm", PROF_ATTN_FWD: "attn_fwd", PROF_ATTN_BWD: "attn_bwd", PROF_NORM: "norm",
@@ -93,6 +94,17 @@ class fal_qk_norm_rope_t(ctypes.Structure):
                 ("theta", c_float), ("eps", c_float), ("ld_qkv", c_int64), ("ld_out", c_int64)]
 
 
+class fal_gated_ffn_t(ctypes.Structure):
+    _fields_ = [("rows", c_int32), ("d_model", c_int32), ("d_ff", c_int32), ("activation", c_int32), ("dtype", c_int32),
+                ("grad_dtype", c_int32), ("ld_x", c_int64), ("ld_y", c_int64), ("ld_gate", c_int64), ("ld_up", c_int64),
+                ("ld_down", c_int64), ("ld_dx", c_int64), ("ld_dgate", c_int64), ("ld_dup", c_int64),
+                ("ld_ddown", c_int64)]
+
+
+# Names of the gated block's activations, in the order of fal_gate_t.
+GATES = ("silu", "gelu_tanh", "gelu")
+
+
 class PolicyLoss(NamedTuple):
     stats: object    # fp32 [4]: loss, its policy part, KL mean, share of rows whose ratio the clip holds
     logp: object     # fp32 [B, T]
@@ -109,6 +121,13 @@ class QkNormRopeGrads(NamedTuple):
     dqkv: object       # gradient of the rows, in their dtype
     dq_weight: object  # fp32 [head_dim], None without a weight
     dk_weight: object
+
+
+class GatedFfnGrads(NamedTuple):
+    dx: object       # in x's dtype, None if it was not asked for
+    dw_gate: object  # in the weights' dtype or float32
+    dw_up: object
+    dw_down: object
 
 
 class FalError(RuntimeError):
@@ -166,6 +185,10 @@ def lib():
         L.fal_qk_norm_rope_workspace_bytes.argtypes = [normp, POINTER(c_size_t)]
         L.fal_qk_norm_rope_fwd.argtypes = [normp] + [c_void_p] * 7
         L.fal_qk_norm_rope_bwd.argtypes = ([normp] + [c_void_p] * 7 + [c_int64] + [c_void_p] * 3 + [c_size_t, c_void_p])
+        ffnp = POINTER(fal_gated_ffn_t)
+        L.fal_gated_ffn_workspace_bytes.argtypes = [ffnp, POINTER(c_size_t), POINTER(c_size_t)]
+        L.fal_gated_ffn_fwd.argtypes = [ffnp] + [c_void_p] * 7 + [c_size_t, c_void_p]
+        L.fal_gated_ffn_bwd.argtypes = [ffnp] + [c_void_p] * 11 + [c_size_t, c_void_p]
         L.fal_status_string.argtypes = [c_int32]
         L.fal_status_string.restype = c_char_p
         L.fal_last_error.argtypes = [c_void_p]
@@ -623,6 +646,126 @@ def qk_norm_rope_bwd(qkv, dout, n_head, q_weight=None, k_weight=None, positions=
                                                 _ptr(positions), _ptr(lens), dout.data_ptr(), dqkv.data_ptr(), ld,
                                                 _ptr(dq), _ptr(dk), ws.data_ptr(), n, stream))
     return QkNormRopeGrads(dqkv, dq, dk)
+
+
+@functools.lru_cache(maxsize=1024)
+def _ffn_workspace(*shape):
+    fwd, bwd = c_size_t(), c_size_t()
+    _check_noctx(lib().fal_gated_ffn_workspace_bytes(byref(fal_gated_ffn_t(*shape)), byref(fwd), byref(bwd)))
+    return fwd.value, bwd.value
+
+
+def _matrix(t, name, like, shape=None):
+    """Row stride of a matrix in x's dtype and device (any leading dimensions
+    of x and y count as rows, if those are equally spaced)."""
+    if t.dtype is not like.dtype or t.device != like.device:
+        _refuse(f"{name} must have x's dtype and device")
+    if shape is not None and t.shape != shape:
+        _refuse(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    width = t.shape[-1]
+    if width > 1 and t.stride(-1) != 1:
+        _refuse(f"{name} must be contiguous in its last dimension")
+    ld = rows = None
+    for n, st in zip(t.shape[-2::-1], t.stride()[-2::-1]):
+        if n == 1:
+            continue
+        if ld is None:
+            ld, rows = st, n
+        elif st != ld * rows:
+            _refuse(f"the rows of {name} must be equally spaced")
+        else:
+            rows *= n
+    return width if ld is None else ld
+
+
+def _ffn_shape(x, w_gate, w_up, w_down, activation):
+    """The call's shape, with dense rows of y."""
+    if activation not in GATES:
+        _refuse(f"activation must be one of {', '.join(GATES)}")
+    if x.dim() < 2 or w_gate.dim() != 2:
+        _refuse("x must be [..., d_model] and w_gate [d_model, d_ff]")
+    code = _dtype_code(x, "x")
+    d, f = x.shape[-1], w_gate.shape[1]
+    ldx = _matrix(x, "x", x)
+    lds = (_matrix(w_gate, "w_gate", x, (d, f)), _matrix(w_up, "w_up", x, (d, f)),
+           _matrix(w_down, "w_down", x, (f, d)))
+    rows = x.numel() // d if d else 0
+    return (_clamp32(rows), _clamp32(d), _clamp32(f), GATES.index(activation), code, code, ldx, d, *lds, 0, 0, 0, 0)
+
+
+def gated_ffn_fwd(x, w_gate, w_up, w_down, activation="silu", y=None, saved=None, *, save=False):
+    """The gated feed-forward block (act(x w_gate) * (x w_up)) w_down
+    (fal_gated_ffn_fwd), activation "silu", "gelu_tanh" or "gelu".
+
+    x: [..., d_model], bfloat16 or float32; weights [in, out] in its dtype, at
+    any row stride (w_gate and w_up may be halves of one matrix).  Returns y, like
+    x, and what the backward needs, float32 [rows, 2 d_ff]: allocated with save,
+    or given as saved, otherwise None."""
+    import torch
+    shape = _ffn_shape(x, w_gate, w_up, w_down, activation)
+    a = fal_gated_ffn_t(*shape)
+    rows, f = shape[0], shape[2]
+    with _call(x.device) as stream:
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        else:
+            a.ld_y = _matrix(y, "y", x, x.shape)
+        if saved is not None:
+            _dense(saved, "saved", (rows, 2 * f), (torch.float32,), x.device)
+        elif save:
+            saved = torch.empty((rows, 2 * f), dtype=torch.float32, device=x.device)
+        n = _ffn_workspace(*shape)[0]
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+        _check_noctx(lib().fal_gated_ffn_fwd(byref(a), x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(),
+                                             w_down.data_ptr(), y.data_ptr(), _ptr(saved), ws.data_ptr(), n, stream))
+    return y, saved
+
+
+def gated_ffn_bwd(x, w_gate, w_up, w_down, saved, dy, activation="silu", dx=None, dw=None, *, input_grad=True,
+                  weight_grads=True, grads_f32=False):
+    """Gradients of gated_ffn_fwd (fal_gated_ffn_bwd) from the saved it
+    returned and the gradient of y: dx (unless input_grad is false) and the
+    weights' (unless weight_grads is false), in the weights' dtype or, with
+    grads_f32, float32.  dx and dw (a sequence of three), if given, have rows at
+    any equal spacing."""
+    import torch
+    shape = list(_ffn_shape(x, w_gate, w_up, w_down, activation))
+    rows, f, device = shape[0], shape[2], x.device
+    weights = (w_gate, w_up, w_down)
+    gtype = torch.float32 if grads_f32 else x.dtype
+    shape[5] = 0 if gtype is torch.float32 else 1
+    shape[7] = _matrix(dy, "dy", x, x.shape)
+    _dense(saved, "saved", (rows, 2 * f), (torch.float32,), device)
+    if not input_grad:
+        dx = None
+    elif dx is not None:
+        shape[11] = _matrix(dx, "dx", x, x.shape)
+    else:
+        shape[11] = x.shape[-1]
+    if not weight_grads:
+        dw = (None, None, None)
+    elif dw is not None:
+        dw = tuple(dw)
+        if len(dw) != 3:
+            _refuse("dw must hold the gradients of w_gate, w_up and w_down")
+        for i, t in enumerate(dw):
+            if t.dtype is not gtype or t.device != device or t.shape != weights[i].shape or (
+                    t.shape[1] > 1 and t.stride(1) != 1):
+                _refuse(f"dw must be {gtype}, of the weights' shapes, with rows of consecutive elements")
+            shape[12 + i] = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    else:
+        shape[12:] = (w.shape[1] for w in weights)
+    with _call(device) as stream:
+        if input_grad and dx is None:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=device)
+        if weight_grads and dw is None:
+            dw = tuple(torch.empty(w.shape, dtype=gtype, device=device) for w in weights)
+        n = _ffn_workspace(*shape)[1]
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
+        _check_noctx(lib().fal_gated_ffn_bwd(byref(fal_gated_ffn_t(*shape)), x.data_ptr(), w_gate.data_ptr(),
+                                             w_up.data_ptr(), w_down.data_ptr(), saved.data_ptr(), dy.data_ptr(),
+                                             _ptr(dx), *(_ptr(t) for t in dw), ws.data_ptr(), n, stream))
+    return GatedFfnGrads(dx, *dw)
 
 
 class Fal:

@@ -111,3 +111,105 @@ def test_head_norm_binding_refuses():
             call(t, **kw)
     with pytest.raises(ValueError, match="dout"):
         fal.qk_norm_rope_bwd(x, x[:, :4], 4, n_kv_head=2)
+
+
+# -------------------------------------------------------------- gated feed-forward --
+def ffn(**kw):
+    v = dict(rows=300, d_model=64, d_ff=128, activation=0, dtype=1, grad_dtype=1, ld_x=64, ld_y=72, ld_gate=128,
+             ld_up=136, ld_down=64, ld_dx=0, ld_dgate=0, ld_dup=0, ld_ddown=0)
+    v.update(kw)
+    return fal.fal_gated_ffn_t(**v)
+
+
+def ffn_bytes(s):
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+    assert fal.lib().fal_gated_ffn_workspace_bytes(byref(s), byref(f), byref(b)) == fal.FAL_OK
+    return f.value, b.value
+
+
+@pytest.mark.parametrize("kw,status,word", [
+    (dict(rows=0), BAD, "rows"), (dict(d_model=0), BAD, "d_model"), (dict(d_ff=0), BAD, "d_ff"),
+    (dict(d_ff=(1 << 20) + 8), BAD, "d_ff"), (dict(activation=3), BAD, "activation"), (dict(activation=-1), BAD, "activation"),
+    (dict(dtype=2), BAD, "dtype"), (dict(grad_dtype=2), BAD, "grad_dtype"), (dict(dtype=0), BAD, "grad_dtype"),
+    (dict(ld_x=56), BAD, "stride"), (dict(ld_y=56), BAD, "stride"), (dict(ld_gate=120), BAD, "stride"),
+    (dict(ld_up=120), BAD, "stride"), (dict(ld_down=56), BAD, "stride"), (dict(ld_dx=56), BAD, "stride"),
+    (dict(ld_dgate=8), BAD, "stride"), (dict(ld_dup=120), BAD, "stride"), (dict(ld_ddown=56), BAD, "stride"),
+    (dict(ld_dx=-1), BAD, "stride"), (dict(ld_dx=(1 << 40) + 8), BAD, "2^40"),
+    (dict(d_model=60), UNSUP, "multiples of 8"), (dict(d_ff=100), UNSUP, "multiples of 8"),
+    (dict(ld_x=68), BAD, "multiples of 8"), (dict(ld_dup=132), BAD, "multiples of 8"),
+    (dict(ld_x=1 << 24), UNSUP, "2 GiB"), (dict(rows=1 << 23), UNSUP, "2 GiB"), (dict(ld_down=1 << 23), UNSUP, "2 GiB"),
+    (dict(dtype=0, grad_dtype=0, rows=1 << 30, d_ff=1 << 10, ld_gate=1 << 10, ld_up=1 << 10), UNSUP, "2^38"),
+])
+def test_gated_ffn_refuses_a_shape(kw, status, word):
+    L, s, n = fal.lib(), ffn(**kw), ctypes.c_size_t()
+    assert L.fal_gated_ffn_workspace_bytes(byref(s), byref(n), byref(n)) == status
+    assert word in message()
+    assert L.fal_gated_ffn_fwd(byref(s), A, B, C, D, E, F, G, 1 << 30, None) == status
+    assert L.fal_gated_ffn_bwd(byref(s), A, B, C, D, E, F, G, H, I, J, K, 1 << 30, None) == status
+
+
+@pytest.mark.parametrize("args,status,word", [
+    ({0: None}, BAD, "NULL shape"), *(({i: None}, BAD, "NULL") for i in range(1, 6)),
+    *(({i: off(A, 8)}, BAD, "misaligned") for i in range(1, 7)),
+    *(({5: p}, BAD, "overlaps") for p in (A, B, C, D, F, G)), *(({6: p}, BAD, "overlaps") for p in (A, B, D, E, G)),
+    *(({7: p}, BAD, "overlaps") for p in (A, E)),
+    ({7: None}, WS, "workspace"), ({7: off(G, 64)}, WS, "workspace"), ({8: 300 * 128 * 2 - 1}, WS, "workspace"),
+])
+def test_gated_ffn_forward_refuses(args, status, word):
+    s = ffn()
+    refused(fal.lib().fal_gated_ffn_fwd, args, [byref(s), A, B, C, D, E, F, G, ffn_bytes(s)[0], None], status, word)
+
+
+@pytest.mark.parametrize("args,status,word", [
+    ({0: None}, BAD, "NULL shape"), *(({i: None}, BAD, "NULL") for i in range(1, 7)),
+    *(({i: None}, BAD, "all be NULL") for i in (8, 9, 10)), *(({i: off(A, 4)}, BAD, "misaligned") for i in range(1, 11)),
+    *(({7: p}, BAD, "overlaps") for p in (A, B, C, D, E, F, H, I, J, K)),
+    *(({10: p}, BAD, "overlaps") for p in (A, B, C, D, E, F, G, H, I, K)),
+    ({9: H}, BAD, "overlaps"), ({9: off(H, 128)}, BAD, "overlaps"), ({11: E}, BAD, "overlaps"),
+    ({11: None}, WS, "workspace"), ({11: off(K, 64)}, WS, "workspace"), ({12: 3 * 300 * 128 * 2 - 1}, WS, "workspace"),
+])
+def test_gated_ffn_backward_refuses(args, status, word):
+    s = ffn()
+    base = [byref(s), A, B, C, D, E, F, G, H, I, J, K, ffn_bytes(s)[1], None]
+    refused(fal.lib().fal_gated_ffn_bwd, args, base, status, word)
+
+
+def test_gated_ffn_halves_of_one_gradient():
+    """Halves of one matrix pass the overlap check; halves that run into each
+    other do not."""
+    L = fal.lib()
+    for ld, apart, fine in ((256, 256, True), (256, 240, False), (256, 272, False), (264, 272, True), (256, 512, False)):
+        s = ffn(ld_dgate=ld, ld_dup=ld)
+        # a workspace that is too small is found before any launch
+        args = [byref(s), A, B, C, D, E, F, G, H, off(H, apart), J, K, ffn_bytes(s)[1], None]
+        if fine:
+            args[4] = None  # stops the call after its first checks
+            assert L.fal_gated_ffn_bwd(*args) == BAD
+        else:
+            assert L.fal_gated_ffn_bwd(*args) == BAD and "overlaps" in message()
+
+
+def test_gated_ffn_workspace():
+    r = lambda n: (n + 255) // 256 * 256  # noqa: E731
+    assert ffn_bytes(ffn()) == (300 * 128 * 2, 3 * 300 * 128 * 2)
+    assert ffn_bytes(ffn(dtype=0, grad_dtype=0, d_ff=101)) == (3 * r(300 * 101 * 4),) * 2
+    assert fal.lib().fal_gated_ffn_workspace_bytes(byref(ffn()), None, None) == fal.FAL_OK
+
+
+def test_gated_ffn_binding_refuses():
+    bf = torch.bfloat16
+    x, wg, wd = torch.zeros(2, 5, 64, dtype=bf), torch.zeros(64, 128, dtype=bf), torch.zeros(128, 64, dtype=bf)
+    for args, kw, word in [((x[0, 0], wg, wg, wd), {}, "x must be"), ((x, wg[0], wg, wd), {}, "x must be"),
+                           ((x.half(), wg, wg, wd), {}, "bfloat16"), ((x, wg, wg, wd), {"activation": "relu"}, "activation"),
+                           ((x, wg.float(), wg, wd), {}, "w_gate"), ((x, wg, wg[:, :64], wd), {}, "w_up"),
+                           ((x, wg, wg, wg), {}, "w_down"), ((x, wg, wg, wg.t()), {}, "w_down"),
+                           ((x.transpose(0, 1), wg, wg, wd), {}, "rows of x"), ((x, wg, wg, wd), {}, "GPU")]:
+        with pytest.raises(ValueError, match=word):
+            fal.gated_ffn_fwd(*args, **kw)
+    saved = torch.zeros(10, 256)
+    for args, kw, word in [((saved[:9], x), {}, "saved"), ((saved.double(), x), {}, "saved"), ((saved, x[:1]), {}, "dy"),
+                           ((saved, x), {"dx": x.float()}, "dx"), ((saved, x), {"dw": (wg, wg)}, "dw"),
+                           ((saved, x), {"dw": (wg, wg, wg)}, "dw"), ((saved, x), {"dw": (wg, wg, wd), "grads_f32": True}, "dw"),
+                           ((saved, x), {}, "GPU")]:
+        with pytest.raises(ValueError, match=word):
+            fal.gated_ffn_bwd(x, wg, wg, wd, *args, **kw)
