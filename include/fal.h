@@ -628,6 +628,60 @@ fal_status_t fal_gated_ffn_bwd(const fal_gated_ffn_t* shape, const void* x, cons
                                const void* w_down, const float* saved, const void* dy, void* dx, void* dw_gate,
                                void* dw_up, void* dw_down, void* workspace, size_t ws_bytes, void* stream);
 
+/* Matrices made orthogonal by Newton-Schulz products: each U [rows, cols] of a
+ * batch becomes X = U / |U|_F (Frobenius norm), then, `steps` times,
+ *   X <- (a I + b X X^T + c (X X^T)^2) X
+ * (for rows > cols the same of its transpose): its singular values go through
+ * a s + b s^3 + c s^5, its singular vectors stay.  Sums are fp32; X and both
+ * factors are held to 22 bits between the products. */
+typedef struct {
+  int32_t count;       /* matrices, >= 1                                     */
+  int32_t rows, cols;  /* >= 1 each, dense rows                              */
+  int32_t steps;       /* 1 .. 32                                            */
+  int32_t dtype;       /* fal_dtype_t of x and out; of params in the update  */
+  float a, b, c;       /* finite; every singular value in [0, 1], and each
+                          step's factor of it, must stay below 2^20 through
+                          all steps                                          */
+  int64_t stride;      /* elements between matrices, >= rows * cols          */
+  int64_t out_stride;  /* ... of out; 0: as stride.  The update has none     */
+} fal_newton_schulz_t;
+
+/* Bytes of workspace the two calls below need (host only). */
+fal_status_t fal_newton_schulz_workspace_bytes(const fal_newton_schulz_t* shape, size_t* bytes);
+
+/*   x, out     device dtype; out may be x with its stride
+ *   workspace  device, 256-byte aligned
+ * A matrix of zeros gives zeros, one that holds an infinity or NaN gives NaN
+ * throughout.  Deterministic.
+ * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes or coefficients,
+ * misalignment or outputs that overlap another argument; FAL_ERR_UNSUPPORTED
+ * for matrices that pass 2^30 - 2^20 elements with both sides rounded up to
+ * 128; FAL_ERR_WORKSPACE; FAL_ERR_HIP when a launch fails. */
+fal_status_t fal_newton_schulz(const fal_newton_schulz_t* shape, const void* x, void* out, void* workspace,
+                               size_t ws_bytes, void* stream);
+
+typedef struct {
+  float lr;            /* >= 0                                               */
+  float beta;          /* of the momentum, in [0, 1)                         */
+  float weight_decay;  /* >= 0                                               */
+  float scale;         /* of the orthogonal update, >= 0                     */
+  int32_t nesterov;    /* 1: U = g + beta m; 0: U = m                        */
+} fal_muon_t;
+
+/* One update of a batch of weight matrices with orthogonal directions:
+ *   m = beta m + g;  U = g + beta m (or m);  X as above;
+ *   master = master (1 - lr weight_decay) - lr scale X.
+ *   master    device fp32, updated in place
+ *   params    device dtype: receives master rounded to it; NULL, or master with
+ *             FAL_F32: no copy
+ *   grads     device fp32, read only
+ *   momentum  device fp32, zero before the first step, updated in place
+ * All four lie alike: matrices [rows, cols], `stride` elements apart (the
+ * matrices of one kind in fal_param_layout's buffers are block_stride apart).
+ * Elements between them are left as they are.  Errors as fal_newton_schulz. */
+fal_status_t fal_muon_step(const fal_newton_schulz_t* shape, const fal_muon_t* hp, float* master, void* params,
+                           const float* grads, float* momentum, void* workspace, size_t ws_bytes, void* stream);
+
 /* fal_model_forward with the per-token scores in place of the loss: logp (and
  * entropy, or NULL) of tokens[:, 1:] as fal_token_logprobs defines them.
  *   mask  device uint8 [B, T] or NULL, over the T predicted tokens

@@ -1,7 +1,7 @@
 // Entry points of the C ABI that take no context, continued: the parts of a
 // gated block (head norms with rotated positions, the gated feed-forward
-// block) declared in include/fal.h.  Argument checks, then one call of the
-// launchers.
+// block) and orthogonal updates of its matrices, declared in include/fal.h.
+// Argument checks, then one call of the launchers.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -127,9 +127,107 @@ bool interleave_free(const void* a, const void* b, int64_t rows, int64_t ld_a, i
   return in >= width * es && in + width * es <= step;
 }
 
+// ---------------------------------------------------- orthogonal updates --
+NewtonSchulz schulz_args(const fal_newton_schulz_t* p) {
+  return {type_of(p->dtype), p->count, p->rows, p->cols, p->steps, p->a, p->b, p->c, p->stride,
+          p->out_stride ? p->out_stride : p->stride};
+}
+
+Refusal check_schulz(const fal_newton_schulz_t* p) {
+  if (!p) return {FAL_ERR_INVALID_ARG, "NULL shape"};
+  if (p->dtype != FAL_F32 && p->dtype != FAL_BF16) return {FAL_ERR_INVALID_ARG, "unknown dtype"};
+  if (p->count < 1 || p->rows < 1 || p->cols < 1) return {FAL_ERR_INVALID_ARG, "count, rows and cols must be >= 1"};
+  if (p->steps < 1 || p->steps > kMaxNewtonSteps) return {FAL_ERR_INVALID_ARG, "steps must lie in [1, 32]"};
+  if (!std::isfinite(p->a) || !std::isfinite(p->b) || !std::isfinite(p->c))
+    return {FAL_ERR_INVALID_ARG, "coefficients must be finite"};
+  // 32-bit byte offsets inside a 16-bit copy of a matrix
+  const int64_t r = ((int64_t)p->rows + 127) / 128 * 128, c = ((int64_t)p->cols + 127) / 128 * 128;
+  if (r * c > ((int64_t)1 << 30) - (1 << 20))
+    return {FAL_ERR_UNSUPPORTED, "matrices of more than 2^30 - 2^20 elements (sides rounded up to 128) are not supported"};
+  const int64_t one = (int64_t)p->rows * p->cols;
+  if (p->stride < one || (p->out_stride && p->out_stride < one))
+    return {FAL_ERR_INVALID_ARG, "stride or out_stride is smaller than a matrix"};
+  if (p->stride > kMaxExtent / p->count || p->out_stride > kMaxExtent / p->count)
+    return {FAL_ERR_INVALID_ARG, "count matrices at this stride exceed the address space"};
+  double sigma[kMaxNewtonSteps + 1];
+  if (!newton_schulz_bounds(schulz_args(p), sigma))
+    return {FAL_ERR_INVALID_ARG, "coefficients let singular values grow past 2^20"};
+  return kFine;
+}
+
+Extent matrices_of(const void* p, const fal_newton_schulz_t* s, int64_t stride, int64_t es) {
+  return {p, ((s->count - 1) * stride + (int64_t)s->rows * s->cols) * es};
+}
+
 }  // namespace
 
 extern "C" {
+
+fal_status_t fal_newton_schulz_workspace_bytes(const fal_newton_schulz_t* shape, size_t* bytes) {
+  return guarded([&] {
+    const Refusal no = check_schulz(shape);
+    if (no.why) return fail(no.st, no.why);
+    if (!bytes) return fail(FAL_ERR_INVALID_ARG, "NULL bytes");
+    *bytes = (size_t)newton_schulz_scratch(schulz_args(shape));
+    return FAL_OK;
+  });
+}
+
+fal_status_t fal_newton_schulz(const fal_newton_schulz_t* shape, const void* x, void* out, void* workspace,
+                               size_t ws_bytes, void* stream) {
+  return guarded([&] {
+    const Refusal no = check_schulz(shape);
+    if (no.why) return fail(no.st, no.why);
+    if (!x || !out) return fail(FAL_ERR_INVALID_ARG, "NULL x or out");
+    const int64_t es = element_bytes(shape->dtype);
+    if (!aligned(x, es) || !aligned(out, es)) return fail(FAL_ERR_INVALID_ARG, "x or out misaligned");
+    const int64_t need = newton_schulz_scratch(schulz_args(shape));
+    if (!workspace || ws_bytes < (size_t)need || !aligned(workspace, kWorkspaceAlign))
+      return fail(FAL_ERR_WORKSPACE, "workspace NULL, too small or not 256-byte aligned");
+    const NewtonSchulz n = schulz_args(shape);
+    const Extent a = matrices_of(x, shape, n.stride, es), o = matrices_of(out, shape, n.out_stride, es),
+                 ws = {workspace, need};
+    if ((!(out == x && n.out_stride == n.stride) && meets(o, {a})) || meets(ws, {a, o}))
+      return fail(FAL_ERR_INVALID_ARG, "out or the workspace overlaps another argument (out may only be x itself, with its stride)");
+    return launched(newton_schulz(n, nullptr, x, out, workspace, static_cast<hipStream_t>(stream)),
+                    "fal_newton_schulz");
+  });
+}
+
+fal_status_t fal_muon_step(const fal_newton_schulz_t* shape, const fal_muon_t* hp, float* master, void* params,
+                           const float* grads, float* momentum, void* workspace, size_t ws_bytes, void* stream) {
+  return guarded([&] {
+    const Refusal no = check_schulz(shape);
+    if (no.why) return fail(no.st, no.why);
+    if (!hp) return fail(FAL_ERR_INVALID_ARG, "NULL hyper-parameters");
+    for (float v : {hp->lr, hp->beta, hp->weight_decay, hp->scale})
+      if (!std::isfinite(v) || v < 0.f)
+        return fail(FAL_ERR_INVALID_ARG, "lr, beta, weight_decay and scale must be finite and >= 0");
+    if (hp->beta >= 1.f) return fail(FAL_ERR_INVALID_ARG, "beta must lie in [0, 1)");
+    if (shape->out_stride) return fail(FAL_ERR_INVALID_ARG, "out_stride must be 0 in an update");
+    if (hp->nesterov != 0 && hp->nesterov != 1) return fail(FAL_ERR_INVALID_ARG, "nesterov must be 0 or 1");
+    if (!master || !grads || !momentum) return fail(FAL_ERR_INVALID_ARG, "NULL master, grads or momentum");
+    if (params == master && shape->dtype == FAL_F32) params = nullptr;
+    const int64_t es = element_bytes(shape->dtype);
+    if (!aligned(master, 4) || !aligned(grads, 4) || !aligned(momentum, 4) || !aligned(params, es))
+      return fail(FAL_ERR_INVALID_ARG, "master, params, grads or momentum misaligned");
+    const int64_t need = newton_schulz_scratch(schulz_args(shape));
+    if (!workspace || ws_bytes < (size_t)need || !aligned(workspace, kWorkspaceAlign))
+      return fail(FAL_ERR_WORKSPACE, "workspace NULL, too small or not 256-byte aligned");
+    if (outputs_meet({matrices_of(master, shape, shape->stride, 4), matrices_of(params, shape, shape->stride, es),
+                      matrices_of(momentum, shape, shape->stride, 4), {workspace, need}},
+                     {matrices_of(grads, shape, shape->stride, 4)}))
+      return fail(FAL_ERR_INVALID_ARG, "master, params, momentum or the workspace overlaps another argument");
+    MuonArgs u;
+    u.grads = grads; u.momentum = momentum; u.master = master;
+    u.beta = hp->beta;
+    u.decay = (float)(1.0 - (double)hp->lr * hp->weight_decay);
+    u.step = (float)((double)hp->lr * hp->scale);
+    u.nesterov = hp->nesterov;
+    return launched(newton_schulz(schulz_args(shape), &u, nullptr, params, workspace, static_cast<hipStream_t>(stream)),
+                    "fal_muon_step");
+  });
+}
 
 fal_status_t fal_gated_ffn_workspace_bytes(const fal_gated_ffn_t* shape, size_t* forward, size_t* backward) {
   return guarded([&] {

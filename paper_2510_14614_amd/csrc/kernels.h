@@ -423,4 +423,30 @@ constexpr int64_t kAdamwMaxElems = (int64_t)0x7fffffff * 2048;
 hipError_t adamw_static_scratch(int lp_mode, float* master, void* lp, const float* g, float* m, float* v, int64_t n,
                                 float max_norm, const AdamwConsts& k, float* norm_out, hipStream_t s);
 
+// --------------------------------------------------- orthogonal updates ----
+// count matrices [rows, cols] (dense rows), `stride` elements apart (of out:
+// out_stride): X = U / |U|_F, then `steps` times X <- (a I + b X X^T + c (X X^T)^2) X (on the smaller
+// side).  Zeros stay zeros; a matrix that is not finite becomes NaN throughout.
+constexpr int kMaxNewtonSteps = 32;
+struct NewtonSchulz {
+  DType dt;  // of x and out
+  int count, rows, cols, steps;
+  float a, b, c;
+  int64_t stride, out_stride;
+};
+// With the update, U comes from gradient and momentum, and the weights move
+// against the result: m = beta m + g, U = g + beta m or m,
+// master = decay master - step X, out (NULL or dtype) its copy.
+struct MuonArgs {
+  const float* grads;
+  float *momentum, *master;
+  float beta, decay, step;
+  int nesterov;
+};
+bool newton_schulz_bounds(const NewtonSchulz& s, double* sigma);  // sigma: steps + 1 values
+// u NULL: out (may be x) from x.  scratch: newton_schulz_scratch bytes.
+hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x, void* out, void* scratch,
+                         hipStream_t stream);
+int64_t newton_schulz_scratch(const NewtonSchulz& s);
+
 }  // namespace fal

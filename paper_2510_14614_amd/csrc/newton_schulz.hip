@@ -1,0 +1,534 @@
+// Matrices made orthogonal by Newton-Schulz products, and the update that takes
+// its direction from them.
+//
+//   X_0 = U / |U|_F;   A = X X^T,  B = a I + b A + c A^2,  X <- B X   (steps times)
+//
+// on the smaller side p of a p x q matrix (a taller one is transposed on the way
+// in and out), so every singular value s goes through the same odd polynomial
+// a s + b s^3 + c s^5.  The update round it:
+//   m <- beta m + g,  U = g + beta m  (or m),  W <- W (1 - lr decay) - lr scale X.
+//
+// Bound by the matrix cores.  The polynomial multiplies small singular values by
+// a each step, 485 fold over five at the usual coefficients, and with them every
+// rounding of X; one 16-bit operand is too coarse for that, and fp32 MFMA run at
+// a sixteenth of the 16-bit rate.  So every matrix is kept as the sum of two fp16
+// ones, 22 bits, and a product is three MFMA: hi hi + hi lo + lo hi, in fp32.
+// fp16's narrow range is no matter here: the polynomial bounds each singular value,
+// and with them every element of X, A and B, so each is stored times a power of
+// two that takes its bound to fp16's largest values.
+// A and B are symmetric: only tiles on and below the diagonal are computed, the
+// others are written from them.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "common.h"
+#include "gemm_pipe.h"
+#include "kernels.h"
+
+namespace fal {
+
+namespace {
+
+typedef _Float16 half_t;
+typedef _Float16 halfx8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kTile = 128;      // tile sides; matrices are padded to it with zeros
+constexpr int kNormBlocksNs = 256;
+
+// A matrix of a batch: hi and lo parts, [count][rows][ld] each.
+struct Split {
+  half_t *hi, *lo;
+};
+
+__device__ __forceinline__ void split4(const float (&v)[4], uint2& hi, uint2& lo) {
+  union { half_t h[4]; uint2 w; } a, b;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    a.h[c] = static_cast<half_t>(v[c]);
+    b.h[c] = static_cast<half_t>(v[c] - static_cast<float>(a.h[c]));
+  }
+  hi = a.w;
+  lo = b.w;
+}
+__device__ __forceinline__ void join4(const uint2& hi, const uint2& lo, float (&v)[4]) {
+  union { uint2 w; half_t h[4]; } a{hi}, b{lo};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) v[c] = static_cast<float>(a.h[c]) + static_cast<float>(b.h[c]);
+}
+
+enum Product : int { GRAM = 0, POLY = 1, APPLY = 2, LAST = 3 };
+
+// What the last product writes: a dtype matrix, or the update of the weights.
+struct Result {
+  int rows, cols, flip;    // of the caller's matrices
+  int64_t stride;          // elements between them
+  void* out;               // dtype
+  int bf16_out;
+  float* master;           // update: out may be NULL
+  float decay, step;       // 1 - lr weight_decay, lr scale
+};
+
+struct NsArgs {
+  Split a, b, c;           // operands and result
+  Split d;                 // POLY: A, beside the product
+  int lda, ldb, ldc, ldd;
+  int64_t sa, sb, sc, sd;  // elements between the matrices of a batch
+  int K, tiles_m, tiles_n, per_matrix, total;
+  float scale;             // of the accumulators
+  float ca, cb;            // POLY: a and b, at the result's scale
+  Result r;
+};
+
+__device__ __forceinline__ double wave_sum_d(double v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, FAL_WAVE);
+  return v;
+}
+__device__ __forceinline__ double block_sum_d(double v, double* red) {
+  v = wave_sum_d(v);
+  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// ---------------------------------------------------------------- input --
+// What is made orthogonal: a dtype matrix, or momentum and gradient.
+struct Source {
+  const void* x;
+  int bf16_in;
+  const float* g;  // update: U = g + beta m, or m
+  float* m;
+  float beta;
+  int nesterov;
+  int rows, cols;
+  int64_t stride;
+};
+
+__device__ __forceinline__ float element(const Source& s, int64_t i) {
+  if (s.g) return s.nesterov ? fmaf(s.beta, s.m[i], s.g[i]) : s.m[i];
+  return s.bf16_in ? to_f(static_cast<const bf16*>(s.x)[i]) : static_cast<const float*>(s.x)[i];
+}
+
+// The momentum's update, and a workgroup's part of each matrix's sum of squares
+// in fp64.
+__global__ __launch_bounds__(256) void ns_norm(Source s, double* part) {
+  __shared__ double red[4];
+  const int64_t n = (int64_t)s.rows * s.cols, base = blockIdx.y * s.stride;
+  double sum = 0.0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    if (s.g) s.m[base + i] = fmaf(s.beta, s.m[base + i], s.g[base + i]);
+    const double v = element(s, base + i);
+    sum = fma(v, v, sum);
+  }
+  sum = block_sum_d(sum, red);
+  if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = sum;
+}
+
+// A 64 x 64 tile of X_0: U / |U|, transposed if its columns are the smaller side,
+// zeros in the padding.
+__global__ __launch_bounds__(256) void ns_first(Source s, const double* part, int nparts, int flip, Split x, int P,
+                                                int Q, float scale) {
+  __shared__ double red[4];
+  __shared__ float tile[64][65];
+  const int mat = blockIdx.z;
+  const double norm2 = block_sum_d((int)threadIdx.x < nparts ? part[mat * nparts + threadIdx.x] : 0.0, red);
+  // (zeros for a matrix of zeros; NaN throughout where U is not finite)
+  const double inv = norm2 == 0.0 ? 0.0 : norm2 <= 1.7e308 ? (double)scale / sqrt(norm2) : __builtin_nan("");
+  const int64_t base = mat * s.stride;
+  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;  // of X
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  for (int i = w; i < 64; i += 4) {
+    // element (r0 + i, c0 + lane) of U, or of X^T's tile
+    const int r = (flip ? c0 : r0) + i, c = (flip ? r0 : c0) + lane;
+    float v = 0.f;
+    if (r < s.rows && c < s.cols) v = (float)((double)element(s, base + (int64_t)r * s.cols + c) * inv);
+    if (flip) tile[lane][i] = v;
+    else tile[i][lane] = v;
+  }
+  __syncthreads();
+  for (int i = w * 4 + lane / 16; i < 64; i += 16) {
+    const int c = lane % 16 * 4;
+    const float v[4] = {tile[i][c], tile[i][c + 1], tile[i][c + 2], tile[i][c + 3]};
+    uint2 hi, lo;
+    split4(v, hi, lo);
+    const int64_t o = (int64_t)mat * P * Q + (int64_t)(r0 + i) * Q + c0 + c;
+    *reinterpret_cast<uint2*>(x.hi + o) = hi;
+    *reinterpret_cast<uint2*>(x.lo + o) = lo;
+  }
+}
+
+// ------------------------------------------------------------- products --
+// Row and column of tile t of a lower triangle, row by row.
+__device__ __forceinline__ void triangle(int t, int& r, int& c) {
+  r = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+  while (r * (r + 1) / 2 > t) --r;
+  while ((r + 1) * (r + 2) / 2 <= t) ++r;
+  c = t - r * (r + 1) / 2;
+}
+
+// Four consecutive elements (m, n .. n + 3) of the product.
+template <int MODE>
+__device__ __forceinline__ void put(const NsArgs& p, int mat, int m, int n, float (&v)[4]) {
+  if (MODE == LAST) return;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) v[c] *= p.scale;
+  if (MODE == POLY) {
+    const int64_t o = mat * p.sd + (int64_t)m * p.ldd + n;
+    float a[4];
+    join4(*reinterpret_cast<const uint2*>(p.d.hi + o), *reinterpret_cast<const uint2*>(p.d.lo + o), a);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] += fmaf(p.cb, a[c], m == n + c ? p.ca : 0.f);
+  }
+  uint2 hi, lo;
+  split4(v, hi, lo);
+  const int64_t o = mat * p.sc + (int64_t)m * p.ldc + n;
+  *reinterpret_cast<uint2*>(p.c.hi + o) = hi;
+  *reinterpret_cast<uint2*>(p.c.lo + o) = lo;
+}
+
+// One element of the last product, at the caller's row and column.
+__device__ __forceinline__ void put_last(const NsArgs& p, int mat, int r, int c, float v) {
+  if (r >= p.r.rows || c >= p.r.cols) return;
+  const int64_t o = mat * p.r.stride + (int64_t)r * p.r.cols + c;
+  v *= p.scale;
+  if (p.r.master) {
+    v = fmaf(p.r.master[o], p.r.decay, -p.r.step * v);
+    p.r.master[o] = v;
+    if (!p.r.out) return;
+  }
+  if (p.r.bf16_out) static_cast<bf16*>(p.r.out)[o] = from_f<bf16>(v);
+  else static_cast<float*>(p.r.out)[o] = v;
+}
+
+// A 128 x 128 tile of a product of split matrices: A k-contiguous, B
+// k-contiguous (GRAM, POLY: rows of the same matrix) or MN-major (X).  Four
+// wavefronts of 64 x 64; slices of 32 k of all four parts in two LDS stages,
+// the fragments of slice s + 1 read and slice s + 2 asked for under the 48 MFMA
+// of slice s.
+template <int MODE>
+__global__ __launch_bounds__(256, 2) void ns_product(NsArgs p) {
+  using namespace pipe;
+  constexpr int BK = MODE == GRAM || MODE == POLY;
+  constexpr int F = 4, WT = 64;
+  typedef Src<kTile, 1> SA;
+  typedef Src<kTile, BK> SB;
+  constexpr int REGION = SA::BYTES, SBYTES = 4 * REGION, L = 4 * SA::IPW;
+  static_assert(SB::BYTES == REGION, "regions");
+  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES];
+
+  const int bid = xcd_remap(blockIdx.x, p.total);
+  const int mat = bid / p.per_matrix, t = bid % p.per_matrix;
+  int tm, tn;
+  if (BK) triangle(t, tm, tn);
+  else grouped_tile(t, p.tiles_m, p.tiles_n, tm, tn);
+  const int m0 = tm * kTile, n0 = tn * kTile;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+
+  SA ah, al;
+  SB bh, bl;
+  auto as = [](const half_t* x) { return reinterpret_cast<const bf16*>(x); };
+  const int M = p.tiles_m * kTile, N = p.tiles_n * kTile;
+  ah.init(0, as(p.a.hi + mat * p.sa), p.lda, m0, M, p.K, wave, lane);
+  al.init(0, as(p.a.lo + mat * p.sa), p.lda, m0, M, p.K, wave, lane);
+  bh.init(0, as(p.b.hi + mat * p.sb), p.ldb, n0, N, p.K, wave, lane);
+  bl.init(0, as(p.b.lo + mat * p.sb), p.ldb, n0, N, p.K, wave, lane);
+  ah.clear(1);
+  al.clear(1);
+  bh.clear(1);
+  bl.clear(1);
+  const int n = p.K / KS;  // K is a multiple of the tile's side
+  auto issue = [&](char* stage, int s) {
+    if (s > 0 && s < n) {
+      ah.advance();
+      al.advance();
+      bh.advance();
+      bl.advance();
+    } else {
+      const int lim = s < n ? KS : 0;  // slices past the end: zeros
+      ah.set(0, 0, lim);
+      al.set(0, 0, lim);
+      bh.set(0, 0, lim);
+      bl.set(0, 0, lim);
+    }
+    ah.load(stage, wave);
+    al.load(stage + REGION, wave);
+    bh.load(stage + 2 * REGION, wave);
+    bl.load(stage + 3 * REGION, wave);
+  };
+  Frag<kTile, 1, F> fa;
+  Frag<kTile, BK, F> fb;
+  fa.init(wm * WT, lane);
+  fb.init(wn * WT, lane);
+  f32x4_t acc[F][F];
+#pragma unroll
+  for (int i = 0; i < F; ++i)
+#pragma unroll
+    for (int j = 0; j < F; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  halfx8_t ra[2][2][F], rb[2][2][F];
+  auto read = [&](const char* stage, int buf) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        ra[buf][h][i] = __builtin_bit_cast(halfx8_t, fa.read(stage + h * REGION, i));
+        rb[buf][h][i] = __builtin_bit_cast(halfx8_t, fb.read(stage + (2 + h) * REGION, i));
+      }
+  };
+  auto mma = [&](int buf) {
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rb[buf][q == 1][j], ra[buf][q == 0][i], acc[i][j], 0, 0, 0);
+  };
+  constexpr int NRD = 2 * F * (1 + (BK ? 1 : 2)), NMF = 3 * F * F;
+  constexpr int DMA_EVERY = (NMF - NRD) / L > 0 ? (NMF - NRD) / L : 1;
+  auto interleave = [&]() {
+    int dma = 0;
+#pragma unroll
+    for (int q = 0; q < NMF; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+      if (q < NRD) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
+      else if ((q - NRD) % DMA_EVERY == 0 && dma < L) {
+        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // buffer load to LDS
+        ++dma;
+      }
+    }
+  };
+  issue(st0, 0);
+  issue(st1, 1);
+  FAL_WAITCNT(L, 0);
+  bar();
+  read(st0, 0);
+  for (int s = 0; s < n; s += 2) {  // n is even
+    FAL_WAITCNT(0, 0);
+    bar();
+    __builtin_amdgcn_sched_barrier(0);
+    issue(st0, s + 2);
+    read(st1, 1);
+    mma(0);
+    interleave();
+    __builtin_amdgcn_sched_barrier(0);
+    FAL_WAITCNT(0, 0);
+    bar();
+    __builtin_amdgcn_sched_barrier(0);
+    issue(st1, s + 3);
+    read(st0, 0);
+    mma(1);
+    interleave();
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  FAL_WAITCNT(0, 0);
+  bar();
+
+  // Epilogue through a strip of 16 rows (or columns) a wavefront in LDS, so that
+  // consecutive lanes write consecutive elements.  Lane 16g + c of block (i, j)
+  // holds row 16i + c, columns 16j + 4g .. +3.
+  constexpr int PITCH = WT + 4;
+  float* strip = reinterpret_cast<float*>(st0) + wave * 16 * PITCH;
+  const int mw = m0 + wm * WT, nw = n0 + wn * WT, g = lane >> 4, cl = lane & 15;
+  const bool rows = MODE != LAST || !p.r.flip;
+  const bool cols = MODE == LAST ? p.r.flip : BK && tm != tn;
+  if (rows) {
+#pragma clang loop unroll(full)
+    for (int i = 0; i < F; ++i) {
+#pragma unroll
+      for (int j = 0; j < F; ++j)
+        *reinterpret_cast<float4*>(strip + cl * PITCH + 16 * j + 4 * g) =
+            make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+      wave_lds_order();
+      if (MODE == LAST) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) put_last(p, mat, mw + 16 * i + k, nw + lane, strip[k * PITCH + lane]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float4 q = *reinterpret_cast<const float4*>(strip + (4 * k + g) * PITCH + 4 * cl);
+          float v[4] = {q.x, q.y, q.z, q.w};
+          put<MODE>(p, mat, mw + 16 * i + 4 * k + g, nw + 4 * cl, v);
+        }
+      }
+      wave_lds_order();
+    }
+  }
+  if (cols) {
+#pragma clang loop unroll(full)
+    for (int j = 0; j < F; ++j) {
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) strip[(4 * g + e) * PITCH + 16 * i + cl] = acc[i][j][e];
+      wave_lds_order();
+      if (MODE == LAST) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) put_last(p, mat, nw + 16 * j + k, mw + lane, strip[k * PITCH + lane]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float4 q = *reinterpret_cast<const float4*>(strip + (4 * k + g) * PITCH + 4 * cl);
+          float v[4] = {q.x, q.y, q.z, q.w};
+          put<MODE>(p, mat, nw + 16 * j + 4 * k + g, mw + 4 * cl, v);
+        }
+      }
+      wave_lds_order();
+    }
+  }
+}
+
+// ---------------------------------------------------------------- sizes --
+int pad(int n) { return (n + kTile - 1) / kTile * kTile; }
+int64_t up(int64_t n) { return (n + 255) / 256 * 256; }
+
+struct Sizes {
+  int P, Q;
+  int64_t x, a;  // bytes of one matrix's X and A, one part
+  int chunk;     // matrices that go through together
+  int nparts;
+};
+
+// Matrices go through in batches that stay in the last-level cache (256 MB) where
+// more than one fits.
+Sizes sizes(const NewtonSchulz& s) {
+  Sizes z;
+  z.P = pad(std::min(s.rows, s.cols));
+  z.Q = pad(std::max(s.rows, s.cols));
+  z.x = (int64_t)z.P * z.Q * 2;
+  z.a = (int64_t)z.P * z.P * 2;
+  z.chunk = (int)std::min<int64_t>(s.count, std::max<int64_t>(1, ((int64_t)256 << 20) / (4 * z.x + 4 * z.a)));
+  z.nparts = (int)std::min<int64_t>(kNormBlocksNs, ((int64_t)s.rows * s.cols + 4095) / 4096);
+  return z;
+}
+
+// The power of two that takes values up to `bound` below fp16's largest.
+int exponent(double bound) { return std::min(40, (int)std::floor(std::log2(32768.0 / bound))); }
+
+// The largest |f(t)| of a quadratic c0 + c1 t + c2 t^2 on [0, top].
+double largest(double c0, double c1, double c2, double top) {
+  auto f = [&](double t) { return std::fabs(c0 + t * (c1 + t * c2)); };
+  double m = std::max(f(0.0), f(top));
+  const double t = c2 != 0.0 ? -c1 / (2.0 * c2) : -1.0;
+  return t > 0.0 && t < top ? std::max(m, f(t)) : m;
+}
+
+}  // namespace
+
+// Bounds of the singular values before each step (and after the last), of
+// sigma (a + b sigma^2 + c sigma^4) from sigma <= 1; false where they pass 2^20.
+bool newton_schulz_bounds(const NewtonSchulz& s, double* sigma) {
+  sigma[0] = 1.0 + 1e-6;
+  for (int k = 0; k < s.steps; ++k) {
+    const double a = s.a, b = s.b, c = s.c, top = sigma[k];
+    auto f = [&](double x) { return std::fabs(x * (a + x * x * (b + x * x * c))); };
+    double m = f(top);
+    // where a + 3 b t + 5 c t^2 = 0, t = sigma^2
+    const double disc = 9.0 * b * b - 20.0 * a * c;
+    double roots[2] = {-1.0, -1.0};
+    if (c != 0.0 && disc >= 0.0) {
+      roots[0] = (-3.0 * b + std::sqrt(disc)) / (10.0 * c);
+      roots[1] = (-3.0 * b - std::sqrt(disc)) / (10.0 * c);
+    } else if (c == 0.0 && b != 0.0) {
+      roots[0] = -a / (3.0 * b);
+    }
+    for (double t : roots)
+      if (t > 0.0 && t < top * top) m = std::max(m, f(std::sqrt(t)));
+    // (roundings move a singular value by far less than this)
+    sigma[k + 1] = m * (1.0 + 1e-3) + 1e-6;
+    if (!(sigma[k + 1] < 1048576.0) || !(largest(a, b, c, top * top) < 1048576.0)) return false;
+  }
+  return true;
+}
+
+int64_t newton_schulz_scratch(const NewtonSchulz& s) {
+  const Sizes z = sizes(s);
+  return up((int64_t)s.count * z.nparts * 8) + z.chunk * (4 * up(z.x) + 4 * up(z.a));
+}
+
+hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x, void* out, void* scratch,
+                         hipStream_t stream) {
+  const Sizes z = sizes(s);
+  double sigma[kMaxNewtonSteps + 1];
+  if (!newton_schulz_bounds(s, sigma)) return hipErrorInvalidValue;
+  const int flip = s.rows > s.cols;
+  double* part = static_cast<double*>(scratch);
+  char* base = static_cast<char*>(scratch) + up((int64_t)s.count * z.nparts * 8);
+  auto take = [&](int64_t bytes) {
+    half_t* t = reinterpret_cast<half_t*>(base);
+    base += bytes;
+    return t;
+  };
+  Split X[2], A, B;
+  for (Split* m : {&X[0], &X[1]}) { m->hi = take(z.chunk * up(z.x)); m->lo = take(z.chunk * up(z.x)); }
+  for (Split* m : {&A, &B}) { m->hi = take(z.chunk * up(z.a)); m->lo = take(z.chunk * up(z.a)); }
+
+  Source src;
+  memset(&src, 0, sizeof(src));
+  src.x = x;
+  src.bf16_in = s.dt == BF16;
+  src.rows = s.rows; src.cols = s.cols; src.stride = s.stride;
+  if (u) { src.g = u->grads; src.m = u->momentum; src.beta = u->beta; src.nesterov = u->nesterov; }
+  Result res;
+  memset(&res, 0, sizeof(res));
+  res.rows = s.rows; res.cols = s.cols; res.flip = flip; res.stride = u ? s.stride : s.out_stride;
+  res.out = out; res.bf16_out = s.dt == BF16;
+  if (u) { res.master = u->master; res.decay = u->decay; res.step = u->step; }
+
+  hipError_t e = hipSuccess;
+  for (int c0 = 0; c0 < s.count && e == hipSuccess; c0 += z.chunk) {
+    const int n = std::min(z.chunk, s.count - c0);
+    const int64_t at = c0 * s.stride;
+    Source in = src;
+    Result to = res;
+    if (u) { in.g += at; in.m += at; to.master += at; }
+    else in.x = static_cast<const char*>(x) + at * (s.dt == BF16 ? 2 : 4);
+    if (out) to.out = static_cast<char*>(out) + c0 * res.stride * (s.dt == BF16 ? 2 : 4);
+    hipLaunchKernelGGL(ns_norm, dim3(z.nparts, n), dim3(256), 0, stream, in, part);
+    int ex = exponent(sigma[0]);
+    hipLaunchKernelGGL(ns_first, dim3(z.Q / 64, z.P / 64, n), dim3(256), 0, stream, in, part, z.nparts, flip, X[0], z.P,
+                       z.Q, (float)std::ldexp(1.0, ex));
+    for (int k = 0; k < s.steps; ++k) {
+      const Split &x0 = X[k & 1], &x1 = X[~k & 1];
+      const double top = sigma[k] * sigma[k];
+      const int ea = exponent(top), eb = exponent(std::max(largest(s.a, s.b, s.c, top), std::fabs((double)s.a))),
+                en = exponent(sigma[k + 1]);
+      const int64_t sx = (int64_t)z.P * z.Q, sp = (int64_t)z.P * z.P;
+      const int tp = z.P / kTile, tq = z.Q / kTile;
+      NsArgs p;
+      memset(&p, 0, sizeof(p));
+      // A = X X^T
+      p.a = p.b = x0; p.lda = p.ldb = z.Q; p.sa = p.sb = sx; p.K = z.Q;
+      p.c = A; p.ldc = z.P; p.sc = sp;
+      p.tiles_m = p.tiles_n = tp; p.per_matrix = tp * (tp + 1) / 2; p.total = p.per_matrix * n;
+      p.scale = (float)std::ldexp(1.0, ea - 2 * ex);
+      hipLaunchKernelGGL(ns_product<GRAM>, dim3(p.total), dim3(256), 0, stream, p);
+      // B = a I + b A + c A A
+      p.a = p.b = p.d = A; p.lda = p.ldb = p.ldd = z.P; p.sa = p.sb = p.sd = sp; p.K = z.P;
+      p.c = B;
+      p.scale = (float)std::ldexp((double)s.c, eb - 2 * ea);
+      p.ca = (float)std::ldexp((double)s.a, eb);
+      p.cb = (float)std::ldexp((double)s.b, eb - ea);
+      hipLaunchKernelGGL(ns_product<POLY>, dim3(p.total), dim3(256), 0, stream, p);
+      // X <- B X
+      p.a = B; p.b = x0; p.ldb = z.Q; p.sb = sx;
+      p.c = x1; p.ldc = z.Q; p.sc = sx;
+      p.tiles_n = tq; p.per_matrix = tp * tq; p.total = p.per_matrix * n;
+      if (k + 1 < s.steps) {
+        p.scale = (float)std::ldexp(1.0, en - eb - ex);
+        hipLaunchKernelGGL(ns_product<APPLY>, dim3(p.total), dim3(256), 0, stream, p);
+      } else {
+        p.scale = (float)std::ldexp(1.0, -eb - ex);
+        p.r = to;
+        hipLaunchKernelGGL(ns_product<LAST>, dim3(p.total), dim3(256), 0, stream, p);
+      }
+      ex = en;
+    }
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace fal

@@ -36,6 +36,7 @@ ABI_FUNCTIONS = (
     "fal_preference_loss", "fal_model_logprobs", "fal_policy_step", "fal_preference_step",
     "fal_qk_norm_rope_workspace_bytes", "fal_qk_norm_rope_fwd", "fal_qk_norm_rope_bwd",
     "fal_gated_ffn_workspace_bytes", "fal_gated_ffn_fwd", "fal_gated_ffn_bwd",
+    "fal_newton_schulz_workspace_bytes", "fal_newton_schulz", "fal_muon_step",
 )
 PROF_GEMM, PROF_ATTN_FWD, PROF_ATTN_BWD, PROF_NORM, PROF_CE, PROF_EMBED, PROF_BIAS, PROF_OPTIM = range(8)
 PROF_NAMES = {PROF_GEMM: "gemm", PROF_ATTN_FWD: "attn_fwd", PROF_ATTN_BWD: "attn_bwd", PROF_NORM: "norm",
@@ -103,6 +104,20 @@ class fal_gated_ffn_t(ctypes.Structure):
 
 # Names of the gated block's activations, in the order of fal_gate_t.
 GATES = ("silu", "gelu_tanh", "gelu")
+
+
+class fal_newton_schulz_t(ctypes.Structure):
+    _fields_ = [("count", c_int32), ("rows", c_int32), ("cols", c_int32), ("steps", c_int32), ("dtype", c_int32),
+                ("a", c_float), ("b", c_float), ("c", c_float), ("stride", c_int64), ("out_stride", c_int64)]
+
+
+class fal_muon_t(ctypes.Structure):
+    _fields_ = [("lr", c_float), ("beta", c_float), ("weight_decay", c_float), ("scale", c_float),
+                ("nesterov", c_int32)]
+
+
+# A polynomial that takes singular values from 0.01 on near 1 in five steps.
+NEWTON_SCHULZ = (3.4444, -4.7750, 2.0315)
 
 
 class PolicyLoss(NamedTuple):
@@ -189,6 +204,10 @@ def lib():
         L.fal_gated_ffn_workspace_bytes.argtypes = [ffnp, POINTER(c_size_t), POINTER(c_size_t)]
         L.fal_gated_ffn_fwd.argtypes = [ffnp] + [c_void_p] * 7 + [c_size_t, c_void_p]
         L.fal_gated_ffn_bwd.argtypes = [ffnp] + [c_void_p] * 11 + [c_size_t, c_void_p]
+        nsp = POINTER(fal_newton_schulz_t)
+        L.fal_newton_schulz_workspace_bytes.argtypes = [nsp, POINTER(c_size_t)]
+        L.fal_newton_schulz.argtypes = [nsp] + [c_void_p] * 3 + [c_size_t, c_void_p]
+        L.fal_muon_step.argtypes = [nsp, POINTER(fal_muon_t)] + [c_void_p] * 5 + [c_size_t, c_void_p]
         L.fal_status_string.argtypes = [c_int32]
         L.fal_status_string.restype = c_char_p
         L.fal_last_error.argtypes = [c_void_p]
@@ -766,6 +785,89 @@ def gated_ffn_bwd(x, w_gate, w_up, w_down, saved, dy, activation="silu", dx=None
                                              w_up.data_ptr(), w_down.data_ptr(), saved.data_ptr(), dy.data_ptr(),
                                              _ptr(dx), *(_ptr(t) for t in dw), ws.data_ptr(), n, stream))
     return GatedFfnGrads(dx, *dw)
+
+
+@functools.lru_cache(maxsize=1024)
+def _schulz_workspace(*shape):
+    n = c_size_t()
+    _check_noctx(lib().fal_newton_schulz_workspace_bytes(byref(fal_newton_schulz_t(*shape)), byref(n)))
+    return n.value
+
+
+def _batch_stride(x, name):
+    """Elements between the contiguous matrices of a batch."""
+    if x.dim() not in (2, 3):
+        _refuse(f"{name} must be [rows, cols] or [count, rows, cols]")
+    rows, cols = x.shape[-2:]
+    if (cols > 1 and x.stride(-1) != 1) or (rows > 1 and x.stride(-2) != cols):
+        _refuse(f"the matrices of {name} must be contiguous")
+    return x.stride(0) if x.dim() == 3 and x.shape[0] > 1 else rows * cols
+
+
+def _schulz_shape(x, name, steps, coefficients, code):
+    """The call's shape: a matrix, or a batch of them at any equal spacing."""
+    stride = _batch_stride(x, name)
+    if len(coefficients) != 3:
+        _refuse("coefficients must be three numbers")
+    return (_clamp32(x.shape[0] if x.dim() == 3 else 1), *(_clamp32(n) for n in x.shape[-2:]), _clamp32(steps), code,
+            *coefficients, stride, 0)
+
+
+def _schulz_like(t, name, like, dtypes):
+    if t.dtype not in dtypes or t.device != like.device:
+        _refuse(f"{name} must be {' or '.join(str(d) for d in dtypes)} on {like.device}")
+    if t.shape != like.shape:
+        _refuse(f"{name} must have shape {tuple(like.shape)}, not {tuple(t.shape)}")
+    return _batch_stride(t, name)
+
+
+def newton_schulz(x, steps=5, coefficients=NEWTON_SCHULZ, out=None):
+    """Newton-Schulz products that make matrices orthogonal (fal_newton_schulz):
+    x / |x| through `steps` of X <- (a I + b X X^T + c (X X^T)^2) X.
+
+    x: [rows, cols] or [count, rows, cols], bfloat16 or float32, contiguous
+    matrices at any equal spacing.  Returns out, like x; out may be x."""
+    import torch
+    shape = _schulz_shape(x, "x", steps, coefficients, _dtype_code(x, "x"))
+    s = fal_newton_schulz_t(*shape)
+    with _call(x.device) as stream:
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        s.out_stride = _schulz_like(out, "out", x, (x.dtype,))
+        n = _schulz_workspace(*shape)
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+        _check_noctx(lib().fal_newton_schulz(byref(s), x.data_ptr(), out.data_ptr(), ws.data_ptr(), n, stream))
+    return out
+
+
+def muon_step(master, grads, momentum, params=None, *, lr=0.02, beta=0.95, weight_decay=0.0, nesterov=True, scale=None,
+              steps=5, coefficients=NEWTON_SCHULZ):
+    """One update of weight matrices with orthogonal directions (fal_muon_step):
+    momentum = beta momentum + grads, then master moves by -lr scale times the
+    orthogonal form of grads + beta momentum (of momentum itself without
+    nesterov), after its decay by lr weight_decay.  scale None: sqrt(max(1, cols /
+    rows)) of weights stored [in, out].
+
+    master, grads, momentum: float32 [rows, cols] or [count, rows, cols] with
+    equal strides, the first and the last updated in place; params: None, or a
+    bfloat16 or float32 copy to write, with the same strides.  Matrices of one
+    kind inside a context's flat buffers are such a batch."""
+    import torch
+    code = 0 if params is None else _dtype_code(params, "params")
+    shape = _schulz_shape(master, "master", steps, coefficients, code)
+    f32 = (torch.float32,)
+    for name, t, dtypes in (("master", master, f32), ("grads", grads, f32), ("momentum", momentum, f32),
+                            ("params", params, (torch.bfloat16, torch.float32))):
+        if t is not None and _schulz_like(t, name, master, dtypes) != shape[8]:
+            _refuse(f"{name} must lie as master does, {shape[8]} elements between matrices")
+    if scale is None:
+        scale = max(1.0, shape[2] / max(shape[1], 1)) ** 0.5
+    s, hp = fal_newton_schulz_t(*shape), fal_muon_t(lr, beta, weight_decay, scale, int(nesterov))
+    with _call(master.device) as stream:
+        n = _schulz_workspace(*shape)
+        ws = torch.empty(n, dtype=torch.uint8, device=master.device)
+        _check_noctx(lib().fal_muon_step(byref(s), byref(hp), master.data_ptr(), _ptr(params), grads.data_ptr(),
+                                         momentum.data_ptr(), ws.data_ptr(), n, stream))
 
 
 class Fal:

@@ -22,6 +22,13 @@ def message():
     return fal.lib().fal_last_error(None).decode()
 
 
+@pytest.fixture(autouse=True)
+def _clear_message():
+    yield
+    assert fal.lib().fal_qk_norm_rope_workspace_bytes(byref(norm()), byref(ctypes.c_size_t())) == fal.FAL_OK
+    assert message() == ""
+
+
 def refused(call, args, base, status, word):
     """call refuses args changed at some places (index -> value)."""
     full = list(base)
@@ -213,3 +220,77 @@ def test_gated_ffn_binding_refuses():
                            ((saved, x), {}, "GPU")]:
         with pytest.raises(ValueError, match=word):
             fal.gated_ffn_bwd(x, wg, wg, wd, *args, **kw)
+
+
+# --------------------------------------------------------------- orthogonal updates --
+def schulz(**kw):
+    v = dict(count=3, rows=100, cols=200, steps=5, dtype=1, a=3.4444, b=-4.775, c=2.0315, stride=20000, out_stride=0)
+    v.update(kw)
+    return fal.fal_newton_schulz_t(**v)
+
+
+def muon(**kw):
+    v = dict(lr=0.02, beta=0.95, weight_decay=0.01, scale=1.0, nesterov=1)
+    v.update(kw)
+    return fal.fal_muon_t(**v)
+
+
+def schulz_bytes(s):
+    n = ctypes.c_size_t()
+    assert fal.lib().fal_newton_schulz_workspace_bytes(byref(s), byref(n)) == fal.FAL_OK
+    return n.value
+
+
+@pytest.mark.parametrize("kw,status,word", [
+    (dict(count=0), BAD, "count"), (dict(rows=0), BAD, "rows"), (dict(cols=0), BAD, "cols"), (dict(steps=0), BAD, "steps"),
+    (dict(steps=33), BAD, "steps"), (dict(dtype=2), BAD, "dtype"), (dict(a=float("nan")), BAD, "finite"),
+    (dict(b=float("inf")), BAD, "finite"), (dict(a=1e30), BAD, "grow"), (dict(c=10.0), BAD, "grow"),
+    (dict(stride=19999), BAD, "stride"), (dict(out_stride=19999), BAD, "stride"), (dict(stride=1 << 46), BAD, "address space"),
+    (dict(out_stride=1 << 46), BAD, "address space"), (dict(rows=1 << 15, cols=1 << 15), UNSUP, "2^30"),
+    (dict(rows=1, cols=1 << 23), UNSUP, "2^30"),
+])
+def test_newton_schulz_refuses_a_shape(kw, status, word):
+    L, s, n = fal.lib(), schulz(**kw), ctypes.c_size_t()
+    assert L.fal_newton_schulz_workspace_bytes(byref(s), byref(n)) == status
+    assert word in message()
+    assert L.fal_newton_schulz(byref(s), A, B, C, 1 << 30, None) == status
+    assert L.fal_muon_step(byref(s), byref(muon()), A, B, C, D, E, 1 << 30, None) == status
+
+
+@pytest.mark.parametrize("args,status,word", [
+    ({0: None}, BAD, "NULL shape"), ({1: None}, BAD, "NULL"), ({2: None}, BAD, "NULL"), ({1: off(A, 1)}, BAD, "misaligned"),
+    ({2: off(B, 1)}, BAD, "misaligned"), ({2: off(A, 256)}, BAD, "overlaps"), ({2: C}, BAD, "overlaps"),
+    ({1: off(C, 256)}, BAD, "overlaps"), ({3: None}, WS, "workspace"), ({3: off(C, 64)}, WS, "workspace"),
+    ({4: 100000}, WS, "workspace"), ({0: byref(schulz(out_stride=20002)), 2: A}, BAD, "overlaps"),
+])
+def test_newton_schulz_refuses(args, status, word):
+    s = schulz()
+    refused(fal.lib().fal_newton_schulz, args, [byref(s), A, B, C, schulz_bytes(s), None], status, word)
+
+
+@pytest.mark.parametrize("args,status,word", [
+    ({0: None}, BAD, "NULL shape"), ({1: None}, BAD, "NULL"), *(({i: None}, BAD, "NULL") for i in (2, 4, 5)),
+    *(({i: off(A, 2)}, BAD, "misaligned") for i in (2, 4, 5)), ({3: off(B, 1)}, BAD, "misaligned"),
+    *(({1: byref(muon(**kw))}, BAD, word) for kw, word in (
+        (dict(lr=-1.0), "lr"), (dict(lr=float("nan")), "lr"), (dict(beta=1.0), "beta"), (dict(weight_decay=-0.1), "weight_decay"),
+        (dict(scale=float("inf")), "scale"), (dict(nesterov=2), "nesterov"))),
+    *(({3: p}, BAD, "overlaps") for p in (A, C, D, E)), ({2: C}, BAD, "overlaps"), ({2: D}, BAD, "overlaps"),
+    ({5: off(C, 128)}, BAD, "overlaps"), ({6: D}, BAD, "overlaps"), ({0: byref(schulz(out_stride=20000))}, BAD, "out_stride"),
+    ({6: None}, WS, "workspace"), ({6: off(E, 64)}, WS, "workspace"), ({7: 100000}, WS, "workspace"),
+])
+def test_muon_refuses(args, status, word):
+    s = schulz()
+    refused(fal.lib().fal_muon_step, args, [byref(s), byref(muon()), A, B, C, D, E, schulz_bytes(s), None], status, word)
+
+
+def test_newton_schulz_binding_refuses():
+    x = torch.zeros(3, 10, 20)
+    for t, kw, word in [(x[0, 0], {}, "x must be"), (x.half(), {}, "bfloat16"), (x.transpose(1, 2), {}, "contiguous"),
+                        (x, {"coefficients": (1.0, 2.0)}, "three"), (x, {"steps": 0}, "GPU")]:
+        with pytest.raises(ValueError, match=word):
+            fal.newton_schulz(t, **kw)
+    for kw, word in [({"grads": x[:2]}, "grads"), ({"grads": x.bfloat16()}, "grads"), ({"momentum": x.double()}, "momentum"),
+                     ({"params": x.half()}, "params"), ({"params": torch.zeros(3, 11, 20)[:, :10]}, "params"),
+                     ({"master": x.bfloat16()}, "master"), ({}, "GPU")]:
+        with pytest.raises(ValueError, match=word):
+            fal.muon_step(**{"master": x, "grads": x, "momentum": x, **kw})
