@@ -28,6 +28,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kMaxPairs = 64;  // half of the widest head
+constexpr int kBwdBlocks = 1024;  // of the backward, four workgroups a compute unit
 
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
@@ -279,21 +280,33 @@ __global__ __launch_bounds__(kWaves * 64) void head_norm_bwd(HeadNorm a, const T
 }
 
 // dw[e] = sum over workgroups of part[b][e], in fp64: 16 columns a workgroup,
-// 16 threads a column.
-__global__ __launch_bounds__(256) void head_norm_weights(const float* part, int nblk, int hd, float* dwq, float* dwk) {
-  __shared__ double red[16][17];
+// 64 threads a column, whose loads are all under way at once (16 threads a
+// column that waited for each took 17 us for 1024 rows of 128, these 5).
+__global__ __launch_bounds__(1024) void head_norm_weights(const float* part, int nblk, int hd, float* dwq, float* dwk) {
+  __shared__ double red[64][17];
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4, e = blockIdx.x * 16 + c;
+  float v[kBwdBlocks / 64];
+#pragma unroll
+  for (int i = 0; i < kBwdBlocks / 64; ++i) v[i] = r + 64 * i < nblk ? part[(int64_t)(r + 64 * i) * 2 * hd + e] : 0.f;
   double s = 0.0;
-  for (int b = r; b < nblk; b += 16) s += part[(int64_t)b * 2 * hd + e];
+#pragma unroll
+  for (int i = 0; i < kBwdBlocks / 64; ++i) s += v[i];
   red[r][c] = s;
   __syncthreads();
+  if (r >= 4) return;
+  s = red[r][c];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) s += red[r + 4 * i][c];
+  red[r][c] = s;
+  // (threads 0 .. 63 are one wavefront)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   if (r) return;
-  for (int i = 1; i < 16; ++i) s += red[i][c];
+  s = (red[0][c] + red[1][c]) + (red[2][c] + red[3][c]);
   float* out = e < hd ? dwq : dwk;
   if (out) out[e % hd] = (float)s;
 }
-
-constexpr int kBwdBlocks = 1024;  // four workgroups a compute unit
 
 int fwd_blocks(const HeadNorm& a) { return (int)std::min<int64_t>((a.tokens + kWaves - 1) / kWaves, 1 << 20); }
 int bwd_blocks(const HeadNorm& a) { return (int)std::min<int64_t>((a.tokens + kWaves - 1) / kWaves, kBwdBlocks); }
@@ -349,7 +362,7 @@ hipError_t head_norm_rope_bwd(DType dt, const HeadNorm& a, const void* x, const 
   }
 #undef FAL_BWD
   if (e != hipSuccess || !sums) return e;
-  hipLaunchKernelGGL(head_norm_weights, dim3(2 * a.hd / 16), dim3(256), 0, s, part, bwd_blocks(a), a.hd, dwq, dwk);
+  hipLaunchKernelGGL(head_norm_weights, dim3(2 * a.hd / 16), dim3(1024), 0, s, part, bwd_blocks(a), a.hd, dwq, dwk);
   return hipGetLastError();
 }
 

@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "common.h"
 #include "gemm_pipe.h"
@@ -34,7 +35,8 @@ typedef _Float16 half_t;
 typedef _Float16 halfx8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 128;      // tile sides; matrices are padded to it with zeros
-constexpr int kNormBlocksNs = 256;
+constexpr int kNormBlocksNs = 1024;
+constexpr int kOneRound = 256;  // tiles that have a compute unit each
 
 // A matrix of a batch: hi and lo parts, [count][rows][ld] each.
 struct Split {
@@ -67,6 +69,7 @@ struct Result {
   int bf16_out;
   float* master;           // update: out may be NULL
   float decay, step;       // 1 - lr weight_decay, lr scale
+  int vec;                 // rows of whole 16-byte groups
 };
 
 struct NsArgs {
@@ -111,15 +114,68 @@ __device__ __forceinline__ float element(const Source& s, int64_t i) {
 }
 
 // The momentum's update, and a workgroup's part of each matrix's sum of squares
-// in fp64.
+// in fp64.  VEC: matrices of whole 16-byte groups, taken four groups at a time so
+// that their loads are under way together.
+template <int VEC>
 __global__ __launch_bounds__(256) void ns_norm(Source s, double* part) {
   __shared__ double red[4];
   const int64_t n = (int64_t)s.rows * s.cols, base = blockIdx.y * s.stride;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   double sum = 0.0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    if (s.g) s.m[base + i] = fmaf(s.beta, s.m[base + i], s.g[base + i]);
-    const double v = element(s, base + i);
-    sum = fma(v, v, sum);
+  if (VEC && s.g) {
+    const float4* g = reinterpret_cast<const float4*>(s.g + base);
+    float4* m = reinterpret_cast<float4*>(s.m + base);
+    constexpr int N = 4;
+    for (int64_t i0 = at; i0 < n / 4; i0 += N * step) {
+      float4 gv[N], mv[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (i0 + k * step < n / 4) { gv[k] = g[i0 + k * step]; mv[k] = m[i0 + k * step]; }
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (i0 + k * step >= n / 4) break;
+        float4 v = mv[k];
+        v.x = fmaf(s.beta, v.x, gv[k].x); v.y = fmaf(s.beta, v.y, gv[k].y);
+        v.z = fmaf(s.beta, v.z, gv[k].z); v.w = fmaf(s.beta, v.w, gv[k].w);
+        m[i0 + k * step] = v;
+        if (s.nesterov) {
+          v.x = fmaf(s.beta, v.x, gv[k].x); v.y = fmaf(s.beta, v.y, gv[k].y);
+          v.z = fmaf(s.beta, v.z, gv[k].z); v.w = fmaf(s.beta, v.w, gv[k].w);
+        }
+        sum = fma((double)v.x, (double)v.x, fma((double)v.y, (double)v.y, sum));
+        sum = fma((double)v.z, (double)v.z, fma((double)v.w, (double)v.w, sum));
+      }
+    }
+  } else if (VEC) {
+    // 16 bytes: four fp32 or eight bf16
+    const uint4* x = static_cast<const uint4*>(s.x) + base / (s.bf16_in ? 8 : 4);
+    const int64_t n16 = n / (s.bf16_in ? 8 : 4);
+    constexpr int N = 4;
+    for (int64_t i0 = at; i0 < n16; i0 += N * step) {
+      uint4 q[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) q[k] = i0 + k * step < n16 ? x[i0 + k * step] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (s.bf16_in) {
+            const double lo = __uint_as_float(w[e] << 16), hi = __uint_as_float(w[e] & 0xFFFF0000u);
+            sum = fma(lo, lo, fma(hi, hi, sum));
+          } else {
+            const double v = __uint_as_float(w[e]);
+            sum = fma(v, v, sum);
+          }
+        }
+      }
+    }
+  } else {
+    for (int64_t i = at; i < n; i += step) {
+      if (s.g) s.m[base + i] = fmaf(s.beta, s.m[base + i], s.g[base + i]);
+      const double v = element(s, base + i);
+      sum = fma(v, v, sum);
+    }
   }
   sum = block_sum_d(sum, red);
   if (threadIdx.x == 0) part[blockIdx.y * gridDim.x + blockIdx.x] = sum;
@@ -132,7 +188,9 @@ __global__ __launch_bounds__(256) void ns_first(Source s, const double* part, in
   __shared__ double red[4];
   __shared__ float tile[64][65];
   const int mat = blockIdx.z;
-  const double norm2 = block_sum_d((int)threadIdx.x < nparts ? part[mat * nparts + threadIdx.x] : 0.0, red);
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < nparts; i += 256) sum += part[mat * nparts + i];
+  const double norm2 = block_sum_d(sum, red);
   // (zeros for a matrix of zeros; NaN throughout where U is not finite)
   const double inv = norm2 == 0.0 ? 0.0 : norm2 <= 1.7e308 ? (double)scale / sqrt(norm2) : __builtin_nan("");
   const int64_t base = mat * s.stride;
@@ -167,55 +225,97 @@ __device__ __forceinline__ void triangle(int t, int& r, int& c) {
   c = t - r * (r + 1) / 2;
 }
 
-// Four consecutive elements (m, n .. n + 3) of the product.
+// What the epilogue reads for four consecutive elements (r, c .. c + 3) of the
+// result, asked for ahead of their use: POLY's A, or the update's weights.
+struct Beside {
+  uint2 hi, lo;
+  float4 w;
+};
 template <int MODE>
-__device__ __forceinline__ void put(const NsArgs& p, int mat, int m, int n, float (&v)[4]) {
-  if (MODE == LAST) return;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) v[c] *= p.scale;
+__device__ __forceinline__ void ask(const NsArgs& p, int mat, int r, int c, Beside& b) {
   if (MODE == POLY) {
-    const int64_t o = mat * p.sd + (int64_t)m * p.ldd + n;
-    float a[4];
-    join4(*reinterpret_cast<const uint2*>(p.d.hi + o), *reinterpret_cast<const uint2*>(p.d.lo + o), a);
+    const int64_t o = mat * p.sd + (int64_t)r * p.ldd + c;
+    b.hi = *reinterpret_cast<const uint2*>(p.d.hi + o);
+    b.lo = *reinterpret_cast<const uint2*>(p.d.lo + o);
+  } else if (MODE == LAST && p.r.master && r < p.r.rows) {
+    const float* w = p.r.master + mat * p.r.stride + (int64_t)r * p.r.cols + c;
+    if (p.r.vec) {
+      if (c < p.r.cols) b.w = *reinterpret_cast<const float4*>(w);
+    } else {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < 4; ++c) v[c] += fmaf(p.cb, a[c], m == n + c ? p.ca : 0.f);
+      for (int e = 0; e < 4; ++e)
+        if (c + e < p.r.cols) v[e] = w[e];
+      b.w = make_float4(v[0], v[1], v[2], v[3]);
+    }
+  }
+}
+
+// Four consecutive elements of the result.
+template <int MODE>
+__device__ __forceinline__ void put(const NsArgs& p, int mat, int r, int c, const float4& acc, const Beside& b) {
+  float v[4] = {acc.x * p.scale, acc.y * p.scale, acc.z * p.scale, acc.w * p.scale};
+  if (MODE == LAST) {
+    if (r >= p.r.rows || c >= p.r.cols) return;
+    const int64_t o = mat * p.r.stride + (int64_t)r * p.r.cols + c;
+    if (p.r.master) {
+      v[0] = fmaf(b.w.x, p.r.decay, -p.r.step * v[0]);
+      v[1] = fmaf(b.w.y, p.r.decay, -p.r.step * v[1]);
+      v[2] = fmaf(b.w.z, p.r.decay, -p.r.step * v[2]);
+      v[3] = fmaf(b.w.w, p.r.decay, -p.r.step * v[3]);
+      if (p.r.vec) {
+        *reinterpret_cast<float4*>(p.r.master + o) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < p.r.cols) p.r.master[o + e] = v[e];
+      }
+      if (!p.r.out) return;
+    }
+    if (p.r.vec) {
+      if (p.r.bf16_out) st4(static_cast<bf16*>(p.r.out) + o, v);
+      else *reinterpret_cast<float4*>(static_cast<float*>(p.r.out) + o) = make_float4(v[0], v[1], v[2], v[3]);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (c + e >= p.r.cols) break;
+      if (p.r.bf16_out) static_cast<bf16*>(p.r.out)[o + e] = from_f<bf16>(v[e]);
+      else static_cast<float*>(p.r.out)[o + e] = v[e];
+    }
+    return;
+  }
+  if (MODE == POLY) {
+    float a[4];
+    join4(b.hi, b.lo, a);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += fmaf(p.cb, a[e], r == c + e ? p.ca : 0.f);
   }
   uint2 hi, lo;
   split4(v, hi, lo);
-  const int64_t o = mat * p.sc + (int64_t)m * p.ldc + n;
+  const int64_t o = mat * p.sc + (int64_t)r * p.ldc + c;
   *reinterpret_cast<uint2*>(p.c.hi + o) = hi;
   *reinterpret_cast<uint2*>(p.c.lo + o) = lo;
 }
 
-// One element of the last product, at the caller's row and column.
-__device__ __forceinline__ void put_last(const NsArgs& p, int mat, int r, int c, float v) {
-  if (r >= p.r.rows || c >= p.r.cols) return;
-  const int64_t o = mat * p.r.stride + (int64_t)r * p.r.cols + c;
-  v *= p.scale;
-  if (p.r.master) {
-    v = fmaf(p.r.master[o], p.r.decay, -p.r.step * v);
-    p.r.master[o] = v;
-    if (!p.r.out) return;
-  }
-  if (p.r.bf16_out) static_cast<bf16*>(p.r.out)[o] = from_f<bf16>(v);
-  else static_cast<float*>(p.r.out)[o] = v;
-}
-
 // A 128 x 128 tile of a product of split matrices: A k-contiguous, B
 // k-contiguous (GRAM, POLY: rows of the same matrix) or MN-major (X).  Four
-// wavefronts of 64 x 64; slices of 32 k of all four parts in two LDS stages,
-// the fragments of slice s + 1 read and slice s + 2 asked for under the 48 MFMA
-// of slice s.
-template <int MODE>
-__global__ __launch_bounds__(256, 2) void ns_product(NsArgs p) {
+// wavefronts of 64 x 64; slices of 32 k of all four parts in NS LDS stages, asked
+// for NS - 1 slices ahead, the fragments of slice s + 1 read under the 48 MFMA of
+// slice s.
+template <int MODE, int OCC, int NS>
+__global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   using namespace pipe;
   constexpr int BK = MODE == GRAM || MODE == POLY;
   constexpr int F = 4, WT = 64;
   typedef Src<kTile, 1> SA;
   typedef Src<kTile, BK> SB;
   constexpr int REGION = SA::BYTES, SBYTES = 4 * REGION, L = 4 * SA::IPW;
-  static_assert(SB::BYTES == REGION, "regions");
-  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES];
+  static_assert(SB::BYTES == REGION && (NS == 2 || NS == 4), "stages");
+  // one array a stage: the compiler tracks loads to LDS array by array
+  constexpr int LATER = NS == 4 ? SBYTES : 16;
+  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES], st2[LATER], st3[LATER];
+  auto stage_ptr = [&](int k) -> char* { return k == 0 ? st0 : k == 1 ? st1 : k == 2 ? st2 : st3; };
 
   const int bid = xcd_remap(blockIdx.x, p.total);
   const int mat = bid / p.per_matrix, t = bid % p.per_matrix;
@@ -300,84 +400,74 @@ __global__ __launch_bounds__(256, 2) void ns_product(NsArgs p) {
       }
     }
   };
-  issue(st0, 0);
-  issue(st1, 1);
-  FAL_WAITCNT(L, 0);
+#pragma unroll
+  for (int k = 0; k < NS; ++k) issue(stage_ptr(k), k);
+  FAL_WAITCNT(L * (NS - 1), 0);
   bar();
   read(st0, 0);
-  for (int s = 0; s < n; s += 2) {  // n is even
-    FAL_WAITCNT(0, 0);
-    bar();
-    __builtin_amdgcn_sched_barrier(0);
-    issue(st0, s + 2);
-    read(st1, 1);
-    mma(0);
-    interleave();
-    __builtin_amdgcn_sched_barrier(0);
-    FAL_WAITCNT(0, 0);
-    bar();
-    __builtin_amdgcn_sched_barrier(0);
-    issue(st1, s + 3);
-    read(st0, 0);
-    mma(1);
-    interleave();
-    __builtin_amdgcn_sched_barrier(0);
+  // Step s: own loads of slice s + 1 and own reads of slice s are done, barrier
+  // (slice s + 1 whole in LDS, slice s's stage free), slice s + NS into that
+  // stage, the MFMA of slice s under the reads of slice s + 1.  (n is a multiple
+  // of NS: K is one of 128)
+  for (int s = 0; s < n; s += NS) {
+#pragma unroll
+    for (int U = 0; U < NS; ++U) {
+      FAL_WAITCNT(L * (NS - 2), 0);
+      bar();
+      __builtin_amdgcn_sched_barrier(0);
+      issue(stage_ptr(U), s + U + NS);
+      read(stage_ptr((U + 1) % NS), (U + 1) & 1);
+      mma(U & 1);
+      interleave();
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
   FAL_WAITCNT(0, 0);
   bar();
 
   // Epilogue through a strip of 16 rows (or columns) a wavefront in LDS, so that
-  // consecutive lanes write consecutive elements.  Lane 16g + c of block (i, j)
+  // consecutive lanes hold consecutive elements.  Lane 16g + c of block (i, j)
   // holds row 16i + c, columns 16j + 4g .. +3.
   constexpr int PITCH = WT + 4;
   float* strip = reinterpret_cast<float*>(st0) + wave * 16 * PITCH;
   const int mw = m0 + wm * WT, nw = n0 + wn * WT, g = lane >> 4, cl = lane & 15;
-  const bool rows = MODE != LAST || !p.r.flip;
-  const bool cols = MODE == LAST ? p.r.flip : BK && tm != tn;
-  if (rows) {
+  // rows of the tile to rows of the result, or its columns to them
+  auto emit = [&](auto columns) {
+    constexpr bool COLS = decltype(columns)::value;
+    const int r0 = COLS ? nw : mw, c = (COLS ? mw : nw) + 4 * cl;
+    Beside beside[F][4];
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) ask<MODE>(p, mat, r0 + 16 * i + 4 * k + g, c, beside[i][k]);
 #pragma clang loop unroll(full)
     for (int i = 0; i < F; ++i) {
 #pragma unroll
-      for (int j = 0; j < F; ++j)
-        *reinterpret_cast<float4*>(strip + cl * PITCH + 16 * j + 4 * g) =
-            make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
-      wave_lds_order();
-      if (MODE == LAST) {
+      for (int j = 0; j < F; ++j) {
+        if (COLS) {
 #pragma unroll
-        for (int k = 0; k < 16; ++k) put_last(p, mat, mw + 16 * i + k, nw + lane, strip[k * PITCH + lane]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float4 q = *reinterpret_cast<const float4*>(strip + (4 * k + g) * PITCH + 4 * cl);
-          float v[4] = {q.x, q.y, q.z, q.w};
-          put<MODE>(p, mat, mw + 16 * i + 4 * k + g, nw + 4 * cl, v);
+          for (int e = 0; e < 4; ++e) strip[(4 * g + e) * PITCH + 16 * j + cl] = acc[j][i][e];
+        } else {
+          *reinterpret_cast<float4*>(strip + cl * PITCH + 16 * j + 4 * g) =
+              make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
         }
       }
       wave_lds_order();
-    }
-  }
-  if (cols) {
-#pragma clang loop unroll(full)
-    for (int j = 0; j < F; ++j) {
 #pragma unroll
-      for (int i = 0; i < F; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) strip[(4 * g + e) * PITCH + 16 * i + cl] = acc[i][j][e];
-      wave_lds_order();
-      if (MODE == LAST) {
-#pragma unroll
-        for (int k = 0; k < 16; ++k) put_last(p, mat, nw + 16 * j + k, mw + lane, strip[k * PITCH + lane]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float4 q = *reinterpret_cast<const float4*>(strip + (4 * k + g) * PITCH + 4 * cl);
-          float v[4] = {q.x, q.y, q.z, q.w};
-          put<MODE>(p, mat, nw + 16 * j + 4 * k + g, mw + 4 * cl, v);
-        }
-      }
+      for (int k = 0; k < 4; ++k)
+        put<MODE>(p, mat, r0 + 16 * i + 4 * k + g, c, *reinterpret_cast<const float4*>(strip + (4 * k + g) * PITCH + 4 * cl),
+                  beside[i][k]);
       wave_lds_order();
     }
-  }
+  };
+  if (MODE != LAST || !p.r.flip) emit(std::false_type());
+  if (MODE == LAST ? p.r.flip : BK && tm != tn) emit(std::true_type());
+}
+
+template <int MODE>
+void launch(const NsArgs& p, hipStream_t s) {
+  if (p.total <= kOneRound) hipLaunchKernelGGL((ns_product<MODE, 1, 4>), dim3(p.total), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((ns_product<MODE, 2, 2>), dim3(p.total), dim3(256), 0, s, p);
 }
 
 // ---------------------------------------------------------------- sizes --
@@ -391,15 +481,19 @@ struct Sizes {
   int nparts;
 };
 
-// Matrices go through in batches that stay in the last-level cache (256 MB) where
-// more than one fits.
+// Matrices go through in as few batches of one size as keep the workspace near 2
+// GiB (batches that fit the last-level cache instead, of 8 and 4 of 12 matrices of
+// 768 x 4608, took 220 us of a product's time where all 12 together take 105: what
+// counts is that a launch fills the chip).
 Sizes sizes(const NewtonSchulz& s) {
   Sizes z;
   z.P = pad(std::min(s.rows, s.cols));
   z.Q = pad(std::max(s.rows, s.cols));
   z.x = (int64_t)z.P * z.Q * 2;
   z.a = (int64_t)z.P * z.P * 2;
-  z.chunk = (int)std::min<int64_t>(s.count, std::max<int64_t>(1, ((int64_t)256 << 20) / (4 * z.x + 4 * z.a)));
+  const int64_t most = std::max<int64_t>(1, ((int64_t)2 << 30) / (4 * z.x + 4 * z.a));
+  const int64_t batches = (s.count + most - 1) / most;
+  z.chunk = (int)((s.count + batches - 1) / batches);
   z.nparts = (int)std::min<int64_t>(kNormBlocksNs, ((int64_t)s.rows * s.cols + 4095) / 4096);
   return z;
 }
@@ -477,6 +571,14 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
   res.out = out; res.bf16_out = s.dt == BF16;
   if (u) { res.master = u->master; res.decay = u->decay; res.step = u->step; }
 
+  auto whole = [](const void* q, int64_t bytes) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && bytes % 16 == 0; };
+  const int64_t es = s.dt == BF16 ? 2 : 4, each = (int64_t)s.rows * s.cols;
+  const bool vec_in = u ? whole(u->grads, each * 4) && whole(u->momentum, s.stride * 4)
+                        : whole(x, each * es) && s.stride * es % 16 == 0;
+  // four columns of every row at once
+  res.vec = s.cols % 4 == 0 && res.stride % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * es) == 0 &&
+            (!u || reinterpret_cast<uintptr_t>(u->master) % 16 == 0);
+
   hipError_t e = hipSuccess;
   for (int c0 = 0; c0 < s.count && e == hipSuccess; c0 += z.chunk) {
     const int n = std::min(z.chunk, s.count - c0);
@@ -486,7 +588,8 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
     if (u) { in.g += at; in.m += at; to.master += at; }
     else in.x = static_cast<const char*>(x) + at * (s.dt == BF16 ? 2 : 4);
     if (out) to.out = static_cast<char*>(out) + c0 * res.stride * (s.dt == BF16 ? 2 : 4);
-    hipLaunchKernelGGL(ns_norm, dim3(z.nparts, n), dim3(256), 0, stream, in, part);
+    if (vec_in) hipLaunchKernelGGL(ns_norm<1>, dim3(z.nparts, n), dim3(256), 0, stream, in, part);
+    else hipLaunchKernelGGL(ns_norm<0>, dim3(z.nparts, n), dim3(256), 0, stream, in, part);
     int ex = exponent(sigma[0]);
     hipLaunchKernelGGL(ns_first, dim3(z.Q / 64, z.P / 64, n), dim3(256), 0, stream, in, part, z.nparts, flip, X[0], z.P,
                        z.Q, (float)std::ldexp(1.0, ex));
@@ -504,25 +607,25 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
       p.c = A; p.ldc = z.P; p.sc = sp;
       p.tiles_m = p.tiles_n = tp; p.per_matrix = tp * (tp + 1) / 2; p.total = p.per_matrix * n;
       p.scale = (float)std::ldexp(1.0, ea - 2 * ex);
-      hipLaunchKernelGGL(ns_product<GRAM>, dim3(p.total), dim3(256), 0, stream, p);
+      launch<GRAM>(p, stream);
       // B = a I + b A + c A A
       p.a = p.b = p.d = A; p.lda = p.ldb = p.ldd = z.P; p.sa = p.sb = p.sd = sp; p.K = z.P;
       p.c = B;
       p.scale = (float)std::ldexp((double)s.c, eb - 2 * ea);
       p.ca = (float)std::ldexp((double)s.a, eb);
       p.cb = (float)std::ldexp((double)s.b, eb - ea);
-      hipLaunchKernelGGL(ns_product<POLY>, dim3(p.total), dim3(256), 0, stream, p);
+      launch<POLY>(p, stream);
       // X <- B X
       p.a = B; p.b = x0; p.ldb = z.Q; p.sb = sx;
       p.c = x1; p.ldc = z.Q; p.sc = sx;
       p.tiles_n = tq; p.per_matrix = tp * tq; p.total = p.per_matrix * n;
       if (k + 1 < s.steps) {
         p.scale = (float)std::ldexp(1.0, en - eb - ex);
-        hipLaunchKernelGGL(ns_product<APPLY>, dim3(p.total), dim3(256), 0, stream, p);
+        launch<APPLY>(p, stream);
       } else {
         p.scale = (float)std::ldexp(1.0, -eb - ex);
         p.r = to;
-        hipLaunchKernelGGL(ns_product<LAST>, dim3(p.total), dim3(256), 0, stream, p);
+        launch<LAST>(p, stream);
       }
       ex = en;
     }
