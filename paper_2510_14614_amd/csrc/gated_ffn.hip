@@ -262,6 +262,231 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
   }
 }
 
+// ---------------------------------------------------------- few rows --
+// Up to kFew rows of bf16 (single tokens of a few texts) are bound by reading the
+// weights once: 67 MB of a 2048 x 5504 block, 14 us at 4.9 TB/s, which tiles of 128
+// rows on the few compute units that their columns give took 107 us over.  Plain
+// fp32 FMA keep up: M FMA an element and 16 bytes a load.  A workgroup takes 64
+// columns (eight lanes of 16 bytes, whole 128-byte lines of the weight's rows) and
+// a range of k; each of its 64 groups of lanes takes every 64th k of it, asks for
+// its first eight rows of weights before anything else, and the groups are added
+// through LDS.
+// The ranges' sums go to scratch as fp32 and are added in order by whoever reads
+// them: the down-projection for g and u (it applies the activation itself, so h is
+// never rounded), a last small kernel for y.
+constexpr int kFew = 8;
+constexpr int kFewWaves = 8, kFewThreads = kFewWaves * 64, kFewGroups = kFewWaves * 8;
+constexpr int kFewBatch = 8;     // rows of weights a lane has under way
+constexpr int kFewSplits = 16;   // most ranges of the down-projection
+
+__device__ __forceinline__ void widen8(const uint4& q, float (&v)[8]) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+
+// One lane's rows of weights: every kFewGroups-th of [k, k1) from w on.
+struct FewRows {
+  uint4 q[kFewBatch];
+  __device__ __forceinline__ void load(const bf16* w, int64_t ld, int k, int k1) {
+#pragma unroll
+    for (int i = 0; i < kFewBatch; ++i)
+      q[i] = k + i * kFewGroups < k1 ? *reinterpret_cast<const uint4*>(w + (int64_t)i * kFewGroups * ld)
+                                     : make_uint4(0, 0, 0, 0);
+  }
+  // v[m][e] += rows of xs [k][M] times the weights
+  template <int M>
+  __device__ __forceinline__ void add(const float* xs, int k, int k1, float (&v)[M][8]) const {
+#pragma unroll
+    for (int i = 0; i < kFewBatch; ++i) {
+      if (k + i * kFewGroups >= k1) break;
+      float a[8];
+      widen8(q[i], a);
+      const float* x = xs + (k + i * kFewGroups) * M;
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[m][e] = fmaf(x[m], a[e], v[m][e]);
+    }
+  }
+};
+
+// Sums a workgroup's groups of lanes: v is this lane's share of columns 8 (lane %
+// 8) .. + 7; row m, column c of the sum goes to out[m * ld + c] (c < width).
+// Between the eight groups of a wavefront the lanes exchange halves, so that each
+// ends with one column of every row.
+template <int M>
+__device__ __forceinline__ void few_sum(float (&v)[M][8], float* lds, float* out, int64_t ld, int width) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool b0 = lane & 8, b1 = lane & 16, b2 = lane & 32;
+  const int col = lane % 8 * 8 + (b0 ? 4 : 0) + (b1 ? 2 : 0) + (b2 ? 1 : 0);
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    float w[4], x[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      w[e] = (b0 ? v[m][e + 4] : v[m][e]) + __shfl_xor(b0 ? v[m][e] : v[m][e + 4], 8, FAL_WAVE);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) x[e] = (b1 ? w[e + 2] : w[e]) + __shfl_xor(b1 ? w[e] : w[e + 2], 16, FAL_WAVE);
+    lds[(m * kFewWaves + wave) * 64 + col] = (b2 ? x[1] : x[0]) + __shfl_xor(b2 ? x[0] : x[1], 32, FAL_WAVE);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < M * 64; i += kFewThreads) {
+    const int c = i & 63, m = i >> 6;
+    const float* s = lds + m * kFewWaves * 64 + c;
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) t += s[w * 64];
+    if (c < width) out[m * ld + c] = t;
+  }
+  __syncthreads();
+}
+
+// part[range][0 .. 1][M][f]: g (blockIdx.z 0) or u over a range of `per` k.  (Both
+// in one workgroup took so many registers that a compute unit held one: 19.8 us
+// for five rows of 2048 x 5504, these 13.0.)
+template <int M>
+__global__ __launch_bounds__(kFewThreads, 4) void few_gate(Gated p, int per, float* part) {
+  __shared__ float lds[M * kFewWaves * 64];
+  extern __shared__ float xs[];  // [per][M]
+  const int k0 = blockIdx.y * per, n = min(p.K - k0, per);
+  const int lane = threadIdx.x & 63, group = (threadIdx.x >> 6) * 8 + lane / 8;
+  const int c = min((int)blockIdx.x * 64 + lane % 8 * 8, p.N - 8);  // (f is a multiple of 8)
+  const int64_t ld = blockIdx.z ? p.ldb1 : p.ldb0;
+  const bf16* w = (blockIdx.z ? p.b1 : p.b0) + (int64_t)(k0 + group) * ld + c;
+  FewRows rows;
+  rows.load(w, ld, group, n);
+  for (int i = threadIdx.x; i < n / 8 * M; i += kFewThreads) {  // (d is a multiple of 8, per of 64)
+    const int m = i % M, k = i / M * 8;
+    float v[8];
+    widen8(*reinterpret_cast<const uint4*>(p.a + m * p.lda + k0 + k), v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) xs[(k + e) * M + m] = v[e];
+  }
+  __syncthreads();
+  float v[M][8] = {};
+  for (int k = group;;) {
+    rows.add<M>(xs, k, n, v);
+    k += kFewBatch * kFewGroups;
+    if (k >= n) break;
+    w += (int64_t)kFewBatch * kFewGroups * ld;
+    rows.load(w, ld, k, n);
+  }
+  few_sum<M>(v, lds, part + ((int64_t)blockIdx.y * 2 + blockIdx.z) * M * p.N + blockIdx.x * 64, p.N,
+             p.N - (int)blockIdx.x * 64);
+}
+
+// part[range][M][d]: h Wd over a range of f, h from `splits` parts of g and u;
+// the first column of workgroups writes them to saved as well.  p.a unused; b0 Wd,
+// K f, N d.
+template <int M>
+__global__ __launch_bounds__(kFewThreads, 4) void few_down(Gated p, int per, const float* gu, int splits, float* part) {
+  __shared__ float lds[M * kFewWaves * 64];
+  extern __shared__ float hs[];  // [per][M]
+  const int k0 = blockIdx.y * per, n = min(p.K - k0, per);
+  const int lane = threadIdx.x & 63, group = (threadIdx.x >> 6) * 8 + lane / 8;
+  const bf16* w = p.b0 + (int64_t)(k0 + group) * p.ldb0 + min((int)blockIdx.x * 64 + lane % 8 * 8, p.N - 8);
+  FewRows down;
+  down.load(w, p.ldb0, group, n);
+  const int64_t mf = (int64_t)M * p.K;
+  for (int i = threadIdx.x; i < n / 4 * M; i += kFewThreads) {  // (f is a multiple of 8, per of 64)
+    const int m = i / (n / 4), k = i % (n / 4) * 4;
+    const float* s = gu + (int64_t)m * p.K + k0 + k;
+    float g[4] = {}, u[4] = {};
+    for (int r0 = 0; r0 < splits; r0 += 4) {
+      float4 pg[4], pu[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (r0 + r < splits) {
+          pg[r] = *reinterpret_cast<const float4*>(s + (r0 + r) * 2 * mf);
+          pu[r] = *reinterpret_cast<const float4*>(s + (r0 + r) * 2 * mf + mf);
+        } else {
+          pg[r] = pu[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        g[0] += pg[r].x; g[1] += pg[r].y; g[2] += pg[r].z; g[3] += pg[r].w;
+        u[0] += pu[r].x; u[1] += pu[r].y; u[2] += pu[r].z; u[3] += pu[r].w;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float a, da;
+      act_and_grad<false>(p.act, g[e], a, da);
+      hs[(k + e) * M + m] = a * u[e];
+    }
+    if (p.saved && blockIdx.x == 0) {
+      float* o = p.saved + (int64_t)m * 2 * p.K + k0 + k;
+      *reinterpret_cast<float4*>(o) = make_float4(g[0], g[1], g[2], g[3]);
+      *reinterpret_cast<float4*>(o + p.K) = make_float4(u[0], u[1], u[2], u[3]);
+    }
+  }
+  __syncthreads();
+  float v[M][8] = {};
+  for (int k = group;;) {
+    down.add<M>(hs, k, n, v);
+    k += kFewBatch * kFewGroups;
+    if (k >= n) break;
+    w += (int64_t)kFewBatch * kFewGroups * p.ldb0;
+    down.load(w, p.ldb0, k, n);
+  }
+  few_sum<M>(v, lds, part + (int64_t)blockIdx.y * M * p.N + blockIdx.x * 64, p.N, p.N - (int)blockIdx.x * 64);
+}
+
+// y[m][c] = sum of the parts, in order.
+__global__ __launch_bounds__(256) void few_out(const float* part, int splits, int M, int d, bf16* y, int64_t ldy) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= M * d) return;
+  float v[kFewSplits];
+#pragma unroll
+  for (int s = 0; s < kFewSplits; ++s) v[s] = s < splits ? part[(int64_t)s * M * d + i] : 0.f;
+  float t = v[0];
+#pragma unroll
+  for (int s = 1; s < kFewSplits; ++s) t += v[s];
+  y[(int64_t)(i / d) * ldy + i % d] = from_f<bf16>(t);
+}
+
+// How many ranges a product's k is cut into: as many rows as the workgroup's first
+// loads ask for, fewer where that leaves compute units without a workgroup, more
+// where the workgroups would not run all at once (2048 x 5504: 688 of 512 rows
+// 14.3 us, 344 of 1024 13.0); a range's rows have to fit LDS.
+constexpr int kFewSlots = 512;  // workgroups that run at once
+constexpr int kFewLds = 11264;  // floats of a range's rows: with the sums, 61 KB
+struct FewSplit {
+  int splits, per;
+};
+FewSplit few_split(int K, int strips, int M) {
+  int per = kFewGroups * kFewBatch;
+  while (per > 2 * kFewGroups && cdiv(K, per) * strips < 256) per /= 2;
+  while ((cdiv(K, per) > kFewSplits || (cdiv(K, per) * strips > kFewSlots && cdiv(K, 2 * per) * strips >= 256)) &&
+         2 * per * M <= kFewLds)
+    per *= 2;
+  return {cdiv(K, per), per};
+}
+FewSplit few_up(const GatedFfn& a) { return few_split(a.d, 2 * cdiv(a.f, 64), a.M); }
+FewSplit few_last(const GatedFfn& a) { return few_split(a.f, cdiv(a.d, 64), a.M); }
+
+bool few_rows(DType dt, const GatedFfn& a) {
+  return dt == BF16 && a.M <= kFew && few_last(a).splits <= kFewSplits;
+}
+
+template <int M>
+hipError_t few_fwd(const GatedFfn& a, Gated p, const bf16* wd, bf16* y, float* scratch, hipStream_t s) {
+  const FewSplit up = few_up(a), down = few_last(a);
+  float* gu = scratch;
+  float* part = scratch + (int64_t)up.splits * 2 * M * a.f;
+  hipLaunchKernelGGL((few_gate<M>), dim3(cdiv(a.f, 64), up.splits, 2), dim3(kFewThreads), up.per * M * 4, s, p, up.per,
+                     gu);
+  p.b0 = wd; p.ldb0 = a.ldd; p.N = a.d; p.K = a.f;
+  hipLaunchKernelGGL((few_down<M>), dim3(cdiv(a.d, 64), down.splits), dim3(kFewThreads), down.per * M * 4, s, p,
+                     down.per, gu, up.splits, part);
+  hipLaunchKernelGGL(few_out, dim3(cdiv((int64_t)M * a.d, 256)), dim3(256), 0, s, part, down.splits, M, a.d, y, a.ldy);
+  return hipGetLastError();
+}
+
 // fp32: h from g | u, and the backward's elementwise part (dh in dg's place).
 __global__ __launch_bounds__(256) void gate_fwd_f32(const float* gu, int64_t n, int f, int act, float* h) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -328,6 +553,8 @@ int64_t round_up(int64_t n) { return (n + 255) / 256 * 256; }
 }  // namespace
 
 int64_t gated_ffn_scratch(DType dt, const GatedFfn& a, int backward) {
+  if (!backward && few_rows(dt, a))
+    return 4 * a.M * ((int64_t)few_up(a).splits * 2 * a.f + (int64_t)few_last(a).splits * a.d);
   const int64_t one = round_up((int64_t)a.M * a.f * (dt == BF16 ? 2 : 4));
   return backward ? 3 * one : dt == BF16 ? one : 3 * one;
 }
@@ -344,6 +571,21 @@ hipError_t gated_ffn_fwd(DType dt, const GatedFfn& a, const void* x, const void*
     p.M = a.M; p.N = a.f; p.K = a.d; p.act = a.act;
     p.saved = saved;
     p.h = static_cast<bf16*>(h);
+    if (few_rows(dt, a)) {
+      const bf16* down = static_cast<const bf16*>(wd);
+      bf16* out = static_cast<bf16*>(y);
+      float* part = static_cast<float*>(scratch);
+      switch (a.M) {
+        case 1: return few_fwd<1>(a, p, down, out, part, s);
+        case 2: return few_fwd<2>(a, p, down, out, part, s);
+        case 3: return few_fwd<3>(a, p, down, out, part, s);
+        case 4: return few_fwd<4>(a, p, down, out, part, s);
+        case 5: return few_fwd<5>(a, p, down, out, part, s);
+        case 6: return few_fwd<6>(a, p, down, out, part, s);
+        case 7: return few_fwd<7>(a, p, down, out, part, s);
+        default: return few_fwd<8>(a, p, down, out, part, s);
+      }
+    }
     e = launch_gated<0>(p, s);
   } else {
     const int64_t n = (int64_t)a.M * a.f;

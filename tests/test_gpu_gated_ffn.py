@@ -140,6 +140,19 @@ def test_bf16_shapes(M, d, f):
     check("bf16", M, d, f, BF16, seed=M)
 
 
+@pytest.mark.parametrize("M", range(1, 10))
+@pytest.mark.parametrize("d,f", [(64, 256), (1000, 72), (136, 2744), (2048, 5504)])
+def test_few_rows(M, d, f):
+    check("few", M, d, f, BF16, ACTS[M % 3], pad=8 * (M % 2), seed=M)
+
+
+def test_few_rows_of_long_products():
+    """Ranges of k cut by what LDS holds of their rows, past 16 of them too."""
+    check("long", 8, 8, 20000, BF16)
+    check("long", 8, 24000, 8, BF16)
+    check("long", 8, 8, 24000, BF16)
+
+
 @pytest.mark.parametrize("M,d,f", [(1, 1, 1), (1, 63, 257), (2, 7, 33), (65, 65, 65), (130, 100, 301), (300, 33, 1000)])
 def test_fp32_shapes(M, d, f):
     check("fp32", M, d, f, F32, seed=M)
