@@ -75,8 +75,9 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
   typedef Src<BN, BWD> SB;
   constexpr int SBYTES = SA::BYTES + NB * SB::BYTES;
   constexpr int L = SA::IPW + NB * SB::IPW;
-  static_assert(NS == 4 && L * (NS - 2) <= 63, "stages");
-  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES], st2[SBYTES], st3[SBYTES];
+  static_assert((NS == 3 || NS == 4) && L * (NS - 2) <= 63, "stages");
+  // one array a stage: the compiler tracks loads to LDS array by array
+  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES], st2[SBYTES], st3[NS == 4 ? SBYTES : 16];
   auto stage_ptr = [&](int k) -> char* { return k == 0 ? st0 : k == 1 ? st1 : k == 2 ? st2 : st3; };
 
   int tmi, tni;
@@ -96,24 +97,21 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
     sc.init(0, p.b1, p.ldb1, n0, p.N, p.K, wave, lane);
     sc.clear(1);
   }
-  const int n = (p.K + KS - 1) / KS, full = p.K / KS;
+  const int n = (p.K + KS - 1) / KS;
+  // (no branch: slices past the end are out of both operands' ranges and read as
+  // zeros, so the main loop is one straight block)
+  sa.start(p.lda, m0, p.M, p.K);
+  sb.start(p.ldb0, n0, p.N, p.K);
+  if (NB == 2) sc.start(p.ldb1, n0, p.N, p.K);
   auto issue = [&](char* stage, int s) {
-    if (s > 0 && s < full) {
-      sa.advance();
-      sb.advance();
-      if (NB == 2) sc.advance();
-    } else {
-      // the first slice, a tail of K or one past the end (zeros)
-      const bool live = s < n;
-      const int k0 = live ? s * KS : 0;
-      const int lim = live ? min(KS, p.K - k0) : 0;
-      sa.set(0, k0, lim);
-      sb.set(0, k0, BWD ? lim : (live ? KS : 0));
-      if (NB == 2) sc.set(0, k0, live ? KS : 0);
-    }
+    sa.limit(p.K - s * KS);
+    sb.limit(p.K - s * KS);
     sa.load(stage, wave);
     sb.load(stage + SA::BYTES, wave);
     if (NB == 2) sc.load(stage + SA::BYTES + SB::BYTES, wave);
+    sa.advance();
+    sb.advance();
+    if (NB == 2) sc.advance();
   };
 
   Frag<BM, 1, FM> fa;
@@ -183,10 +181,11 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
   bar();
   read(st0, 0);
   // slices past the end load zeros in both operands and add nothing
-  const int tend = (n + NS - 1) / NS * NS;
-  for (int t = 0; t < tend; t += NS) {
+  constexpr int UNR = NS % 2 ? 2 * NS : NS;  // whole cycles of stages and of register buffers
+  const int tend = (n + UNR - 1) / UNR * UNR;
+  for (int t = 0; t < tend; t += UNR) {
 #pragma unroll
-    for (int U = 0; U < NS; ++U) {
+    for (int U = 0; U < UNR; ++U) {
       FAL_WAITCNT(L * (NS - 3), LGK);
       bar();
       __builtin_amdgcn_sched_barrier(0);
@@ -200,13 +199,28 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
   bar();
 
   // Epilogue: strips of 16 rows through LDS, so that consecutive lanes hold
-  // consecutive columns; g, u and dh meet in one lane.
+  // consecutive columns; g, u and dh meet in one lane.  A strip goes in units of
+  // up to four accesses; the backward asks for the g and u of a unit while it works on
+  // the one before (8192 x 5504: 340 us where each access waited for its own, 322 so).
   constexpr int PITCH = NB * WTN + 4, LPR = WTN / 4, RPI = 64 / LPR;
-  static_assert(2 * 16 * PITCH * 4 <= SBYTES, "epilogue staging exceeds a stage");
+  constexpr int APU = 16 / RPI < 4 ? 16 / RPI : 4, UPS = 16 / RPI / APU;  // accesses a unit, units a strip
+  static_assert(2 * 16 * PITCH * 4 <= SBYTES, "epilogue staging");
   float* strip = reinterpret_cast<float*>(wm ? st1 : st0) + wn * 16 * PITCH;
   const int rr = lane / LPR, cc = lane % LPR * 4;
   const int64_t nn = n0 + wn * WTN + cc;
   const int mw = m0 + wm * WTM;
+  float4 sg[2][APU], su[2][APU];
+  // (addresses past the matrix are held at its end: no branch between the loads)
+  const float* saved = p.saved + min(nn, (int64_t)p.N - 4);
+  auto ask = [&](int unit) {
+#pragma unroll
+    for (int k = 0; k < APU; ++k) {
+      const int64_t m = min(mw + (APU * unit + k) * RPI + rr, p.M - 1);
+      sg[unit & 1][k] = *reinterpret_cast<const float4*>(saved + m * 2 * p.N);
+      su[unit & 1][k] = *reinterpret_cast<const float4*>(saved + m * 2 * p.N + p.N);
+    }
+  };
+  if (BWD) ask(0);
 #pragma clang loop unroll(full)
   for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -217,19 +231,23 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
             make_float4(acc[b][i][j][0], acc[b][i][j][1], acc[b][i][j][2], acc[b][i][j][3]);
     wave_lds_order();
 #pragma unroll
-    for (int k = 0; k < 16 / RPI; ++k) {
-      const int r = k * RPI + rr;
+    for (int k = 0; k < APU * UPS; ++k) {
+      const int r = k * RPI + rr, unit = i * UPS + k / APU;
+      if (BWD && k % APU == 0 && unit + 1 < FM * UPS) ask(unit + 1);
       const int64_t m = mw + 16 * i + r;
       const float4 v0 = *reinterpret_cast<const float4*>(strip + r * PITCH + cc);
       float4 v1 = make_float4(0.f, 0.f, 0.f, 0.f);
       if (NB == 2) v1 = *reinterpret_cast<const float4*>(strip + r * PITCH + WTN + cc);
       // (f is a multiple of 8: a lane's four columns are all inside or none is)
-      if (m >= p.M || nn >= p.N) continue;
+      const bool in = m < p.M && nn < p.N;
       const int64_t o = m * p.N + nn;
       if (!BWD) {
-        if (p.saved) {
-          *reinterpret_cast<float4*>(p.saved + m * 2 * p.N + nn) = v0;
-          *reinterpret_cast<float4*>(p.saved + m * 2 * p.N + p.N + nn) = v1;
+        if (p.saved && in) {
+          // (read only by the backward: kept out of the caches)
+          __builtin_nontemporal_store(f32x4_t{v0.x, v0.y, v0.z, v0.w},
+                                      reinterpret_cast<f32x4_t*>(p.saved + m * 2 * p.N + nn));
+          __builtin_nontemporal_store(f32x4_t{v1.x, v1.y, v1.z, v1.w},
+                                      reinterpret_cast<f32x4_t*>(p.saved + m * 2 * p.N + p.N + nn));
         }
         const float g[4] = {v0.x, v0.y, v0.z, v0.w}, u[4] = {v1.x, v1.y, v1.z, v1.w};
         float h[4];
@@ -239,10 +257,9 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
           act_and_grad<false>(p.act, g[c], a, da);
           h[c] = a * u[c];
         }
-        st4(p.h + o, h);
+        if (in) st4(p.h + o, h);
       } else {
-        const float4 g4 = *reinterpret_cast<const float4*>(p.saved + m * 2 * p.N + nn);
-        const float4 u4 = *reinterpret_cast<const float4*>(p.saved + m * 2 * p.N + p.N + nn);
+        const float4 g4 = sg[unit & 1][k % APU], u4 = su[unit & 1][k % APU];
         const float dh[4] = {v0.x, v0.y, v0.z, v0.w}, g[4] = {g4.x, g4.y, g4.z, g4.w}, u[4] = {u4.x, u4.y, u4.z, u4.w};
         float h[4], dg[4], du[4];
 #pragma unroll
@@ -253,9 +270,11 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
           dg[c] = dh[c] * u[c] * da;
           du[c] = dh[c] * a;
         }
-        st4(p.h + o, h);
-        st4(p.dg + o, dg);
-        st4(p.du + o, du);
+        if (in) {
+          st4(p.h + o, h);
+          st4(p.dg + o, dg);
+          st4(p.du + o, du);
+        }
       }
     }
     wave_lds_order();
@@ -487,26 +506,70 @@ hipError_t few_fwd(const GatedFfn& a, Gated p, const bf16* wd, bf16* y, float* s
   return hipGetLastError();
 }
 
-// fp32: h from g | u, and the backward's elementwise part (dh in dg's place).
-__global__ __launch_bounds__(256) void gate_fwd_f32(const float* gu, int64_t n, int f, int act, float* h) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  const int64_t m = i / f, c = i % f;
-  float a, da;
-  act_and_grad<true>(act, gu[m * 2 * f + c], a, da);
-  h[i] = a * gu[m * 2 * f + f + c];
+// ------------------------------------------------ joined products --
+// Elementwise kernels after products whose k was split among workgroups (or, in
+// fp32, after whole ones): `parts` fp32 sums lie `stride` floats apart and are
+// added in order, four columns a thread where rows allow it (V 4, else 1).
+template <int V>
+__device__ __forceinline__ void sum_parts(const float* p, int parts, int64_t stride, float (&v)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = p[e];
+#pragma unroll 4
+  for (int i = 1; i < parts; ++i)
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] += p[i * stride + e];
 }
-__global__ __launch_bounds__(256) void gate_bwd_f32(const float* gu, int64_t n, int f, int act, float* dg, float* du,
-                                                    float* h) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+
+// h = act(g) u, g and u [M][f] parts; saved (g | u) may be NULL or, with one part,
+// where g and u are.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void join_gate(const float* g, const float* u, int64_t ld, int parts, int64_t stride,
+                                                 int64_t n, int f, int act, float* saved, T* h) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
   if (i >= n) return;
   const int64_t m = i / f, c = i % f;
-  const float u = gu[m * 2 * f + f + c], dh = dg[i];
-  float a, da;
-  act_and_grad<true>(act, gu[m * 2 * f + c], a, da);
-  h[i] = a * u;
-  dg[i] = dh * u * da;
-  du[i] = dh * a;
+  float gv[V], uv[V];
+  sum_parts<V>(g + m * ld + c, parts, stride, gv);
+  sum_parts<V>(u + m * ld + c, parts, stride, uv);
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    float a, da;
+    act_and_grad<sizeof(T) == 4>(act, gv[e], a, da);
+    h[i + e] = from_f<T>(a * uv[e]);
+    if (saved) {
+      saved[m * 2 * f + c + e] = gv[e];
+      saved[m * 2 * f + f + c + e] = uv[e];
+    }
+  }
+}
+
+// dg, du and h from parts of dh (one part may be dg) and the saved g | u.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void join_gate_bwd(const float* dh, int parts, int64_t stride, const float* saved,
+                                                     int64_t n, int f, int act, T* dg, T* du, T* h) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
+  if (i >= n) return;
+  const int64_t m = i / f, c = i % f;
+  float d[V];
+  sum_parts<V>(dh + i, parts, stride, d);
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float g = saved[m * 2 * f + c + e], u = saved[m * 2 * f + f + c + e];
+    float a, da;
+    act_and_grad<sizeof(T) == 4>(act, g, a, da);
+    h[i + e] = from_f<T>(a * u);
+    dg[i + e] = from_f<T>(d[e] * u * da);
+    du[i + e] = from_f<T>(d[e] * a);
+  }
+}
+
+// out[m][c] = the parts' sum (bf16, N a multiple of 8).
+__global__ __launch_bounds__(256) void join_rows(const float* part, int parts, int64_t n, int N, bf16* out, int64_t ldo) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  float v[4];
+  sum_parts<4>(part + i, parts, n, v);
+  st4(out + i / N * ldo + i % N, v);
 }
 
 GemmProblem product(const void* A, int64_t lda, const void* B, int64_t ldb, int M, int N, int K, void* out,
@@ -528,87 +591,178 @@ hipError_t run(DType dt, int a_kmaj, int b_kmaj, std::initializer_list<GemmProbl
   return gemm(dt, a_kmaj, b_kmaj, g, 0, s, &why, split, split_floats);
 }
 
-// The larger tile while it fills the chip (launch times as gemm()'s model has
-// them for tiles of the same size: 0.85 us a slice and 10 a round of 256; 0.54
-// and 3 a round of 512).
+dim3 blocks_of(int64_t n, int per) { return dim3((unsigned)((n + 256 * per - 1) / (256 * per))); }
+
+// The larger tile once it gives every compute unit one (8192 x 2048 x 5504, 2752
+// tiles: forward 412 us against the smaller one's 494, backward 322 against 333;
+// 1501 x 1000 x 2744, 132 of them: backward 64 against 49).  Tiles of 256 rows, one
+// workgroup a compute unit, whose epilogues nothing covers, took 474 and 386.
 template <int BWD>
 hipError_t launch_gated(Gated p, hipStream_t s) {
-  constexpr int BN = BWD ? 256 : 128, BNS = BWD ? 128 : 64;
-  auto tiles = [&](int bm, int bn) { return (int64_t)cdiv(p.M, bm) * cdiv(p.N, bn); };
-  const double ns = cdiv(p.K, pipe::KS);
-  const double large = cdiv(tiles(256, BN), 256) * (10.0 + ns * 0.85);
-  const int64_t small_tiles = tiles(128, BNS), rounds = small_tiles / 512, rest = small_tiles % 512;
-  const double small = rounds * (3.0 + ns * 0.54) + (rest ? 3.0 + ns * (rest > 256 ? 0.54 : 0.39) : 0.0);
-  const int bm = large <= small ? 256 : 128, bn = large <= small ? BN : BNS;
-  p.tiles_m = cdiv(p.M, bm);
-  p.tiles_n = cdiv(p.N, bn);
-  const dim3 grid((unsigned)tiles(bm, bn)), block(256);
-  if (large <= small) hipLaunchKernelGGL((gated_mfma<BWD, 256, BN, 1, 4>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((gated_mfma<BWD, 128, BNS, 2, 4>), grid, block, 0, s, p);
+  constexpr int BN = BWD ? 256 : 128;
+  const int64_t large = (int64_t)cdiv(p.M, 128) * cdiv(p.N, BN), small = (int64_t)cdiv(p.M, 128) * cdiv(p.N, BN / 2);
+  p.tiles_m = cdiv(p.M, 128);
+  p.tiles_n = cdiv(p.N, large >= 256 ? BN : BN / 2);
+  if (large >= 256)
+    hipLaunchKernelGGL((gated_mfma<BWD, 128, BN, 2, 3>), dim3((unsigned)large), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((gated_mfma<BWD, 128, BN / 2, 2, 4>), dim3((unsigned)small), dim3(256), 0, s, p);
   return hipGetLastError();
+}
+
+// bf16 products with few tiles of 128 x 128: k in up to `most` parts, each a problem
+// of its own in one launch, whose fp32 sums the kernel after them adds.  Parts of at
+// least 256 k, and no more of them than run at once (1501 x 1000 x 2744: 48 us whole,
+// 25 in four and 5 joined; dx, two products of that size, 91 us whole, 34 and 6).
+struct Cut {
+  int parts, per;
+};
+Cut cut(int M, int N, int K, int products, int most) {
+  const int64_t tiles = (int64_t)cdiv(M, 128) * cdiv(N, 128) * products;
+  for (int s = most; s > 1; s /= 2) {
+    const int per = (cdiv(K, s) + 63) / 64 * 64;
+    if (tiles * s <= 512 && per >= 256 && cdiv(K, per) == s) return {s, per};
+  }
+  return {1, K};
 }
 
 int64_t round_up(int64_t n) { return (n + 255) / 256 * 256; }
 
+// What a bf16 call cuts (parts 1: that product runs whole).
+struct Cuts {
+  Cut gate, down;  // forward: x Wg and x Wu, h Wd
+  Cut dh, dx;      // backward: dy Wd^T, each of dx's two products
+};
+Cuts cuts(const GatedFfn& a) {
+  return {cut(a.M, a.f, a.d, 2, 2), cut(a.M, a.d, a.f, 1, 4), cut(a.M, a.f, a.d, 1, 4), cut(a.M, a.d, a.f, 2, 2)};
+}
+// dx's two products are separate problems where that fills the chip better.
+bool dx_apart(const GatedFfn& a) { return (int64_t)cdiv(a.M, 128) * cdiv(a.d, 128) <= 256; }
+
 }  // namespace
 
 int64_t gated_ffn_scratch(DType dt, const GatedFfn& a, int backward) {
+  const int64_t one = round_up((int64_t)a.M * a.f * (dt == BF16 ? 2 : 4)), mf = (int64_t)a.M * a.f * 4,
+                md = (int64_t)a.M * a.d * 4;
+  if (dt == F32) return 3 * one;
   if (!backward && few_rows(dt, a))
     return 4 * a.M * ((int64_t)few_up(a).splits * 2 * a.f + (int64_t)few_last(a).splits * a.d);
-  const int64_t one = round_up((int64_t)a.M * a.f * (dt == BF16 ? 2 : 4));
-  return backward ? 3 * one : dt == BF16 ? one : 3 * one;
+  const Cuts k = cuts(a);
+  // the parts of one product are read before the next one's are written
+  if (!backward) return one + std::max(k.gate.parts > 1 ? 2 * k.gate.parts * mf : 0, k.down.parts > 1 ? k.down.parts * md : 0);
+  return 3 * one + std::max(k.dh.parts > 1 ? k.dh.parts * mf : 0, dx_apart(a) ? 2 * k.dx.parts * md : 0);
 }
 
 hipError_t gated_ffn_fwd(DType dt, const GatedFfn& a, const void* x, const void* wg, const void* wu, const void* wd,
                          void* y, float* saved, void* scratch, hipStream_t s) {
   hipError_t e;
   void* h = scratch;
-  if (dt == BF16) {
-    Gated p;
-    memset(&p, 0, sizeof(p));
-    p.a = static_cast<const bf16*>(x); p.b0 = static_cast<const bf16*>(wg); p.b1 = static_cast<const bf16*>(wu);
-    p.lda = a.ldx; p.ldb0 = a.ldg; p.ldb1 = a.ldu;
-    p.M = a.M; p.N = a.f; p.K = a.d; p.act = a.act;
-    p.saved = saved;
-    p.h = static_cast<bf16*>(h);
-    if (few_rows(dt, a)) {
-      const bf16* down = static_cast<const bf16*>(wd);
-      bf16* out = static_cast<bf16*>(y);
-      float* part = static_cast<float*>(scratch);
-      switch (a.M) {
-        case 1: return few_fwd<1>(a, p, down, out, part, s);
-        case 2: return few_fwd<2>(a, p, down, out, part, s);
-        case 3: return few_fwd<3>(a, p, down, out, part, s);
-        case 4: return few_fwd<4>(a, p, down, out, part, s);
-        case 5: return few_fwd<5>(a, p, down, out, part, s);
-        case 6: return few_fwd<6>(a, p, down, out, part, s);
-        case 7: return few_fwd<7>(a, p, down, out, part, s);
-        default: return few_fwd<8>(a, p, down, out, part, s);
-      }
-    }
-    e = launch_gated<0>(p, s);
-  } else {
-    const int64_t n = (int64_t)a.M * a.f;
+  const int64_t n = (int64_t)a.M * a.f, md = (int64_t)a.M * a.d;
+  if (dt == F32) {
     float* gu = saved ? saved : reinterpret_cast<float*>(static_cast<char*>(scratch) + round_up(n * 4));
-    e = run(F32, 1, 0, {product(x, a.ldx, wg, a.ldg, a.M, a.f, a.d, gu, 2 * (int64_t)a.f, 1),
-                        product(x, a.ldx, wu, a.ldu, a.M, a.f, a.d, gu + a.f, 2 * (int64_t)a.f, 1)}, s);
+    const int64_t ld = 2 * (int64_t)a.f;
+    e = run(F32, 1, 0, {product(x, a.ldx, wg, a.ldg, a.M, a.f, a.d, gu, ld, 1),
+                        product(x, a.ldx, wu, a.ldu, a.M, a.f, a.d, gu + a.f, ld, 1)}, s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(gate_fwd_f32, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, gu, n, a.f, a.act,
-                       static_cast<float*>(h));
+    if (a.f % 4 == 0)
+      hipLaunchKernelGGL((join_gate<float, 4>), blocks_of(n, 4), dim3(256), 0, s, gu, gu + a.f, ld, 1, 0, n, a.f, a.act,
+                         nullptr, static_cast<float*>(h));
+    else
+      hipLaunchKernelGGL((join_gate<float, 1>), blocks_of(n, 1), dim3(256), 0, s, gu, gu + a.f, ld, 1, 0, n, a.f, a.act,
+                         nullptr, static_cast<float*>(h));
     e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return run(F32, 1, 0, {product(h, a.f, wd, a.ldd, a.M, a.d, a.f, y, a.ldy, 1)}, s);
+  }
+  Gated p;
+  memset(&p, 0, sizeof(p));
+  const bf16* xb = static_cast<const bf16*>(x);
+  const bf16 *gate = static_cast<const bf16*>(wg), *up = static_cast<const bf16*>(wu), *down = static_cast<const bf16*>(wd);
+  p.a = xb; p.b0 = gate; p.b1 = up;
+  p.lda = a.ldx; p.ldb0 = a.ldg; p.ldb1 = a.ldu;
+  p.M = a.M; p.N = a.f; p.K = a.d; p.act = a.act;
+  p.saved = saved;
+  p.h = static_cast<bf16*>(h);
+  if (few_rows(dt, a)) {
+    bf16* out = static_cast<bf16*>(y);
+    float* part = static_cast<float*>(scratch);
+    switch (a.M) {
+      case 1: return few_fwd<1>(a, p, down, out, part, s);
+      case 2: return few_fwd<2>(a, p, down, out, part, s);
+      case 3: return few_fwd<3>(a, p, down, out, part, s);
+      case 4: return few_fwd<4>(a, p, down, out, part, s);
+      case 5: return few_fwd<5>(a, p, down, out, part, s);
+      case 6: return few_fwd<6>(a, p, down, out, part, s);
+      case 7: return few_fwd<7>(a, p, down, out, part, s);
+      default: return few_fwd<8>(a, p, down, out, part, s);
+    }
+  }
+  const Cuts k = cuts(a);
+  float* part = reinterpret_cast<float*>(static_cast<char*>(scratch) + round_up(n * 2));
+  if (k.gate.parts > 1) {
+    // (two parts: as many problems as a launch holds)
+    const int k1 = k.gate.per, k2 = a.d - k1;
+    e = run(BF16, 1, 0, {product(xb, a.ldx, gate, a.ldg, a.M, a.f, k1, part, a.f, 1),
+                         product(xb + k1, a.ldx, gate + k1 * a.ldg, a.ldg, a.M, a.f, k2, part + n, a.f, 1),
+                         product(xb, a.ldx, up, a.ldu, a.M, a.f, k1, part + 2 * n, a.f, 1),
+                         product(xb + k1, a.ldx, up + k1 * a.ldu, a.ldu, a.M, a.f, k2, part + 3 * n, a.f, 1)}, s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((join_gate<bf16, 4>), blocks_of(n, 4), dim3(256), 0, s, part, part + 2 * n, a.f, 2, n, n, a.f,
+                       a.act, saved, p.h);
+    e = hipGetLastError();
+  } else {
+    e = launch_gated<0>(p, s);
   }
   if (e != hipSuccess) return e;
-  return run(dt, 1, 0, {product(h, a.f, wd, a.ldd, a.M, a.d, a.f, y, a.ldy, dt == F32)}, s);
+  if (k.down.parts == 1) return run(BF16, 1, 0, {product(h, a.f, wd, a.ldd, a.M, a.d, a.f, y, a.ldy, 0)}, s);
+  GemmGroup g;
+  memset(&g, 0, sizeof(g));
+  for (; g.n < k.down.parts; ++g.n) {
+    const int k0 = g.n * k.down.per;
+    g.p[g.n] = product(p.h + k0, a.f, down + k0 * a.ldd, a.ldd, a.M, a.d, std::min(k.down.per, a.f - k0),
+                       part + g.n * md, a.d, 1);
+  }
+  const char* why;
+  e = gemm(BF16, 1, 0, g, 0, s, &why);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(join_rows, blocks_of(md, 4), dim3(256), 0, s, part, g.n, md, a.d, static_cast<bf16*>(y), a.ldy);
+  return hipGetLastError();
 }
 
 hipError_t gated_ffn_bwd(DType dt, const GatedFfn& a, const void* x, const void* wg, const void* wu, const void* wd,
                          const float* saved, const void* dy, void* dx, void* dwg, void* dwu, void* dwd, void* scratch,
                          hipStream_t s) {
-  const int64_t n = (int64_t)a.M * a.f, one = round_up(n * (dt == BF16 ? 2 : 4));
+  const int64_t n = (int64_t)a.M * a.f, md = (int64_t)a.M * a.d, one = round_up(n * (dt == BF16 ? 2 : 4));
   char* base = static_cast<char*>(scratch);
   void *dg = base, *du = base + one, *h = base + 2 * one;
+  float* part = reinterpret_cast<float*>(base + 3 * one);
+  const Cuts k = cuts(a);
+  const char* why;
   hipError_t e;
-  if (dt == BF16) {
+  if (dt == F32) {
+    e = run(F32, 1, 1, {product(dy, a.ldy, wd, a.ldd, a.M, a.f, a.d, dg, a.f, 1)}, s);
+    if (e != hipSuccess) return e;
+    float *g32 = static_cast<float*>(dg), *u32 = static_cast<float*>(du), *h32 = static_cast<float*>(h);
+    if (a.f % 4 == 0)
+      hipLaunchKernelGGL((join_gate_bwd<float, 4>), blocks_of(n, 4), dim3(256), 0, s, g32, 1, 0, saved, n, a.f, a.act, g32,
+                         u32, h32);
+    else
+      hipLaunchKernelGGL((join_gate_bwd<float, 1>), blocks_of(n, 1), dim3(256), 0, s, g32, 1, 0, saved, n, a.f, a.act, g32,
+                         u32, h32);
+    e = hipGetLastError();
+  } else if (k.dh.parts > 1) {
+    GemmGroup g;
+    memset(&g, 0, sizeof(g));
+    for (; g.n < k.dh.parts; ++g.n) {
+      const int k0 = g.n * k.dh.per;
+      g.p[g.n] = product(static_cast<const bf16*>(dy) + k0, a.ldy, static_cast<const bf16*>(wd) + k0, a.ldd, a.M, a.f,
+                         std::min(k.dh.per, a.d - k0), part + g.n * n, a.f, 1);
+    }
+    e = gemm(BF16, 1, 1, g, 0, s, &why);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((join_gate_bwd<bf16, 4>), blocks_of(n, 4), dim3(256), 0, s, part, g.n, n, saved, n, a.f, a.act,
+                       static_cast<bf16*>(dg), static_cast<bf16*>(du), static_cast<bf16*>(h));
+    e = hipGetLastError();
+  } else {
     Gated p;
     memset(&p, 0, sizeof(p));
     p.a = static_cast<const bf16*>(dy); p.b0 = static_cast<const bf16*>(wd);
@@ -617,15 +771,26 @@ hipError_t gated_ffn_bwd(DType dt, const GatedFfn& a, const void* x, const void*
     p.saved = const_cast<float*>(saved);
     p.h = static_cast<bf16*>(h); p.dg = static_cast<bf16*>(dg); p.du = static_cast<bf16*>(du);
     e = launch_gated<1>(p, s);
-  } else {
-    e = run(F32, 1, 1, {product(dy, a.ldy, wd, a.ldd, a.M, a.f, a.d, dg, a.f, 1)}, s);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(gate_bwd_f32, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, saved, n, a.f, a.act,
-                       static_cast<float*>(dg), static_cast<float*>(du), static_cast<float*>(h));
-    e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
-  if (dx) {
+  if (dx && dt == BF16 && dx_apart(a)) {
+    GemmGroup g;
+    memset(&g, 0, sizeof(g));
+    const bf16 *d[2] = {static_cast<const bf16*>(dg), static_cast<const bf16*>(du)};
+    const bf16 *w[2] = {static_cast<const bf16*>(wg), static_cast<const bf16*>(wu)};
+    const int64_t ld[2] = {a.ldg, a.ldu};
+    for (int b = 0; b < 2; ++b)
+      for (int i = 0; i < k.dx.parts; ++i, ++g.n) {
+        const int k0 = i * k.dx.per;
+        g.p[g.n] = product(d[b] + k0, a.f, w[b] + k0, ld[b], a.M, a.d, std::min(k.dx.per, a.f - k0), part + g.n * md, a.d,
+                           1);
+      }
+    e = gemm(BF16, 1, 1, g, 0, s, &why);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(join_rows, blocks_of(md, 4), dim3(256), 0, s, part, g.n, md, a.d, static_cast<bf16*>(dx), a.lddx);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  } else if (dx) {
     GemmProblem p = product(dg, a.f, wg, a.ldg, a.M, a.d, a.f, dx, a.lddx, dt == F32);
     p.A2 = du; p.lda2 = a.f; p.B2 = wu; p.ldb2 = a.ldu; p.K2 = a.f;
     e = run(dt, 1, 1, {p}, s);

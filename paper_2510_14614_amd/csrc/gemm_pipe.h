@@ -160,8 +160,22 @@ struct Src {
 #pragma unroll
     for (int v = 0; v < NV; ++v) vo[v] = bad ? kOob : (seg ? voff[1][v] : voff[0][v]);
   }
+  // set() to the first slice of segment 0 of an operand below 2 GiB, for kernels
+  // whose state only advances from there.  Its bytes are counted without init()'s
+  // 64-bit minimum: that is left in a vector register, uniform as it is, and a load
+  // whose descriptor holds it becomes a loop over lanes.
+  __device__ __forceinline__ void start(int64_t ld, int r0, int Rmax, int Kseg) {
+    set(0, 0, W);
+    rn = KMAJ ? (int)((Rmax - r0) * ld * 2) : (int)((Kseg * ld - r0) * 2);
+  }
   // Next slice of the same segment (full and live).
   __device__ __forceinline__ void advance() { so += W * ks; }
+  // Chunks of segment 0 at slice offset >= lim out of range from here on
+  // (k-contiguous operands; an MN-major one's rows past K are out of its buffer's
+  // range by themselves).
+  __device__ __forceinline__ void limit(int lim) {
+    if (KMAJ) vo[0] = kof >= lim ? kOob : voff[0][0];
+  }
   // Issue this wavefront's loads of the current slice into the region at dst.
   __device__ __forceinline__ void load(char* dst, int wave) const {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(

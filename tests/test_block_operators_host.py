@@ -173,7 +173,7 @@ def test_gated_ffn_forward_refuses(args, status, word):
     *(({7: p}, BAD, "overlaps") for p in (A, B, C, D, E, F, H, I, J, K)),
     *(({10: p}, BAD, "overlaps") for p in (A, B, C, D, E, F, G, H, I, K)),
     ({9: H}, BAD, "overlaps"), ({9: off(H, 128)}, BAD, "overlaps"), ({11: E}, BAD, "overlaps"),
-    ({11: None}, WS, "workspace"), ({11: off(K, 64)}, WS, "workspace"), ({12: 3 * 300 * 128 * 2 - 1}, WS, "workspace"),
+    ({11: None}, WS, "workspace"), ({11: off(K, 64)}, WS, "workspace"), ({12: 3 * 300 * 128 * 2}, WS, "workspace"),
 ])
 def test_gated_ffn_backward_refuses(args, status, word):
     s = ffn()
@@ -198,7 +198,11 @@ def test_gated_ffn_halves_of_one_gradient():
 
 def test_gated_ffn_workspace():
     r = lambda n: (n + 255) // 256 * 256  # noqa: E731
-    assert ffn_bytes(ffn()) == (300 * 128 * 2, 3 * 300 * 128 * 2)
+    # h; dg, du and h, and two fp32 parts of dx
+    assert ffn_bytes(ffn()) == (300 * 128 * 2, 3 * 300 * 128 * 2 + 2 * 300 * 64 * 4)
+    # tiles that fill the chip: dx in one launch
+    big = ffn(rows=8192, d_model=2048, ld_x=2048, ld_y=2048, ld_down=2048, d_ff=2048, ld_gate=2048, ld_up=2048)
+    assert ffn_bytes(big) == (8192 * 2048 * 2, 3 * 8192 * 2048 * 2)
     assert ffn_bytes(ffn(dtype=0, grad_dtype=0, d_ff=101)) == (3 * r(300 * 101 * 4),) * 2
     assert fal.lib().fal_gated_ffn_workspace_bytes(byref(ffn()), None, None) == fal.FAL_OK
 

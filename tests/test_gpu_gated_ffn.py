@@ -146,6 +146,13 @@ def test_few_rows(M, d, f):
     check("few", M, d, f, BF16, ACTS[M % 3], pad=8 * (M % 2), seed=M)
 
 
+@pytest.mark.parametrize("M,d,f", [(40, 2048, 256), (40, 256, 2048), (100, 1000, 1096), (500, 1000, 520),
+                                   (1501, 1000, 2744), (130, 520, 4096)])
+def test_products_cut_along_k(M, d, f):
+    """Few tiles and long sums: parts of k in workgroups of their own."""
+    check("cut", M, d, f, BF16, ACTS[M % 3], pad=8, seed=M)
+
+
 def test_few_rows_of_long_products():
     """Ranges of k cut by what LDS holds of their rows, past 16 of them too."""
     check("long", 8, 8, 20000, BF16)
