@@ -298,6 +298,20 @@ __device__ __forceinline__ void put(const NsArgs& p, int mat, int r, int c, cons
   *reinterpret_cast<uint2*>(p.c.lo + o) = lo;
 }
 
+// One element of the last product.
+__device__ __forceinline__ void put_one(const NsArgs& p, int mat, int r, int c, float v) {
+  if (r >= p.r.rows || c >= p.r.cols) return;
+  const int64_t o = mat * p.r.stride + (int64_t)r * p.r.cols + c;
+  v *= p.scale;
+  if (p.r.master) {
+    v = fmaf(p.r.master[o], p.r.decay, -p.r.step * v);
+    p.r.master[o] = v;
+    if (!p.r.out) return;
+  }
+  if (p.r.bf16_out) static_cast<bf16*>(p.r.out)[o] = from_f<bf16>(v);
+  else static_cast<float*>(p.r.out)[o] = v;
+}
+
 // A 128 x 128 tile of a product of split matrices: A k-contiguous, B
 // k-contiguous (GRAM, POLY: rows of the same matrix) or MN-major (X).  Four
 // wavefronts of 64 x 64; slices of 32 k of all four parts in NS LDS stages, asked
@@ -470,6 +484,224 @@ void launch(const NsArgs& p, hipStream_t s) {
   else hipLaunchKernelGGL((ns_product<MODE, 2, 2>), dim3(p.total), dim3(256), 0, s, p);
 }
 
+// --------------------------------------------------------- small matrices --
+// A matrix whose parts fit the LDS of one compute unit goes through all its steps
+// in one workgroup: one launch instead of 2 + 3 a step, each of which is latency
+// (four matrices of 64 x 192, five steps: 17 launches 142 us a call, this 30).
+// LDS holds X [P][Q + 8] and, in one place one after the other, A and B [P][P + 8],
+// hi and lo parts each; P is rounded up to 32, Q to 64, and zero there.
+constexpr int kSmallLds = 155648, kSmallWaves = 16, kSmallSide = 128;
+
+struct SmallArgs {
+  int P, Q, p, q, flip, steps;
+  float x_scale;     // of X: 2^ex
+  float a_scale;     // accumulators to A: 2^(ea - 2 ex)
+  float c_scale, ca, cb;  // B's parts: c 2^(eb - 2 ea), a 2^eb, b 2^(eb - ea)
+  float apply_scale; // accumulators to X: 2^-eb
+  float out_scale;   // ... to the result: 2^-(eb + ex)
+};
+
+__device__ __forceinline__ halfx8_t row8(const half_t* m, int pitch, int row0, int k0, int lane) {
+  return *reinterpret_cast<const halfx8_t*>(m + (row0 + (lane & 15)) * pitch + k0 + 8 * (lane >> 4));
+}
+// The same of a matrix's columns: eight consecutive k of column n0 + lane % 16.
+__device__ __forceinline__ halfx8_t col8(const half_t* m, int pitch, int n0, int k0, int lane) {
+  const bf16* at = reinterpret_cast<const bf16*>(m + (k0 + 8 * (lane >> 4) + ((lane & 15) >> 2)) * pitch + n0 + 4 * (lane & 3));
+  const i16x4_t v[2] = {lds_read_tr(at), lds_read_tr(at + 4 * pitch)};
+  return *reinterpret_cast<const halfx8_t*>(v);
+}
+__device__ __forceinline__ void mma3(const halfx8_t (&a)[2], const halfx8_t (&b)[2], f32x4_t (&acc)[3]) {
+  acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0], a[1], acc[0], 0, 0, 0);
+  acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[1], a[0], acc[1], 0, 0, 0);
+  acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0], a[0], acc[2], 0, 0, 0);
+}
+
+// NB: blocks of 16 along P.
+template <int NB>
+__global__ __launch_bounds__(kSmallWaves * 64) void ns_small(Source s, SmallArgs a, NsArgs to) {
+  constexpr int P = 16 * NB, PA = P + 8, kBlocks = NB * (NB + 1) / 2, kHeld = (kBlocks + kSmallWaves - 1) / kSmallWaves;
+  __shared__ __attribute__((aligned(16))) char lds[kSmallLds];
+  __shared__ double red[kSmallWaves];
+  const int PX = a.Q + 8;
+  half_t* X[2] = {reinterpret_cast<half_t*>(lds), reinterpret_cast<half_t*>(lds) + P * PX};
+  half_t* A[2] = {X[1] + P * PX, X[1] + P * PX + P * PA};
+  constexpr int kThreads = kSmallWaves * 64;
+  const int mat = blockIdx.x, tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // the momentum's update and the norm, then X; kBatch loads a thread under way
+  constexpr int kBatch = 8;
+  const int n = s.rows * s.cols;
+  const int64_t base = mat * s.stride;
+  auto batch = [&](int i0, float (&v)[kBatch], bool first) {
+    float m[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int64_t i = base + min(i0 + k * kThreads, n - 1);
+      if (s.g) {
+        v[k] = s.g[i];
+        m[k] = s.m[i];
+      } else {
+        v[k] = s.bf16_in ? to_f(static_cast<const bf16*>(s.x)[i]) : static_cast<const float*>(s.x)[i];
+      }
+    }
+    if (s.g) {
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        if (first) {
+          m[k] = fmaf(s.beta, m[k], v[k]);
+          if (i0 + k * kThreads < n) s.m[base + i0 + k * kThreads] = m[k];
+        }
+        v[k] = s.nesterov ? fmaf(s.beta, m[k], v[k]) : m[k];
+      }
+    }
+  };
+  double sum = 0.0;
+  for (int i0 = tid; i0 < n; i0 += kBatch * kThreads) {
+    float v[kBatch];
+    batch(i0, v, true);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (i0 + k * kThreads < n) sum = fma((double)v[k], (double)v[k], sum);
+  }
+  sum = wave_sum_d(sum);
+  if (lane == 0) red[wave] = sum;
+  for (int i = tid; i < P * PX / 4; i += kThreads)
+    reinterpret_cast<uint2*>(X[0])[i] = reinterpret_cast<uint2*>(X[1])[i] = make_uint2(0, 0);
+  __syncthreads();
+  double norm2 = 0.0;
+  for (int w = 0; w < kSmallWaves; ++w) norm2 += red[w];
+  const double inv = norm2 == 0.0 ? 0.0 : norm2 <= 1.7e308 ? (double)a.x_scale / sqrt(norm2) : __builtin_nan("");
+  for (int i0 = tid; i0 < n; i0 += kBatch * kThreads) {
+    float u[kBatch];
+    batch(i0, u, false);
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int i = i0 + b * kThreads;
+      if (i >= n) continue;
+      const int r = i / s.cols, k = i % s.cols, at = (a.flip ? k : r) * PX + (a.flip ? r : k);
+      const float v = (float)((double)u[b] * inv);
+      const half_t hi = static_cast<half_t>(v);
+      X[0][at] = hi;
+      X[1][at] = static_cast<half_t>(v - static_cast<float>(hi));
+    }
+  }
+  __syncthreads();
+
+  int bi[kHeld], bj[kHeld];  // this wavefront's blocks of A and B
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) triangle(min(wave + i * kSmallWaves, kBlocks - 1), bi[i], bj[i]);
+  // four elements of a symmetric matrix, and their mirror images
+  auto write_a = [&](int bi, int bj, const float (&v)[4]) {
+    uint2 hi, lo;
+    split4(v, hi, lo);
+    const int m = 16 * bi + c, k = 16 * bj + 4 * g;
+    *reinterpret_cast<uint2*>(A[0] + m * PA + k) = hi;
+    *reinterpret_cast<uint2*>(A[1] + m * PA + k) = lo;
+    if (bi != bj) {
+      union { uint2 w; half_t h[4]; } h{hi}, l{lo};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        A[0][(k + e) * PA + m] = h.h[e];
+        A[1][(k + e) * PA + m] = l.h[e];
+      }
+    }
+  };
+  for (int step = 0; step < a.steps; ++step) {
+    // A = X X^T, blocks on and below the diagonal
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      if (wave + i * kSmallWaves < kBlocks) {
+        f32x4_t acc[3] = {};
+        for (int k = 0; k < a.Q; k += 64) {
+          halfx8_t x[2][2], y[2][2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              x[w][h] = row8(X[h], PX, 16 * bi[i], k + 32 * w, lane);
+              y[w][h] = row8(X[h], PX, 16 * bj[i], k + 32 * w, lane);
+            }
+          mma3(x[0], y[0], acc);
+          mma3(x[1], y[1], acc);
+        }
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = ((acc[0][e] + acc[1][e]) + acc[2][e]) * a.a_scale;
+      write_a(bi[i], bj[i], v);
+      }
+    }
+    __syncthreads();
+    // B = a I + b A + c A A, held in registers until A has been read
+    float held[kHeld][4];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      if (wave + i * kSmallWaves < kBlocks) {
+        f32x4_t acc[3] = {};
+#pragma unroll
+        for (int k = 0; k < P; k += 32) {
+        const halfx8_t x[2] = {row8(A[0], PA, 16 * bi[i], k, lane), row8(A[1], PA, 16 * bi[i], k, lane)};
+        const halfx8_t y[2] = {row8(A[0], PA, 16 * bj[i], k, lane), row8(A[1], PA, 16 * bj[i], k, lane)};
+        mma3(x, y, acc);
+      }
+      const int m = 16 * bi[i] + c, k = 16 * bj[i] + 4 * g;
+      float old[4];
+      join4(*reinterpret_cast<const uint2*>(A[0] + m * PA + k), *reinterpret_cast<const uint2*>(A[1] + m * PA + k), old);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        held[i][e] = fmaf((acc[0][e] + acc[1][e]) + acc[2][e], a.c_scale, fmaf(a.cb, old[e], m == k + e ? a.ca : 0.f));
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (wave + i * kSmallWaves < kBlocks) write_a(bi[i], bj[i], held[i]);
+    __syncthreads();
+    // X <- B X: a wavefront owns whole columns, so it may write where it has read
+    const bool last = step + 1 == a.steps;
+    for (int col = wave; col < a.Q / 16; col += kSmallWaves) {
+      f32x4_t acc[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < P; k += 32) {
+        const halfx8_t y[2] = {col8(X[0], PX, 16 * col, k, lane), col8(X[1], PX, 16 * col, k, lane)};
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          const halfx8_t x[2] = {row8(A[0], PA, 16 * i, k, lane), row8(A[1], PA, 16 * i, k, lane)};
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(y[0], x[1], acc[i], 0, 0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(y[1], x[0], acc[i], 0, 0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(y[0], x[0], acc[i], 0, 0, 0);
+        }
+      }
+      wave_lds_order();
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int m = 16 * i + c, k = 16 * col + 4 * g;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][e];
+        if (!last) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] *= a.apply_scale;
+          uint2 hi, lo;
+          split4(v, hi, lo);
+          *reinterpret_cast<uint2*>(X[0] + m * PX + k) = hi;
+          *reinterpret_cast<uint2*>(X[1] + m * PX + k) = lo;
+        } else if (a.flip) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) put_one(to, mat, k + e, m, v[e]);
+        } else {
+          Beside w;
+          ask<LAST>(to, mat, m, k, w);
+          put<LAST>(to, mat, m, k, make_float4(v[0], v[1], v[2], v[3]), w);
+        }
+      }
+      wave_lds_order();
+    }
+    __syncthreads();
+  }
+}
+
 // ---------------------------------------------------------------- sizes --
 int pad(int n) { return (n + kTile - 1) / kTile * kTile; }
 int64_t up(int64_t n) { return (n + 255) / 256 * 256; }
@@ -509,6 +741,15 @@ double largest(double c0, double c1, double c2, double top) {
   return t > 0.0 && t < top ? std::max(m, f(t)) : m;
 }
 
+// Whether a matrix fits one workgroup, and its padded sides there.
+bool small(const NewtonSchulz& s, SmallArgs* a) {
+  a->p = std::min(s.rows, s.cols);
+  a->q = std::max(s.rows, s.cols);
+  a->P = (a->p + 31) / 32 * 32;
+  a->Q = (a->q + 63) / 64 * 64;
+  return a->P <= kSmallSide && 4ll * a->P * (a->Q + 8) + 4ll * a->P * (a->P + 8) <= kSmallLds;
+}
+
 }  // namespace
 
 // Bounds of the singular values before each step (and after the last), of
@@ -537,7 +778,40 @@ bool newton_schulz_bounds(const NewtonSchulz& s, double* sigma) {
   return true;
 }
 
+namespace {
+
+// The whole call in one launch, with one set of scales: where the singular values'
+// bounds of all steps lie within a factor of 16 (each factor of two costs the
+// smallest elements a bit).
+bool small_scales(const NewtonSchulz& s, const double* sigma, SmallArgs* a) {
+  if (!small(s, a)) return false;
+  double most = sigma[0], least = sigma[0], factor = 0.0;
+  for (int k = 0; k < s.steps; ++k) {
+    most = std::max(most, sigma[k]);
+    least = std::min(least, sigma[k]);
+    factor = std::max(factor, std::max(largest(s.a, s.b, s.c, sigma[k] * sigma[k]), std::fabs((double)s.a)));
+  }
+  if (most > 16.0 * least) return false;
+  const int ex = exponent(most), ea = exponent(most * most), eb = exponent(factor);
+  auto p2 = [](double v, int e) { return (float)std::ldexp(v, e); };
+  a->flip = s.rows > s.cols;
+  a->steps = s.steps;
+  a->x_scale = p2(1.0, ex);
+  a->a_scale = p2(1.0, ea - 2 * ex);
+  a->c_scale = p2(s.c, eb - 2 * ea);
+  a->ca = p2(s.a, eb);
+  a->cb = p2(s.b, eb - ea);
+  a->apply_scale = p2(1.0, -eb);
+  a->out_scale = p2(1.0, -eb - ex);
+  return true;
+}
+
+}  // namespace
+
 int64_t newton_schulz_scratch(const NewtonSchulz& s) {
+  double sigma[kMaxNewtonSteps + 1];
+  SmallArgs a;
+  if (newton_schulz_bounds(s, sigma) && small_scales(s, sigma, &a)) return 256;  // (none is used)
   const Sizes z = sizes(s);
   return up((int64_t)s.count * z.nparts * 8) + z.chunk * (4 * up(z.x) + 4 * up(z.a));
 }
@@ -578,6 +852,22 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
   // four columns of every row at once
   res.vec = s.cols % 4 == 0 && res.stride % 4 == 0 && reinterpret_cast<uintptr_t>(out) % (4 * es) == 0 &&
             (!u || reinterpret_cast<uintptr_t>(u->master) % 16 == 0);
+
+  SmallArgs one;
+  if (small_scales(s, sigma, &one)) {
+    NsArgs to;
+    memset(&to, 0, sizeof(to));
+    to.r = res;
+    to.scale = one.out_scale;
+    const dim3 grid(s.count), block(kSmallWaves * 64);
+    switch (one.P) {
+      case 32: hipLaunchKernelGGL(ns_small<2>, grid, block, 0, stream, src, one, to); break;
+      case 64: hipLaunchKernelGGL(ns_small<4>, grid, block, 0, stream, src, one, to); break;
+      case 96: hipLaunchKernelGGL(ns_small<6>, grid, block, 0, stream, src, one, to); break;
+      default: hipLaunchKernelGGL(ns_small<8>, grid, block, 0, stream, src, one, to); break;
+    }
+    return hipGetLastError();
+  }
 
   hipError_t e = hipSuccess;
   for (int c0 = 0; c0 < s.count && e == hipSuccess; c0 += z.chunk) {

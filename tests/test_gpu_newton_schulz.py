@@ -109,7 +109,8 @@ def check(count, rows, cols, dtype, steps=5, coef=COEF, seed=0, scale=1e-3):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (5, 1), (3, 3), (16, 40), (64, 64), (65, 63), (127, 300),
-                                       (128, 128), (129, 257), (300, 129), (256, 512)])
+                                       (128, 128), (128, 160), (161, 128), (31, 1100), (129, 257), (300, 129),
+                                       (256, 512), (2, 3000), (100, 700), (901, 70)])
 def test_shapes(dtype, rows, cols):
     check(2, rows, cols, dtype, seed=rows + cols)
 
