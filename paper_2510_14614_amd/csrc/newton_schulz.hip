@@ -21,7 +21,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <type_traits>
 
 #include "common.h"
 #include "gemm_pipe.h"
@@ -37,6 +36,9 @@ typedef _Float16 halfx8_t __attribute__((ext_vector_type(8)));
 constexpr int kTile = 128;      // tile sides; matrices are padded to it with zeros
 constexpr int kNormBlocksNs = 1024;
 constexpr int kOneRound = 256;  // tiles that have a compute unit each
+// slices that a launch more has to save (512 x 512, five steps: 198 us, with 16 of
+// them 262)
+constexpr int kJoinSlices = 12;
 
 // A matrix of a batch: hi and lo parts, [count][rows][ld] each.
 struct Split {
@@ -80,6 +82,8 @@ struct NsArgs {
   int K, tiles_m, tiles_n, per_matrix, total;
   float scale;             // of the accumulators
   float ca, cb;            // POLY: a and b, at the result's scale
+  int splits, per;         // ranges of K, slices of one
+  float* part;             // [matrix][range][tile][a thread's accumulators]
   Result r;
 };
 
@@ -229,7 +233,7 @@ __device__ __forceinline__ void triangle(int t, int& r, int& c) {
 // result, asked for ahead of their use: POLY's A, or the update's weights.
 struct Beside {
   uint2 hi, lo;
-  float4 w;
+  float4 w;  // (single elements of four rows where rows are no whole 16-byte groups)
 };
 template <int MODE>
 __device__ __forceinline__ void ask(const NsArgs& p, int mat, int r, int c, Beside& b) {
@@ -238,17 +242,26 @@ __device__ __forceinline__ void ask(const NsArgs& p, int mat, int r, int c, Besi
     b.hi = *reinterpret_cast<const uint2*>(p.d.hi + o);
     b.lo = *reinterpret_cast<const uint2*>(p.d.lo + o);
   } else if (MODE == LAST && p.r.master && r < p.r.rows) {
-    const float* w = p.r.master + mat * p.r.stride + (int64_t)r * p.r.cols + c;
-    if (p.r.vec) {
-      if (c < p.r.cols) b.w = *reinterpret_cast<const float4*>(w);
-    } else {
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (c + e < p.r.cols) v[e] = w[e];
-      b.w = make_float4(v[0], v[1], v[2], v[3]);
-    }
+    if (c < p.r.cols)
+      b.w = *reinterpret_cast<const float4*>(p.r.master + mat * p.r.stride + (int64_t)r * p.r.cols + c);
   }
+}
+
+// The result's element (r, c), of rows that are no whole 16-byte groups.
+__device__ __forceinline__ float ask_one(const NsArgs& p, int mat, int r, int c) {
+  return p.r.master && r < p.r.rows && c < p.r.cols ? p.r.master[mat * p.r.stride + (int64_t)r * p.r.cols + c] : 0.f;
+}
+__device__ __forceinline__ void put_one(const NsArgs& p, int mat, int r, int c, float v, float w) {
+  if (r >= p.r.rows || c >= p.r.cols) return;
+  const int64_t o = mat * p.r.stride + (int64_t)r * p.r.cols + c;
+  v *= p.scale;
+  if (p.r.master) {
+    v = fmaf(w, p.r.decay, -p.r.step * v);
+    p.r.master[o] = v;
+    if (!p.r.out) return;
+  }
+  if (p.r.bf16_out) static_cast<bf16*>(p.r.out)[o] = from_f<bf16>(v);
+  else static_cast<float*>(p.r.out)[o] = v;
 }
 
 // Four consecutive elements of the result.
@@ -263,26 +276,11 @@ __device__ __forceinline__ void put(const NsArgs& p, int mat, int r, int c, cons
       v[1] = fmaf(b.w.y, p.r.decay, -p.r.step * v[1]);
       v[2] = fmaf(b.w.z, p.r.decay, -p.r.step * v[2]);
       v[3] = fmaf(b.w.w, p.r.decay, -p.r.step * v[3]);
-      if (p.r.vec) {
-        *reinterpret_cast<float4*>(p.r.master + o) = make_float4(v[0], v[1], v[2], v[3]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (c + e < p.r.cols) p.r.master[o + e] = v[e];
-      }
+      *reinterpret_cast<float4*>(p.r.master + o) = make_float4(v[0], v[1], v[2], v[3]);
       if (!p.r.out) return;
     }
-    if (p.r.vec) {
-      if (p.r.bf16_out) st4(static_cast<bf16*>(p.r.out) + o, v);
-      else *reinterpret_cast<float4*>(static_cast<float*>(p.r.out) + o) = make_float4(v[0], v[1], v[2], v[3]);
-      return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (c + e >= p.r.cols) break;
-      if (p.r.bf16_out) static_cast<bf16*>(p.r.out)[o + e] = from_f<bf16>(v[e]);
-      else static_cast<float*>(p.r.out)[o + e] = v[e];
-    }
+    if (p.r.bf16_out) st4(static_cast<bf16*>(p.r.out) + o, v);
+    else *reinterpret_cast<float4*>(static_cast<float*>(p.r.out) + o) = make_float4(v[0], v[1], v[2], v[3]);
     return;
   }
   if (MODE == POLY) {
@@ -298,18 +296,84 @@ __device__ __forceinline__ void put(const NsArgs& p, int mat, int r, int c, cons
   *reinterpret_cast<uint2*>(p.c.lo + o) = lo;
 }
 
-// One element of the last product.
-__device__ __forceinline__ void put_one(const NsArgs& p, int mat, int r, int c, float v) {
-  if (r >= p.r.rows || c >= p.r.cols) return;
-  const int64_t o = mat * p.r.stride + (int64_t)r * p.r.cols + c;
-  v *= p.scale;
-  if (p.r.master) {
-    v = fmaf(p.r.master[o], p.r.decay, -p.r.step * v);
-    p.r.master[o] = v;
-    if (!p.r.out) return;
+// The epilogue works on strips of 16 rows (COLS: columns) of a wavefront's 64 x 64,
+// passed through LDS so that consecutive lanes hold consecutive elements: lane 16g +
+// c of block (i, j) holds row 16i + c, columns 16j + 4g .. +3.  A tile's columns are
+// rows of the result where it is mirrored or transposed.
+constexpr int kStripPitch = 64 + 4;
+template <int MODE, bool COLS>
+struct Strip {
+  Beside beside[4];
+  int r, c;  // this lane's first row and its columns
+  // Strip q of the wavefront's quarter of tile (tm, tn).
+  __device__ __forceinline__ void ask_for(const NsArgs& p, int mat, int tm, int tn, int q) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int mw = tm * kTile + (wave >> 1) * 64, nw = tn * kTile + (wave & 1) * 64;
+    if (MODE == LAST && !p.r.vec) {
+      // a lane to a column
+      r = (COLS ? nw : mw) + 16 * q;
+      c = (COLS ? mw : nw) + lane;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        beside[k].w = make_float4(ask_one(p, mat, r + 4 * k, c), ask_one(p, mat, r + 4 * k + 1, c),
+                                  ask_one(p, mat, r + 4 * k + 2, c), ask_one(p, mat, r + 4 * k + 3, c));
+      return;
+    }
+    r = (COLS ? nw : mw) + 16 * q + (lane >> 4);
+    c = (COLS ? mw : nw) + 4 * (lane & 15);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) ask<MODE>(p, mat, r + 4 * k, c, beside[k]);
   }
-  if (p.r.bf16_out) static_cast<bf16*>(p.r.out)[o] = from_f<bf16>(v);
-  else static_cast<float*>(p.r.out)[o] = v;
+  // blocks: (q, 0 .. 3), COLS: (0 .. 3, q).
+  __device__ __forceinline__ void emit(const NsArgs& p, int mat, const f32x4_t (&blocks)[4], float* strip) const {
+    const int lane = threadIdx.x & 63, g = lane >> 4, cl = lane & 15;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (COLS) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) strip[(4 * g + e) * kStripPitch + 16 * j + cl] = blocks[j][e];
+      } else {
+        *reinterpret_cast<f32x4_t*>(strip + cl * kStripPitch + 16 * j + 4 * g) = blocks[j];
+      }
+    }
+    wave_lds_order();
+    if (MODE == LAST && !p.r.vec) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float* s = strip + 4 * k * kStripPitch + lane;
+        put_one(p, mat, r + 4 * k, c, s[0], beside[k].w.x);
+        put_one(p, mat, r + 4 * k + 1, c, s[kStripPitch], beside[k].w.y);
+        put_one(p, mat, r + 4 * k + 2, c, s[2 * kStripPitch], beside[k].w.z);
+        put_one(p, mat, r + 4 * k + 3, c, s[3 * kStripPitch], beside[k].w.w);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        put<MODE>(p, mat, r + 4 * k, c, *reinterpret_cast<const float4*>(strip + (4 * k + g) * kStripPitch + 4 * cl),
+                  beside[k]);
+    }
+    wave_lds_order();
+  }
+};
+template <int MODE>
+__device__ __forceinline__ bool emits(const NsArgs& p, int tm, int tn, bool cols) {
+  if (MODE == LAST) return cols == (p.r.flip != 0);
+  return !cols || ((MODE == GRAM || MODE == POLY) && tm != tn);
+}
+
+// A whole tile, every strip's operands asked for at once.
+template <int MODE, bool COLS>
+__device__ __forceinline__ void ns_emit(const NsArgs& p, int mat, int tm, int tn, const f32x4_t (&acc)[4][4], float* strip) {
+  Strip<MODE, COLS> s[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) s[q].ask_for(p, mat, tm, tn, q);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    f32x4_t blocks[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) blocks[j] = COLS ? acc[j][q] : acc[q][j];
+    s[q].emit(p, mat, blocks, strip);
+  }
 }
 
 // A 128 x 128 tile of a product of split matrices: A k-contiguous, B
@@ -332,7 +396,7 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   auto stage_ptr = [&](int k) -> char* { return k == 0 ? st0 : k == 1 ? st1 : k == 2 ? st2 : st3; };
 
   const int bid = xcd_remap(blockIdx.x, p.total);
-  const int mat = bid / p.per_matrix, t = bid % p.per_matrix;
+  const int t = bid % p.per_matrix, range = bid / p.per_matrix % p.splits, mat = bid / p.per_matrix / p.splits;
   int tm, tn;
   if (BK) triangle(t, tm, tn);
   else grouped_tile(t, p.tiles_m, p.tiles_n, tm, tn);
@@ -353,7 +417,8 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   al.clear(1);
   bh.clear(1);
   bl.clear(1);
-  const int n = p.K / KS;  // K is a multiple of the tile's side
+  // this range's slices (both it and K are multiples of 128)
+  const int k0 = range * p.per * KS, n = min(p.per, p.K / KS - range * p.per);
   auto issue = [&](char* stage, int s) {
     if (s > 0 && s < n) {
       ah.advance();
@@ -362,10 +427,10 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
       bl.advance();
     } else {
       const int lim = s < n ? KS : 0;  // slices past the end: zeros
-      ah.set(0, 0, lim);
-      al.set(0, 0, lim);
-      bh.set(0, 0, lim);
-      bl.set(0, 0, lim);
+      ah.set(0, k0, lim);
+      al.set(0, k0, lim);
+      bh.set(0, k0, lim);
+      bl.set(0, k0, lim);
     }
     ah.load(stage, wave);
     al.load(stage + REGION, wave);
@@ -422,7 +487,7 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   // Step s: own loads of slice s + 1 and own reads of slice s are done, barrier
   // (slice s + 1 whole in LDS, slice s's stage free), slice s + NS into that
   // stage, the MFMA of slice s under the reads of slice s + 1.  (n is a multiple
-  // of NS: K is one of 128)
+  // of four)
   for (int s = 0; s < n; s += NS) {
 #pragma unroll
     for (int U = 0; U < NS; ++U) {
@@ -439,49 +504,77 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   FAL_WAITCNT(0, 0);
   bar();
 
-  // Epilogue through a strip of 16 rows (or columns) a wavefront in LDS, so that
-  // consecutive lanes hold consecutive elements.  Lane 16g + c of block (i, j)
-  // holds row 16i + c, columns 16j + 4g .. +3.
-  constexpr int PITCH = WT + 4;
-  float* strip = reinterpret_cast<float*>(st0) + wave * 16 * PITCH;
-  const int mw = m0 + wm * WT, nw = n0 + wn * WT, g = lane >> 4, cl = lane & 15;
-  // rows of the tile to rows of the result, or its columns to them
-  auto emit = [&](auto columns) {
-    constexpr bool COLS = decltype(columns)::value;
-    const int r0 = COLS ? nw : mw, c = (COLS ? mw : nw) + 4 * cl;
-    Beside beside[F][4];
+  if (p.splits > 1) {
+    float* o = p.part + ((int64_t)bid * 256 + threadIdx.x) * 4;
 #pragma unroll
     for (int i = 0; i < F; ++i)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) ask<MODE>(p, mat, r0 + 16 * i + 4 * k + g, c, beside[i][k]);
-#pragma clang loop unroll(full)
-    for (int i = 0; i < F; ++i) {
+      for (int j = 0; j < F; ++j) *reinterpret_cast<f32x4_t*>(o + (i * F + j) * (int64_t)p.total * 1024) = acc[i][j];
+    return;
+  }
+  float* strip = reinterpret_cast<float*>(st0) + wave * 16 * kStripPitch;
+  if (emits<MODE>(p, tm, tn, false)) ns_emit<MODE, false>(p, mat, tm, tn, acc, strip);
+  if (emits<MODE>(p, tm, tn, true)) ns_emit<MODE, true>(p, mat, tm, tn, acc, strip);
+}
+
+// A tile's ranges added in order, and its epilogue: a workgroup for each of its
+// strips (one for a whole tile took 12.7 us for 18 tiles of 8 ranges, these 7.6).
+template <int MODE, bool COLS>
+__device__ __forceinline__ void join_strip(const NsArgs& p, int mat, int t, int tm, int tn, int q, float* strip) {
+  Strip<MODE, COLS> s;
+  s.ask_for(p, mat, tm, tn, q);
+  f32x4_t sum[4];
+  const int64_t block = (int64_t)p.total * 1024, range = (int64_t)p.per_matrix * 1024;
+  const float* o = p.part + (((int64_t)mat * p.splits * p.per_matrix + t) * 256 + threadIdx.x) * 4;
+  for (int r0 = 0; r0 < p.splits; r0 += 4) {
+    f32x4_t v[4][4];
 #pragma unroll
-      for (int j = 0; j < F; ++j) {
-        if (COLS) {
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) strip[(4 * g + e) * PITCH + 16 * j + cl] = acc[j][i][e];
-        } else {
-          *reinterpret_cast<float4*>(strip + cl * PITCH + 16 * j + 4 * g) =
-              make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
-        }
-      }
-      wave_lds_order();
+      for (int j = 0; j < 4; ++j)
+        if (r0 + r < p.splits)
+          v[r][j] = *reinterpret_cast<const f32x4_t*>(o + (r0 + r) * range + (COLS ? 4 * j + q : 4 * q + j) * block);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        put<MODE>(p, mat, r0 + 16 * i + 4 * k + g, c, *reinterpret_cast<const float4*>(strip + (4 * k + g) * PITCH + 4 * cl),
-                  beside[i][k]);
-      wave_lds_order();
-    }
-  };
-  if (MODE != LAST || !p.r.flip) emit(std::false_type());
-  if (MODE == LAST ? p.r.flip : BK && tm != tn) emit(std::true_type());
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (r0 + r < p.splits) sum[j] = r0 + r ? sum[j] + v[r][j] : v[r][j];
+  }
+  s.emit(p, mat, sum, strip);
+}
+template <int MODE>
+__global__ __launch_bounds__(256, 2) void ns_join(NsArgs p) {
+  __shared__ __attribute__((aligned(16))) float lds[4][16 * kStripPitch];
+  const int q = blockIdx.x & 3, t = blockIdx.x / 4 % p.per_matrix, mat = blockIdx.x / 4 / p.per_matrix;
+  int tm, tn;
+  if (MODE == GRAM || MODE == POLY) triangle(t, tm, tn);
+  else grouped_tile(t, p.tiles_m, p.tiles_n, tm, tn);
+  float* strip = lds[threadIdx.x >> 6];
+  if (emits<MODE>(p, tm, tn, false)) join_strip<MODE, false>(p, mat, t, tm, tn, q, strip);
+  if (emits<MODE>(p, tm, tn, true)) join_strip<MODE, true>(p, mat, t, tm, tn, q, strip);
+}
+
+// Products of few tiles and many slices: K in as many ranges as the compute units
+// take at once, of at least four slices, where that saves more than the joining
+// launch costs.
+int ranges(int tiles, int K, int* per) {
+  const int slices = K / pipe::KS;
+  *per = slices;
+  if (tiles > kOneRound / 2) return 1;
+  const int s = std::min(kOneRound / tiles, slices / 4), each = cdiv(cdiv(slices, s), 4) * 4;
+  if (slices - each < kJoinSlices) return 1;
+  *per = each;
+  return cdiv(slices, each);
 }
 
 template <int MODE>
-void launch(const NsArgs& p, hipStream_t s) {
+void launch(NsArgs p, int matrices, hipStream_t s) {
+  const int tiles = p.per_matrix * matrices;
+  p.splits = ranges(tiles, p.K, &p.per);
+  p.total = tiles * p.splits;
   if (p.total <= kOneRound) hipLaunchKernelGGL((ns_product<MODE, 1, 4>), dim3(p.total), dim3(256), 0, s, p);
   else hipLaunchKernelGGL((ns_product<MODE, 2, 2>), dim3(p.total), dim3(256), 0, s, p);
+  if (p.splits > 1) hipLaunchKernelGGL(ns_join<MODE>, dim3(4 * tiles), dim3(256), 0, s, p);
 }
 
 // --------------------------------------------------------- small matrices --
@@ -687,9 +780,12 @@ __global__ __launch_bounds__(kSmallWaves * 64) void ns_small(Source s, SmallArgs
           split4(v, hi, lo);
           *reinterpret_cast<uint2*>(X[0] + m * PX + k) = hi;
           *reinterpret_cast<uint2*>(X[1] + m * PX + k) = lo;
-        } else if (a.flip) {
+        } else if (a.flip || !to.r.vec) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) put_one(to, mat, k + e, m, v[e]);
+          for (int e = 0; e < 4; ++e) {
+            const int row = a.flip ? k + e : m, at = a.flip ? m : k + e;
+            put_one(to, mat, row, at, v[e], ask_one(to, mat, row, at));
+          }
         } else {
           Beside w;
           ask<LAST>(to, mat, m, k, w);
@@ -711,6 +807,7 @@ struct Sizes {
   int64_t x, a;  // bytes of one matrix's X and A, one part
   int chunk;     // matrices that go through together
   int nparts;
+  int64_t part;  // bytes of the ranges' sums
 };
 
 // Matrices go through in as few batches of one size as keep the workspace near 2
@@ -727,6 +824,17 @@ Sizes sizes(const NewtonSchulz& s) {
   const int64_t batches = (s.count + most - 1) / most;
   z.chunk = (int)((s.count + batches - 1) / batches);
   z.nparts = (int)std::min<int64_t>(kNormBlocksNs, ((int64_t)s.rows * s.cols + 4095) / 4096);
+  const int tp = z.P / kTile, tq = z.Q / kTile;
+  z.part = 0;
+  for (int n : {z.chunk, s.count % z.chunk}) {  // (a last batch may be smaller, and its products cut)
+    if (!n) continue;
+    int per;
+    const int gram = tp * (tp + 1) / 2 * n, apply = tp * tq * n;
+    const int most = std::max({ranges(gram, z.Q, &per) > 1 ? ranges(gram, z.Q, &per) * gram : 0,
+                               ranges(gram, z.P, &per) > 1 ? ranges(gram, z.P, &per) * gram : 0,
+                               ranges(apply, z.P, &per) > 1 ? ranges(apply, z.P, &per) * apply : 0});
+    z.part = std::max(z.part, (int64_t)most * kTile * kTile * 4);
+  }
   return z;
 }
 
@@ -813,7 +921,7 @@ int64_t newton_schulz_scratch(const NewtonSchulz& s) {
   SmallArgs a;
   if (newton_schulz_bounds(s, sigma) && small_scales(s, sigma, &a)) return 256;  // (none is used)
   const Sizes z = sizes(s);
-  return up((int64_t)s.count * z.nparts * 8) + z.chunk * (4 * up(z.x) + 4 * up(z.a));
+  return up((int64_t)s.count * z.nparts * 8) + z.chunk * (4 * up(z.x) + 4 * up(z.a)) + z.part;
 }
 
 hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x, void* out, void* scratch,
@@ -832,6 +940,7 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
   Split X[2], A, B;
   for (Split* m : {&X[0], &X[1]}) { m->hi = take(z.chunk * up(z.x)); m->lo = take(z.chunk * up(z.x)); }
   for (Split* m : {&A, &B}) { m->hi = take(z.chunk * up(z.a)); m->lo = take(z.chunk * up(z.a)); }
+  float* sums = reinterpret_cast<float*>(base);
 
   Source src;
   memset(&src, 0, sizeof(src));
@@ -892,30 +1001,31 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
       const int tp = z.P / kTile, tq = z.Q / kTile;
       NsArgs p;
       memset(&p, 0, sizeof(p));
+      p.part = sums;
       // A = X X^T
       p.a = p.b = x0; p.lda = p.ldb = z.Q; p.sa = p.sb = sx; p.K = z.Q;
       p.c = A; p.ldc = z.P; p.sc = sp;
-      p.tiles_m = p.tiles_n = tp; p.per_matrix = tp * (tp + 1) / 2; p.total = p.per_matrix * n;
+      p.tiles_m = p.tiles_n = tp; p.per_matrix = tp * (tp + 1) / 2;
       p.scale = (float)std::ldexp(1.0, ea - 2 * ex);
-      launch<GRAM>(p, stream);
+      launch<GRAM>(p, n, stream);
       // B = a I + b A + c A A
       p.a = p.b = p.d = A; p.lda = p.ldb = p.ldd = z.P; p.sa = p.sb = p.sd = sp; p.K = z.P;
       p.c = B;
       p.scale = (float)std::ldexp((double)s.c, eb - 2 * ea);
       p.ca = (float)std::ldexp((double)s.a, eb);
       p.cb = (float)std::ldexp((double)s.b, eb - ea);
-      launch<POLY>(p, stream);
+      launch<POLY>(p, n, stream);
       // X <- B X
       p.a = B; p.b = x0; p.ldb = z.Q; p.sb = sx;
       p.c = x1; p.ldc = z.Q; p.sc = sx;
-      p.tiles_n = tq; p.per_matrix = tp * tq; p.total = p.per_matrix * n;
+      p.tiles_n = tq; p.per_matrix = tp * tq;
       if (k + 1 < s.steps) {
         p.scale = (float)std::ldexp(1.0, en - eb - ex);
-        launch<APPLY>(p, stream);
+        launch<APPLY>(p, n, stream);
       } else {
         p.scale = (float)std::ldexp(1.0, -eb - ex);
         p.r = to;
-        launch<LAST>(p, stream);
+        launch<LAST>(p, n, stream);
       }
       ex = en;
     }

@@ -126,11 +126,24 @@ def test_coefficients(coef):
     check(1, 96, 130, F32, coef=coef, steps=4)
 
 
+def test_more_matrices_than_one_batch_holds():
+    """2.6 MB of parts a matrix: 900 of them pass the 2 GiB that go through
+    together, so they go in two batches of 450."""
+    x = make(0, 900, 200, 1000, BF16)
+    got = fal.newton_schulz(x)
+    some = [0, 1, 449, 450, 899]
+    want, bounds = exact(x[some], 5, COEF)
+    hold(got[some], want, bounds, in_fp32(x[some], 5, COEF), 2.0 ** -8)
+    # (orthogonal rows: every matrix has its norm, within the polynomial's band)
+    norms = torch.linalg.matrix_norm(got.float())
+    assert ((norms > 0.6 * 200 ** 0.5) & (norms < 1.3 * 200 ** 0.5)).all()
+
+
+@pytest.mark.parametrize("count,rows,cols", [(1, 200, 4000), (3, 1001, 333), (1, 640, 700), (1, 1024, 1024), (2, 130, 9000)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
-def test_more_matrices_than_one_batch_holds(dtype):
-    """Some 5 MB of parts a matrix: 60 of them go through in two batches."""
-    x, got = check(60, 200, 1000, dtype)
-    assert torch.equal(fal.newton_schulz(x[57], 5), got[57])
+def test_products_cut_along_k(count, rows, cols, dtype):
+    """Few tiles and long sums: ranges of k in workgroups of their own."""
+    check(count, rows, cols, dtype, seed=rows)
 
 
 def test_large():
