@@ -63,10 +63,10 @@ struct Gated {
 
 // One output tile of BM rows and BN columns of f.  Forward (BWD 0): both
 // projections at once, x k-contiguous, weights MN-major.  Backward: dh, both
-// operands k-contiguous.  The main loop is that of gemm_bf16_pipe: NS stages of
-// 32 k, the fragments of slice s + 1 read under the MFMAs of slice s, slice s +
-// NS - 1 asked for behind them, one barrier a slice.
-template <int BWD, int BM, int BN, int OCC, int NS>
+// operands k-contiguous.  The main loop is that of gemm_bf16_pipe: three stages of
+// 32 k, the fragments of slice s + 1 read under the MFMAs of slice s, slice s + 2
+// asked for behind them, one barrier a slice.
+template <int BWD, int BM, int BN, int OCC>
 __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
   using namespace pipe;
   constexpr int NB = BWD ? 1 : 2;
@@ -75,10 +75,10 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
   typedef Src<BN, BWD> SB;
   constexpr int SBYTES = SA::BYTES + NB * SB::BYTES;
   constexpr int L = SA::IPW + NB * SB::IPW;
-  static_assert((NS == 3 || NS == 4) && L * (NS - 2) <= 63, "stages");
   // one array a stage: the compiler tracks loads to LDS array by array
-  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES], st2[SBYTES], st3[NS == 4 ? SBYTES : 16];
-  auto stage_ptr = [&](int k) -> char* { return k == 0 ? st0 : k == 1 ? st1 : k == 2 ? st2 : st3; };
+  constexpr int NS = 3;
+  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES], st2[SBYTES];
+  auto stage_ptr = [&](int k) -> char* { return k == 0 ? st0 : k == 1 ? st1 : st2; };
 
   int tmi, tni;
   grouped_tile(xcd_remap(blockIdx.x, p.tiles_m * p.tiles_n), p.tiles_m, p.tiles_n, tmi, tni);
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(256, OCC) void gated_mfma(Gated p) {
   bar();
   read(st0, 0);
   // slices past the end load zeros in both operands and add nothing
-  constexpr int UNR = NS % 2 ? 2 * NS : NS;  // whole cycles of stages and of register buffers
+  constexpr int UNR = 2 * NS;  // whole cycles of stages and of register buffers
   const int tend = (n + UNR - 1) / UNR * UNR;
   for (int t = 0; t < tend; t += UNR) {
 #pragma unroll
@@ -593,19 +593,19 @@ hipError_t run(DType dt, int a_kmaj, int b_kmaj, std::initializer_list<GemmProbl
 
 dim3 blocks_of(int64_t n, int per) { return dim3((unsigned)((n + 256 * per - 1) / (256 * per))); }
 
-// The larger tile once it gives every compute unit one (8192 x 2048 x 5504, 2752
-// tiles: forward 412 us against the smaller one's 494, backward 322 against 333;
-// 1501 x 1000 x 2744, 132 of them: backward 64 against 49).  Tiles of 256 rows, one
-// workgroup a compute unit, whose epilogues nothing covers, took 474 and 386.
+// The larger tile, two workgroups a compute unit, once it gives every compute unit
+// two (8192 x 2048 x 5504, 2752 tiles: forward 412 us, backward 322); three of 64
+// columns below that (1501 x 1000 x 2744, 264 large tiles: 46 against 39 forward, 64
+// against 38 backward).  Tiles of 256 rows, one workgroup a compute unit, whose
+// epilogues nothing covers, took 474 and 386 of the first.
 template <int BWD>
 hipError_t launch_gated(Gated p, hipStream_t s) {
   constexpr int BN = BWD ? 256 : 128;
-  const int64_t large = (int64_t)cdiv(p.M, 128) * cdiv(p.N, BN), small = (int64_t)cdiv(p.M, 128) * cdiv(p.N, BN / 2);
+  const int64_t large = (int64_t)cdiv(p.M, 128) * cdiv(p.N, BN), small = (int64_t)cdiv(p.M, 128) * cdiv(p.N, 64);
   p.tiles_m = cdiv(p.M, 128);
-  p.tiles_n = cdiv(p.N, large >= 256 ? BN : BN / 2);
-  if (large >= 256)
-    hipLaunchKernelGGL((gated_mfma<BWD, 128, BN, 2, 3>), dim3((unsigned)large), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((gated_mfma<BWD, 128, BN / 2, 2, 4>), dim3((unsigned)small), dim3(256), 0, s, p);
+  p.tiles_n = cdiv(p.N, large >= 512 ? BN : 64);
+  if (large >= 512) hipLaunchKernelGGL((gated_mfma<BWD, 128, BN, 2>), dim3((unsigned)large), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((gated_mfma<BWD, 128, 64, 3>), dim3((unsigned)small), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "common.h"
 #include "gemm_pipe.h"
@@ -83,7 +84,9 @@ struct NsArgs {
   float scale;             // of the accumulators
   float ca, cb;            // POLY: a and b, at the result's scale
   int splits, per;         // ranges of K, slices of one
-  float* part;             // [matrix][range][tile][a thread's accumulators]
+  float* part;             // the ranges' accumulators
+  int M, N;                // sides, multiples of 128
+  int tiles, whole;        // large tiles: in all, and those that are not cut
   Result r;
 };
 
@@ -305,10 +308,9 @@ template <int MODE, bool COLS>
 struct Strip {
   Beside beside[4];
   int r, c;  // this lane's first row and its columns
-  // Strip q of the wavefront's quarter of tile (tm, tn).
-  __device__ __forceinline__ void ask_for(const NsArgs& p, int mat, int tm, int tn, int q) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int mw = tm * kTile + (wave >> 1) * 64, nw = tn * kTile + (wave & 1) * 64;
+  // Strip q of the 64 x 64 at (mw, nw).
+  __device__ __forceinline__ void ask_for(const NsArgs& p, int mat, int mw, int nw, int q) {
+    const int lane = threadIdx.x & 63;
     if (MODE == LAST && !p.r.vec) {
       // a lane to a column
       r = (COLS ? nw : mw) + 16 * q;
@@ -361,17 +363,19 @@ __device__ __forceinline__ bool emits(const NsArgs& p, int tm, int tn, bool cols
   return !cols || ((MODE == GRAM || MODE == POLY) && tm != tn);
 }
 
-// A whole tile, every strip's operands asked for at once.
-template <int MODE, bool COLS>
-__device__ __forceinline__ void ns_emit(const NsArgs& p, int mat, int tm, int tn, const f32x4_t (&acc)[4][4], float* strip) {
+// The 64 x 64 at (mw, nw), blocks (I, J) .. of a wavefront's, every strip's operands
+// asked for at once.
+template <int MODE, bool COLS, int FM, int FN, int I = 0, int J = 0>
+__device__ __forceinline__ void ns_emit(const NsArgs& p, int mat, int mw, int nw, const f32x4_t (&acc)[FM][FN],
+                                        float* strip) {
   Strip<MODE, COLS> s[4];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) s[q].ask_for(p, mat, tm, tn, q);
+  for (int q = 0; q < 4; ++q) s[q].ask_for(p, mat, mw, nw, q);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     f32x4_t blocks[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) blocks[j] = COLS ? acc[j][q] : acc[q][j];
+    for (int j = 0; j < 4; ++j) blocks[j] = COLS ? acc[I + j][J + q] : acc[I + q][J + j];
     s[q].emit(p, mat, blocks, strip);
   }
 }
@@ -513,19 +517,22 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
     return;
   }
   float* strip = reinterpret_cast<float*>(st0) + wave * 16 * kStripPitch;
-  if (emits<MODE>(p, tm, tn, false)) ns_emit<MODE, false>(p, mat, tm, tn, acc, strip);
-  if (emits<MODE>(p, tm, tn, true)) ns_emit<MODE, true>(p, mat, tm, tn, acc, strip);
+  const int mw = m0 + wm * WT, nw = n0 + wn * WT;
+  if (emits<MODE>(p, tm, tn, false)) ns_emit<MODE, false, F, F>(p, mat, mw, nw, acc, strip);
+  if (emits<MODE>(p, tm, tn, true)) ns_emit<MODE, true, F, F>(p, mat, mw, nw, acc, strip);
 }
 
-// A tile's ranges added in order, and its epilogue: a workgroup for each of its
-// strips (one for a whole tile took 12.7 us for 18 tiles of 8 ranges, these 7.6).
-template <int MODE, bool COLS>
-__device__ __forceinline__ void join_strip(const NsArgs& p, int mat, int t, int tm, int tn, int q, float* strip) {
+// A tile's ranges added in order, and its epilogue: a workgroup for each strip of its
+// wavefronts' 64 x 64 (one for a whole tile took 12.7 us for 18 tiles of 8 ranges,
+// these 7.6).  F: blocks along a wavefront's columns.  The sums of block (i, j) lie
+// `total` * 1024 floats from those of the next, a range's `tiles` * 1024.
+template <int MODE, bool COLS, int F>
+__device__ __forceinline__ void join_strip(const NsArgs& p, int mat, int mw, int nw, const float* o, int64_t tiles, int I,
+                                           int J, int q, float* strip) {
   Strip<MODE, COLS> s;
-  s.ask_for(p, mat, tm, tn, q);
+  s.ask_for(p, mat, mw, nw, q);
   f32x4_t sum[4];
-  const int64_t block = (int64_t)p.total * 1024, range = (int64_t)p.per_matrix * 1024;
-  const float* o = p.part + (((int64_t)mat * p.splits * p.per_matrix + t) * 256 + threadIdx.x) * 4;
+  const int64_t block = (int64_t)p.total * 1024, range = tiles * 1024;
   for (int r0 = 0; r0 < p.splits; r0 += 4) {
     f32x4_t v[4][4];
 #pragma unroll
@@ -533,7 +540,8 @@ __device__ __forceinline__ void join_strip(const NsArgs& p, int mat, int t, int 
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (r0 + r < p.splits)
-          v[r][j] = *reinterpret_cast<const f32x4_t*>(o + (r0 + r) * range + (COLS ? 4 * j + q : 4 * q + j) * block);
+          v[r][j] = *reinterpret_cast<const f32x4_t*>(o + (r0 + r) * range +
+                                                      (COLS ? F * (I + j) + J + q : F * (I + q) + J + j) * block);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -549,9 +557,188 @@ __global__ __launch_bounds__(256, 2) void ns_join(NsArgs p) {
   int tm, tn;
   if (MODE == GRAM || MODE == POLY) triangle(t, tm, tn);
   else grouped_tile(t, p.tiles_m, p.tiles_n, tm, tn);
-  float* strip = lds[threadIdx.x >> 6];
-  if (emits<MODE>(p, tm, tn, false)) join_strip<MODE, false>(p, mat, t, tm, tn, q, strip);
-  if (emits<MODE>(p, tm, tn, true)) join_strip<MODE, true>(p, mat, t, tm, tn, q, strip);
+  const int wave = threadIdx.x >> 6, mw = tm * kTile + (wave >> 1) * 64, nw = tn * kTile + (wave & 1) * 64;
+  const float* o = p.part + (((int64_t)mat * p.splits * p.per_matrix + t) * 256 + threadIdx.x) * 4;
+  float* strip = lds[wave];
+  if (emits<MODE>(p, tm, tn, false)) join_strip<MODE, false, 4>(p, mat, mw, nw, o, p.per_matrix, 0, 0, q, strip);
+  if (emits<MODE>(p, tm, tn, true)) join_strip<MODE, true, 4>(p, mat, mw, nw, o, p.per_matrix, 0, 0, q, strip);
+}
+
+// ----------------------------------------------------------- large tiles --
+// X X^T of many columns on tiles of 256 x 256, a wavefront's 128 x 128: half the
+// bytes through LDS for a product.  A slice's three products run one after the
+// other, so that each part's fragments are read while two others multiply and no
+// part is held twice:
+//   A.hi B.lo  (reads B.hi),  A.hi B.hi  (reads A.lo),
+//   barrier: this slice is read, the next one has landed,
+//   A.lo B.hi  (reads the next slice's A.hi and B.lo, asks for the one after).
+// Whole rounds of a tile a compute unit go first; what is left of the tiles is cut
+// along k so that it fills the chip once more, and joined (2 x 2048 x 5504, 72 tiles
+// in three ranges: 154 us and 22 joined, at the library's rate of a fp16 product;
+// 272 tiles of 128 x 128 219).  The other products gain nothing: B X on 256 x 128
+// tiles took 279 us against 251, A A of 2048 rows 63 and 26 joined against 86.
+constexpr int kBig = 256;
+
+__device__ __forceinline__ void big_tile(const NsArgs& p, int tile, int& mat, int& tm, int& tn) {
+  mat = tile / p.per_matrix;
+  triangle(tile % p.per_matrix, tm, tn);
+}
+
+__global__ __launch_bounds__(256, 1) void ns_big(NsArgs p) {
+  using namespace pipe;
+  constexpr int F = 8, WT = 128;
+  typedef Src<kBig, 1> S;
+  constexpr int REGION = S::BYTES, SBYTES = 4 * REGION, L = 4 * S::IPW;
+  __shared__ __attribute__((aligned(1024))) char st0[SBYTES], st1[SBYTES];
+  int tile, range = 0, slot = 0;
+  if ((int)blockIdx.x < p.whole) {
+    tile = xcd_remap(blockIdx.x, p.whole);
+  } else {
+    const int rest = p.tiles - p.whole;
+    slot = xcd_remap(blockIdx.x - p.whole, p.total);
+    tile = p.whole + slot % rest;
+    range = slot / rest;
+  }
+  const bool cut = (int)blockIdx.x >= p.whole && p.splits > 1;
+  int mat, tm, tn;
+  big_tile(p, tile, mat, tm, tn);
+  const int m0 = tm * kBig, n0 = tn * kBig;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const int slices = p.K / KS, s0 = cut ? range * p.per : 0, n = cut ? min(p.per, slices - s0) : slices;
+
+  S ah, al, bh, bl;
+  auto start = [&](S& x, const half_t* at, int r0) {
+    x.init(0, reinterpret_cast<const bf16*>(at + mat * p.sa), p.lda, r0, p.M, p.K, wave, lane);
+    x.clear(1);
+    x.start(p.lda, r0, p.M, p.K);
+    x.so = (uint32_t)(s0 * KS) * x.ks;
+  };
+  start(ah, p.a.hi, m0);
+  start(al, p.a.lo, m0);
+  start(bh, p.a.hi, n0);
+  start(bl, p.a.lo, n0);
+  auto issue = [&](char* stage) {
+    ah.load(stage, wave);
+    al.load(stage + REGION, wave);
+    bh.load(stage + 2 * REGION, wave);
+    bl.load(stage + 3 * REGION, wave);
+    ah.advance();
+    al.advance();
+    bh.advance();
+    bl.advance();
+  };
+  Frag<kBig, 1, F> fa, fb;
+  fa.init(wm * WT, lane);
+  fb.init(wn * WT, lane);
+  f32x4_t acc[F][F];
+#pragma unroll
+  for (int i = 0; i < F; ++i)
+#pragma unroll
+    for (int j = 0; j < F; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  halfx8_t ahi[F], alo[F], bhi[F], blo[F];
+  auto read = [&](halfx8_t (&r)[F], const Frag<kBig, 1, F>& f, const char* region) {
+#pragma unroll
+    for (int i = 0; i < F; ++i) r[i] = __builtin_bit_cast(halfx8_t, f.read(region, i));
+  };
+  auto mma = [&](const halfx8_t (&a)[F], const halfx8_t (&b)[F]) {
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], a[i], acc[i][j], 0, 0, 0);
+  };
+  // one LDS read an MFA from the first on, loads after them
+  auto interleave = [&](int reads, int loads) {
+#pragma unroll
+    for (int q = 0; q < F * F; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFA
+      if (q < reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
+      else if (q - reads < loads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // buffer load to LDS
+    }
+  };
+  // keeps 256 accumulators in the accumulation registers (left to itself the
+  // allocator moves two of three through the others and back each slice)
+  auto hold = [&]() {
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int j = 0; j < F; ++j) asm volatile("" : "+a"(acc[i][j]));
+  };
+  auto step = [&](char* now, const char* next) {
+    hold();
+    read(bhi, fb, now + 2 * REGION);
+    mma(ahi, blo);
+    interleave(F, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    read(alo, fa, now + REGION);
+    mma(ahi, bhi);
+    interleave(F, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    FAL_WAITCNT(0, 0);
+    bar();
+    __builtin_amdgcn_sched_barrier(0);
+    issue(now);
+    read(blo, fb, next + 3 * REGION);
+    read(ahi, fa, next);
+    mma(alo, bhi);
+    interleave(2 * F, L);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  issue(st0);
+  issue(st1);
+  FAL_WAITCNT(L, 0);
+  bar();
+  read(blo, fb, st0 + 3 * REGION);
+  read(ahi, fa, st0);
+  // (n is even.  Slices past it are asked for and not multiplied: what lies behind,
+  // or zeros past the buffers' range.)
+  for (int s = 0; s < n; s += 2) {
+    step(st0, st1);
+    step(st1, st0);
+  }
+  hold();
+  FAL_WAITCNT(0, 0);
+  bar();
+
+  if (cut) {
+    float* o = p.part + ((int64_t)slot * 256 + threadIdx.x) * 4;
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int j = 0; j < F; ++j) *reinterpret_cast<f32x4_t*>(o + (i * F + j) * (int64_t)p.total * 1024) = acc[i][j];
+    return;
+  }
+  float* strip = reinterpret_cast<float*>(st0) + wave * 16 * kStripPitch;
+  const int mw = m0 + wm * WT, nw = n0 + wn * WT;
+  auto quarter = [&](auto hi, auto hj) {
+    constexpr int I = 4 * decltype(hi)::value, J = 4 * decltype(hj)::value;
+    // (the sides are multiples of 128: a quarter lies inside or past the end)
+    if (mw + 16 * I >= p.M || nw + 16 * J >= p.M) return;
+    ns_emit<GRAM, false, F, F, I, J>(p, mat, mw + 16 * I, nw + 16 * J, acc, strip);
+    if (tm != tn) ns_emit<GRAM, true, F, F, I, J>(p, mat, mw + 16 * I, nw + 16 * J, acc, strip);
+  };
+  typedef std::integral_constant<int, 0> zero;
+  typedef std::integral_constant<int, 1> one;
+  quarter(zero(), zero());
+  quarter(zero(), one());
+  quarter(one(), zero());
+  quarter(one(), one());
+}
+
+__global__ __launch_bounds__(256, 2) void ns_big_join(NsArgs p) {
+  __shared__ __attribute__((aligned(16))) float lds[4][16 * kStripPitch];
+  const int q = blockIdx.x & 3, J = blockIdx.x & 4, I = blockIdx.x >> 1 & 4, rest = blockIdx.x >> 4;
+  int mat, tm, tn;
+  big_tile(p, p.whole + rest, mat, tm, tn);
+  const int wave = threadIdx.x >> 6;
+  const int mw = tm * kBig + (wave >> 1) * 128 + 16 * I, nw = tn * kBig + (wave & 1) * 128 + 16 * J;
+  if (mw >= p.M || nw >= p.M) return;
+  const float* o = p.part + ((int64_t)rest * 256 + threadIdx.x) * 4;
+  float* strip = lds[wave];
+  const int tiles = p.tiles - p.whole;
+  join_strip<GRAM, false, 8>(p, mat, mw, nw, o, tiles, I, J, q, strip);
+  if (tm != tn) join_strip<GRAM, true, 8>(p, mat, mw, nw, o, tiles, I, J, q, strip);
 }
 
 // Products of few tiles and many slices: K in as many ranges as the compute units
@@ -567,14 +754,76 @@ int ranges(int tiles, int K, int* per) {
   return cdiv(slices, each);
 }
 
+// How a product runs.
+struct Plan {
+  int big, tiles, whole, splits, per;
+  int64_t part() const {  // bytes of the ranges' sums
+    return splits > 1 ? (int64_t)(tiles - whole) * splits * (big ? kBig * kBig : kTile * kTile) * 4 : 0;
+  }
+};
+
+Plan plan_tiles(int tiles, int K) {
+  Plan t = {0, tiles, 0, 1, 0};
+  t.splits = ranges(tiles, K, &t.per);
+  return t;
+}
+
+// X X^T: large tiles where their estimated time is the smaller one (us: a slice of
+// 32 k on a large tile, and on one of 128 x 128 alone on its compute unit or sharing
+// it; what each round and a joining launch add; ranges' sums written and read at 8
+// TB/s).
+Plan plan_gram(int P, int K, int matrices) {
+  constexpr double kBigSlice = 2.45, kPair = 1.04, kAlone = 0.65, kBigRound = 12.0, kRound = 8.0, kJoin = 6.0;
+  auto count = [&](int side) { return cdiv(P, side) * (cdiv(P, side) + 1) / 2 * matrices; };
+  const int slices = K / pipe::KS;
+  Plan b = {1, count(kBig), 0, 1, slices};
+  b.whole = b.tiles / kOneRound * kOneRound;
+  const int rest = b.tiles - b.whole;
+  double big = b.whole / kOneRound * (kBigRound + slices * kBigSlice);
+  if (rest) {
+    const int s = std::max(1, std::min(kOneRound / rest, slices / 4)), each = cdiv(cdiv(slices, s), 2) * 2;
+    const double join = kJoin + (double)rest * s * kBig * kBig * 4 / 4e6;
+    if (s > 1 && (slices - each) * kBigSlice > join) {
+      b.per = each;
+      b.splits = cdiv(slices, each);
+      big += join;
+    }
+    big += kBigRound + b.per * kBigSlice;
+  }
+  const Plan t = plan_tiles(count(kTile), K);
+  const int n = t.tiles * t.splits, rounds = n / (2 * kOneRound), last = n % (2 * kOneRound);
+  double small = n <= kOneRound ? kRound + t.per * kAlone : rounds * (kRound + t.per * kPair);
+  if (n > kOneRound && last) small += kRound + t.per * (last > kOneRound ? kPair : kAlone);
+  if (t.splits > 1) small += kJoin + t.part() / 4e6;
+  return big < small ? b : t;
+}
+
+template <int MODE>
+Plan plan(int M, int N, int K, int matrices) {
+  const int tm = M / kTile, tn = N / kTile;
+  if (MODE == GRAM) return plan_gram(M, K, matrices);
+  return plan_tiles((MODE == POLY ? tm * (tm + 1) / 2 : tm * tn) * matrices, K);
+}
+
 template <int MODE>
 void launch(NsArgs p, int matrices, hipStream_t s) {
-  const int tiles = p.per_matrix * matrices;
-  p.splits = ranges(tiles, p.K, &p.per);
-  p.total = tiles * p.splits;
+  const Plan q = plan<MODE>(p.M, p.N, p.K, matrices);
+  p.tiles_m = p.M / kTile;
+  p.tiles_n = p.N / kTile;
+  p.per_matrix = q.tiles / matrices;
+  p.splits = q.splits;
+  p.per = q.per;
+  p.tiles = q.tiles;
+  p.whole = q.whole;
+  p.total = (q.tiles - q.whole) * q.splits;
+  if (q.big) {
+    hipLaunchKernelGGL(ns_big, dim3(q.whole + p.total), dim3(256), 0, s, p);
+    if (q.splits > 1) hipLaunchKernelGGL(ns_big_join, dim3(16 * (q.tiles - q.whole)), dim3(256), 0, s, p);
+    return;
+  }
   if (p.total <= kOneRound) hipLaunchKernelGGL((ns_product<MODE, 1, 4>), dim3(p.total), dim3(256), 0, s, p);
   else hipLaunchKernelGGL((ns_product<MODE, 2, 2>), dim3(p.total), dim3(256), 0, s, p);
-  if (p.splits > 1) hipLaunchKernelGGL(ns_join<MODE>, dim3(4 * tiles), dim3(256), 0, s, p);
+  if (q.splits > 1) hipLaunchKernelGGL(ns_join<MODE>, dim3(4 * q.tiles), dim3(256), 0, s, p);
 }
 
 // --------------------------------------------------------- small matrices --
@@ -824,17 +1073,11 @@ Sizes sizes(const NewtonSchulz& s) {
   const int64_t batches = (s.count + most - 1) / most;
   z.chunk = (int)((s.count + batches - 1) / batches);
   z.nparts = (int)std::min<int64_t>(kNormBlocksNs, ((int64_t)s.rows * s.cols + 4095) / 4096);
-  const int tp = z.P / kTile, tq = z.Q / kTile;
   z.part = 0;
-  for (int n : {z.chunk, s.count % z.chunk}) {  // (a last batch may be smaller, and its products cut)
-    if (!n) continue;
-    int per;
-    const int gram = tp * (tp + 1) / 2 * n, apply = tp * tq * n;
-    const int most = std::max({ranges(gram, z.Q, &per) > 1 ? ranges(gram, z.Q, &per) * gram : 0,
-                               ranges(gram, z.P, &per) > 1 ? ranges(gram, z.P, &per) * gram : 0,
-                               ranges(apply, z.P, &per) > 1 ? ranges(apply, z.P, &per) * apply : 0});
-    z.part = std::max(z.part, (int64_t)most * kTile * kTile * 4);
-  }
+  for (int n : {z.chunk, s.count % z.chunk})  // (a last batch may be smaller, and its products cut)
+    if (n)
+      z.part = std::max({z.part, plan<GRAM>(z.P, z.P, z.Q, n).part(), plan<POLY>(z.P, z.P, z.P, n).part(),
+                         plan<APPLY>(z.P, z.Q, z.P, n).part()});
   return z;
 }
 
@@ -998,14 +1241,13 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
       const int ea = exponent(top), eb = exponent(std::max(largest(s.a, s.b, s.c, top), std::fabs((double)s.a))),
                 en = exponent(sigma[k + 1]);
       const int64_t sx = (int64_t)z.P * z.Q, sp = (int64_t)z.P * z.P;
-      const int tp = z.P / kTile, tq = z.Q / kTile;
       NsArgs p;
       memset(&p, 0, sizeof(p));
       p.part = sums;
       // A = X X^T
       p.a = p.b = x0; p.lda = p.ldb = z.Q; p.sa = p.sb = sx; p.K = z.Q;
       p.c = A; p.ldc = z.P; p.sc = sp;
-      p.tiles_m = p.tiles_n = tp; p.per_matrix = tp * (tp + 1) / 2;
+      p.M = p.N = z.P;
       p.scale = (float)std::ldexp(1.0, ea - 2 * ex);
       launch<GRAM>(p, n, stream);
       // B = a I + b A + c A A
@@ -1018,7 +1260,7 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
       // X <- B X
       p.a = B; p.b = x0; p.ldb = z.Q; p.sb = sx;
       p.c = x1; p.ldc = z.Q; p.sc = sx;
-      p.tiles_n = tq; p.per_matrix = tp * tq;
+      p.N = z.Q;
       if (k + 1 < s.steps) {
         p.scale = (float)std::ldexp(1.0, en - eb - ex);
         launch<APPLY>(p, n, stream);

@@ -146,6 +146,17 @@ def test_products_cut_along_k(count, rows, cols, dtype):
     check(count, rows, cols, dtype, seed=rows)
 
 
+@pytest.mark.parametrize("count", [2, 8])  # 72 and 288 tiles of 256 x 256
+def test_products_on_large_tiles(count):
+    x = make(9, count, 2000, 5000, F32)
+    got = fal.newton_schulz(x, steps=3)
+    some = [0, count - 1]
+    want, bounds = exact(x[some], 3, COEF)
+    hold(got[some], want, bounds, in_fp32(x[some], 3, COEF), U)
+    norms = torch.linalg.matrix_norm(got)
+    assert ((norms - norms.mean()).abs() < 0.02 * norms.mean()).all()
+
+
 def test_large():
     check(1, 700, 2100, BF16)
     check(1, 1000, 640, F32)
