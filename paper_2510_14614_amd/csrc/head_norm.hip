@@ -16,7 +16,10 @@
 // All heads of a token share its angles: lane j computes the j-th pair's once,
 // and the wavefront passes them round through LDS.  Angles are products in fp64,
 // reduced to a turn before their sine and cosine in fp32: a position of 10^6
-// loses nothing.
+// loses nothing.  The next heads are asked for while one group of heads is worked on.
+// Measured: 8 x 1024 tokens, 36 heads of 64 in bf16 17.5 us forward and 21.3
+// backward (4.3 and 4.7 TB/s; a large copy reaches 4.9), 2 x 8192 tokens, 48 heads
+// of 128 87 and 120 us (4.6 and 4.75).
 #include <algorithm>
 
 #include "common.h"
@@ -28,22 +31,42 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kMaxPairs = 64;  // half of the widest head
-constexpr int kBwdBlocks = 1024;  // of the backward, four workgroups a compute unit
+// Workgroups of the backward, each with a row of the weights' sums: three a compute
+// unit, what its registers allow at once (2 x 8192 tokens, 48 heads of 128: 120 us,
+// the rate of a copy; with 1024, a third of which wait, 146; with 1024 at four a
+// compute unit and registers in memory 130).
+constexpr int kBwdBlocks = 768;
 
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
-  const uint4 w = *reinterpret_cast<const uint4*>(p);
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(u[i] << 16);
-    v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+// Eight elements as they lie in memory, and widened.
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const float4*>(p);
+    b = *reinterpret_cast<const float4*>(p + 4);
   }
-}
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    *reinterpret_cast<float4*>(p) = a;
+    *reinterpret_cast<float4*>(p + 4) = b;
+  }
+};
+template <> struct Raw<bf16> {
+  uint4 w;
+  __device__ __forceinline__ void load(const bf16* p) { w = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(u[i] << 16);
+      v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+  }
+  __device__ __forceinline__ void store(bf16* p) const { *reinterpret_cast<uint4*>(p) = w; }
+};
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
@@ -166,18 +189,17 @@ __global__ __launch_bounds__(kWaves * 64) void head_norm_fwd(HeadNorm a, const T
       for (int h = l.head0; h < all; h += L::HPW) store8(yr + (int64_t)h * HD, zero);
       continue;
     }
+    // (heads past the last one repeat it and are not stored: whole wavefronts run
+    // the loop, since sums and partners come from other lanes)
+    Raw<T> next;
+    next.load(xr + (int64_t)min(l.head0, turned - 1) * HD);
     Turn t;
     l.turn(a, position_of(a, m), 1.f, lane, table[wave], t);
-    // (whole wavefronts run the loop: the sums and partners come from other lanes)
     for (int h0 = 0; h0 < turned; h0 += L::HPW) {
       const int h = h0 + l.head0;
       float v[8];
-      if (h < turned) {
-        load8(xr + (int64_t)h * HD, v);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.f;
-      }
+      next.get(v);
+      if (h0 + L::HPW < turned) next.load(xr + (int64_t)min(h + L::HPW, turned - 1) * HD);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum = fmaf(v[i], v[i], sum);
@@ -189,9 +211,8 @@ __global__ __launch_bounds__(kWaves * 64) void head_norm_fwd(HeadNorm a, const T
     }
     if (!in_place)
       for (int h = turned + l.head0; h < all; h += L::HPW) {
-        float v[8];
-        load8(xr + (int64_t)h * HD, v);
-        store8(yr + (int64_t)h * HD, v);
+        next.load(xr + (int64_t)h * HD);
+        next.store(yr + (int64_t)h * HD);
       }
   }
 }
@@ -219,17 +240,23 @@ __global__ __launch_bounds__(kWaves * 64) void head_norm_bwd(HeadNorm a, const T
       for (int h = l.head0; h < all; h += L::HPW) store8(dr + (int64_t)h * HD, zero);
       continue;
     }
+    Raw<T> nx, ng;
+    nx.load(xr + (int64_t)min(l.head0, turned - 1) * HD);
+    ng.load(gr + (int64_t)min(l.head0, turned - 1) * HD);
     Turn t;
     l.turn(a, position_of(a, m), -1.f, lane, table[wave], t);
     for (int h0 = 0; h0 < turned; h0 += L::HPW) {
       const int h = h0 + l.head0;
       float v[8], g[8];
-      if (h < turned) {
-        load8(xr + (int64_t)h * HD, v);
-        load8(gr + (int64_t)h * HD, g);
-      } else {
+      nx.get(v);
+      ng.get(g);
+      if (h0 + L::HPW < turned) {
+        nx.load(xr + (int64_t)min(h + L::HPW, turned - 1) * HD);
+        ng.load(gr + (int64_t)min(h + L::HPW, turned - 1) * HD);
+      }
+      if (h >= turned) {  // adds nothing to the weights' sums
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = g[i] = 0.f;
+        for (int i = 0; i < 8; ++i) g[i] = 0.f;
       }
       float sum = 0.f;
 #pragma unroll
@@ -253,9 +280,8 @@ __global__ __launch_bounds__(kWaves * 64) void head_norm_bwd(HeadNorm a, const T
     }
     if (!in_place)
       for (int h = turned + l.head0; h < all; h += L::HPW) {
-        float v[8];
-        load8(gr + (int64_t)h * HD, v);
-        store8(dr + (int64_t)h * HD, v);
+        ng.load(gr + (int64_t)h * HD);
+        ng.store(dr + (int64_t)h * HD);
       }
   }
   if (!part) return;
@@ -281,7 +307,8 @@ __global__ __launch_bounds__(kWaves * 64) void head_norm_bwd(HeadNorm a, const T
 
 // dw[e] = sum over workgroups of part[b][e], in fp64: 16 columns a workgroup,
 // 64 threads a column, whose loads are all under way at once (16 threads a
-// column that waited for each took 17 us for 1024 rows of 128, these 5).
+// column that waited for each took 17 us for 1024 rows of 128, these 6.7, and 5.4
+// for 768).
 __global__ __launch_bounds__(1024) void head_norm_weights(const float* part, int nblk, int hd, float* dwq, float* dwk) {
   __shared__ double red[64][17];
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4, e = blockIdx.x * 16 + c;

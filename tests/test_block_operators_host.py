@@ -97,10 +97,10 @@ def test_head_norms_backward_refuses(args, status, word):
 
 
 def test_head_norm_workspace():
-    # two rows of fp32 a workgroup of four tokens, up to 1024 workgroups
+    # two rows of fp32 a workgroup of four tokens, up to 768 workgroups
     assert norm_bytes(norm()) == 150 * 2 * 64 * 4
     assert norm_bytes(norm(batch=1, seq_len=1)) == 2 * 64 * 4
-    assert norm_bytes(norm(batch=64, seq_len=8192)) == 1024 * 2 * 64 * 4
+    assert norm_bytes(norm(batch=64, seq_len=8192)) == 768 * 2 * 64 * 4
     assert fal.lib().fal_qk_norm_rope_workspace_bytes(byref(norm()), None) == BAD
 
 
