@@ -553,7 +553,8 @@ fal_status_t fal_qk_norm_rope_workspace_bytes(const fal_qk_norm_rope_t* shape, s
  *              zeros.
  *   out        device dtype; may be qkv itself with the same row stride (the
  *              backward then has no input to go by)
- * Angles are products in fp64, everything else fp32, rounded once.
+ * Angles are products in fp64, everything else fp32, rounded once.  (Squares
+ * are summed in fp32: a head whose sum passes its range becomes zeros.)
  * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes, misalignment or
  * an output that overlaps an input; FAL_ERR_UNSUPPORTED for another head_dim
  * or a rotary_dim that is no multiple of 8; FAL_ERR_HIP when a launch fails. */
@@ -604,7 +605,8 @@ fal_status_t fal_gated_ffn_workspace_bytes(const fal_gated_ffn_t* shape, size_t*
  *              NULL where none follows
  *   workspace  device, 256-byte aligned
  * Products of bf16 operands are summed in fp32; act(x Wg) * (x Wu) is rounded
- * to bf16 once, as the operand of the last product, and y once.
+ * to bf16 at most once, as the operand of the last product (calls of up to 8
+ * rows keep it in fp32), and y once.
  * bf16 takes matrices of 16-byte aligned rows: d, f and the strides multiples
  * of 8, each operand below 2 GiB.  fp32 takes any size.
  * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes, misalignment or
@@ -632,8 +634,10 @@ fal_status_t fal_gated_ffn_bwd(const fal_gated_ffn_t* shape, const void* x, cons
  * batch becomes X = U / |U|_F (Frobenius norm), then, `steps` times,
  *   X <- (a I + b X X^T + c (X X^T)^2) X
  * (for rows > cols the same of its transpose): its singular values go through
- * a s + b s^3 + c s^5, its singular vectors stay.  Sums are fp32; X and both
- * factors are held to 22 bits between the products. */
+ * a s + b s^3 + c s^5, its singular vectors stay.  Norms are summed in fp64,
+ * products in fp32; X and both factors are held to 22 bits between the products.
+ * (Sums over k are cut by what fills the chip, so a matrix's last bits depend on
+ * the number of matrices beside it.) */
 typedef struct {
   int32_t count;       /* matrices, >= 1                                     */
   int32_t rows, cols;  /* >= 1 each, dense rows                              */
@@ -678,7 +682,8 @@ typedef struct {
  *   momentum  device fp32, zero before the first step, updated in place
  * All four lie alike: matrices [rows, cols], `stride` elements apart (the
  * matrices of one kind in fal_param_layout's buffers are block_stride apart).
- * Elements between them are left as they are.  Errors as fal_newton_schulz. */
+ * Elements between them are left as they are.  A matrix whose gradient or
+ * momentum is not finite becomes NaN.  Errors as fal_newton_schulz. */
 fal_status_t fal_muon_step(const fal_newton_schulz_t* shape, const fal_muon_t* hp, float* master, void* params,
                            const float* grads, float* momentum, void* workspace, size_t ws_bytes, void* stream);
 
