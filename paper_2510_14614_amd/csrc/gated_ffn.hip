@@ -563,13 +563,15 @@ __global__ __launch_bounds__(256) void join_gate_bwd(const float* dh, int parts,
   }
 }
 
-// out[m][c] = the parts' sum (bf16, N a multiple of 8).
-__global__ __launch_bounds__(256) void join_rows(const float* part, int parts, int64_t n, int N, bf16* out, int64_t ldo) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+// out[m][c] = the parts' sum.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void join_rows(const float* part, int parts, int64_t n, int N, T* out, int64_t ldo) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
   if (i >= n) return;
-  float v[4];
-  sum_parts<4>(part + i, parts, n, v);
-  st4(out + i / N * ldo + i % N, v);
+  float v[V];
+  sum_parts<V>(part + i, parts, n, v);
+#pragma unroll
+  for (int e = 0; e < V; ++e) out[i / N * ldo + i % N + e] = from_f<T>(v[e]);
 }
 
 GemmProblem product(const void* A, int64_t lda, const void* B, int64_t ldb, int M, int N, int K, void* out,
@@ -582,13 +584,12 @@ GemmProblem product(const void* A, int64_t lda, const void* B, int64_t ldb, int 
   return p;
 }
 
-hipError_t run(DType dt, int a_kmaj, int b_kmaj, std::initializer_list<GemmProblem> ps, hipStream_t s,
-               float* split = nullptr, int64_t split_floats = 0) {
+hipError_t run(DType dt, int a_kmaj, int b_kmaj, std::initializer_list<GemmProblem> ps, hipStream_t s) {
   GemmGroup g;
   memset(&g, 0, sizeof(g));
   for (const GemmProblem& p : ps) g.p[g.n++] = p;
   const char* why;
-  return gemm(dt, a_kmaj, b_kmaj, g, 0, s, &why, split, split_floats);
+  return gemm(dt, a_kmaj, b_kmaj, g, 0, s, &why);
 }
 
 dim3 blocks_of(int64_t n, int per) { return dim3((unsigned)((n + 256 * per - 1) / (256 * per))); }
@@ -627,36 +628,114 @@ Cut cut(int M, int N, int K, int products, int most) {
 
 int64_t round_up(int64_t n) { return (n + 255) / 256 * 256; }
 
-// What a bf16 call cuts (parts 1: that product runs whole).
+// The same of fp32 sums over f: where tiles are few (forward and backward of
+// 20 x 1000 x 3000: 199 us whole, 110 in parts; 500 x 2000 x 4000: 991 and 881;
+// 64 x 64 x 256, where the join costs what it saves: 55), and from 4096 terms on,
+// because a sum adds one rounding a term and four shorter ones halve the error
+// (9504 terms: 1.2e-6 of the norm, 6e-7 in four; 1000 x 4096 x 11008: 7964 us
+// whole, 7609 in parts).
+Cut cut_f32(int M, int N, int K, int most) {
+  const int per = (cdiv(K, most) + 3) / 4 * 4;
+  const bool few = (int64_t)cdiv(M, 64) * cdiv(N, 64) * most <= 1024 && K >= 512;
+  return K >= 4096 || few ? Cut{cdiv(K, per), per} : Cut{1, K};
+}
+
+// What a call cuts (parts 1: that product runs whole).
 struct Cuts {
   Cut gate, down;  // forward: x Wg and x Wu, h Wd
   Cut dh, dx;      // backward: dy Wd^T, each of dx's two products
+  bool apart;      // dx's two products are problems of their own
 };
-Cuts cuts(const GatedFfn& a) {
-  return {cut(a.M, a.f, a.d, 2, 2), cut(a.M, a.d, a.f, 1, 4), cut(a.M, a.f, a.d, 1, 4), cut(a.M, a.d, a.f, 2, 2)};
+Cuts cuts(DType dt, const GatedFfn& a) {
+  if (dt == F32) {
+    const Cut whole = {1, a.d}, dx = cut_f32(a.M, a.d, a.f, 2);
+    return {whole, cut_f32(a.M, a.d, a.f, 4), whole, dx, dx.parts > 1};
+  }
+  return {cut(a.M, a.f, a.d, 2, 2), cut(a.M, a.d, a.f, 1, 4), cut(a.M, a.f, a.d, 1, 4), cut(a.M, a.d, a.f, 2, 2),
+          (int64_t)cdiv(a.M, 128) * cdiv(a.d, 128) <= 256};
 }
-// dx's two products are separate problems where that fills the chip better.
-bool dx_apart(const GatedFfn& a) { return (int64_t)cdiv(a.M, 128) * cdiv(a.d, 128) <= 256; }
+
+// out [M, N] at ldo = the sum of all of g's problems, which write their parts here.
+hipError_t run_parts(DType dt, int b_kmaj, GemmGroup& g, float* part, void* out, int64_t ldo, hipStream_t s) {
+  const int M = g.p[0].M, N = g.p[0].N;
+  const int64_t n = (int64_t)M * N;
+  for (int i = 0; i < g.n; ++i) {
+    g.p[i].out = part + i * n;
+    g.p[i].ldo = N;
+    g.p[i].out_f32 = 1;
+  }
+  const char* why;
+  const hipError_t e = gemm(dt, 1, b_kmaj, g, 0, s, &why);
+  if (e != hipSuccess) return e;
+  if (dt == BF16)
+    hipLaunchKernelGGL((join_rows<bf16, 4>), blocks_of(n, 4), dim3(256), 0, s, part, g.n, n, N, static_cast<bf16*>(out), ldo);
+  else if (N % 4 == 0)
+    hipLaunchKernelGGL((join_rows<float, 4>), blocks_of(n, 4), dim3(256), 0, s, part, g.n, n, N, static_cast<float*>(out),
+                       ldo);
+  else
+    hipLaunchKernelGGL((join_rows<float, 1>), blocks_of(n, 1), dim3(256), 0, s, part, g.n, n, N, static_cast<float*>(out),
+                       ldo);
+  return hipGetLastError();
+}
+
+const void* at(DType dt, const void* p, int64_t elements) {
+  return static_cast<const char*>(p) + elements * (dt == BF16 ? 2 : 4);
+}
+
+// y = h Wd, in parts of k where k.parts says so.
+hipError_t down_product(DType dt, const GatedFfn& a, const Cut& k, const void* h, const void* wd, void* y, float* part,
+                        hipStream_t s) {
+  if (k.parts == 1) return run(dt, 1, 0, {product(h, a.f, wd, a.ldd, a.M, a.d, a.f, y, a.ldy, dt == F32)}, s);
+  GemmGroup g;
+  memset(&g, 0, sizeof(g));
+  for (; g.n < k.parts; ++g.n) {
+    const int k0 = g.n * k.per;
+    g.p[g.n] = product(at(dt, h, k0), a.f, at(dt, wd, k0 * a.ldd), a.ldd, a.M, a.d, std::min(k.per, a.f - k0), nullptr,
+                       0, 1);
+  }
+  return run_parts(dt, 0, g, part, y, a.ldy, s);
+}
+
+// dx = dg Wg^T + du Wu^T, in one launch over both or in parts.
+hipError_t dx_product(DType dt, const GatedFfn& a, const Cuts& k, const void* dg, const void* du, const void* wg,
+                      const void* wu, void* dx, float* part, hipStream_t s) {
+  if (!k.apart) {
+    GemmProblem p = product(dg, a.f, wg, a.ldg, a.M, a.d, a.f, dx, a.lddx, dt == F32);
+    p.A2 = du; p.lda2 = a.f; p.B2 = wu; p.ldb2 = a.ldu; p.K2 = a.f;
+    return run(dt, 1, 1, {p}, s);
+  }
+  GemmGroup g;
+  memset(&g, 0, sizeof(g));
+  for (int b = 0; b < 2; ++b)
+    for (int i = 0; i < k.dx.parts; ++i) {
+      const int k0 = i * k.dx.per;
+      g.p[g.n++] = product(at(dt, b ? du : dg, k0), a.f, at(dt, b ? wu : wg, k0), b ? a.ldu : a.ldg, a.M, a.d,
+                           std::min(k.dx.per, a.f - k0), nullptr, 0, 1);
+    }
+  return run_parts(dt, 1, g, part, dx, a.lddx, s);
+}
 
 }  // namespace
 
 int64_t gated_ffn_scratch(DType dt, const GatedFfn& a, int backward) {
   const int64_t one = round_up((int64_t)a.M * a.f * (dt == BF16 ? 2 : 4)), mf = (int64_t)a.M * a.f * 4,
                 md = (int64_t)a.M * a.d * 4;
-  if (dt == F32) return 3 * one;
   if (!backward && few_rows(dt, a))
     return 4 * a.M * ((int64_t)few_up(a).splits * 2 * a.f + (int64_t)few_last(a).splits * a.d);
-  const Cuts k = cuts(a);
-  // the parts of one product are read before the next one's are written
-  if (!backward) return one + std::max(k.gate.parts > 1 ? 2 * k.gate.parts * mf : 0, k.down.parts > 1 ? k.down.parts * md : 0);
-  return 3 * one + std::max(k.dh.parts > 1 ? k.dh.parts * mf : 0, dx_apart(a) ? 2 * k.dx.parts * md : 0);
+  const Cuts k = cuts(dt, a);
+  // (the parts of one product are read before the next one's are written)
+  const int64_t down = k.down.parts > 1 ? k.down.parts * md : 0, dx = k.apart ? 2 * k.dx.parts * md : 0;
+  // fp32: h, and g | u where they are not saved
+  if (!backward) return (dt == F32 ? 3 * one : one) + std::max(k.gate.parts > 1 ? 2 * k.gate.parts * mf : 0, down);
+  return 3 * one + std::max(k.dh.parts > 1 ? k.dh.parts * mf : 0, dx);
 }
 
 hipError_t gated_ffn_fwd(DType dt, const GatedFfn& a, const void* x, const void* wg, const void* wu, const void* wd,
                          void* y, float* saved, void* scratch, hipStream_t s) {
   hipError_t e;
   void* h = scratch;
-  const int64_t n = (int64_t)a.M * a.f, md = (int64_t)a.M * a.d;
+  const int64_t n = (int64_t)a.M * a.f;
+  const Cuts k = cuts(dt, a);
   if (dt == F32) {
     float* gu = saved ? saved : reinterpret_cast<float*>(static_cast<char*>(scratch) + round_up(n * 4));
     const int64_t ld = 2 * (int64_t)a.f;
@@ -671,7 +750,8 @@ hipError_t gated_ffn_fwd(DType dt, const GatedFfn& a, const void* x, const void*
                          nullptr, static_cast<float*>(h));
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return run(F32, 1, 0, {product(h, a.f, wd, a.ldd, a.M, a.d, a.f, y, a.ldy, 1)}, s);
+    float* part = reinterpret_cast<float*>(static_cast<char*>(scratch) + 3 * round_up(n * 4));
+    return down_product(F32, a, k.down, h, wd, y, part, s);
   }
   Gated p;
   memset(&p, 0, sizeof(p));
@@ -696,7 +776,6 @@ hipError_t gated_ffn_fwd(DType dt, const GatedFfn& a, const void* x, const void*
       default: return few_fwd<8>(a, p, down, out, part, s);
     }
   }
-  const Cuts k = cuts(a);
   float* part = reinterpret_cast<float*>(static_cast<char*>(scratch) + round_up(n * 2));
   if (k.gate.parts > 1) {
     // (two parts: as many problems as a launch holds)
@@ -713,29 +792,17 @@ hipError_t gated_ffn_fwd(DType dt, const GatedFfn& a, const void* x, const void*
     e = launch_gated<0>(p, s);
   }
   if (e != hipSuccess) return e;
-  if (k.down.parts == 1) return run(BF16, 1, 0, {product(h, a.f, wd, a.ldd, a.M, a.d, a.f, y, a.ldy, 0)}, s);
-  GemmGroup g;
-  memset(&g, 0, sizeof(g));
-  for (; g.n < k.down.parts; ++g.n) {
-    const int k0 = g.n * k.down.per;
-    g.p[g.n] = product(p.h + k0, a.f, down + k0 * a.ldd, a.ldd, a.M, a.d, std::min(k.down.per, a.f - k0),
-                       part + g.n * md, a.d, 1);
-  }
-  const char* why;
-  e = gemm(BF16, 1, 0, g, 0, s, &why);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(join_rows, blocks_of(md, 4), dim3(256), 0, s, part, g.n, md, a.d, static_cast<bf16*>(y), a.ldy);
-  return hipGetLastError();
+  return down_product(BF16, a, k.down, h, wd, y, part, s);
 }
 
 hipError_t gated_ffn_bwd(DType dt, const GatedFfn& a, const void* x, const void* wg, const void* wu, const void* wd,
                          const float* saved, const void* dy, void* dx, void* dwg, void* dwu, void* dwd, void* scratch,
                          hipStream_t s) {
-  const int64_t n = (int64_t)a.M * a.f, md = (int64_t)a.M * a.d, one = round_up(n * (dt == BF16 ? 2 : 4));
+  const int64_t n = (int64_t)a.M * a.f, one = round_up(n * (dt == BF16 ? 2 : 4));
   char* base = static_cast<char*>(scratch);
   void *dg = base, *du = base + one, *h = base + 2 * one;
   float* part = reinterpret_cast<float*>(base + 3 * one);
-  const Cuts k = cuts(a);
+  const Cuts k = cuts(dt, a);
   const char* why;
   hipError_t e;
   if (dt == F32) {
@@ -773,27 +840,8 @@ hipError_t gated_ffn_bwd(DType dt, const GatedFfn& a, const void* x, const void*
     e = launch_gated<1>(p, s);
   }
   if (e != hipSuccess) return e;
-  if (dx && dt == BF16 && dx_apart(a)) {
-    GemmGroup g;
-    memset(&g, 0, sizeof(g));
-    const bf16 *d[2] = {static_cast<const bf16*>(dg), static_cast<const bf16*>(du)};
-    const bf16 *w[2] = {static_cast<const bf16*>(wg), static_cast<const bf16*>(wu)};
-    const int64_t ld[2] = {a.ldg, a.ldu};
-    for (int b = 0; b < 2; ++b)
-      for (int i = 0; i < k.dx.parts; ++i, ++g.n) {
-        const int k0 = i * k.dx.per;
-        g.p[g.n] = product(d[b] + k0, a.f, w[b] + k0, ld[b], a.M, a.d, std::min(k.dx.per, a.f - k0), part + g.n * md, a.d,
-                           1);
-      }
-    e = gemm(BF16, 1, 1, g, 0, s, &why);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(join_rows, blocks_of(md, 4), dim3(256), 0, s, part, g.n, md, a.d, static_cast<bf16*>(dx), a.lddx);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  } else if (dx) {
-    GemmProblem p = product(dg, a.f, wg, a.ldg, a.M, a.d, a.f, dx, a.lddx, dt == F32);
-    p.A2 = du; p.lda2 = a.f; p.B2 = wu; p.ldb2 = a.ldu; p.K2 = a.f;
-    e = run(dt, 1, 1, {p}, s);
+  if (dx) {
+    e = dx_product(dt, a, k, dg, du, wg, wu, dx, part, s);
     if (e != hipSuccess) return e;
   }
   if (!dwg) return hipSuccess;

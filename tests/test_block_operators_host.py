@@ -204,6 +204,9 @@ def test_gated_ffn_workspace():
     big = ffn(rows=8192, d_model=2048, ld_x=2048, ld_y=2048, ld_down=2048, d_ff=2048, ld_gate=2048, ld_up=2048)
     assert ffn_bytes(big) == (8192 * 2048 * 2, 3 * 8192 * 2048 * 2)
     assert ffn_bytes(ffn(dtype=0, grad_dtype=0, d_ff=101)) == (3 * r(300 * 101 * 4),) * 2
+    # four fp32 parts of y and of dx
+    long = ffn(dtype=0, grad_dtype=0, d_ff=5000, ld_gate=5000, ld_up=5000)
+    assert ffn_bytes(long) == (3 * r(300 * 5000 * 4) + 4 * 300 * 64 * 4,) * 2
     assert fal.lib().fal_gated_ffn_workspace_bytes(byref(ffn()), None, None) == fal.FAL_OK
 
 

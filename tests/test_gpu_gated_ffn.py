@@ -151,6 +151,21 @@ def test_few_rows(M, d, f):
 def test_products_cut_along_k(M, d, f):
     """Few tiles and long sums: parts of k in workgroups of their own."""
     check("cut", M, d, f, BF16, ACTS[M % 3], pad=8, seed=M)
+    check("cut", M, d + 1, f + 3, F32, ACTS[M % 3], pad=1, seed=M)
+
+
+@pytest.mark.parametrize("M,d,f", [(33, 67, 5001), (300, 260, 8192), (700, 1500, 4097)])
+def test_long_fp32_sums(M, d, f):
+    """Sums over f in four parts, also held in the norm."""
+    x, wg, wu, wd, dy = make(M, M, d, f, F32)
+    y, saved = fal.gated_ffn_fwd(x, wg, wu, wd, save=True)
+    dx = fal.gated_ffn_bwd(x, wg, wu, wd, saved, dy, weight_grads=False).dx
+    ref = reference(*(t.double() for t in (x, wg, wu, wd, dy)), "silu", U, U)
+    assert worst(y, *ref["y"]) <= 1 and worst(dx, *ref["dx"]) <= 1
+    # independent roundings of a sum in four parts: sqrt(f / 4) halves of u a term's
+    # mean size, and as many again from h and its factors
+    for got, want in ((y, ref["y"][0]), (dx, ref["dx"][0])):
+        assert float((got.double() - want).norm() / want.norm()) <= 2 * (f / 4) ** 0.5 * U
 
 
 def test_few_rows_of_long_products():
