@@ -35,7 +35,7 @@ typedef _Float16 half_t;
 typedef _Float16 halfx8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 128;      // tile sides; matrices are padded to it with zeros
-constexpr int kNormBlocksNs = 1024;
+constexpr int kNormParts = 1024;
 constexpr int kOneRound = 256;  // tiles that have a compute unit each
 // slices that a launch more has to save (512 x 512, five steps: 198 us, with 16 of
 // them 262)
@@ -835,7 +835,7 @@ void launch(NsArgs p, int matrices, hipStream_t s) {
 constexpr int kSmallLds = 155648, kSmallWaves = 16, kSmallSide = 128;
 
 struct SmallArgs {
-  int P, Q, p, q, flip, steps;
+  int P, Q, flip, steps;
   float x_scale;     // of X: 2^ex
   float a_scale;     // accumulators to A: 2^(ea - 2 ex)
   float c_scale, ca, cb;  // B's parts: c 2^(eb - 2 ea), a 2^eb, b 2^(eb - ea)
@@ -1072,7 +1072,7 @@ Sizes sizes(const NewtonSchulz& s) {
   const int64_t most = std::max<int64_t>(1, ((int64_t)2 << 30) / (4 * z.x + 4 * z.a));
   const int64_t batches = (s.count + most - 1) / most;
   z.chunk = (int)((s.count + batches - 1) / batches);
-  z.nparts = (int)std::min<int64_t>(kNormBlocksNs, ((int64_t)s.rows * s.cols + 4095) / 4096);
+  z.nparts = (int)std::min<int64_t>(kNormParts, ((int64_t)s.rows * s.cols + 4095) / 4096);
   z.part = 0;
   for (int n : {z.chunk, s.count % z.chunk})  // (a last batch may be smaller, and its products cut)
     if (n)
@@ -1094,10 +1094,8 @@ double largest(double c0, double c1, double c2, double top) {
 
 // Whether a matrix fits one workgroup, and its padded sides there.
 bool small(const NewtonSchulz& s, SmallArgs* a) {
-  a->p = std::min(s.rows, s.cols);
-  a->q = std::max(s.rows, s.cols);
-  a->P = (a->p + 31) / 32 * 32;
-  a->Q = (a->q + 63) / 64 * 64;
+  a->P = (std::min(s.rows, s.cols) + 31) / 32 * 32;
+  a->Q = (std::max(s.rows, s.cols) + 63) / 64 * 64;
   return a->P <= kSmallSide && 4ll * a->P * (a->Q + 8) + 4ll * a->P * (a->P + 8) <= kSmallLds;
 }
 
