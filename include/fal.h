@@ -582,7 +582,7 @@ fal_status_t fal_qk_norm_rope_bwd(const fal_qk_norm_rope_t* shape, const void* q
  * Wu may be the halves of one [d, 2f] matrix). */
 typedef enum { FAL_GATE_SILU = 0, FAL_GATE_GELU_TANH = 1, FAL_GATE_GELU_ERF = 2 } fal_gate_t;
 typedef struct {
-  int32_t rows;       /* M >= 1                                             */
+  int32_t rows;       /* M >= 1; M d, M f and d f at most 2^33              */
   int32_t d_model;    /* d, 1 .. 2^20                                       */
   int32_t d_ff;       /* f, 1 .. 2^20                                       */
   int32_t activation; /* fal_gate_t                                         */
@@ -639,7 +639,7 @@ fal_status_t fal_gated_ffn_bwd(const fal_gated_ffn_t* shape, const void* x, cons
  * (Sums over k are cut by what fills the chip, so a matrix's last bits depend on
  * the number of matrices beside it.) */
 typedef struct {
-  int32_t count;       /* matrices, >= 1                                     */
+  int32_t count;       /* matrices, 1 .. 2^22                                */
   int32_t rows, cols;  /* >= 1 each, dense rows                              */
   int32_t steps;       /* 1 .. 32                                            */
   int32_t dtype;       /* fal_dtype_t of x and out; of params in the update  */

@@ -4,6 +4,7 @@
 // Argument checks, then one call of the launchers.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -67,6 +68,8 @@ HeadNorm norm_args(const fal_qk_norm_rope_t* p, const void* wq, const void* wk, 
 }
 
 // ----------------------------------------------------- gated feed-forward --
+constexpr int64_t kMaxProduct = (int64_t)1 << 33;  // elements of a product
+
 Refusal check_gated(const fal_gated_ffn_t* p) {
   if (!p) return {FAL_ERR_INVALID_ARG, "NULL shape"};
   if (p->dtype != FAL_F32 && p->dtype != FAL_BF16) return {FAL_ERR_INVALID_ARG, "unknown dtype"};
@@ -86,8 +89,11 @@ Refusal check_gated(const fal_gated_ffn_t* p) {
     return {FAL_ERR_INVALID_ARG, "a gradient's row stride is smaller than a row"};
   for (int64_t ld : {p->ld_x, p->ld_y, p->ld_gate, p->ld_up, p->ld_down, p->ld_dx, p->ld_dgate, p->ld_dup, p->ld_ddown})
     if (ld > kMaxStride) return {FAL_ERR_INVALID_ARG, "row stride above 2^40 elements"};
-  // (f32 launches count elements of [M, f] a thread each)
-  if (p->rows * f > ((int64_t)1 << 38)) return {FAL_ERR_UNSUPPORTED, "rows * d_ff above 2^38 is not supported"};
+  for (int64_t ld : {p->ld_x, p->ld_y, p->ld_dx})
+    if (ld > kMaxExtent / p->rows) return {FAL_ERR_INVALID_ARG, "rows at this stride exceed the address space"};
+  // (a launch's tiles of up to four products are counted in 32 bits)
+  if (p->rows * std::max(d, f) > kMaxProduct || d * f > kMaxProduct)
+    return {FAL_ERR_UNSUPPORTED, "rows * d_ff, rows * d_model or d_model * d_ff above 2^33 is not supported"};
   if (p->dtype == FAL_F32) return kFine;
   if (d % 8 || f % 8) return {FAL_ERR_UNSUPPORTED, "bf16 d_model and d_ff must be multiples of 8 (not supported otherwise)"};
   if (p->ld_x % 8 || p->ld_y % 8 || p->ld_gate % 8 || p->ld_up % 8 || p->ld_down % 8 || p->ld_dx % 8 ||
@@ -137,6 +143,8 @@ Refusal check_schulz(const fal_newton_schulz_t* p) {
   if (!p) return {FAL_ERR_INVALID_ARG, "NULL shape"};
   if (p->dtype != FAL_F32 && p->dtype != FAL_BF16) return {FAL_ERR_INVALID_ARG, "unknown dtype"};
   if (p->count < 1 || p->rows < 1 || p->cols < 1) return {FAL_ERR_INVALID_ARG, "count, rows and cols must be >= 1"};
+  // (one workgroup a matrix where they are small)
+  if (p->count > 1 << 22) return {FAL_ERR_UNSUPPORTED, "more than 2^22 matrices are not supported"};
   if (p->steps < 1 || p->steps > kMaxNewtonSteps) return {FAL_ERR_INVALID_ARG, "steps must lie in [1, 32]"};
   if (!std::isfinite(p->a) || !std::isfinite(p->b) || !std::isfinite(p->c))
     return {FAL_ERR_INVALID_ARG, "coefficients must be finite"};

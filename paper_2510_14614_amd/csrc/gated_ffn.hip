@@ -520,12 +520,18 @@ __device__ __forceinline__ void sum_parts(const float* p, int parts, int64_t str
     for (int e = 0; e < V; ++e) v[e] += p[i * stride + e];
 }
 
+// This thread's number (one axis of a grid holds fewer than 2^32 threads).
+constexpr int64_t kJoinRow = 1 << 22;  // workgroups in a row of the grid
+__device__ __forceinline__ int64_t join_thread() {
+  return (blockIdx.y * kJoinRow + blockIdx.x) * 256 + threadIdx.x;
+}
+
 // h = act(g) u, g and u [M][f] parts; saved (g | u) may be NULL or, with one part,
 // where g and u are.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void join_gate(const float* g, const float* u, int64_t ld, int parts, int64_t stride,
                                                  int64_t n, int f, int act, float* saved, T* h) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
+  const int64_t i = join_thread() * V;
   if (i >= n) return;
   const int64_t m = i / f, c = i % f;
   float gv[V], uv[V];
@@ -547,7 +553,7 @@ __global__ __launch_bounds__(256) void join_gate(const float* g, const float* u,
 template <typename T, int V>
 __global__ __launch_bounds__(256) void join_gate_bwd(const float* dh, int parts, int64_t stride, const float* saved,
                                                      int64_t n, int f, int act, T* dg, T* du, T* h) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
+  const int64_t i = join_thread() * V;
   if (i >= n) return;
   const int64_t m = i / f, c = i % f;
   float d[V];
@@ -566,7 +572,7 @@ __global__ __launch_bounds__(256) void join_gate_bwd(const float* dh, int parts,
 // out[m][c] = the parts' sum.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void join_rows(const float* part, int parts, int64_t n, int N, T* out, int64_t ldo) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
+  const int64_t i = join_thread() * V;
   if (i >= n) return;
   float v[V];
   sum_parts<V>(part + i, parts, n, v);
@@ -592,7 +598,10 @@ hipError_t run(DType dt, int a_kmaj, int b_kmaj, std::initializer_list<GemmProbl
   return gemm(dt, a_kmaj, b_kmaj, g, 0, s, &why);
 }
 
-dim3 blocks_of(int64_t n, int per) { return dim3((unsigned)((n + 256 * per - 1) / (256 * per))); }
+dim3 blocks_of(int64_t n, int per) {
+  const int64_t blocks = (n + 256 * per - 1) / (256 * per), x = std::min<int64_t>(blocks, kJoinRow);
+  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
 
 // The larger tile, two workgroups a compute unit, once it gives every compute unit
 // two (8192 x 2048 x 5504, 2752 tiles: forward 412 us, backward 322); three of 64

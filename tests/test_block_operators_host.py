@@ -145,7 +145,12 @@ def ffn_bytes(s):
     (dict(d_model=60), UNSUP, "multiples of 8"), (dict(d_ff=100), UNSUP, "multiples of 8"),
     (dict(ld_x=68), BAD, "multiples of 8"), (dict(ld_dup=132), BAD, "multiples of 8"),
     (dict(ld_x=1 << 24), UNSUP, "2 GiB"), (dict(rows=1 << 23), UNSUP, "2 GiB"), (dict(ld_down=1 << 23), UNSUP, "2 GiB"),
-    (dict(dtype=0, grad_dtype=0, rows=1 << 30, d_ff=1 << 10, ld_gate=1 << 10, ld_up=1 << 10), UNSUP, "2^38"),
+    (dict(dtype=0, grad_dtype=0, rows=1 << 30, d_ff=1 << 10, ld_gate=1 << 10, ld_up=1 << 10), UNSUP, "2^33"),
+    (dict(dtype=0, grad_dtype=0, rows=1 << 30), UNSUP, "2^33"),
+    (dict(dtype=0, grad_dtype=0, rows=1 << 30, ld_x=1 << 40), BAD, "address space"),
+    (dict(dtype=0, grad_dtype=0, rows=1 << 30, ld_dx=1 << 40), BAD, "address space"),
+    (dict(dtype=0, grad_dtype=0, rows=1, d_model=1 << 17, d_ff=1 << 17, ld_x=1 << 17, ld_y=1 << 17, ld_down=1 << 17,
+          ld_gate=1 << 17, ld_up=1 << 17), UNSUP, "2^33"),
 ])
 def test_gated_ffn_refuses_a_shape(kw, status, word):
     L, s, n = fal.lib(), ffn(**kw), ctypes.c_size_t()
@@ -249,7 +254,7 @@ def schulz_bytes(s):
 
 
 @pytest.mark.parametrize("kw,status,word", [
-    (dict(count=0), BAD, "count"), (dict(rows=0), BAD, "rows"), (dict(cols=0), BAD, "cols"), (dict(steps=0), BAD, "steps"),
+    (dict(count=0), BAD, "count"), (dict(count=(1 << 22) + 1), UNSUP, "2^22"), (dict(rows=0), BAD, "rows"), (dict(cols=0), BAD, "cols"), (dict(steps=0), BAD, "steps"),
     (dict(steps=33), BAD, "steps"), (dict(dtype=2), BAD, "dtype"), (dict(a=float("nan")), BAD, "finite"),
     (dict(b=float("inf")), BAD, "finite"), (dict(a=1e30), BAD, "grow"), (dict(c=10.0), BAD, "grow"),
     (dict(stride=19999), BAD, "stride"), (dict(out_stride=19999), BAD, "stride"), (dict(stride=1 << 46), BAD, "address space"),

@@ -168,6 +168,22 @@ def test_long_fp32_sums(M, d, f):
         assert float((got.double() - want).norm() / want.norm()) <= 2 * (f / 4) ** 0.5 * U
 
 
+def test_more_elements_than_one_axis_of_a_grid():
+    """2^32 elements of h and more, a thread each: the last rows against fp64."""
+    M, d, f = (1 << 32) // 8193 + 131, 16, 8193
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("needs 120 GB")
+    x, wg, wu, wd, dy = make(5, M, d, f, F32)
+    y, saved = fal.gated_ffn_fwd(x, wg, wu, wd, save=True)
+    dx = fal.gated_ffn_bwd(x, wg, wu, wd, saved, dy, weight_grads=False).dx
+    del saved
+    for rows in (slice(0, 9), slice(M - 200, M)):
+        ref = reference(*(t.double() for t in (x[rows], wg, wu, wd, dy[rows])), "silu", U, U)
+        assert worst(y[rows], *ref["y"]) <= 1 and worst(dx[rows], *ref["dx"]) <= 1
+    del x, y, dx, dy
+    torch.cuda.empty_cache()
+
+
 def test_few_rows_of_long_products():
     """Ranges of k cut by what LDS holds of their rows, past 16 of them too."""
     check("long", 8, 8, 20000, BF16)
