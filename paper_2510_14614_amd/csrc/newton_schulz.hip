@@ -37,9 +37,6 @@ typedef _Float16 halfx8_t __attribute__((ext_vector_type(8)));
 constexpr int kTile = 128;      // tile sides; matrices are padded to it with zeros
 constexpr int kNormParts = 1024;
 constexpr int kOneRound = 256;  // tiles that have a compute unit each
-// slices that a launch more has to save (512 x 512, five steps: 198 us, with 16 of
-// them 262)
-constexpr int kJoinSlices = 12;
 
 // A matrix of a batch: hi and lo parts, [count][rows][ld] each.
 struct Split {
@@ -299,99 +296,108 @@ __device__ __forceinline__ void put(const NsArgs& p, int mat, int r, int c, cons
   *reinterpret_cast<uint2*>(p.c.lo + o) = lo;
 }
 
-// The epilogue works on strips of 16 rows (COLS: columns) of a wavefront's 64 x 64,
+// The epilogue works on strips of 16 rows (COLS: columns) of a wavefront's W x W,
 // passed through LDS so that consecutive lanes hold consecutive elements: lane 16g +
 // c of block (i, j) holds row 16i + c, columns 16j + 4g .. +3.  A tile's columns are
 // rows of the result where it is mirrored or transposed.
-constexpr int kStripPitch = 64 + 4;
-template <int MODE, bool COLS>
+template <int MODE, bool COLS, int W = 64>
 struct Strip {
-  Beside beside[4];
+  static constexpr int PITCH = W + 4;
+  static constexpr int N = W / 16;          // blocks of a strip, and accesses of a lane
+  static constexpr int LPR = W / 4;         // lanes of a row
+  static constexpr int RPA = 64 / LPR;      // rows of an access
+  static constexpr int ROWS = 16 * W / 64;  // rows of a lane that holds one column
+  Beside beside[N];
   int r, c;  // this lane's first row and its columns
-  // Strip q of the 64 x 64 at (mw, nw).
+  // Strip q of the W x W at (mw, nw).
   __device__ __forceinline__ void ask_for(const NsArgs& p, int mat, int mw, int nw, int q) {
     const int lane = threadIdx.x & 63;
+    r = (COLS ? nw : mw) + 16 * q;
+    c = COLS ? mw : nw;
     if (MODE == LAST && !p.r.vec) {
       // a lane to a column
-      r = (COLS ? nw : mw) + 16 * q;
-      c = (COLS ? mw : nw) + lane;
+      r += lane / W * ROWS;
+      c += lane % W;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < N; ++k)
         beside[k].w = make_float4(ask_one(p, mat, r + 4 * k, c), ask_one(p, mat, r + 4 * k + 1, c),
                                   ask_one(p, mat, r + 4 * k + 2, c), ask_one(p, mat, r + 4 * k + 3, c));
       return;
     }
-    r = (COLS ? nw : mw) + 16 * q + (lane >> 4);
-    c = (COLS ? mw : nw) + 4 * (lane & 15);
+    r += lane / LPR;
+    c += 4 * (lane % LPR);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) ask<MODE>(p, mat, r + 4 * k, c, beside[k]);
+    for (int k = 0; k < N; ++k) ask<MODE>(p, mat, r + RPA * k, c, beside[k]);
   }
-  // blocks: (q, 0 .. 3), COLS: (0 .. 3, q).
-  __device__ __forceinline__ void emit(const NsArgs& p, int mat, const f32x4_t (&blocks)[4], float* strip) const {
+  // blocks: (q, 0 .. N - 1), COLS: (0 .. N - 1, q).
+  __device__ __forceinline__ void emit(const NsArgs& p, int mat, const f32x4_t (&blocks)[N], float* strip) const {
     const int lane = threadIdx.x & 63, g = lane >> 4, cl = lane & 15;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < N; ++j) {
       if (COLS) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) strip[(4 * g + e) * kStripPitch + 16 * j + cl] = blocks[j][e];
+        for (int e = 0; e < 4; ++e) strip[(4 * g + e) * PITCH + 16 * j + cl] = blocks[j][e];
       } else {
-        *reinterpret_cast<f32x4_t*>(strip + cl * kStripPitch + 16 * j + 4 * g) = blocks[j];
+        *reinterpret_cast<f32x4_t*>(strip + cl * PITCH + 16 * j + 4 * g) = blocks[j];
       }
     }
     wave_lds_order();
     if (MODE == LAST && !p.r.vec) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float* s = strip + 4 * k * kStripPitch + lane;
+      for (int k = 0; k < N; ++k) {
+        const float* s = strip + (lane / W * ROWS + 4 * k) * PITCH + lane % W;
         put_one(p, mat, r + 4 * k, c, s[0], beside[k].w.x);
-        put_one(p, mat, r + 4 * k + 1, c, s[kStripPitch], beside[k].w.y);
-        put_one(p, mat, r + 4 * k + 2, c, s[2 * kStripPitch], beside[k].w.z);
-        put_one(p, mat, r + 4 * k + 3, c, s[3 * kStripPitch], beside[k].w.w);
+        put_one(p, mat, r + 4 * k + 1, c, s[PITCH], beside[k].w.y);
+        put_one(p, mat, r + 4 * k + 2, c, s[2 * PITCH], beside[k].w.z);
+        put_one(p, mat, r + 4 * k + 3, c, s[3 * PITCH], beside[k].w.w);
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        put<MODE>(p, mat, r + 4 * k, c, *reinterpret_cast<const float4*>(strip + (4 * k + g) * kStripPitch + 4 * cl),
+      for (int k = 0; k < N; ++k)
+        put<MODE>(p, mat, r + RPA * k, c,
+                  *reinterpret_cast<const float4*>(strip + (RPA * k + lane / LPR) * PITCH + 4 * (lane % LPR)),
                   beside[k]);
     }
     wave_lds_order();
   }
 };
+constexpr int kStrip = 16 * Strip<GRAM, false>::PITCH;  // floats of LDS
 template <int MODE>
 __device__ __forceinline__ bool emits(const NsArgs& p, int tm, int tn, bool cols) {
   if (MODE == LAST) return cols == (p.r.flip != 0);
   return !cols || ((MODE == GRAM || MODE == POLY) && tm != tn);
 }
 
-// The 64 x 64 at (mw, nw), blocks (I, J) .. of a wavefront's, every strip's operands
+// The W x W at (mw, nw), blocks (I, J) .. of a wavefront's, every strip's operands
 // asked for at once.
-template <int MODE, bool COLS, int FM, int FN, int I = 0, int J = 0>
+template <int MODE, bool COLS, int W, int FM, int FN, int I = 0, int J = 0>
 __device__ __forceinline__ void ns_emit(const NsArgs& p, int mat, int mw, int nw, const f32x4_t (&acc)[FM][FN],
                                         float* strip) {
-  Strip<MODE, COLS> s[4];
+  constexpr int N = W / 16;
+  Strip<MODE, COLS, W> s[N];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) s[q].ask_for(p, mat, mw, nw, q);
+  for (int q = 0; q < N; ++q) s[q].ask_for(p, mat, mw, nw, q);
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    f32x4_t blocks[4];
+  for (int q = 0; q < N; ++q) {
+    f32x4_t blocks[N];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) blocks[j] = COLS ? acc[I + j][J + q] : acc[I + q][J + j];
+    for (int j = 0; j < N; ++j) blocks[j] = COLS ? acc[I + j][J + q] : acc[I + q][J + j];
     s[q].emit(p, mat, blocks, strip);
   }
 }
 
-// A 128 x 128 tile of a product of split matrices: A k-contiguous, B
+// A T x T tile of a product of split matrices: A k-contiguous, B
 // k-contiguous (GRAM, POLY: rows of the same matrix) or MN-major (X).  Four
-// wavefronts of 64 x 64; slices of 32 k of all four parts in NS LDS stages, asked
-// for NS - 1 slices ahead, the fragments of slice s + 1 read under the 48 MFMA of
-// slice s.
-template <int MODE, int OCC, int NS>
+// wavefronts of T/2 x T/2; slices of 32 k of all four parts in NS LDS stages, asked
+// for NS - 1 slices ahead, the fragments of slice s + 1 read under the MFMA (48 of
+// a tile of 128) of slice s.
+template <int MODE, int T, int OCC, int NS>
 __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   using namespace pipe;
   constexpr int BK = MODE == GRAM || MODE == POLY;
-  constexpr int F = 4, WT = 64;
-  typedef Src<kTile, 1> SA;
-  typedef Src<kTile, BK> SB;
+  constexpr int WT = T / 2, F = WT / 16;
+  typedef Src<T, 1> SA;
+  typedef Src<T, BK> SB;
   constexpr int REGION = SA::BYTES, SBYTES = 4 * REGION, L = 4 * SA::IPW;
   static_assert(SB::BYTES == REGION && (NS == 2 || NS == 4), "stages");
   // one array a stage: the compiler tracks loads to LDS array by array
@@ -404,7 +410,7 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   int tm, tn;
   if (BK) triangle(t, tm, tn);
   else grouped_tile(t, p.tiles_m, p.tiles_n, tm, tn);
-  const int m0 = tm * kTile, n0 = tn * kTile;
+  const int m0 = tm * T, n0 = tn * T;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
@@ -412,7 +418,7 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   SA ah, al;
   SB bh, bl;
   auto as = [](const half_t* x) { return reinterpret_cast<const bf16*>(x); };
-  const int M = p.tiles_m * kTile, N = p.tiles_n * kTile;
+  const int M = p.M, N = p.N;
   ah.init(0, as(p.a.hi + mat * p.sa), p.lda, m0, M, p.K, wave, lane);
   al.init(0, as(p.a.lo + mat * p.sa), p.lda, m0, M, p.K, wave, lane);
   bh.init(0, as(p.b.hi + mat * p.sb), p.ldb, n0, N, p.K, wave, lane);
@@ -441,8 +447,8 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
     bh.load(stage + 2 * REGION, wave);
     bl.load(stage + 3 * REGION, wave);
   };
-  Frag<kTile, 1, F> fa;
-  Frag<kTile, BK, F> fb;
+  Frag<T, 1, F> fa;
+  Frag<T, BK, F> fb;
   fa.init(wm * WT, lane);
   fb.init(wn * WT, lane);
   f32x4_t acc[F][F];
@@ -508,7 +514,7 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
   FAL_WAITCNT(0, 0);
   bar();
 
-  if (p.splits > 1) {
+  if (MODE == GRAM && p.splits > 1) {
     float* o = p.part + ((int64_t)bid * 256 + threadIdx.x) * 4;
 #pragma unroll
     for (int i = 0; i < F; ++i)
@@ -516,20 +522,22 @@ __global__ __launch_bounds__(256, OCC) void ns_product(NsArgs p) {
       for (int j = 0; j < F; ++j) *reinterpret_cast<f32x4_t*>(o + (i * F + j) * (int64_t)p.total * 1024) = acc[i][j];
     return;
   }
-  float* strip = reinterpret_cast<float*>(st0) + wave * 16 * kStripPitch;
+  constexpr int STRIP = 16 * Strip<MODE, false, WT>::PITCH;
+  static_assert(4 * STRIP * 4 <= SBYTES, "epilogue staging");
+  float* strip = reinterpret_cast<float*>(st0) + wave * STRIP;
   const int mw = m0 + wm * WT, nw = n0 + wn * WT;
-  if (emits<MODE>(p, tm, tn, false)) ns_emit<MODE, false, F, F>(p, mat, mw, nw, acc, strip);
-  if (emits<MODE>(p, tm, tn, true)) ns_emit<MODE, true, F, F>(p, mat, mw, nw, acc, strip);
+  if (emits<MODE>(p, tm, tn, false)) ns_emit<MODE, false, WT, F, F>(p, mat, mw, nw, acc, strip);
+  if (emits<MODE>(p, tm, tn, true)) ns_emit<MODE, true, WT, F, F>(p, mat, mw, nw, acc, strip);
 }
 
 // A tile's ranges added in order, and its epilogue: a workgroup for each strip of its
 // wavefronts' 64 x 64 (one for a whole tile took 12.7 us for 18 tiles of 8 ranges,
 // these 7.6).  F: blocks along a wavefront's columns.  The sums of block (i, j) lie
 // `total` * 1024 floats from those of the next, a range's `tiles` * 1024.
-template <int MODE, bool COLS, int F>
+template <bool COLS, int F>
 __device__ __forceinline__ void join_strip(const NsArgs& p, int mat, int mw, int nw, const float* o, int64_t tiles, int I,
                                            int J, int q, float* strip) {
-  Strip<MODE, COLS> s;
+  Strip<GRAM, COLS> s;
   s.ask_for(p, mat, mw, nw, q);
   f32x4_t sum[4];
   const int64_t block = (int64_t)p.total * 1024, range = tiles * 1024;
@@ -550,18 +558,15 @@ __device__ __forceinline__ void join_strip(const NsArgs& p, int mat, int mw, int
   }
   s.emit(p, mat, sum, strip);
 }
-template <int MODE>
 __global__ __launch_bounds__(256, 2) void ns_join(NsArgs p) {
-  __shared__ __attribute__((aligned(16))) float lds[4][16 * kStripPitch];
+  __shared__ __attribute__((aligned(16))) float lds[4][kStrip];
   const int q = blockIdx.x & 3, t = blockIdx.x / 4 % p.per_matrix, mat = blockIdx.x / 4 / p.per_matrix;
   int tm, tn;
-  if (MODE == GRAM || MODE == POLY) triangle(t, tm, tn);
-  else grouped_tile(t, p.tiles_m, p.tiles_n, tm, tn);
+  triangle(t, tm, tn);
   const int wave = threadIdx.x >> 6, mw = tm * kTile + (wave >> 1) * 64, nw = tn * kTile + (wave & 1) * 64;
   const float* o = p.part + (((int64_t)mat * p.splits * p.per_matrix + t) * 256 + threadIdx.x) * 4;
-  float* strip = lds[wave];
-  if (emits<MODE>(p, tm, tn, false)) join_strip<MODE, false, 4>(p, mat, mw, nw, o, p.per_matrix, 0, 0, q, strip);
-  if (emits<MODE>(p, tm, tn, true)) join_strip<MODE, true, 4>(p, mat, mw, nw, o, p.per_matrix, 0, 0, q, strip);
+  join_strip<false, 4>(p, mat, mw, nw, o, p.per_matrix, 0, 0, q, lds[wave]);
+  if (tm != tn) join_strip<true, 4>(p, mat, mw, nw, o, p.per_matrix, 0, 0, q, lds[wave]);
 }
 
 // ----------------------------------------------------------- large tiles --
@@ -709,14 +714,14 @@ __global__ __launch_bounds__(256, 1) void ns_big(NsArgs p) {
       for (int j = 0; j < F; ++j) *reinterpret_cast<f32x4_t*>(o + (i * F + j) * (int64_t)p.total * 1024) = acc[i][j];
     return;
   }
-  float* strip = reinterpret_cast<float*>(st0) + wave * 16 * kStripPitch;
+  float* strip = reinterpret_cast<float*>(st0) + wave * kStrip;
   const int mw = m0 + wm * WT, nw = n0 + wn * WT;
   auto quarter = [&](auto hi, auto hj) {
     constexpr int I = 4 * decltype(hi)::value, J = 4 * decltype(hj)::value;
     // (the sides are multiples of 128: a quarter lies inside or past the end)
     if (mw + 16 * I >= p.M || nw + 16 * J >= p.M) return;
-    ns_emit<GRAM, false, F, F, I, J>(p, mat, mw + 16 * I, nw + 16 * J, acc, strip);
-    if (tm != tn) ns_emit<GRAM, true, F, F, I, J>(p, mat, mw + 16 * I, nw + 16 * J, acc, strip);
+    ns_emit<GRAM, false, 64, F, F, I, J>(p, mat, mw + 16 * I, nw + 16 * J, acc, strip);
+    if (tm != tn) ns_emit<GRAM, true, 64, F, F, I, J>(p, mat, mw + 16 * I, nw + 16 * J, acc, strip);
   };
   typedef std::integral_constant<int, 0> zero;
   typedef std::integral_constant<int, 1> one;
@@ -727,7 +732,7 @@ __global__ __launch_bounds__(256, 1) void ns_big(NsArgs p) {
 }
 
 __global__ __launch_bounds__(256, 2) void ns_big_join(NsArgs p) {
-  __shared__ __attribute__((aligned(16))) float lds[4][16 * kStripPitch];
+  __shared__ __attribute__((aligned(16))) float lds[4][kStrip];
   const int q = blockIdx.x & 3, J = blockIdx.x & 4, I = blockIdx.x >> 1 & 4, rest = blockIdx.x >> 4;
   int mat, tm, tn;
   big_tile(p, p.whole + rest, mat, tm, tn);
@@ -737,46 +742,37 @@ __global__ __launch_bounds__(256, 2) void ns_big_join(NsArgs p) {
   const float* o = p.part + ((int64_t)rest * 256 + threadIdx.x) * 4;
   float* strip = lds[wave];
   const int tiles = p.tiles - p.whole;
-  join_strip<GRAM, false, 8>(p, mat, mw, nw, o, tiles, I, J, q, strip);
-  if (tm != tn) join_strip<GRAM, true, 8>(p, mat, mw, nw, o, tiles, I, J, q, strip);
+  join_strip<false, 8>(p, mat, mw, nw, o, tiles, I, J, q, strip);
+  if (tm != tn) join_strip<true, 8>(p, mat, mw, nw, o, tiles, I, J, q, strip);
 }
 
-// Products of few tiles and many slices: K in as many ranges as the compute units
-// take at once, of at least four slices, where that saves more than the joining
-// launch costs.
-int ranges(int tiles, int K, int* per) {
-  const int slices = K / pipe::KS;
-  *per = slices;
-  if (tiles > kOneRound / 2) return 1;
-  const int s = std::min(kOneRound / tiles, slices / 4), each = cdiv(cdiv(slices, s), 4) * 4;
-  if (slices - each < kJoinSlices) return 1;
-  *per = each;
-  return cdiv(slices, each);
-}
-
-// How a product runs.
+// How a product runs: tiles of side x side, the first `whole` of them (large ones
+// only) uncut and the others in `splits` ranges of `per` slices.
 struct Plan {
-  int big, tiles, whole, splits, per;
+  int side, tiles, whole, splits, per;
   int64_t part() const {  // bytes of the ranges' sums
-    return splits > 1 ? (int64_t)(tiles - whole) * splits * (big ? kBig * kBig : kTile * kTile) * 4 : 0;
+    return splits > 1 ? (int64_t)(tiles - whole) * splits * side * side * 4 : 0;
   }
 };
 
-Plan plan_tiles(int tiles, int K) {
-  Plan t = {0, tiles, 0, 1, 0};
-  t.splits = ranges(tiles, K, &t.per);
-  return t;
-}
+// Tiles of 64 x 64 while two a compute unit hold them all: more workgroups, each a
+// quarter as long (five steps of 384 x 384: 227 us on tiles of 128, 115 on these; 3 x
+// 1001 x 333 268 and 165; 4 x 512 x 2048, whose B X would be 1024 of them, 269 with
+// and 247 without).
+constexpr int kFine = 64, kFineTiles = 512;
 
-// X X^T: large tiles where their estimated time is the smaller one (us: a slice of
-// 32 k on a large tile, and on one of 128 x 128 alone on its compute unit or sharing
-// it; what each round and a joining launch add; ranges' sums written and read at 8
-// TB/s).
+// X X^T, which may have many more slices than rows, on the tiles whose estimated time
+// is the smallest (us: a slice of 32 k on a tile of each size, alone on its compute
+// unit or sharing it; what each round and a joining launch add; ranges' sums written
+// and read at 8 TB/s).  Tiles of 128 that leave half the compute units empty take K in
+// ranges of at least four slices (256 x 4096: 209 us, 252 on fine tiles; 1024 x 2048
+// 292 and 277; 3 x 1024 x 2048 502 and 526).
 Plan plan_gram(int P, int K, int matrices) {
-  constexpr double kBigSlice = 2.45, kPair = 1.04, kAlone = 0.65, kBigRound = 12.0, kRound = 8.0, kJoin = 6.0;
+  constexpr double kBigSlice = 2.45, kPair = 1.04, kAlone = 0.65, kFineAlone = 0.27, kFineTwo = 0.4, kFinePair = 0.7;
+  constexpr double kBigRound = 12.0, kRound = 8.0, kFineRound = 4.0, kJoin = 6.0;
   auto count = [&](int side) { return cdiv(P, side) * (cdiv(P, side) + 1) / 2 * matrices; };
   const int slices = K / pipe::KS;
-  Plan b = {1, count(kBig), 0, 1, slices};
+  Plan b = {kBig, count(kBig), 0, 1, slices};
   b.whole = b.tiles / kOneRound * kOneRound;
   const int rest = b.tiles - b.whole;
   double big = b.whole / kOneRound * (kBigRound + slices * kBigSlice);
@@ -790,40 +786,53 @@ Plan plan_gram(int P, int K, int matrices) {
     }
     big += kBigRound + b.per * kBigSlice;
   }
-  const Plan t = plan_tiles(count(kTile), K);
+  Plan t = {kTile, count(kTile), 0, 1, slices};
+  if (t.tiles <= kOneRound / 2) {
+    t.per = cdiv(cdiv(slices, std::min(kOneRound / t.tiles, slices / 4)), 4) * 4;
+    t.splits = cdiv(slices, t.per);
+  }
   const int n = t.tiles * t.splits, rounds = n / (2 * kOneRound), last = n % (2 * kOneRound);
   double small = n <= kOneRound ? kRound + t.per * kAlone : rounds * (kRound + t.per * kPair);
   if (n > kOneRound && last) small += kRound + t.per * (last > kOneRound ? kPair : kAlone);
   if (t.splits > 1) small += kJoin + t.part() / 4e6;
+  const Plan f = {kFine, count(kFine), 0, 1, slices};
+  const double filled = (double)(f.tiles - kOneRound) / kOneRound;
+  const double fine = kFineRound + slices * (filled <= 0.0 ? kFineAlone : kFineTwo + filled * (kFinePair - kFineTwo));
+  if (f.tiles <= kFineTiles && fine < std::min(big, small)) return f;
   return big < small ? b : t;
 }
 
 template <int MODE>
 Plan plan(int M, int N, int K, int matrices) {
-  const int tm = M / kTile, tn = N / kTile;
   if (MODE == GRAM) return plan_gram(M, K, matrices);
-  return plan_tiles((MODE == POLY ? tm * (tm + 1) / 2 : tm * tn) * matrices, K);
+  auto count = [&](int side) {
+    const int tm = M / side, tn = N / side;
+    return (MODE == POLY ? tm * (tm + 1) / 2 : tm * tn) * matrices;
+  };
+  const int side = count(kFine) <= kFineTiles ? kFine : kTile;
+  return {side, count(side), 0, 1, K / pipe::KS};
 }
 
 template <int MODE>
 void launch(NsArgs p, int matrices, hipStream_t s) {
   const Plan q = plan<MODE>(p.M, p.N, p.K, matrices);
-  p.tiles_m = p.M / kTile;
-  p.tiles_n = p.N / kTile;
+  p.tiles_m = p.M / q.side;
+  p.tiles_n = p.N / q.side;
   p.per_matrix = q.tiles / matrices;
   p.splits = q.splits;
   p.per = q.per;
   p.tiles = q.tiles;
   p.whole = q.whole;
   p.total = (q.tiles - q.whole) * q.splits;
-  if (q.big) {
+  if (MODE == GRAM && q.side == kBig) {
     hipLaunchKernelGGL(ns_big, dim3(q.whole + p.total), dim3(256), 0, s, p);
     if (q.splits > 1) hipLaunchKernelGGL(ns_big_join, dim3(16 * (q.tiles - q.whole)), dim3(256), 0, s, p);
     return;
   }
-  if (p.total <= kOneRound) hipLaunchKernelGGL((ns_product<MODE, 1, 4>), dim3(p.total), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((ns_product<MODE, 2, 2>), dim3(p.total), dim3(256), 0, s, p);
-  if (q.splits > 1) hipLaunchKernelGGL(ns_join<MODE>, dim3(4 * q.tiles), dim3(256), 0, s, p);
+  if (q.side == kFine) hipLaunchKernelGGL((ns_product<MODE, kFine, 2, 4>), dim3(p.total), dim3(256), 0, s, p);
+  else if (p.total <= kOneRound) hipLaunchKernelGGL((ns_product<MODE, kTile, 1, 4>), dim3(p.total), dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((ns_product<MODE, kTile, 2, 2>), dim3(p.total), dim3(256), 0, s, p);
+  if (q.splits > 1) hipLaunchKernelGGL(ns_join, dim3(4 * q.tiles), dim3(256), 0, s, p);
 }
 
 // --------------------------------------------------------- small matrices --
@@ -1074,10 +1083,8 @@ Sizes sizes(const NewtonSchulz& s) {
   z.chunk = (int)((s.count + batches - 1) / batches);
   z.nparts = (int)std::min<int64_t>(kNormParts, ((int64_t)s.rows * s.cols + 4095) / 4096);
   z.part = 0;
-  for (int n : {z.chunk, s.count % z.chunk})  // (a last batch may be smaller, and its products cut)
-    if (n)
-      z.part = std::max({z.part, plan<GRAM>(z.P, z.P, z.Q, n).part(), plan<POLY>(z.P, z.P, z.P, n).part(),
-                         plan<APPLY>(z.P, z.Q, z.P, n).part()});
+  for (int n : {z.chunk, s.count % z.chunk})  // (a last batch may be smaller, and X X^T cut)
+    if (n) z.part = std::max(z.part, plan_gram(z.P, z.Q, n).part());
   return z;
 }
 

@@ -162,6 +162,18 @@ def test_large():
     check(1, 1000, 640, F32)
 
 
+@pytest.mark.parametrize("count,rows,cols", [(1, 1401, 1503), (2, 1503, 1400), (1, 130, 130), (3, 900, 1700), (12, 260, 390)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_products_on_every_tile(count, rows, cols, dtype):
+    """B X of 144 and 288 tiles of 128 x 128, of 336, and of 64 x 64."""
+    check(count, rows, cols, dtype, steps=3, seed=rows)
+
+
+@pytest.mark.parametrize("case", [(1, 1401, 1503), (1, 1503, 1400), (3, 200, 333)])
+def test_update_on_every_tile(case):
+    test_update(case, BF16, True)
+
+
 def test_tall_matrices_are_wide_ones_transposed():
     x = make(3, 3, 150, 90, F32)
     got = fal.newton_schulz(x)
