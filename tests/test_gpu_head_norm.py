@@ -139,7 +139,7 @@ def check(label, B, T, H, kv, hd, dtype, r=None, interleaved=False, theta=10000.
     one = torch.ones(hd, device="cuda", dtype=torch.float64)
     w = torch.cat([(v.double() if weights else one).expand(n, hd) for v, n in ((wq, H), (wk, kv))])
     turn = rotation(None, at, hd, hd if r is None else r, theta, interleaved, "cuda")
-    terms = math.ceil(B * T / 3072) * math.ceil(turned / (512 // hd))
+    terms = math.ceil(B * T / (4 * 768)) * math.ceil(turned / (512 // hd))
     ref = reference(x, g, w, turn, terms, 2.0 ** -8 if dtype == BF16 else U)
     errs = {"out": worst(out[live][:, :turned * hd].unflatten(-1, (turned, hd)), *ref["out"]),
             "dx": worst(grads.dqkv[live][:, :turned * hd].unflatten(-1, (turned, hd)), *ref["dx"])}
