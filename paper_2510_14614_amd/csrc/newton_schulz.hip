@@ -838,7 +838,8 @@ void launch(NsArgs p, int matrices, hipStream_t s) {
 // --------------------------------------------------------- small matrices --
 // A matrix whose parts fit the LDS of one compute unit goes through all its steps
 // in one workgroup: one launch instead of 2 + 3 a step, each of which is latency
-// (four matrices of 64 x 192, five steps: 17 launches 142 us a call, this 30).
+// (four matrices of 64 x 192, five steps: 17 launches 87 us a call, this 31; one of
+// 128 x 160, the largest that fits, 85 and 84).
 // LDS holds X [P][Q + 8] and, in one place one after the other, A and B [P][P + 8],
 // hi and lo parts each; P is rounded up to 32, Q to 64, and zero there.
 constexpr int kSmallLds = 155648, kSmallWaves = 16, kSmallSide = 128;
