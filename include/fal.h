@@ -608,7 +608,7 @@ fal_status_t fal_gated_ffn_workspace_bytes(const fal_gated_ffn_t* shape, size_t*
  * to bf16 at most once, as the operand of the last product (calls of up to 8
  * rows keep it in fp32), and y once.
  * bf16 takes matrices of 16-byte aligned rows: d, f and the strides multiples
- * of 8, each operand below 2 GiB.  fp32 takes any size.
+ * of 8, each operand below 2 GiB.  fp32 takes any size up to 2^33 elements.
  * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes, misalignment or
  * an output that overlaps another argument; FAL_ERR_UNSUPPORTED for bf16 d or
  * f that is no multiple of 8 and operands past those limits;
@@ -660,7 +660,7 @@ fal_status_t fal_newton_schulz_workspace_bytes(const fal_newton_schulz_t* shape,
  * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes or coefficients,
  * misalignment or outputs that overlap another argument; FAL_ERR_UNSUPPORTED
  * for matrices that pass 2^30 - 2^20 elements with both sides rounded up to
- * 128; FAL_ERR_WORKSPACE; FAL_ERR_HIP when a launch fails. */
+ * 128, and for more than 2^22 of them; FAL_ERR_WORKSPACE; FAL_ERR_HIP when a launch fails. */
 fal_status_t fal_newton_schulz(const fal_newton_schulz_t* shape, const void* x, void* out, void* workspace,
                                size_t ws_bytes, void* stream);
 
