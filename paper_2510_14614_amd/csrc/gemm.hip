@@ -945,4 +945,10 @@ hipError_t gemm(DType dt, int a_kmaj, int b_kmaj, GemmGroup& g, int gelu_tanh, h
   return gemm_f32(a_kmaj, b_kmaj, g, gelu_tanh, s, splitk_scratch, splitk_floats);
 }
 
+// A bf16 operand's buffer range from row r0 of its output dimension, for host
+// tests (not part of the C ABI).
+extern "C" int64_t fal_gemm_operand_bytes(int32_t kmaj, int64_t ld, int32_t r0, int32_t rows, int32_t K) {
+  return pipe::operand_bytes(kmaj, ld, r0, rows, K);
+}
+
 }  // namespace fal

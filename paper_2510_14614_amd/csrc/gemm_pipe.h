@@ -72,6 +72,15 @@ __device__ __forceinline__ int mn_g(int k) {
   return R >= 128 ? (k & 3) | (((k >> 3) & 1) << 2) : ((k >> 1) & 1) | (((k >> 3) & 1) << 1);
 }
 
+// Bytes that an operand's buffer spans from its element (r0, 0), r0 the tile's first
+// row of the output dimension.  MN-major: up to the last whole 16-byte chunk of the
+// last k-row's own Rmax elements, not to the end of its stride: of a matrix that is
+// the right-hand columns of a wider one, what follows them there belongs to nobody.
+// k-contiguous: whole strides; loads past K are pointed out of range one by one.
+__host__ __device__ __forceinline__ int64_t operand_bytes(int kmaj, int64_t ld, int r0, int Rmax, int K) {
+  return kmaj ? (Rmax - r0) * ld * 2 : ((K - 1) * ld + ((Rmax + 7) & ~7) - r0) * 2;
+}
+
 typedef __attribute__((address_space(3))) void lds_void_t;
 __device__ __forceinline__ lds_void_t* lds_ptr(const void* p) {
   return (lds_void_t*)((__attribute__((address_space(3))) char*)(const_cast<void*>(p)));
@@ -110,8 +119,7 @@ struct Src {
   __device__ __forceinline__ void init(int seg, const bf16* X, int64_t ld, int r0, int Rmax, int Kseg, int wave,
                                        int lane) {
     base[seg] = reinterpret_cast<uint64_t>(KMAJ ? X + (int64_t)r0 * ld : X + r0);
-    const int64_t ext = KMAJ ? (int64_t)(Rmax - r0) * ld * 2 : ((int64_t)Kseg * ld - r0) * 2;
-    nbytes[seg] = (int)min<int64_t>(ext, 0x7fffffff);
+    nbytes[seg] = (int)min<int64_t>(operand_bytes(KMAJ, ld, r0, Rmax, Kseg), 0x7fffffff);
     kstep[seg] = KMAJ ? 2u : (uint32_t)(ld * 2);
     istep[seg] = (uint32_t)(4 * RPI * ld * 2);
     if (KMAJ) {
@@ -166,7 +174,7 @@ struct Src {
   // whose descriptor holds it becomes a loop over lanes.
   __device__ __forceinline__ void start(int64_t ld, int r0, int Rmax, int Kseg) {
     set(0, 0, W);
-    rn = KMAJ ? (int)((Rmax - r0) * ld * 2) : (int)((Kseg * ld - r0) * 2);
+    rn = (int)operand_bytes(KMAJ, ld, r0, Rmax, Kseg);
   }
   // Next slice of the same segment (full and live).
   __device__ __forceinline__ void advance() { so += W * ks; }

@@ -307,3 +307,26 @@ def test_another_stream():
         got = fal.gated_ffn_bwd(*t[:4], got_saved, t[4])
     s.synchronize()
     assert torch.equal(got_y, y) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def right_half(t):
+    """t as the right-hand columns of a matrix that ends with it, NaN beside."""
+    buf = torch.full((t.shape[0], 2 * t.shape[1]), float("nan"), dtype=t.dtype, device=t.device)
+    buf[:, t.shape[1]:] = t
+    return buf[:, t.shape[1]:]
+
+
+@pytest.mark.parametrize("M,d,f", [(5, 72, 200), (50, 64, 120), (300, 1000, 1096), (1501, 1000, 2744), (2500, 72, 2312)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_right_hand_columns(dtype, M, d, f):
+    """Every operand the right-hand columns of a matrix of its own, on ragged
+    tiles, products in parts and the larger tiles."""
+    x, wg, wu, wd, dy = make(M + d, M, d, f, dtype)
+    r = 2.0 ** -8 if dtype == BF16 else U
+    ref = reference(*(t.double() for t in (x, wg, wu, wd, dy)), "silu", r, r)
+    x, wg, wu, wd, dy = (right_half(t) for t in (x, wg, wu, wd, dy))
+    y, saved = fal.gated_ffn_fwd(x, wg, wu, wd, save=True)
+    grads = fal.gated_ffn_bwd(x, wg, wu, wd, saved, dy)
+    errs = {k: worst(y if k == "y" else getattr(grads, k), *v) for k, v in ref.items()}
+    log(f"{(M, d, f)} {dtype}: errors over their bounds { {k: round(v, 3) for k, v in errs.items()} }")
+    assert all(v <= 1 for v in errs.values()), errs
