@@ -868,9 +868,13 @@ __device__ __forceinline__ void mma3(const halfx8_t (&a)[2], const halfx8_t (&b)
   acc[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[0], a[0], acc[2], 0, 0, 0);
 }
 
+// Workgroups in a row of the grid: 2^22 of them, a matrix each, would be 2^32 threads
+// on one axis, one more than a launch takes.
+constexpr int kSmallRow = 1 << 20;
+
 // NB: blocks of 16 along P.
 template <int NB>
-__global__ __launch_bounds__(kSmallWaves * 64) void ns_small(Source s, SmallArgs a, NsArgs to) {
+__global__ __launch_bounds__(kSmallWaves * 64) void ns_small(Source s, SmallArgs a, NsArgs to, int count) {
   constexpr int P = 16 * NB, PA = P + 8, kBlocks = NB * (NB + 1) / 2, kHeld = (kBlocks + kSmallWaves - 1) / kSmallWaves;
   __shared__ __attribute__((aligned(16))) char lds[kSmallLds];
   __shared__ double red[kSmallWaves];
@@ -878,7 +882,8 @@ __global__ __launch_bounds__(kSmallWaves * 64) void ns_small(Source s, SmallArgs
   half_t* X[2] = {reinterpret_cast<half_t*>(lds), reinterpret_cast<half_t*>(lds) + P * PX};
   half_t* A[2] = {X[1] + P * PX, X[1] + P * PX + P * PA};
   constexpr int kThreads = kSmallWaves * 64;
-  const int mat = blockIdx.x, tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int mat = blockIdx.y * kSmallRow + blockIdx.x, tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
+  if (mat >= count) return;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the momentum's update and the norm, then X; kBatch loads a thread under way
   constexpr int kBatch = 8;
@@ -1217,12 +1222,13 @@ hipError_t newton_schulz(const NewtonSchulz& s, const MuonArgs* u, const void* x
     memset(&to, 0, sizeof(to));
     to.r = res;
     to.scale = one.out_scale;
-    const dim3 grid(s.count), block(kSmallWaves * 64);
+    const int row = std::min(s.count, kSmallRow);
+    const dim3 grid(row, cdiv(s.count, row)), block(kSmallWaves * 64);
     switch (one.P) {
-      case 32: hipLaunchKernelGGL(ns_small<2>, grid, block, 0, stream, src, one, to); break;
-      case 64: hipLaunchKernelGGL(ns_small<4>, grid, block, 0, stream, src, one, to); break;
-      case 96: hipLaunchKernelGGL(ns_small<6>, grid, block, 0, stream, src, one, to); break;
-      default: hipLaunchKernelGGL(ns_small<8>, grid, block, 0, stream, src, one, to); break;
+      case 32: hipLaunchKernelGGL(ns_small<2>, grid, block, 0, stream, src, one, to, s.count); break;
+      case 64: hipLaunchKernelGGL(ns_small<4>, grid, block, 0, stream, src, one, to, s.count); break;
+      case 96: hipLaunchKernelGGL(ns_small<6>, grid, block, 0, stream, src, one, to, s.count); break;
+      default: hipLaunchKernelGGL(ns_small<8>, grid, block, 0, stream, src, one, to, s.count); break;
     }
     return hipGetLastError();
   }

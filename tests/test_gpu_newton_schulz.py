@@ -342,3 +342,18 @@ def test_another_stream():
         got = fal.newton_schulz(x)
     s.synchronize()
     assert torch.equal(got, want)
+
+
+def test_as_many_small_matrices_as_a_call_takes():
+    """2^22 of them, a workgroup of 1024 threads each: more threads than one
+    axis of a grid holds."""
+    n = 1 << 22
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = torch.randn(n, 2, 3, generator=g, device="cuda")
+    got = fal.newton_schulz(x, steps=2)
+    for some in (slice(0, 3), slice((1 << 20) - 2, (1 << 20) + 2), slice(n - 3, n)):
+        want, bounds = exact(x[some], 2, COEF)
+        hold(got[some], want, bounds, in_fp32(x[some], 2, COEF), U)
+    # the larger of two singular values starts at 0.7 at least, and the polynomial
+    # takes 0.7 .. 1.2 to 0.68 .. 1.2
+    assert (torch.linalg.matrix_norm(got) > 0.67).all()
