@@ -1094,8 +1094,12 @@ Sizes sizes(const NewtonSchulz& s) {
   return z;
 }
 
-// The power of two that takes values up to `bound` below fp16's largest.
-int exponent(double bound) { return std::min(40, (int)std::floor(std::log2(32768.0 / bound))); }
+// The power of two that takes values up to `bound` below fp16's largest; at most 40,
+// which keeps the products of scales in fp32's range (a bound of zero has no largest).
+int exponent(double bound) {
+  const double e = std::floor(std::log2(32768.0 / bound));
+  return e < 40.0 ? (int)e : 40;
+}
 
 // The largest |f(t)| of a quadratic c0 + c1 t + c2 t^2 on [0, top].
 double largest(double c0, double c1, double c2, double top) {

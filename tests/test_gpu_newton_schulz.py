@@ -357,3 +357,17 @@ def test_as_many_small_matrices_as_a_call_takes():
     # the larger of two singular values starts at 0.7 at least, and the polynomial
     # takes 0.7 .. 1.2 to 0.68 .. 1.2
     assert (torch.linalg.matrix_norm(got) > 0.67).all()
+
+
+@pytest.mark.parametrize("count,rows,cols", [(2, 40, 60), (2, 150, 700), (1, 900, 200)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_polynomial_of_zeros(dtype, count, rows, cols):
+    """a = b = c = 0: X is 0 after the first step, and the update nothing but
+    the weights' decay."""
+    x = make(7, count, rows, cols, dtype)
+    for steps in (1, 3):
+        assert (fal.newton_schulz(x, steps, (0.0, 0.0, 0.0)) == 0).all()
+    master, momentum = (make(s, count, rows, cols, F32) for s in (8, 9))
+    want = master * torch.tensor(1 - 0.1 * 0.5, device="cuda")
+    fal.muon_step(master, x.float(), momentum, lr=0.1, weight_decay=0.5, coefficients=(0.0, 0.0, 0.0))
+    assert torch.equal(master, want)
