@@ -582,7 +582,7 @@ fal_status_t fal_qk_norm_rope_bwd(const fal_qk_norm_rope_t* shape, const void* q
  * Wu may be the halves of one [d, 2f] matrix). */
 typedef enum { FAL_GATE_SILU = 0, FAL_GATE_GELU_TANH = 1, FAL_GATE_GELU_ERF = 2 } fal_gate_t;
 typedef struct {
-  int32_t rows;       /* M >= 1; M d, M f and d f at most 2^33              */
+  int32_t rows;       /* M, 1 .. 2^29 - 64; M d, M f and d f at most 2^33   */
   int32_t d_model;    /* d, 1 .. 2^20                                       */
   int32_t d_ff;       /* f, 1 .. 2^20                                       */
   int32_t activation; /* fal_gate_t                                         */
@@ -611,7 +611,7 @@ fal_status_t fal_gated_ffn_workspace_bytes(const fal_gated_ffn_t* shape, size_t*
  * of 8, each operand below 2 GiB.  fp32 takes any size up to 2^33 elements.
  * Errors: FAL_ERR_INVALID_ARG for NULL pointers, bad sizes, misalignment or
  * an output that overlaps another argument; FAL_ERR_UNSUPPORTED for bf16 d or
- * f that is no multiple of 8 and operands past those limits;
+ * f that is no multiple of 8 and for operands and rows past those limits;
  * FAL_ERR_WORKSPACE; FAL_ERR_HIP when a launch fails. */
 fal_status_t fal_gated_ffn_fwd(const fal_gated_ffn_t* shape, const void* x, const void* w_gate, const void* w_up,
                                const void* w_down, void* y, float* saved, void* workspace, size_t ws_bytes,

@@ -69,6 +69,9 @@ HeadNorm norm_args(const fal_qk_norm_rope_t* p, const void* wq, const void* wk, 
 
 // ----------------------------------------------------- gated feed-forward --
 constexpr int64_t kMaxProduct = (int64_t)1 << 33;  // elements of a product
+// Rows of fp32: tiles of 64 of them, two products of 256 threads a tile in one launch,
+// are fewer than 2^32 threads.
+constexpr int32_t kMaxRows = (1 << 29) - 64;
 
 Refusal check_gated(const fal_gated_ffn_t* p) {
   if (!p) return {FAL_ERR_INVALID_ARG, "NULL shape"};
@@ -94,6 +97,7 @@ Refusal check_gated(const fal_gated_ffn_t* p) {
   // (a launch's tiles of up to four products are counted in 32 bits)
   if (p->rows * std::max(d, f) > kMaxProduct || d * f > kMaxProduct)
     return {FAL_ERR_UNSUPPORTED, "rows * d_ff, rows * d_model or d_model * d_ff above 2^33 is not supported"};
+  if (p->rows > kMaxRows) return {FAL_ERR_UNSUPPORTED, "more than 2^29 - 64 rows are not supported"};
   if (p->dtype == FAL_F32) return kFine;
   if (d % 8 || f % 8) return {FAL_ERR_UNSUPPORTED, "bf16 d_model and d_ff must be multiples of 8 (not supported otherwise)"};
   if (p->ld_x % 8 || p->ld_y % 8 || p->ld_gate % 8 || p->ld_up % 8 || p->ld_down % 8 || p->ld_dx % 8 ||

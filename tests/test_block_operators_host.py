@@ -306,3 +306,18 @@ def test_newton_schulz_binding_refuses():
                      ({"master": x.bfloat16()}, "master"), ({}, "GPU")]:
         with pytest.raises(ValueError, match=word):
             fal.muon_step(**{"master": x, "grads": x, "momentum": x, **kw})
+
+
+def test_gated_ffn_refuses_more_rows_than_a_launch_has_threads():
+    """fp32 rows of one column: 2^29 - 64 of them are 2^23 - 1 tiles of 64 in
+    each of two products, 256 threads a tile."""
+    L, n = fal.lib(), ctypes.c_size_t()
+    one = dict(dtype=0, grad_dtype=0, d_model=1, d_ff=1, ld_x=1, ld_y=1, ld_gate=1, ld_up=1, ld_down=1)
+    most = (1 << 29) - 64
+    assert 2 * -(-most // 64) * 256 < 1 << 32 <= 2 * -(-(most + 1) // 64) * 256
+    assert ffn_bytes(ffn(rows=most, **one))[0] == 3 * 4 * most
+    for rows in (most + 1, 1 << 30, (1 << 31) - 1):
+        s = ffn(rows=rows, **one)
+        assert L.fal_gated_ffn_workspace_bytes(byref(s), byref(n), byref(n)) == UNSUP and "2^29 - 64" in message()
+        assert L.fal_gated_ffn_fwd(byref(s), A, B, C, D, E, F, G, 1 << 30, None) == UNSUP
+        assert L.fal_gated_ffn_bwd(byref(s), A, B, C, D, E, F, G, H, I, J, K, 1 << 30, None) == UNSUP

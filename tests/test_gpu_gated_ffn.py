@@ -330,3 +330,46 @@ def test_right_hand_columns(dtype, M, d, f):
     errs = {k: worst(y if k == "y" else getattr(grads, k), *v) for k, v in ref.items()}
     log(f"{(M, d, f)} {dtype}: errors over their bounds { {k: round(v, 3) for k, v in errs.items()} }")
     assert all(v <= 1 for v in errs.values()), errs
+
+
+def test_as_many_rows_as_a_call_takes():
+    """fp32 rows of one column, as many tiles as a launch holds."""
+    M = (1 << 29) - 64
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    x, wg, wu, wd, dy = make(4, M, 1, 1, F32)
+    y, saved = fal.gated_ffn_fwd(x, wg, wu, wd, save=True)
+    dx = fal.gated_ffn_bwd(x, wg, wu, wd, saved, dy, weight_grads=False).dx
+    del saved
+    for rows in (slice(0, 200), slice(M // 2, M // 2 + 200), slice(M - 200, M)):
+        ref = reference(*(t.double() for t in (x[rows], wg, wu, wd, dy[rows])), "silu", U, U)
+        assert worst(y[rows], *ref["y"]) <= 1 and worst(dx[rows], *ref["dx"]) <= 1
+    del x, y, dx, dy
+    torch.cuda.empty_cache()
+
+
+# (columns of one matrix, first column of dw_gate and of dw_up) for f = 120
+LAYOUTS = [(240, 0, 120), (240, 120, 0), (264, 0, 136), (264, 8, 144), (272, 152, 16)]
+
+
+@pytest.mark.parametrize("width,at_gate,at_up", LAYOUTS)
+@pytest.mark.parametrize("dtype,grads_f32", [(F32, False), (BF16, False), (BF16, True)])
+def test_gradients_in_one_matrix(dtype, grads_f32, width, at_gate, at_up):
+    """dw_gate and dw_up side by side in either order, with and without columns
+    beside and between them, which stay as they are."""
+    M, d, f = 70, 64, 120
+    x, wg, wu, wd, dy = make(6, M, d, f, dtype)
+    _, saved = fal.gated_ffn_fwd(x, wg, wu, wd, save=True)
+    want = fal.gated_ffn_bwd(x, wg, wu, wd, saved, dy, grads_f32=grads_f32)
+    both = torch.full((d, width), 7.0, dtype=want.dw_gate.dtype, device="cuda")
+    halves = both[:, at_gate:at_gate + f], both[:, at_up:at_up + f]
+    got = fal.gated_ffn_bwd(x, wg, wu, wd, saved, dy, dw=(*halves, torch.empty_like(want.dw_down)), grads_f32=grads_f32)
+    assert got.dw_gate is halves[0] and got.dw_up is halves[1]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for h in halves:
+        h.fill_(7.0)
+    assert (both == 7.0).all()
+    # columns that both would write
+    with pytest.raises(fal.FalError, match="overlap"):
+        fal.gated_ffn_bwd(x, wg, wu, wd, saved, dy, dw=(both[:, :f], both[:, f - 8:2 * f - 8], got.dw_down),
+                          grads_f32=grads_f32)
