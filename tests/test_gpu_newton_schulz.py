@@ -371,3 +371,37 @@ def test_a_polynomial_of_zeros(dtype, count, rows, cols):
     want = master * torch.tensor(1 - 0.1 * 0.5, device="cuda")
     fal.muon_step(master, x.float(), momentum, lr=0.1, weight_decay=0.5, coefficients=(0.0, 0.0, 0.0))
     assert torch.equal(master, want)
+
+
+def uneven(kind, seed, count, rows, cols, dtype):
+    """Matrices whose singular values differ much."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n = lambda *s: torch.randn(count, *s, generator=g, device="cuda")  # noqa: E731
+    p = min(rows, cols)
+    if kind == "rank":
+        # rank 5 at most, exactly so in bf16: whole numbers up to 20
+        whole = lambda *s: torch.randint(-2, 3, (count, *s), generator=g, device="cuda").float()  # noqa: E731
+        return torch.matmul(whole(rows, min(5, p)), whole(min(5, p), cols)).to(dtype)
+    if kind == "one":
+        return torch.matmul(n(rows, 1), n(1, cols)).to(dtype)
+    if kind == "decay":
+        # singular values from 1 down to 1e-6, evenly in their logarithm
+        s = torch.logspace(0, -6, p, device="cuda")
+        left, right = torch.linalg.qr(n(rows, p))[0], torch.linalg.qr(n(cols, p))[0]
+        return torch.matmul(left * s, right.transpose(1, 2).contiguous()).to(dtype)
+    # a few strong directions over noise, as gradients have them
+    few = min(8, p)
+    s = torch.arange(1, few + 1, device="cuda", dtype=F32).pow(-0.7)
+    return (torch.matmul(n(rows, few) * s, n(few, cols)) + 0.03 * n(rows, cols)).mul_(1e-3).to(dtype)
+
+
+# one launch; tiles of 64; X X^T cut along k; tiles of 128; of 256
+@pytest.mark.parametrize("count,rows,cols", [(3, 64, 192), (2, 160, 100), (3, 1001, 333), (1, 256, 4096), (1, 1401, 1503),
+                                             (1, 2000, 5000)])
+@pytest.mark.parametrize("kind", ["rank", "one", "decay", "strong"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_uneven_singular_values(dtype, kind, count, rows, cols):
+    x = uneven(kind, rows, count, rows, cols, dtype)
+    got = fal.newton_schulz(x)
+    want, bounds = exact(x, 5, COEF)
+    hold(got, want, bounds, in_fp32(x, 5, COEF), 2.0 ** -8 if dtype == BF16 else U)
