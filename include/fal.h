@@ -635,7 +635,9 @@ fal_status_t fal_gated_ffn_bwd(const fal_gated_ffn_t* shape, const void* x, cons
  *   X <- (a I + b X X^T + c (X X^T)^2) X
  * (for rows > cols the same of its transpose): its singular values go through
  * a s + b s^3 + c s^5, its singular vectors stay.  Norms are summed in fp64,
- * products in fp32; X and both factors are held to 22 bits between the products.
+ * products in fp32.  Between the products X and both factors are held as pairs of
+ * fp16 values, scaled by the largest singular values that the polynomial allows
+ * (10^-6 at least): 22 bits, fewer for elements far smaller than those.
  * (Sums over k are cut by what fills the chip, so a matrix's last bits depend on
  * the number of matrices beside it.) */
 typedef struct {

@@ -24,7 +24,7 @@ int64_t packed_width(const fal_qk_norm_rope_t* p) {
   return (p->n_head + 2 * kv) * p->head_dim;
 }
 
-// A row stride of packed rows (name: the message's subject).
+// Whether packed rows may lie `ld` elements apart.
 Refusal check_stride(const fal_qk_norm_rope_t* p, int64_t ld) {
   if (ld < packed_width(p)) return {FAL_ERR_INVALID_ARG, "a row stride is smaller than a row"};
   if (ld % (p->dtype == FAL_BF16 ? 8 : 4)) return {FAL_ERR_INVALID_ARG, "row strides must be multiples of 16 bytes"};
@@ -126,8 +126,8 @@ GatedFfn gated_args(const fal_gated_ffn_t* p) {
   return a;
 }
 
-// The bytes that two [rows, width] matrices of one row stride share, the halves
-// of one matrix sharing none.
+// Whether two [rows, width] matrices share no element: apart, or of one row stride
+// with their columns beside each other, as the halves of one matrix are.
 bool interleave_free(const void* a, const void* b, int64_t rows, int64_t ld_a, int64_t ld_b, int64_t width,
                      int64_t es) {
   if (!meets(rows_of(a, rows, ld_a, width, es), {rows_of(b, rows, ld_b, width, es)})) return true;

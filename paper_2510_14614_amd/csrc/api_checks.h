@@ -1,5 +1,7 @@
-// Host-side argument checks shared by the entry points of the C ABI.  Each
-// returns NULL or the message of the first argument that does not hold.
+// Shared by the entry points of the C ABI: how one that takes no context ends (its
+// status, the message behind it, no exception), its refusals and limits, the byte
+// ranges of arrays, and hyper-parameter checks, which return NULL or the message of
+// the first argument that does not hold.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -604,10 +604,11 @@ dim3 blocks_of(int64_t n, int per) {
 }
 
 // The larger tile, two workgroups a compute unit, once it gives every compute unit
-// two (8192 x 2048 x 5504, 2752 tiles: forward 412 us, backward 322); three of 64
-// columns below that (1501 x 1000 x 2744, 264 large tiles: 46 against 39 forward, 64
-// against 38 backward).  Tiles of 256 rows, one workgroup a compute unit, whose
-// epilogues nothing covers, took 474 and 386 of the first.
+// two (8192 x 2048 x 5504, 2752 tiles: forward 407 us against 469 on those of 64
+// columns, backward 317 against 402, measured side by side); three of 64 columns
+// below that (1501 x 1000 x 2744, 264 large tiles: 46 against 39 forward, 64 against
+// 38 backward).  Tiles of 256 rows, one workgroup a compute unit, whose epilogues
+// nothing covers, took 474 and 386 where the larger tile took 412 and 322.
 template <int BWD>
 hipError_t launch_gated(Gated p, hipStream_t s) {
   constexpr int BN = BWD ? 256 : 128;

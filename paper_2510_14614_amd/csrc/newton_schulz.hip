@@ -653,11 +653,11 @@ __global__ __launch_bounds__(256, 1) void ns_big(NsArgs p) {
 #pragma unroll
       for (int j = 0; j < F; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], a[i], acc[i][j], 0, 0, 0);
   };
-  // one LDS read an MFA from the first on, loads after them
+  // one LDS read an MFMA from the first on, loads after them
   auto interleave = [&](int reads, int loads) {
 #pragma unroll
     for (int q = 0; q < F * F; ++q) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFA
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
       if (q < reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // LDS read
       else if (q - reads < loads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);  // buffer load to LDS
     }
@@ -981,10 +981,10 @@ __global__ __launch_bounds__(kSmallWaves * 64) void ns_small(Source s, SmallArgs
           mma3(x[0], y[0], acc);
           mma3(x[1], y[1], acc);
         }
-      float v[4];
+        float v[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = ((acc[0][e] + acc[1][e]) + acc[2][e]) * a.a_scale;
-      write_a(bi[i], bj[i], v);
+        for (int e = 0; e < 4; ++e) v[e] = ((acc[0][e] + acc[1][e]) + acc[2][e]) * a.a_scale;
+        write_a(bi[i], bj[i], v);
       }
     }
     __syncthreads();
@@ -996,16 +996,16 @@ __global__ __launch_bounds__(kSmallWaves * 64) void ns_small(Source s, SmallArgs
         f32x4_t acc[3] = {};
 #pragma unroll
         for (int k = 0; k < P; k += 32) {
-        const halfx8_t x[2] = {row8(A[0], PA, 16 * bi[i], k, lane), row8(A[1], PA, 16 * bi[i], k, lane)};
-        const halfx8_t y[2] = {row8(A[0], PA, 16 * bj[i], k, lane), row8(A[1], PA, 16 * bj[i], k, lane)};
-        mma3(x, y, acc);
-      }
-      const int m = 16 * bi[i] + c, k = 16 * bj[i] + 4 * g;
-      float old[4];
-      join4(*reinterpret_cast<const uint2*>(A[0] + m * PA + k), *reinterpret_cast<const uint2*>(A[1] + m * PA + k), old);
+          const halfx8_t x[2] = {row8(A[0], PA, 16 * bi[i], k, lane), row8(A[1], PA, 16 * bi[i], k, lane)};
+          const halfx8_t y[2] = {row8(A[0], PA, 16 * bj[i], k, lane), row8(A[1], PA, 16 * bj[i], k, lane)};
+          mma3(x, y, acc);
+        }
+        const int m = 16 * bi[i] + c, k = 16 * bj[i] + 4 * g;
+        float old[4];
+        join4(*reinterpret_cast<const uint2*>(A[0] + m * PA + k), *reinterpret_cast<const uint2*>(A[1] + m * PA + k), old);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        held[i][e] = fmaf((acc[0][e] + acc[1][e]) + acc[2][e], a.c_scale, fmaf(a.cb, old[e], m == k + e ? a.ca : 0.f));
+        for (int e = 0; e < 4; ++e)
+          held[i][e] = fmaf((acc[0][e] + acc[1][e]) + acc[2][e], a.c_scale, fmaf(a.cb, old[e], m == k + e ? a.ca : 0.f));
       }
     }
     __syncthreads();
